@@ -1,0 +1,161 @@
+// Root-mean-square norm with the residual's addition, the step in front of a linear layer:
+//   h = x + r                                  float32; stored to the residual stream in r's type
+//   y = h / sqrt(mean(h^2) + eps) * w          float32; rounded once to bfloat16, or quantized to MXFP8
+// MXFP8: per 32 elements e = clamp(floor(log2 amax) - 8, -127, ...), byte e + 127, code = E4M3(y / 2^e) to nearest even,
+// saturating at 448 (the OCP rule with E4M3's largest exponent, 8; amax / 2^e lies in [256, 512)).  The scale bytes go to the
+// library's tiled layout: the result is the activation operand of the kind::mxf8f6f4 GEMM.
+#pragma once
+#include <cuda_bf16.h>
+#include "mxint4_quantize.cuh"
+#include "quantize.cuh"
+#include "sm100_ptx.cuh"
+
+namespace torq {
+
+enum : int { RES_NONE = 0, RES_BF16 = 1, RES_F32 = 2 };
+
+// Plain loads (the residual may be updated in place), kept out of the L1: every element is read once.
+__device__ __forceinline__ uint4 load_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ void bf16x8_to_float(const uint4& a, float (&v)[8]) {
+  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+  }
+}
+__device__ __forceinline__ uint4 float_to_bf16x8(const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Eight elements at index i of a bfloat16 or float32 array.
+__device__ __forceinline__ void load8_once(const void* p, int64_t i, bool f32, float (&v)[8]) {
+  if (f32) {
+    const uint4 a = load_once(static_cast<const float*>(p) + i), b = load_once(static_cast<const float*>(p) + i + 4);
+    v[0] = __uint_as_float(a.x); v[1] = __uint_as_float(a.y); v[2] = __uint_as_float(a.z); v[3] = __uint_as_float(a.w);
+    v[4] = __uint_as_float(b.x); v[5] = __uint_as_float(b.y); v[6] = __uint_as_float(b.z); v[7] = __uint_as_float(b.w);
+  } else {
+    bf16x8_to_float(load_once(static_cast<const __nv_bfloat16*>(p) + i), v);
+  }
+}
+
+// One row per blockDim.x threads (blockDim.y rows per CTA, more than one only when a row is one warp's), a thread holds VPT
+// pieces of eight elements, blockDim.x pieces apart, in registers: one pass over memory.  rows = M, or with scales M rounded
+// up to 128: the rows behind the last one only get their zero scale bytes.
+template <int VPT, bool MX>
+__global__ void __launch_bounds__(VPT == 4 ? 512 : 1024)
+add_rmsnorm_kernel(const void* X, int x_f32, const void* R, void* R_out, int res, const __nv_bfloat16* __restrict__ weight,
+                   float eps, int64_t M, int64_t rows, int d, void* out, uint8_t* __restrict__ scales) {
+  __shared__ float part[2][32];
+  const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
+  const int pieces = d / 8;
+  griddep_launch_dependents();
+  griddep_wait();
+  uint4 w[VPT];
+#pragma unroll
+  for (int k = 0; k < VPT; ++k) {
+    const int p = tid + k * nt;
+    w[k] = p < pieces ? __ldg(reinterpret_cast<const uint4*>(weight) + p) : make_uint4(0, 0, 0, 0);
+  }
+  const int kb4 = (d / 32 + 3) / 4;
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y; row < rows; row += (int64_t)gridDim.x * blockDim.y) {
+    if (MX && row >= M) {                                // all threads of a row agree
+      for (int c = tid; c < kb4; c += nt)
+        *reinterpret_cast<uint32_t*>(scales + scale_offset(row, 4 * c, kb4)) = 0u;
+      continue;
+    }
+    const int64_t base = row * d;
+    float h[VPT][8];
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int p = tid + k * nt;
+      if (p < pieces) load8_once(X, base + 8 * p, x_f32, h[k]);
+      else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[k][i] = 0.f;
+      }
+    }
+    if (res != RES_NONE) {
+      float r[VPT][8];
+#pragma unroll
+      for (int k = 0; k < VPT; ++k) {
+        const int p = tid + k * nt;
+        if (p < pieces) load8_once(R, base + 8 * p, res == RES_F32, r[k]);
+        else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) r[k][i] = 0.f;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < VPT; ++k) {
+        const int p = tid + k * nt;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[k][i] += r[k][i];
+        if (p < pieces) {
+          if (res == RES_F32) {
+            float4* o = reinterpret_cast<float4*>(static_cast<float*>(R_out) + base + 8 * p);
+            o[0] = make_float4(h[k][0], h[k][1], h[k][2], h[k][3]);
+            o[1] = make_float4(h[k][4], h[k][5], h[k][6], h[k][7]);
+          } else {
+            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(R_out) + base + 8 * p) = float_to_bf16x8(h[k]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < VPT; ++k)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum = fmaf(h[k][i], h[k][i], sum);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+    if (nt > 32) {                                       // the two buffers in turn: one barrier per row
+      if (lane == 0) part[turn][tid >> 5] = sum;
+      __syncthreads();
+      sum = lane < (nt >> 5) ? part[turn][lane] : 0.f;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+      turn ^= 1;
+    }
+    const float rstd = 1.0f / sqrtf(sum / (float)d + eps);
+#pragma unroll
+    for (int k = 0; k < VPT; ++k) {
+      const int p = tid + k * nt;
+      float wv[8], y[8];
+      bf16x8_to_float(w[k], wv);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = h[k][i] * rstd * wv[i];
+      if constexpr (!MX) {
+        if (p < pieces) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + base + 8 * p) = float_to_bf16x8(y);
+      } else {
+        // four lanes share a block of 32, sixteen a word of four scale bytes
+        float amax = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(y[i]));
+        amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
+        amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
+        const uint32_t ef = __float_as_uint(amax) >> 23, sbyte = ef > 8u ? ef - 8u : 0u;
+        const float inv = __uint_as_float((254u - sbyte) << 23);
+        if (p < pieces)
+          *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out) + base + 8 * p) =
+              make_uint2(pack4_e4m3(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), pack4_e4m3(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+        uint32_t word = sbyte << (8 * ((lane >> 2) & 3));
+        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
+        word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
+        if ((lane & 15) == 0 && p < 16 * kb4) *reinterpret_cast<uint32_t*>(scales + scale_offset(row, p / 4, kb4)) = word;
+      }
+    }
+  }
+}
+
+}  // namespace torq

@@ -22,6 +22,7 @@
 #include "calibrate.cuh"
 #include "wait_selftest.cuh"
 #include "prepare_weights.cuh"
+#include "add_rmsnorm.cuh"
 #include "sm100_ptx.cuh"
 
 namespace torq {
@@ -208,11 +209,11 @@ static inline torq_status launch_status() {
 // this kernel overlaps the tail of the kernel before it (the kernel itself waits for that kernel
 // to complete before it touches global memory).
 template <typename... KArgs, typename... Args>
-static void launch_tc(void (*kernel)(KArgs...), int cluster, int grid, int threads, int smem, cudaStream_t s,
+static void launch_tc(void (*kernel)(KArgs...), int cluster, dim3 grid, dim3 threads, int smem, cudaStream_t s,
                       Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid, 1, 1);
-  cfg.blockDim = dim3((unsigned)threads, 1, 1);
+  cfg.gridDim = grid;
+  cfg.blockDim = threads;
   cfg.dynamicSmemBytes = (size_t)smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[2];
@@ -945,6 +946,48 @@ static torq_status gemm_impl(const void* Aq, const void* As, const void* Wq, con
   return launch_status();
 }
 
+// ---- the operators around the layer ------------------------------------------------------------------------------
+
+static inline bool dtype_ok(torq_dtype t) { return t == TORQ_F32 || t == TORQ_BF16; }
+
+// mx: MXFP8 codes and scales, else bfloat16 (out_scales NULL).
+static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const void* residual, void* residual_out, torq_dtype r_dtype,
+                                    const void* weight, float eps, int64_t M, int64_t d, void* out, void* out_scales, bool mx, void* stream) {
+  if (!X || !weight || !out || (mx && !out_scales) || (residual == nullptr) != (residual_out == nullptr)) return TORQ_ERR_NULL;
+  if (M < 1 || d < 32 || d % 32 != 0 || M > (1 << 30) || d > 16384 || !(eps >= 0.0f && eps <= 3.0e38f) || !dtype_ok(x_dtype) ||
+      (residual && !dtype_ok(r_dtype)))
+    return TORQ_ERR_SHAPE;
+  if (!aligned16(X) || !aligned16(residual) || !aligned16(residual_out) || !aligned16(weight) || !aligned16(out) || !aligned16(out_scales))
+    return TORQ_ERR_ALIGN;
+  DeviceState* st = device_state();
+  if (!st) return TORQ_ERR_LAUNCH;
+  if (!st->arch_ok) return TORQ_ERR_ARCH;
+  const int pieces = (int)(d / 8);
+  const int64_t rows = mx ? (M + 127) / 128 * 128 : M;
+  // Up to 1024 columns a row is one warp's, four rows to a CTA.  Above, a CTA's: one piece of eight per thread while the rows
+  // are few, two or four where a CTA has several.
+  int vpt, threads, per_cta = 1;
+  if (pieces <= 128) {
+    vpt = pieces <= 32 ? 1 : (pieces <= 64 ? 2 : 4);
+    threads = 32;
+    per_cta = 4;
+  } else {
+    vpt = pieces <= 1024 && M <= 2 * st->sm_count ? 1 : (pieces <= 1024 ? 2 : 4);
+    threads = (pieces + 32 * vpt - 1) / (32 * vpt) * 32;
+  }
+  const int64_t ctas = (rows + per_cta - 1) / per_cta, per_sm = 2048 / (threads * per_cta) < 16 ? 2048 / (threads * per_cta) : 16;
+  const int64_t most = per_sm * st->sm_count;
+  const dim3 grid((unsigned)(ctas < most ? ctas : most)), block((unsigned)threads, (unsigned)per_cta);
+  const int res = !residual ? RES_NONE : (r_dtype == TORQ_F32 ? RES_F32 : RES_BF16);
+  auto launch = [&](auto kernel) {
+    launch_tc(kernel, 1, grid, block, 0, static_cast<cudaStream_t>(stream), X, x_dtype == TORQ_F32 ? 1 : 0, residual, residual_out, res,
+              static_cast<const __nv_bfloat16*>(weight), eps, M, rows, (int)d, out, static_cast<uint8_t*>(out_scales));
+  };
+  if (mx) launch(vpt == 1 ? add_rmsnorm_kernel<1, true> : (vpt == 2 ? add_rmsnorm_kernel<2, true> : add_rmsnorm_kernel<4, true>));
+  else launch(vpt == 1 ? add_rmsnorm_kernel<1, false> : (vpt == 2 ? add_rmsnorm_kernel<2, false> : add_rmsnorm_kernel<4, false>));
+  return launch_status();
+}
+
 extern "C" {
 
 torq_status torq_mxfp4_gemm(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M,
@@ -1416,6 +1459,19 @@ torq_status torq_merge_rotations(const void* R_inter, const void* R_intra, int64
       static_cast<const __nv_bfloat16*>(R_inter), static_cast<const __nv_bfloat16*>(R_intra), d,
       static_cast<float*>(R_merged_f32));
   return launch_status();
+}
+
+// ---- the operators around the layer ------------------------------------------------------------------------------
+
+torq_status torq_add_rmsnorm(const void* X, torq_dtype x_dtype, const void* residual, void* residual_out, torq_dtype r_dtype,
+                             const void* weight, float eps, int64_t M, int64_t d, void* out, void* stream) {
+  return add_rmsnorm_impl(X, x_dtype, residual, residual_out, r_dtype, weight, eps, M, d, out, nullptr, false, stream);
+}
+
+torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void* residual, void* residual_out, torq_dtype r_dtype,
+                                   const void* weight, float eps, int64_t M, int64_t d, void* out_bytes, void* out_scales,
+                                   void* stream) {
+  return add_rmsnorm_impl(X, x_dtype, residual, residual_out, r_dtype, weight, eps, M, d, out_bytes, out_scales, true, stream);
 }
 
 }  // extern "C"

@@ -101,6 +101,10 @@ def lib() -> ctypes.CDLL:
     L.torq_mxint4_gemm.restype = ci
     L.torq_rotated_linear_mxint4.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, vp, ci, vp, sz, vp, vp, vp]
     L.torq_rotated_linear_mxint4.restype = ci
+    L.torq_add_rmsnorm.argtypes = [vp, ci, vp, vp, ci, vp, f32, i64, i64, vp, vp]
+    L.torq_add_rmsnorm.restype = ci
+    L.torq_add_rmsnorm_mxfp8.argtypes = [vp, ci, vp, vp, ci, vp, f32, i64, i64, vp, vp, vp]
+    L.torq_add_rmsnorm_mxfp8.restype = ci
     L.torq_block_covariance.argtypes = [vp, i64, i64, vp, vp]
     L.torq_block_covariance.restype = ci
     L.torq_givens_equalize.argtypes = [vp, i64, ctypes.c_double, vp, vp, vp, vp]
@@ -656,6 +660,73 @@ def torq_prepare_weights_mxint4(R_inter, R_intra, W, workspace=None, stream=None
 
 
 prepare_weights_mxint4 = torq_prepare_weights_mxint4
+
+
+# ---- operators around the layer: norm, products of few tokens, gated projections -----------------------
+def _operand(t, dtypes, name, shape=None, at_least=None):
+    """A contiguous CUDA tensor of the current device, of one of `dtypes`, of that shape, or with room for so many elements."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or not t.is_cuda or not t.is_contiguous():
+        what = f"{t.dtype} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name}: expected a contiguous CUDA tensor of {' or '.join(str(d) for d in dtypes)}, got {what}")
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name}: is on {t.device}, the call goes to the current device, cuda:{torch._C._cuda_getDevice()}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected the shape {tuple(shape)}, got {tuple(t.shape)}")
+    if at_least is not None and t.numel() < at_least:
+        raise ValueError(f"{name}: expected room for {at_least} elements, got {tuple(t.shape)}")
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+_BYTES = (torch.uint8,)
+
+
+def _dtype_code(t):
+    return TORQ_F32 if t.dtype is torch.float32 else TORQ_BF16
+
+
+def _norm_operands(X, weight, residual, residual_out):
+    _operand(X, _FLOATS, "X")
+    if X.dim() != 2:
+        raise ValueError(f"X: expected two dimensions, got {tuple(X.shape)}")
+    M, d = X.shape
+    _operand(weight, (torch.bfloat16,), "weight", (d,))
+    if residual is None:
+        if residual_out is not None:
+            raise ValueError("residual_out without a residual")
+        return M, d, None, TORQ_BF16
+    _operand(residual, _FLOATS, "residual", (M, d))
+    if residual_out is None:
+        residual_out = torch.empty_like(residual)
+    _operand(residual_out, (residual.dtype,), "residual_out", (M, d))
+    return M, d, residual_out, _dtype_code(residual)
+
+
+def torq_add_rmsnorm(X, weight, residual=None, eps: float = 1e-6, out=None, residual_out=None, stream=None):
+    """h = X + residual; y = h / sqrt(mean(h^2) + eps) * weight.  X, residual [M,d] float32 or bfloat16, weight [d] bf16.
+    Returns y [M,d] bf16, or (y, h) with a residual, h in its type (residual_out=residual: in place)."""
+    M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out)
+    if out is None:
+        out = torch.empty((M, d), dtype=torch.bfloat16, device=X.device)
+    _operand(out, (torch.bfloat16,), "out", (M, d))
+    _raise(lib().torq_add_rmsnorm(_ptr(X), _dtype_code(X), _ptr(residual), _ptr(h), r_dtype, _ptr(weight), eps, M, d, _ptr(out),
+                                  _stream(stream)), "torq_add_rmsnorm")
+    return out if h is None else (out, h)
+
+
+def torq_add_rmsnorm_mxfp8(X, weight, residual=None, eps: float = 1e-6, out_bytes=None, out_scales=None, residual_out=None,
+                           stream=None):
+    """torq_add_rmsnorm with y as MXFP8: (E4M3 bytes [M,d] uint8, tiled E8M0 scale bytes[, h]), the A operand of
+    torq_mxint4_gemm."""
+    M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out)
+    if out_bytes is None:
+        out_bytes = torch.empty((M, d), dtype=torch.uint8, device=X.device)
+    if out_scales is None:
+        out_scales = torch.empty(torq_scales_bytes(M, d), dtype=torch.uint8, device=X.device)
+    _operand(out_bytes, _BYTES, "out_bytes", (M, d))
+    _operand(out_scales, _BYTES, "out_scales", at_least=torq_scales_bytes(M, d))
+    _raise(lib().torq_add_rmsnorm_mxfp8(_ptr(X), _dtype_code(X), _ptr(residual), _ptr(h), r_dtype, _ptr(weight), eps, M, d,
+                                        _ptr(out_bytes), _ptr(out_scales), _stream(stream)), "torq_add_rmsnorm_mxfp8")
+    return (out_bytes, out_scales) if h is None else (out_bytes, out_scales, h)
 
 
 # ---- calibration of the inter-block rotation (Section 5.1, Algorithm 1; offline) -----------------------

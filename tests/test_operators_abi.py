@@ -1,0 +1,39 @@
+"""The operators around the layer, what needs no GPU: argument errors of the C entry points are status codes before anything
+touches a device, and the Python calls refuse tensors that are not the current GPU's."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2605_19561_b200 import torq
+
+ONE, ODD = ctypes.c_void_p(16), ctypes.c_void_p(24)      # never dereferenced on these paths
+NULL, SHAPE, ALIGN = 1, 2, 3
+
+
+@pytest.mark.parametrize("mx", [False, True])
+def test_norm_argument_errors(mx):
+    L = torq.lib()
+
+    def call(X=ONE, xt=1, r=None, ro=None, rt=1, w=ONE, eps=1e-6, M=4, d=64, out=ONE, scales=ONE):
+        if mx:
+            return L.torq_add_rmsnorm_mxfp8(X, xt, r, ro, rt, w, eps, M, d, out, scales, None)
+        return L.torq_add_rmsnorm(X, xt, r, ro, rt, w, eps, M, d, out, None)
+
+    assert call(X=None) == NULL and call(w=None) == NULL and call(out=None) == NULL
+    if mx:
+        assert call(scales=None) == NULL and call(scales=ODD) == ALIGN
+    assert call(r=ONE) == NULL and call(ro=ONE) == NULL                            # one without the other
+    assert call(M=0) == SHAPE and call(M=-3) == SHAPE and call(M=1 << 40) == SHAPE
+    assert call(d=0) == SHAPE and call(d=48) == SHAPE and call(d=16416) == SHAPE
+    assert call(xt=2) == SHAPE and call(r=ONE, ro=ONE, rt=5) == SHAPE
+    assert call(eps=-1e-6) == SHAPE and call(eps=float("nan")) == SHAPE and call(eps=float("inf")) == SHAPE
+    assert call(X=ODD) == ALIGN and call(w=ODD) == ALIGN and call(out=ODD) == ALIGN and call(r=ODD, ro=ONE) == ALIGN
+    assert call(r=ONE, ro=ODD) == ALIGN
+
+
+def test_norm_refuses_host_tensors():
+    x = torch.zeros(2, 128, dtype=torch.bfloat16)
+    for f in (lambda: torq.torq_add_rmsnorm(x, x[0]), lambda: torq.torq_add_rmsnorm_mxfp8(x, x[0]), lambda: torq.torq_add_rmsnorm(None, x[0])):
+        with pytest.raises(ValueError):
+            f()
