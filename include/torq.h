@@ -339,6 +339,32 @@ torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void
                                    const void* weight, float eps, int64_t M, int64_t d, void* out_bytes, void* out_scales,
                                    void* stream);
 
+/* Products of few tokens with 4-bit weights and activations that stay in bfloat16 (weights that were quantized without a rotation, or
+ * activations that were rotated before): Y[m,n] = sum_k x[m,k] w^[n,k], w^ the dequantized weights.
+ *   X [M, K] bf16;  Wq [N, K/2], Ws: the weight operands of torq_mxfp4_gemm / torq_nvfp4_gemm; MXINT4: Wn [N, K/2] in the STORED form
+ *   (half the bytes of the operand form torq_mxint4_gemm takes), nibble -8 included;  Y [M, N] of y_dtype
+ * Products exact, sums float32: x is widened to float16 after a power of two per token and 128 of K that brings the largest magnitude into
+ * [2^14, 2^15), so what is smaller than 2^-31 of that magnitude loses bits (as it would beside it in a float32 sum).  Weights of
+ * magnitude 2^100 and more may overflow.  The weights are read once per 32 tokens (once altogether up to there): made for decoding,
+ * any M <= 2^20 is served.  K % 128 == 0, N % 8 == 0.  One launch, no scratch. */
+torq_status torq_mxfp4_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
+                              void* stream);
+torq_status torq_nvfp4_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K, void* Y,
+                              torq_dtype y_dtype, void* stream);
+torq_status torq_mxint4_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
+                               void* stream);
+
+/* The gated pair of projections of a feed-forward block, in one launch:
+ *   Y[m,n] = silu(g) u,  g = sum_k x[m,k] w^[n,k],  u = sum_k x[m,k] w^[N+n,k],  silu(g) = g / (1 + exp(-g)), float32 up to Y
+ * Both projections are one weight matrix of 2 N rows, gate rows first (Wq [2N, K/2], Ws of 2 N rows); Y [M, N] of y_dtype.
+ * Otherwise as the products above.  N % 128 == 0, K % 128 == 0. */
+torq_status torq_mxfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                    torq_dtype y_dtype, void* stream);
+torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K,
+                                    void* Y, torq_dtype y_dtype, void* stream);
+torq_status torq_mxint4_gated_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                     torq_dtype y_dtype, void* stream);
+
 /* ---- calibration of the inter-block rotation (Section 5.1; offline, not on the inference path) ----
  * Covariance across the blocks of a token, pooled over the T calibration tokens and the 32
  * positions of a block (block means taken as zero, as Section 5.1 assumes):

@@ -23,6 +23,7 @@
 #include "wait_selftest.cuh"
 #include "prepare_weights.cuh"
 #include "add_rmsnorm.cuh"
+#include "matvec.cuh"
 #include "sm100_ptx.cuh"
 
 namespace torq {
@@ -102,6 +103,15 @@ static bool opt_in_format() {
          opt_in_smem(gemm_fewtok_kernel<FMT, 1>, few_gemm) && opt_in_smem(gemm_fewtok_kernel<FMT, 2>, few_gemm);
 }
 
+// The products of few tokens of one format.
+template <int FMT>
+static bool opt_in_matvec() {
+  using C = MatvecCfg<FMT>;
+  return opt_in_smem(matvec_kernel<FMT, 1, false>, C::smem_bytes(1, false, 8)) && opt_in_smem(matvec_kernel<FMT, 1, true>, C::smem_bytes(1, true, 8)) &&
+         opt_in_smem(matvec_kernel<FMT, 2, false>, C::smem_bytes(2, false, 8)) && opt_in_smem(matvec_kernel<FMT, 2, true>, C::smem_bytes(2, true, 8)) &&
+         opt_in_smem(matvec_kernel<FMT, 4, false>, C::smem_bytes(4, false, 8)) && opt_in_smem(matvec_kernel<FMT, 4, true>, C::smem_bytes(4, true, 8));
+}
+
 // CTA pairs of a kernel that fills its SMs.
 template <typename K>
 static int max_active_pairs(K kernel, int threads, int smem, int sm_count) {
@@ -136,6 +146,7 @@ static DeviceState* device_state() {
     }
     const bool ok = opt_in_smem(fewtok_fit_kernel, RotFewCfg::max_smem_bytes()) && opt_in_format<FMT_MXFP4>() &&
                     opt_in_format<FMT_NVFP4>() && opt_in_format<FMT_MXINT4>() &&
+                    opt_in_matvec<FMT_MXFP4>() && opt_in_matvec<FMT_NVFP4>() && opt_in_matvec<FMT_MXINT4>() &&
                     opt_in_smem(rotate_quantize_kernel<256, FMT_F32OUT>, RotCfg<256>::SMEM_BYTES) &&
                     opt_in_smem(rotate_quantize_pair_kernel<FMT_F32OUT>, RotPairCfg::SMEM_BYTES);
     if (!ok) return nullptr;
@@ -988,6 +999,40 @@ static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const voi
   return launch_status();
 }
 
+// CTAs in a cluster of the few-token product: the largest of 8, 4, 2, 1 that keeps all CTAs resident at once.
+static int matvec_cluster(int64_t tiles, int64_t k_tiles, int ctas_per_sm, int sm_count) {
+  int S = 8;
+  while (S > 1 && (S > k_tiles || tiles * S > (int64_t)ctas_per_sm * sm_count)) S /= 2;
+  return S;
+}
+
+template <int FMT, bool GATED>
+static torq_status matvec_impl(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
+                               float alpha, void* stream) {
+  using C = MatvecCfg<FMT>;
+  if (!X || !Wq || !Ws || !Y) return TORQ_ERR_NULL;
+  if (M < 1 || K < 128 || K % 128 != 0 || M > (1 << 20) || N > (1 << 29) || K > (1 << 24) || (GATED ? N < 128 || N % 128 != 0 : N < 8 || N % 8 != 0))
+    return TORQ_ERR_SHAPE;
+  if (!dtype_ok(y_dtype)) return TORQ_ERR_SHAPE;
+  if (!aligned16(X) || !aligned16(Wq) || !aligned16(Ws) || !aligned16(Y)) return TORQ_ERR_ALIGN;
+  DeviceState* st = device_state();
+  if (!st) return TORQ_ERR_LAUNCH;
+  if (!st->arch_ok) return TORQ_ERR_ARCH;
+  CUtensorMap tmW;
+  if (!encode_2d(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(GATED ? 2 * N : N), (uint64_t)(K / 2), 64, 128)) return TORQ_ERR_LAUNCH;
+  const int nt = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
+  const int64_t tiles = GATED ? N / 64 : (N + 127) / 128, groups = (M + 8 * nt - 1) / (8 * nt);
+  const int S = matvec_cluster(tiles * groups, (K + C::BK - 1) / C::BK, nt == 1 ? 3 : 2, st->sm_count);
+  const dim3 grid((unsigned)(tiles * S), (unsigned)groups);
+  auto launch = [&](auto kernel) {
+    launch_tc(kernel, S, grid, dim3(C::THREADS), C::smem_bytes(nt, GATED, S), static_cast<cudaStream_t>(stream), tmW,
+              static_cast<const __nv_bfloat16*>(X), static_cast<const uint8_t*>(Ws), Y, y_dtype == TORQ_BF16 ? 1 : 0, (int)M, (int)N, (int)K, S,
+              alpha, st->err_word);
+  };
+  launch(nt == 1 ? matvec_kernel<FMT, 1, GATED> : (nt == 2 ? matvec_kernel<FMT, 2, GATED> : matvec_kernel<FMT, 4, GATED>));
+  return launch_status();
+}
+
 extern "C" {
 
 torq_status torq_mxfp4_gemm(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M,
@@ -1472,6 +1517,38 @@ torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void
                                    const void* weight, float eps, int64_t M, int64_t d, void* out_bytes, void* out_scales,
                                    void* stream) {
   return add_rmsnorm_impl(X, x_dtype, residual, residual_out, r_dtype, weight, eps, M, d, out_bytes, out_scales, true, stream);
+}
+
+torq_status torq_mxfp4_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
+                              void* stream) {
+  return matvec_impl<FMT_MXFP4, false>(X, Wq, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+}
+
+torq_status torq_nvfp4_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K, void* Y,
+                              torq_dtype y_dtype, void* stream) {
+  if (!scale_ok(w_tensor_scale)) return TORQ_ERR_SHAPE;
+  return matvec_impl<FMT_NVFP4, false>(X, Wq, Ws, M, N, K, Y, y_dtype, w_tensor_scale, stream);
+}
+
+torq_status torq_mxint4_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
+                               void* stream) {
+  return matvec_impl<FMT_MXINT4, false>(X, Wn, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+}
+
+torq_status torq_mxfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                    torq_dtype y_dtype, void* stream) {
+  return matvec_impl<FMT_MXFP4, true>(X, Wq, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+}
+
+torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K,
+                                    void* Y, torq_dtype y_dtype, void* stream) {
+  if (!scale_ok(w_tensor_scale)) return TORQ_ERR_SHAPE;
+  return matvec_impl<FMT_NVFP4, true>(X, Wq, Ws, M, N, K, Y, y_dtype, w_tensor_scale, stream);
+}
+
+torq_status torq_mxint4_gated_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                     torq_dtype y_dtype, void* stream) {
+  return matvec_impl<FMT_MXINT4, true>(X, Wn, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
 }
 
 }  // extern "C"

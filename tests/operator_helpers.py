@@ -103,3 +103,42 @@ def check_mxfp8(codes, scales, ref):
     p = untile(scales, -(-M // 128) * 128, -(-(d // 32) // 4) * 4).clone()
     p[:M, :d // 32] = 0
     assert not p.any()
+
+
+# ---- products -----------------------------------------------------------------------------------------------------
+def silu(v):
+    return v * torch.sigmoid(v)
+
+
+def check_sums(Y, x, w, steps):
+    """|Y - x w^T| <= steps 2^-22 sum |x| |w| + the rounding of the result.  Products are exact; `steps` additions in float32
+    follow one another on the way of a product into the result, each off by at most 2^-23 of the largest partial sum if it
+    truncates; the factor of two leaves room for the power of two that the largest partial sum may exceed the final one by."""
+    ref, mag = x @ w.t(), x.abs() @ w.abs().t()
+    tol = steps * 2.0 ** -22 * mag + HALF_STEP[Y.dtype] * ref.abs() + 1e-40
+    assert torch.isfinite(Y).all()
+    worst = ((Y.double() - ref).abs() / tol).max().item()
+    assert worst <= 1.0, worst
+
+
+def check_gated(Y, x, w, steps):
+    """The error of both sums as above, through silu(g) u (the derivative of silu is at most 1.1), exp and the quotient at 2^-21."""
+    N = w.shape[0] // 2
+    g, u = x @ w[:N].t(), x @ w[N:].t()
+    e = steps * 2.0 ** -22
+    dg, du = e * (x.abs() @ w[:N].abs().t()), e * (x.abs() @ w[N:].abs().t())
+    ref = silu(g) * u
+    tol = 1.1 * dg * (u.abs() + du) + silu(g).abs() * du + ref.abs() * (HALF_STEP[Y.dtype] + 2.0 ** -21) + 1e-40
+    assert torch.isfinite(Y).all()
+    worst = ((Y.double() - ref).abs() / tol).max().item()
+    assert worst <= 1.0, worst
+
+
+def matvec_steps(K):
+    """Of the few-token products, in the kernel's order: 8 instructions and 4 block sums per 128 of K, one sum per 128, 8 CTAs."""
+    return 12 + K // 128 + 8
+
+
+def gemm_steps(K):
+    """Of the GEMMs: at most one instruction per 32 of K, twice because what is added inside one is aligned before it is added."""
+    return 2 * (K // 32 + 8)

@@ -37,3 +37,30 @@ def test_norm_refuses_host_tensors():
     for f in (lambda: torq.torq_add_rmsnorm(x, x[0]), lambda: torq.torq_add_rmsnorm_mxfp8(x, x[0]), lambda: torq.torq_add_rmsnorm(None, x[0])):
         with pytest.raises(ValueError):
             f()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4", "mxint4"])
+def test_matvec_argument_errors(fmt, gated):
+    f = getattr(torq.lib(), f"torq_{fmt}_{'gated_' if gated else ''}matvec")
+
+    def call(X=ONE, W=ONE, s=ONE, ts=1.0, M=3, N=128, K=256, Y=ONE, t=0):
+        return f(X, W, s, *((ts,) if fmt == "nvfp4" else ()), M, N, K, Y, t, None)
+
+    for k in ("X", "W", "s", "Y"):
+        assert call(**{k: None}) == NULL and call(**{k: ODD}) == ALIGN
+    assert call(M=0) == SHAPE and call(M=(1 << 20) + 1) == SHAPE
+    assert call(K=192) == SHAPE and call(K=0) == SHAPE and call(K=1 << 25) == SHAPE
+    assert call(N=0) == SHAPE and call(N=-128) == SHAPE and call(N=132) == SHAPE and call(N=1 << 30) == SHAPE
+    if gated:
+        assert call(N=64) == SHAPE and call(N=192) == SHAPE
+    assert call(t=2) == SHAPE
+    if fmt == "nvfp4":
+        assert call(ts=0.0) == SHAPE and call(ts=-1.0) == SHAPE and call(ts=float("inf")) == SHAPE and call(ts=float("nan")) == SHAPE
+
+
+def test_matvec_refuses_host_tensors():
+    x, w, s = torch.zeros(2, 128, dtype=torch.bfloat16), torch.zeros(128, 64, dtype=torch.uint8), torch.zeros(512, dtype=torch.uint8)
+    for f in (lambda: torq.torq_mxfp4_matvec(x, w, s), lambda: torq.torq_mxint4_gated_matvec(x, w, s), lambda: torq.torq_nvfp4_matvec(None, w, s, 1.0)):
+        with pytest.raises(ValueError):
+            f()
