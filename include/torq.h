@@ -327,11 +327,11 @@ torq_status torq_rotated_linear_mxint4(const void* X, const void* R_inter, const
  *   h = x + r (float32);  y = h / sqrt(mean_d(h^2) + eps) * w (float32)
  *   X [M, d] of x_dtype; residual [M, d] of r_dtype or NULL (h = x); residual_out [M, d] of r_dtype gets h, rounded once; it may be
  *   `residual` itself, or X where the types agree, and is NULL exactly where residual is; weight [d] bf16; eps >= 0.
- * The norm is taken of h before it is rounded.  torq_add_rmsnorm: out [M, d] bf16, rounded once: the X of the rotation entry
- * points.  torq_add_rmsnorm_mxfp8: out_bytes [M, d] FP8 E4M3 and out_scales, torq_scales_bytes(M, d) bytes in the tiled
+ * The norm is taken of h before it is rounded.  torq_add_rmsnorm: out [M, d] bf16, rounded once: the X of the rotation and
+ * matvec entry points.  torq_add_rmsnorm_mxfp8: out_bytes [M, d] FP8 E4M3 and out_scales, torq_scales_bytes(M, d) bytes in the tiled
  * layout, one E8M0 byte per 32 elements: byte = e + 127, e = clamp(floor(log2 amax) - 8, -127, 127) (amax == 0 -> byte 0), codes
- * E4M3(y / 2^e) to nearest even, saturating at 448, padding bytes 0x00: the A operand that torq_mxint4_gemm takes (any E4M3
- * bytes with E8M0 scales are).  The squares of a row must sum to less than float32's largest value.
+ * E4M3(y / 2^e) to nearest even, saturating at 448, padding bytes 0x00: the A operand that torq_mxint4_gemm and
+ * torq_mxint4_gated_gemm take (any E4M3 bytes with E8M0 scales are).  The squares of a row must sum to less than float32's largest value.
  * 32 <= d <= 16384, d % 32 == 0.  One launch.  Apart from residual_out the outputs overlap nothing. */
 torq_status torq_add_rmsnorm(const void* X, torq_dtype x_dtype, const void* residual, void* residual_out, torq_dtype r_dtype,
                              const void* weight, float eps, int64_t M, int64_t d, void* out, void* stream);
@@ -364,6 +364,17 @@ torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* W
                                     void* Y, torq_dtype y_dtype, void* stream);
 torq_status torq_mxint4_gated_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
                                      torq_dtype y_dtype, void* stream);
+
+/* The same on quantized activations, the activation and the product in the epilogue of the block-scaled GEMM (M rows, from
+ * decoding to prefill): operands as torq_mxfp4_gemm, torq_nvfp4_gemm and torq_mxint4_gemm take them, weights of 2 N rows, gate
+ * rows first; Y [M, N].  The A operand of the MXINT4 form may be any E4M3 bytes with E8M0 scales, torq_add_rmsnorm_mxfp8's among
+ * them.  N % 128 == 0, K % 128 == 0.  One launch. */
+torq_status torq_mxfp4_gated_gemm(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                  torq_dtype y_dtype, void* stream);
+torq_status torq_nvfp4_gated_gemm(const void* Aq, const void* As, float a_tensor_scale, const void* Wq, const void* Ws, float w_tensor_scale,
+                                  int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype, void* stream);
+torq_status torq_mxint4_gated_gemm(const void* A8, const void* As, const void* W8, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                   torq_dtype y_dtype, void* stream);
 
 /* ---- calibration of the inter-block rotation (Section 5.1; offline, not on the inference path) ----
  * Covariance across the blocks of a token, pooled over the T calibration tokens and the 32

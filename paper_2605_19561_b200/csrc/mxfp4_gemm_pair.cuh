@@ -28,9 +28,16 @@
 // FMT_MXINT4: integer codes as E4M3 operand bytes (kind::mxf8f6f4, E8M0 scale per 32 elements of K):
 // a stage is 128 elements of K, one scale chunk, four instructions of K = 32 taking bytes 0..3 of
 // the chunk's 4-byte cells.
+//
+// GATED: the pair of projections of a feed-forward block, W [2 N, K] with the gate rows first, Y [M, N] = silu(gate) * up.
+// The 256 columns of a tile are 128 gates and the 128 ups of the same features: the two halves of the W tile, one per CTA, and
+// their scale chunks come from rows n and N + n, nothing else changes before the epilogue.  There warp (q, h) reads the gates
+// 64 h ... 64 h + 63 and their ups and stores half as many columns, so Y and the traffic of a separate product (gate and up
+// written and read again) are saved.  N % 128 == 0: whole tiles and whole scale chunks; no 192-column tiles.
 #pragma once
 #include <cuda_bf16.h>
 #include <type_traits>
+#include "activation.cuh"
 #include "pair_handshake.cuh"
 #include "sm100_ptx.cuh"
 
@@ -63,7 +70,7 @@ struct GemmPairCfgT {
 };
 using GemmPairCfg = GemmPairCfgT<FMT_MXFP4>;
 
-template <int FMT = FMT_MXFP4>
+template <int FMT = FMT_MXFP4, bool GATED = false>
 __global__ void __launch_bounds__(320, 1)
 mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                        const __grid_constant__ CUtensorMap tmSFA, const __grid_constant__ CUtensorMap tmSFB,
@@ -155,6 +162,17 @@ mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       const uint32_t leader_full = map_to_cta(full_bar(s), 0);
       const int bn_half = narrow ? kNarrowCols / 2 : BN / 2;
       if (rank == 0) mbar_arrive_expect_tx(full_bar(s), 2 * (C::STAGE_TX - (BN / 2 - bn_half) * 128));
+      if constexpr (GATED) {                             // rows of W in units of 128: gates tcol / 256, ups N / 128 further on
+        const int gate = tcol >> 8, up = (N >> 7) + gate;
+        tma_load_2d_pair(st + C::A_BYTES, &tmB, kt * 128, 128 * (rank == 0 ? gate : up), leader_full);
+#pragma unroll
+        for (int b = 0; b < C::SF_BOXES; ++b) {
+          const uint32_t sf = st + C::A_BYTES + C::B_BYTES + C::SFA_BYTES + b * 2 * C::SF_BOX_BYTES;
+          tma_load_2d_pair(sf, &tmSFB, kt * CH * 128 + b * 256, gate, leader_full);
+          tma_load_2d_pair(sf + C::SF_BOX_BYTES, &tmSFB, kt * CH * 128 + b * 256, up, leader_full);
+        }
+        return;
+      }
       tma_load_2d_pair(st + C::A_BYTES, narrow ? &tmBn : &tmB, kt * 128, tcol + (int)rank * bn_half, leader_full);
 #pragma unroll
       for (int b = 0; b < C::SF_BOXES; ++b)
@@ -292,25 +310,33 @@ mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       bool narrow;
       mixed_tile_coords(tile, tiles, mp, tcol, narrow);
       const int mt = 2 * mp + (int)rank;
-      const bool half_only = narrow && h == 1;           // columns 128..191 of a 192-column tile
+      const bool half_only = !GATED && narrow && h == 1;   // columns 128..191 of a 192-column tile
       ok = mbar_wait_cluster(accf_bar, tcount & 1, cta_abort, err_word, SITE_EPI_ACC_FULL);
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
       tc_fence_after_sync();
-      const uint32_t tacc = tmem_base + ((uint32_t)(q * 32) << 16) + h * 128;
+      const uint32_t tacc = tmem_base + ((uint32_t)(q * 32) << 16) + h * (GATED ? 64 : 128);
+      constexpr int SECOND = GATED ? 128 : 64;           // v2, v3: this warp's further columns, or the ups of its gates
       uint32_t v0[32], v1[32], v2[32], v3[32];
       tmem_ld_32x32(tacc, v0);
       tmem_ld_32x32(tacc + 32, v1);
       if (!half_only) {
-        tmem_ld_32x32(tacc + 64, v2);
-        tmem_ld_32x32(tacc + 96, v3);
+        tmem_ld_32x32(tacc + SECOND, v2);
+        tmem_ld_32x32(tacc + SECOND + 32, v3);
       }
       tmem_ld_wait();
       tc_fence_before_sync();
       __syncwarp();
       const bool more = accumulator_is_waited_for(tile, npairs, 1, total_tiles);
       if (lane == 0 && more) mbar_arrive_cluster(map_to_cta(acce_bar, 0));   // free again
-      if constexpr (FMT == FMT_NVFP4) {                    // product of the two tensor scales
+      if constexpr (GATED) {
+        auto gated = [&](uint32_t g, uint32_t u) {
+          const float a = FMT == FMT_NVFP4 ? alpha : 1.0f;
+          return __float_as_uint(silu(__uint_as_float(g) * a) * (__uint_as_float(u) * a));
+        };
+#pragma unroll
+        for (int j = 0; j < 32; ++j) { v0[j] = gated(v0[j], v2[j]); v1[j] = gated(v1[j], v3[j]); }
+      } else if constexpr (FMT == FMT_NVFP4) {             // product of the two tensor scales
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
           v0[j] = __float_as_uint(__uint_as_float(v0[j]) * alpha);
@@ -323,7 +349,7 @@ mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       // with row % 8 as the 128-byte TMA swizzle expects) -> TMA store of a [32 rows x 128 B] box.
       // The store clips rows >= M and columns >= N by itself.
       const int row0 = mt * C::BM + q * 32;
-      const int col0 = tcol + h * 128;
+      const int col0 = GATED ? (tcol >> 1) + h * 64 : tcol + h * 128;
       const uint32_t stage_buf = smem_base + out_off + (uint32_t)(warp - 2) * C::OUT_WARP_BYTES;
       const uint32_t my_row = stage_buf + lane * 128;
       const uint32_t sw = (uint32_t)(lane & 7);
@@ -370,7 +396,7 @@ mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
           flush(col);
         };
         half64(v0, v1, col0);
-        if (!half_only) half64(v2, v3, col0 + 64);
+        if (!GATED && !half_only) half64(v2, v3, col0 + 64);
       } else {
         auto quarter32 = [&](const uint32_t (&v)[32], int col) {
           reuse();
@@ -380,7 +406,7 @@ mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
         };
         quarter32(v0, col0);
         quarter32(v1, col0 + 32);
-        if (!half_only) {
+        if (!GATED && !half_only) {
           quarter32(v2, col0 + 64);
           quarter32(v3, col0 + 96);
         }

@@ -98,6 +98,7 @@ static bool opt_in_format() {
          opt_in_smem(rotate_fewtok_kernel<FMT, 1, false, RotFewCfg::SHARED_STAGES>, few_rot) &&
          opt_in_smem(rotate_fewtok_kernel<FMT, 1>, few_rot) && opt_in_smem(rotate_fewtok_kernel<FMT, 2>, few_rot) &&
          opt_in_smem(mxfp4_gemm_pair_kernel<FMT>, GemmPairCfgT<FMT>::SMEM_BYTES) &&
+         opt_in_smem(mxfp4_gemm_pair_kernel<FMT, true>, GemmPairCfgT<FMT>::SMEM_BYTES) &&
          opt_in_smem(mxfp4_gemm_wide_kernel<FMT, 128>, kWideSmem) && opt_in_smem(mxfp4_gemm_wide_kernel<FMT, 256>, kWideSmem) &&
          opt_in_smem(mxfp4_gemm_wide_kernel<FMT, 384>, kWideSmem) && opt_in_smem(gemm_fewtok_kernel<FMT, 1, true>, few_gemm) &&
          opt_in_smem(gemm_fewtok_kernel<FMT, 1>, few_gemm) && opt_in_smem(gemm_fewtok_kernel<FMT, 2>, few_gemm);
@@ -1033,6 +1034,39 @@ static torq_status matvec_impl(const void* X, const void* Wq, const void* Ws, in
   return launch_status();
 }
 
+// The gated pair of projections on quantized activations: the pair kernel at every number of rows.
+template <int FMT>
+static torq_status gated_gemm_impl(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                   torq_dtype y_dtype, float alpha, void* stream) {
+  using C = GemmPairCfgT<FMT>;
+  if (!Aq || !As || !Wq || !Ws || !Y) return TORQ_ERR_NULL;
+  if (M < 1 || N < 128 || K < 128 || K % 128 != 0 || N % 128 != 0 || M > (1 << 30) || N > (1 << 29) || K > (1 << 24)) return TORQ_ERR_SHAPE;
+  if ((M + 255) / 256 * (N / 128) > (1 << 30)) return TORQ_ERR_SHAPE;   // tiles are counted in 32 bits
+  if (!dtype_ok(y_dtype)) return TORQ_ERR_SHAPE;
+  if (!aligned16(Aq) || !aligned16(As) || !aligned16(Wq) || !aligned16(Ws) || !aligned16(Y)) return TORQ_ERR_ALIGN;
+  DeviceState* st = device_state();
+  if (!st) return TORQ_ERR_LAUNCH;
+  if (!st->arch_ok) return TORQ_ERR_ARCH;
+  const uint64_t krow = (uint64_t)(FMT == FMT_MXINT4 ? K : K / 2), kb4 = (uint64_t)(K / (FMT == FMT_NVFP4 ? 64 : 128));
+  const bool ybf = y_dtype == TORQ_BF16;
+  CUtensorMap tmA, tmB, tmSFA, tmSFB, tmY;
+  if (!encode_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Aq, (uint64_t)M, krow, 128, 128) ||
+      !encode_2d(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(2 * N), krow, 128, 128) ||
+      !encode_2d(&tmSFA, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, As, (uint64_t)((M + 127) / 128), kb4 * 128, 1, C::SF_BOX_WORDS,
+                 CU_TENSOR_MAP_SWIZZLE_NONE) ||
+      !encode_2d(&tmSFB, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, Ws, (uint64_t)(2 * N / 128), kb4 * 128, 1, C::SF_BOX_WORDS,
+                 CU_TENSOR_MAP_SWIZZLE_NONE) ||
+      !encode_2d(&tmY, ybf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, ybf ? 2 : 4, Y, (uint64_t)M, (uint64_t)N, 32,
+                 ybf ? 64 : 32))
+    return TORQ_ERR_LAUNCH;
+  MixedTiles list = mixed_tiles_make((int)((M + 255) / 256), (int)(N / 128), 0);
+  list.group = plan_gemm_tiles(M, 2 * N, krow, st->gemm_pairs).group;
+  const int pairs = list.total < st->gemm_pairs ? list.total : st->gemm_pairs;
+  launch_tc(mxfp4_gemm_pair_kernel<FMT, true>, 2, 2 * pairs, C::THREADS, C::SMEM_BYTES, static_cast<cudaStream_t>(stream), tmA, tmB, tmSFA, tmSFB,
+            tmY, tmB, list, ybf ? 1 : 0, (int)M, (int)N, (int)K, alpha, st->err_word);
+  return launch_status();
+}
+
 extern "C" {
 
 torq_status torq_mxfp4_gemm(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M,
@@ -1549,6 +1583,22 @@ torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* W
 torq_status torq_mxint4_gated_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
                                      torq_dtype y_dtype, void* stream) {
   return matvec_impl<FMT_MXINT4, true>(X, Wn, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+}
+
+torq_status torq_mxfp4_gated_gemm(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                  torq_dtype y_dtype, void* stream) {
+  return gated_gemm_impl<FMT_MXFP4>(Aq, As, Wq, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+}
+
+torq_status torq_nvfp4_gated_gemm(const void* Aq, const void* As, float a_tensor_scale, const void* Wq, const void* Ws, float w_tensor_scale,
+                                  int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype, void* stream) {
+  if (!scale_ok(a_tensor_scale) || !scale_ok(w_tensor_scale)) return TORQ_ERR_SHAPE;
+  return gated_gemm_impl<FMT_NVFP4>(Aq, As, Wq, Ws, M, N, K, Y, y_dtype, a_tensor_scale * w_tensor_scale, stream);
+}
+
+torq_status torq_mxint4_gated_gemm(const void* A8, const void* As, const void* W8, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                   torq_dtype y_dtype, void* stream) {
+  return gated_gemm_impl<FMT_MXINT4>(A8, As, W8, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
 }
 
 }  // extern "C"

@@ -111,6 +111,11 @@ def lib() -> ctypes.CDLL:
     for name in ("torq_nvfp4_matvec", "torq_nvfp4_gated_matvec"):
         getattr(L, name).argtypes = [vp, vp, vp, f32, i64, i64, i64, vp, ci, vp]
         getattr(L, name).restype = ci
+    for name in ("torq_mxfp4_gated_gemm", "torq_mxint4_gated_gemm"):
+        getattr(L, name).argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, ci, vp]
+        getattr(L, name).restype = ci
+    L.torq_nvfp4_gated_gemm.argtypes = [vp, vp, f32, vp, vp, f32, i64, i64, i64, vp, ci, vp]
+    L.torq_nvfp4_gated_gemm.restype = ci
     L.torq_block_covariance.argtypes = [vp, i64, i64, vp, vp]
     L.torq_block_covariance.restype = ci
     L.torq_givens_equalize.argtypes = [vp, i64, ctypes.c_double, vp, vp, vp, vp]
@@ -722,7 +727,7 @@ def torq_add_rmsnorm(X, weight, residual=None, eps: float = 1e-6, out=None, resi
 def torq_add_rmsnorm_mxfp8(X, weight, residual=None, eps: float = 1e-6, out_bytes=None, out_scales=None, residual_out=None,
                            stream=None):
     """torq_add_rmsnorm with y as MXFP8: (E4M3 bytes [M,d] uint8, tiled E8M0 scale bytes[, h]), the A operand of
-    torq_mxint4_gemm."""
+    torq_mxint4_gemm and torq_mxint4_gated_gemm."""
     M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out)
     if out_bytes is None:
         out_bytes = torch.empty((M, d), dtype=torch.uint8, device=X.device)
@@ -735,19 +740,23 @@ def torq_add_rmsnorm_mxfp8(X, weight, residual=None, eps: float = 1e-6, out_byte
     return (out_bytes, out_scales) if h is None else (out_bytes, out_scales, h)
 
 
+_IN_BF16 = object()
+
+
 def _product(name, A, As, Wq, Ws, scales, per_byte, gated, out_dtype, Y, stream):
-    """Y = A W^T of one format.  As None: A is bf16 [M,K]; else codes of `per_byte` to a byte, as Wq's are.  scales: the
+    """Y = A W^T of one format.  As _IN_BF16: A is bf16 [M,K]; else codes of `per_byte` to a byte, as Wq's are.  scales: the
     tensor scales behind each operand's scale bytes (NVFP4)."""
-    _operand(A, (torch.bfloat16,) if As is None else _BYTES, "X" if As is None else "A")
+    bf16 = As is _IN_BF16
+    _operand(A, (torch.bfloat16,) if bf16 else _BYTES, "X" if bf16 else "A")
     _operand(Wq, _BYTES, "W")
     if A.dim() != 2 or Wq.dim() != 2:
         raise ValueError(f"{name}: expected matrices, got {tuple(A.shape)} and {tuple(Wq.shape)}")
     M, rows, K = A.shape[0], Wq.shape[0], Wq.shape[1] * per_byte
-    if A.shape[1] * (1 if As is None else per_byte) != K:
+    if A.shape[1] * (1 if bf16 else per_byte) != K:
         raise ValueError(f"{name}: {tuple(A.shape)} and {tuple(Wq.shape)} have different K")
     scales_bytes = torq_nvfp4_scales_bytes if scales else torq_scales_bytes
     _operand(Ws, _BYTES, "Ws", at_least=scales_bytes(rows, K))
-    if As is not None:
+    if not bf16:
         _operand(As, _BYTES, "As", at_least=scales_bytes(M, K))
     if gated and rows % 2:
         raise ValueError(f"{name}: W has gate and up rows, got an odd number of them")
@@ -755,39 +764,55 @@ def _product(name, A, As, Wq, Ws, scales, per_byte, gated, out_dtype, Y, stream)
     if Y is None:
         Y = torch.empty((M, N), dtype=out_dtype, device=A.device)
     _operand(Y, _FLOATS, "Y", (M, N))
-    x = (_ptr(A),) if As is None else (_ptr(A), _ptr(As), *scales[:1])
+    x = (_ptr(A),) if bf16 else (_ptr(A), _ptr(As), *scales[:1])
     _raise(getattr(lib(), name)(*x, _ptr(Wq), _ptr(Ws), *scales[-1:], M, N, K, _ptr(Y), _dtype_code(Y), _stream(stream)), name)
     return Y
 
 
 def torq_mxfp4_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """X [M,K] bf16 (few tokens) times MXFP4 weights Wq [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product("torq_mxfp4_matvec", X, None, Wq, Ws, (), 2, False, out_dtype, Y, stream)
+    return _product("torq_mxfp4_matvec", X, _IN_BF16, Wq, Ws, (), 2, False, out_dtype, Y, stream)
 
 
 def torq_nvfp4_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, stream=None):
     """X [M,K] bf16 (few tokens) times NVFP4 weights Wq [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product("torq_nvfp4_matvec", X, None, Wq, Ws, (w_tensor_scale,), 2, False, out_dtype, Y, stream)
+    return _product("torq_nvfp4_matvec", X, _IN_BF16, Wq, Ws, (w_tensor_scale,), 2, False, out_dtype, Y, stream)
 
 
 def torq_mxint4_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """X [M,K] bf16 (few tokens) times MXINT4 weights in their stored form Wn [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product("torq_mxint4_matvec", X, None, Wn, Ws, (), 2, False, out_dtype, Y, stream)
+    return _product("torq_mxint4_matvec", X, _IN_BF16, Wn, Ws, (), 2, False, out_dtype, Y, stream)
 
 
 def torq_mxfp4_gated_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """silu(X Wg^T) * (X Wu^T) of few tokens, X [M,K] bf16, Wq [2N,K/2] MXFP4 with the gate rows first -> Y [M,N]."""
-    return _product("torq_mxfp4_gated_matvec", X, None, Wq, Ws, (), 2, True, out_dtype, Y, stream)
+    return _product("torq_mxfp4_gated_matvec", X, _IN_BF16, Wq, Ws, (), 2, True, out_dtype, Y, stream)
 
 
 def torq_nvfp4_gated_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, stream=None):
     """The same with NVFP4 weights."""
-    return _product("torq_nvfp4_gated_matvec", X, None, Wq, Ws, (w_tensor_scale,), 2, True, out_dtype, Y, stream)
+    return _product("torq_nvfp4_gated_matvec", X, _IN_BF16, Wq, Ws, (w_tensor_scale,), 2, True, out_dtype, Y, stream)
 
 
 def torq_mxint4_gated_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """The same with MXINT4 weights in their stored form."""
-    return _product("torq_mxint4_gated_matvec", X, None, Wn, Ws, (), 2, True, out_dtype, Y, stream)
+    return _product("torq_mxint4_gated_matvec", X, _IN_BF16, Wn, Ws, (), 2, True, out_dtype, Y, stream)
+
+
+def torq_mxfp4_gated_gemm(Aq, As, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
+    """silu(A Wg^T) * (A Wu^T): Aq [M,K/2], Wq [2N,K/2] MXFP4 codes with the gate rows first, As, Ws tiled -> Y [M,N]."""
+    return _product("torq_mxfp4_gated_gemm", Aq, As, Wq, Ws, (), 2, True, out_dtype, Y, stream)
+
+
+def torq_nvfp4_gated_gemm(Aq, As, a_tensor_scale: float, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None,
+                          stream=None):
+    """The same on NVFP4 operands."""
+    return _product("torq_nvfp4_gated_gemm", Aq, As, Wq, Ws, (a_tensor_scale, w_tensor_scale), 2, True, out_dtype, Y, stream)
+
+
+def torq_mxint4_gated_gemm(A8, As, W8, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
+    """The same on operand bytes: A8 [M,K] E4M3 with E8M0 scales (MXINT4 or torq_add_rmsnorm_mxfp8's), W8 [2N,K]."""
+    return _product("torq_mxint4_gated_gemm", A8, As, W8, Ws, (), 1, True, out_dtype, Y, stream)
 
 
 # ---- calibration of the inter-block rotation (Section 5.1, Algorithm 1; offline) -----------------------

@@ -64,3 +64,27 @@ def test_matvec_refuses_host_tensors():
     for f in (lambda: torq.torq_mxfp4_matvec(x, w, s), lambda: torq.torq_mxint4_gated_matvec(x, w, s), lambda: torq.torq_nvfp4_matvec(None, w, s, 1.0)):
         with pytest.raises(ValueError):
             f()
+
+
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4", "mxint4"])
+def test_gated_gemm_argument_errors(fmt):
+    f = getattr(torq.lib(), f"torq_{fmt}_gated_gemm")
+
+    def call(A=ONE, sa=ONE, W=ONE, s=ONE, ta=1.0, tw=1.0, M=3, N=128, K=256, Y=ONE, t=0):
+        if fmt == "nvfp4":
+            return f(A, sa, ta, W, s, tw, M, N, K, Y, t, None)
+        return f(A, sa, W, s, M, N, K, Y, t, None)
+
+    for k in ("A", "sa", "W", "s", "Y"):
+        assert call(**{k: None}) == NULL and call(**{k: ODD}) == ALIGN
+    assert call(M=0) == SHAPE and call(M=(1 << 30) + 1) == SHAPE and call(M=1 << 30, N=1 << 29) == SHAPE
+    assert call(K=192) == SHAPE and call(N=64) == SHAPE and call(N=192) == SHAPE and call(N=1 << 30) == SHAPE and call(t=7) == SHAPE
+    if fmt == "nvfp4":
+        assert call(ta=0.0) == SHAPE and call(tw=float("nan")) == SHAPE
+
+
+def test_gated_gemm_refuses_host_tensors():
+    w, s = torch.zeros(256, 64, dtype=torch.uint8), torch.zeros(1024, dtype=torch.uint8)
+    for f in (torq.torq_mxfp4_gated_gemm, torq.torq_mxint4_gated_gemm):
+        with pytest.raises(ValueError):
+            f(w, s, w, s)
