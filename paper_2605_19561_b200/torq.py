@@ -144,6 +144,8 @@ def lib() -> ctypes.CDLL:
 _MXFP4, _MXINT4, _STRUCTURED, _NVFP4 = range(4)
 _LAYER_ENTRIES = ("torq_rotated_linear", "torq_rotated_linear_mxint4", "torq_rotated_linear_structured",
                   "torq_rotated_linear_nvfp4")
+_OPERATORS = (*(f"torq_{fmt}_{op}" for op in ("matvec", "gated_matvec", "gated_gemm") for fmt in ("mxfp4", "nvfp4", "mxint4")),
+              "torq_add_rmsnorm", "torq_add_rmsnorm_mxfp8")
 
 
 def _layer(*args):                               # until the first call has put the native function here
@@ -153,6 +155,17 @@ def _layer(*args):                               # until the first call has put 
 
 
 def _layer_native():
+    binding = _native_binding()
+    return binding and binding.layer
+
+
+_binding_module = None                           # None: not looked for yet; False: cannot be had
+
+
+def _native_binding():
+    global _binding_module
+    if _binding_module is not None:
+        return _binding_module or None
     L = lib()
     try:
         spec = importlib.util.spec_from_file_location(__package__ + "._torq_binding", _build.build_binding())
@@ -160,10 +173,13 @@ def _layer_native():
         spec.loader.exec_module(binding)
     except (ImportError, OSError, RuntimeError) as e:
         warnings.warn(f"the native binding of the layer calls is missing, they cost 5 us more on the host: {e}")
+        _binding_module = False
         return None
-    for kind, name in enumerate(_LAYER_ENTRIES):
-        binding.set_entry(kind, ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
-    return binding.layer
+    for set_address, names in ((binding.set_entry, _LAYER_ENTRIES), (binding.set_operator, _OPERATORS)):
+        for kind, name in enumerate(names):
+            set_address(kind, ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
+    _binding_module = binding
+    return binding
 
 
 def _layer_ctypes(kind, X, R, R_intra, Wq, Ws, Y, workspace, dbg_codes, dbg_scales, stream, x_scale=None, w_scale=None):
@@ -712,40 +728,74 @@ def _norm_operands(X, weight, residual, residual_out):
     return M, d, residual_out, _dtype_code(residual)
 
 
+def _product_native(*args):                      # until the first call has put the native function here
+    global _product_native
+    binding = _native_binding()
+    _product_native = binding.product if binding else lambda *args: -1
+    return _product_native(*args)
+
+
+def _norm_native(*args):
+    global _norm_native
+    binding = _native_binding()
+    _norm_native = binding.norm if binding else lambda *args: -1
+    return _norm_native(*args)
+
+
+def _norm(mx, X, weight, residual, eps, out, out_scales, residual_out, stream):
+    """The norm through ctypes, with reasons for what it refuses: the tuple of results."""
+    M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out)
+    if out is None:
+        out = torch.empty((M, d), dtype=torch.uint8 if mx else torch.bfloat16, device=X.device)
+    _operand(out, _BYTES if mx else (torch.bfloat16,), "out_bytes" if mx else "out", (M, d))
+    args = (_ptr(X), _dtype_code(X), _ptr(residual), _ptr(h), r_dtype, _ptr(weight), eps, M, d, _ptr(out))
+    if not mx:
+        _raise(lib().torq_add_rmsnorm(*args, _stream(stream)), "torq_add_rmsnorm")
+        return (out,) if h is None else (out, h)
+    if out_scales is None:
+        out_scales = torch.empty(torq_scales_bytes(M, d), dtype=torch.uint8, device=X.device)
+    _operand(out_scales, _BYTES, "out_scales", at_least=torq_scales_bytes(M, d))
+    _raise(lib().torq_add_rmsnorm_mxfp8(*args, _ptr(out_scales), _stream(stream)), "torq_add_rmsnorm_mxfp8")
+    return (out, out_scales) if h is None else (out, out_scales, h)
+
+
 def torq_add_rmsnorm(X, weight, residual=None, eps: float = 1e-6, out=None, residual_out=None, stream=None):
     """h = X + residual; y = h / sqrt(mean(h^2) + eps) * weight.  X, residual [M,d] float32 or bfloat16, weight [d] bf16.
     Returns y [M,d] bf16, or (y, h) with a residual, h in its type (residual_out=residual: in place)."""
-    M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out)
-    if out is None:
-        out = torch.empty((M, d), dtype=torch.bfloat16, device=X.device)
-    _operand(out, (torch.bfloat16,), "out", (M, d))
-    _raise(lib().torq_add_rmsnorm(_ptr(X), _dtype_code(X), _ptr(residual), _ptr(h), r_dtype, _ptr(weight), eps, M, d, _ptr(out),
-                                  _stream(stream)), "torq_add_rmsnorm")
-    return out if h is None else (out, h)
+    r = _norm_native(False, X, weight, residual, eps, out, None, residual_out, _handle(stream))
+    if r.__class__ is int:
+        if r > 0:
+            raise TorqError(r, "torq_add_rmsnorm")
+        r = _norm(False, X, weight, residual, eps, out, None, residual_out, stream)
+    return r[0] if residual is None else r
 
 
 def torq_add_rmsnorm_mxfp8(X, weight, residual=None, eps: float = 1e-6, out_bytes=None, out_scales=None, residual_out=None,
                            stream=None):
     """torq_add_rmsnorm with y as MXFP8: (E4M3 bytes [M,d] uint8, tiled E8M0 scale bytes[, h]), the A operand of
     torq_mxint4_gemm and torq_mxint4_gated_gemm."""
-    M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out)
-    if out_bytes is None:
-        out_bytes = torch.empty((M, d), dtype=torch.uint8, device=X.device)
-    if out_scales is None:
-        out_scales = torch.empty(torq_scales_bytes(M, d), dtype=torch.uint8, device=X.device)
-    _operand(out_bytes, _BYTES, "out_bytes", (M, d))
-    _operand(out_scales, _BYTES, "out_scales", at_least=torq_scales_bytes(M, d))
-    _raise(lib().torq_add_rmsnorm_mxfp8(_ptr(X), _dtype_code(X), _ptr(residual), _ptr(h), r_dtype, _ptr(weight), eps, M, d,
-                                        _ptr(out_bytes), _ptr(out_scales), _stream(stream)), "torq_add_rmsnorm_mxfp8")
-    return (out_bytes, out_scales) if h is None else (out_bytes, out_scales, h)
+    r = _norm_native(True, X, weight, residual, eps, out_bytes, out_scales, residual_out, _handle(stream))
+    if r.__class__ is int:
+        if r > 0:
+            raise TorqError(r, "torq_add_rmsnorm_mxfp8")
+        r = _norm(True, X, weight, residual, eps, out_bytes, out_scales, residual_out, stream)
+    return r
 
 
 _IN_BF16 = object()
 
 
-def _product(name, A, As, Wq, Ws, scales, per_byte, gated, out_dtype, Y, stream):
-    """Y = A W^T of one format.  As _IN_BF16: A is bf16 [M,K]; else codes of `per_byte` to a byte, as Wq's are.  scales: the
-    tensor scales behind each operand's scale bytes (NVFP4)."""
+def _product(kind, A, As, Wq, Ws, out_dtype, Y, stream, a_scale=0.0, w_scale=0.0):
+    """Y = A W^T of one format and kind (a number in _OPERATORS).  As _IN_BF16: A is bf16 [M,K]; else codes, as Wq's are."""
+    if Y is not None or out_dtype in _FLOATS:
+        r = _product_native(kind, A, As, Wq, Ws, Y, out_dtype is torch.float32, _handle(stream), a_scale, w_scale)
+        if r.__class__ is not int:
+            return r
+        if r > 0:
+            raise TorqError(r, _OPERATORS[kind])
+    # through ctypes, with reasons for what it refuses
+    name, per_byte, gated = _OPERATORS[kind], 1 if kind == 8 else 2, kind >= 3
+    scales = (a_scale, w_scale) if kind % 3 == 1 else ()
     bf16 = As is _IN_BF16
     _operand(A, (torch.bfloat16,) if bf16 else _BYTES, "X" if bf16 else "A")
     _operand(Wq, _BYTES, "W")
@@ -771,48 +821,48 @@ def _product(name, A, As, Wq, Ws, scales, per_byte, gated, out_dtype, Y, stream)
 
 def torq_mxfp4_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """X [M,K] bf16 (few tokens) times MXFP4 weights Wq [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product("torq_mxfp4_matvec", X, _IN_BF16, Wq, Ws, (), 2, False, out_dtype, Y, stream)
+    return _product(0, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream)
 
 
 def torq_nvfp4_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, stream=None):
     """X [M,K] bf16 (few tokens) times NVFP4 weights Wq [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product("torq_nvfp4_matvec", X, _IN_BF16, Wq, Ws, (w_tensor_scale,), 2, False, out_dtype, Y, stream)
+    return _product(1, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, w_scale=w_tensor_scale)
 
 
 def torq_mxint4_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """X [M,K] bf16 (few tokens) times MXINT4 weights in their stored form Wn [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product("torq_mxint4_matvec", X, _IN_BF16, Wn, Ws, (), 2, False, out_dtype, Y, stream)
+    return _product(2, X, _IN_BF16, Wn, Ws, out_dtype, Y, stream)
 
 
 def torq_mxfp4_gated_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """silu(X Wg^T) * (X Wu^T) of few tokens, X [M,K] bf16, Wq [2N,K/2] MXFP4 with the gate rows first -> Y [M,N]."""
-    return _product("torq_mxfp4_gated_matvec", X, _IN_BF16, Wq, Ws, (), 2, True, out_dtype, Y, stream)
+    return _product(3, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream)
 
 
 def torq_nvfp4_gated_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, stream=None):
     """The same with NVFP4 weights."""
-    return _product("torq_nvfp4_gated_matvec", X, _IN_BF16, Wq, Ws, (w_tensor_scale,), 2, True, out_dtype, Y, stream)
+    return _product(4, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, w_scale=w_tensor_scale)
 
 
 def torq_mxint4_gated_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """The same with MXINT4 weights in their stored form."""
-    return _product("torq_mxint4_gated_matvec", X, _IN_BF16, Wn, Ws, (), 2, True, out_dtype, Y, stream)
+    return _product(5, X, _IN_BF16, Wn, Ws, out_dtype, Y, stream)
 
 
 def torq_mxfp4_gated_gemm(Aq, As, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """silu(A Wg^T) * (A Wu^T): Aq [M,K/2], Wq [2N,K/2] MXFP4 codes with the gate rows first, As, Ws tiled -> Y [M,N]."""
-    return _product("torq_mxfp4_gated_gemm", Aq, As, Wq, Ws, (), 2, True, out_dtype, Y, stream)
+    return _product(6, Aq, As, Wq, Ws, out_dtype, Y, stream)
 
 
 def torq_nvfp4_gated_gemm(Aq, As, a_tensor_scale: float, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None,
                           stream=None):
     """The same on NVFP4 operands."""
-    return _product("torq_nvfp4_gated_gemm", Aq, As, Wq, Ws, (a_tensor_scale, w_tensor_scale), 2, True, out_dtype, Y, stream)
+    return _product(7, Aq, As, Wq, Ws, out_dtype, Y, stream, a_tensor_scale, w_tensor_scale)
 
 
 def torq_mxint4_gated_gemm(A8, As, W8, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """The same on operand bytes: A8 [M,K] E4M3 with E8M0 scales (MXINT4 or torq_add_rmsnorm_mxfp8's), W8 [2N,K]."""
-    return _product("torq_mxint4_gated_gemm", A8, As, W8, Ws, (), 1, True, out_dtype, Y, stream)
+    return _product(8, A8, As, W8, Ws, out_dtype, Y, stream)
 
 
 # ---- calibration of the inter-block rotation (Section 5.1, Algorithm 1; offline) -----------------------

@@ -142,3 +142,18 @@ def test_feed_forward_block_captured_and_on_another_stream():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(captured, both()))
     assert torq.torq_last_device_error() == 0
+
+
+def test_calls_through_ctypes_are_the_same(monkeypatch):
+    """The native marshalling and the one that stands in for it where it cannot be had."""
+    d, F, M = 512, 1408, 4
+    up, down = ffn_weights(gen(0), d, F)
+    x, r, w = norm_inputs(M, d, torch.bfloat16, torch.bfloat16)
+
+    def both():
+        return (*ffn_decode(x, r, w, up, down), *ffn_prefill(x, r, w, up, down), torq.torq_add_rmsnorm(x, w), *torq.torq_add_rmsnorm_mxfp8(x, w))
+
+    want = both()
+    monkeypatch.setattr(torq, "_product_native", lambda *a: -1)
+    monkeypatch.setattr(torq, "_norm_native", lambda *a: -1)
+    assert all(torch.equal(a, b) and a.dtype is b.dtype for a, b in zip(both(), want, strict=True))
