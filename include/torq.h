@@ -345,8 +345,8 @@ torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void
  *   (half the bytes of the operand form torq_mxint4_gemm takes), nibble -8 included;  Y [M, N] of y_dtype
  * Products exact, sums float32: x is widened to float16 after a power of two per token and 128 of K that brings the largest magnitude into
  * [2^14, 2^15), so what is smaller than 2^-31 of that magnitude loses bits (as it would beside it in a float32 sum).  Weights of
- * magnitude 2^100 and more may overflow.  The weights are read once per 32 tokens (once altogether up to there): made for decoding,
- * any M <= 2^20 is served.  K % 128 == 0, N % 8 == 0.  One launch, no scratch. */
+ * magnitude 2^100 and more may overflow.  The weights are read once per 32 tokens (16 or 8 where K is long): made for decoding, any M
+ * <= 2^18 is served.  K % 128 == 0, K <= 65536, N % 8 == 0.  One launch, no scratch. */
 torq_status torq_mxfp4_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
                               void* stream);
 torq_status torq_nvfp4_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K, void* Y,
@@ -357,7 +357,7 @@ torq_status torq_mxint4_matvec(const void* X, const void* Wn, const void* Ws, in
 /* The gated pair of projections of a feed-forward block, in one launch:
  *   Y[m,n] = silu(g) u,  g = sum_k x[m,k] w^[n,k],  u = sum_k x[m,k] w^[N+n,k],  silu(g) = g / (1 + exp(-g)), float32 up to Y
  * Both projections are one weight matrix of 2 N rows, gate rows first (Wq [2N, K/2], Ws of 2 N rows); Y [M, N] of y_dtype.
- * Otherwise as the products above.  N % 128 == 0, K % 128 == 0. */
+ * Otherwise as the products above.  N % 128 == 0. */
 torq_status torq_mxfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
                                     torq_dtype y_dtype, void* stream);
 torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K,

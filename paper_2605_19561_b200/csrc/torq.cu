@@ -104,13 +104,15 @@ static bool opt_in_format() {
          opt_in_smem(gemm_fewtok_kernel<FMT, 1>, few_gemm) && opt_in_smem(gemm_fewtok_kernel<FMT, 2>, few_gemm);
 }
 
+constexpr int kMaxSmem = 232448;             // of a CTA that has its SM to itself
 // The products of few tokens of one format.
-template <int FMT>
+template <int FMT, int NT>
 static bool opt_in_matvec() {
-  using C = MatvecCfg<FMT>;
-  return opt_in_smem(matvec_kernel<FMT, 1, false>, C::smem_bytes(1, false, 8)) && opt_in_smem(matvec_kernel<FMT, 1, true>, C::smem_bytes(1, true, 8)) &&
-         opt_in_smem(matvec_kernel<FMT, 2, false>, C::smem_bytes(2, false, 8)) && opt_in_smem(matvec_kernel<FMT, 2, true>, C::smem_bytes(2, true, 8)) &&
-         opt_in_smem(matvec_kernel<FMT, 4, false>, C::smem_bytes(4, false, 8)) && opt_in_smem(matvec_kernel<FMT, 4, true>, C::smem_bytes(4, true, 8));
+  return opt_in_smem(matvec_kernel<FMT, NT, false>, kMaxSmem) && opt_in_smem(matvec_kernel<FMT, NT, true>, kMaxSmem);
+}
+template <int FMT>
+static bool opt_in_matvecs() {
+  return opt_in_matvec<FMT, 1>() && opt_in_matvec<FMT, 2>() && opt_in_matvec<FMT, 4>();
 }
 
 // CTA pairs of a kernel that fills its SMs.
@@ -147,7 +149,7 @@ static DeviceState* device_state() {
     }
     const bool ok = opt_in_smem(fewtok_fit_kernel, RotFewCfg::max_smem_bytes()) && opt_in_format<FMT_MXFP4>() &&
                     opt_in_format<FMT_NVFP4>() && opt_in_format<FMT_MXINT4>() &&
-                    opt_in_matvec<FMT_MXFP4>() && opt_in_matvec<FMT_NVFP4>() && opt_in_matvec<FMT_MXINT4>() &&
+                    opt_in_matvecs<FMT_MXFP4>() && opt_in_matvecs<FMT_NVFP4>() && opt_in_matvecs<FMT_MXINT4>() &&
                     opt_in_smem(rotate_quantize_kernel<256, FMT_F32OUT>, RotCfg<256>::SMEM_BYTES) &&
                     opt_in_smem(rotate_quantize_pair_kernel<FMT_F32OUT>, RotPairCfg::SMEM_BYTES);
     if (!ok) return nullptr;
@@ -1000,19 +1002,32 @@ static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const voi
   return launch_status();
 }
 
-// CTAs in a cluster of the few-token product: the largest of 8, 4, 2, 1 that keeps all CTAs resident at once.
-static int matvec_cluster(int64_t tiles, int64_t k_tiles, int ctas_per_sm, int sm_count) {
+template <int FMT, int NT, bool GATED>
+static torq_status matvec_launch(DeviceState* st, const CUtensorMap& tmW, const void* X, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                 torq_dtype y_dtype, float alpha, cudaStream_t s) {
+  using C = MatvecCfg<FMT, NT>;
+  const int tokens = (int)(M < 8 * NT ? M : 8 * NT), k_tiles = (int)((K + C::BK - 1) / C::BK);
+  const int64_t tiles = GATED ? N / 64 : (N + 127) / 128, groups = (M + 8 * NT - 1) / (8 * NT);
+  // CTAs in a cluster: the most that keep all CTAs resident at once, 8 to 1 (us, S = 1 / 2 / 4 / 8, MXFP4, 1 token: 5120 x 5120 (40 tiles)
+  // 12.6 / 10.6 / 8.9 / 7.1; 5120 x 51200 (400 tiles) 31.8 / 34.1 / 38.9 / 54.5), but not so few that the x of a range leaves room for one CTA
+  // on an SM only (8 tokens, 5120 x 51200, S = 1 / 2 53.8 / 45.3).
   int S = 8;
-  while (S > 1 && (S > k_tiles || tiles * S > (int64_t)ctas_per_sm * sm_count)) S /= 2;
-  return S;
+  auto smem_of = [&](int s) { return C::smem_bytes(tokens, (k_tiles + s - 1) / s, GATED); };
+  while (S > 1 && (S > k_tiles || (tiles * groups * S > (int64_t)C::CTAS_PER_SM * st->sm_count && smem_of(S / 2) <= 112 * 1024))) S /= 2;
+  const int smem = smem_of(S);
+  launch_tc(matvec_kernel<FMT, NT, GATED>, S, dim3((unsigned)(tiles * S), (unsigned)groups), dim3(C::THREADS), smem, s, tmW,
+            static_cast<const __nv_bfloat16*>(X), static_cast<const uint8_t*>(Ws), Y, y_dtype == TORQ_BF16 ? 1 : 0, (int)M, (int)N, (int)K, S, alpha,
+            st->err_word);
+  return launch_status();
 }
+
+static_assert(MatvecCfg<FMT_NVFP4, 1>::smem_bytes(8, 32, true) <= kMaxSmem, "K of up to 65536");
 
 template <int FMT, bool GATED>
 static torq_status matvec_impl(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
                                float alpha, void* stream) {
-  using C = MatvecCfg<FMT>;
   if (!X || !Wq || !Ws || !Y) return TORQ_ERR_NULL;
-  if (M < 1 || K < 128 || K % 128 != 0 || M > (1 << 20) || N > (1 << 29) || K > (1 << 24) || (GATED ? N < 128 || N % 128 != 0 : N < 8 || N % 8 != 0))
+  if (M < 1 || K < 128 || K % 128 != 0 || M > (1 << 18) || N > (1 << 29) || K > (1 << 16) || (GATED ? N < 128 || N % 128 != 0 : N < 8 || N % 8 != 0))
     return TORQ_ERR_SHAPE;
   if (!dtype_ok(y_dtype)) return TORQ_ERR_SHAPE;
   if (!aligned16(X) || !aligned16(Wq) || !aligned16(Ws) || !aligned16(Y)) return TORQ_ERR_ALIGN;
@@ -1021,17 +1036,14 @@ static torq_status matvec_impl(const void* X, const void* Wq, const void* Ws, in
   if (!st->arch_ok) return TORQ_ERR_ARCH;
   CUtensorMap tmW;
   if (!encode_2d(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(GATED ? 2 * N : N), (uint64_t)(K / 2), 64, 128)) return TORQ_ERR_LAUNCH;
-  const int nt = M <= 8 ? 1 : (M <= 16 ? 2 : 4);
-  const int64_t tiles = GATED ? N / 64 : (N + 127) / 128, groups = (M + 8 * nt - 1) / (8 * nt);
-  const int S = matvec_cluster(tiles * groups, (K + C::BK - 1) / C::BK, nt == 1 ? 3 : 2, st->sm_count);
-  const dim3 grid((unsigned)(tiles * S), (unsigned)groups);
-  auto launch = [&](auto kernel) {
-    launch_tc(kernel, S, grid, dim3(C::THREADS), C::smem_bytes(nt, GATED, S), static_cast<cudaStream_t>(stream), tmW,
-              static_cast<const __nv_bfloat16*>(X), static_cast<const uint8_t*>(Ws), Y, y_dtype == TORQ_BF16 ? 1 : 0, (int)M, (int)N, (int)K, S,
-              alpha, st->err_word);
-  };
-  launch(nt == 1 ? matvec_kernel<FMT, 1, GATED> : (nt == 2 ? matvec_kernel<FMT, 2, GATED> : matvec_kernel<FMT, 4, GATED>));
-  return launch_status();
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  // 8, 16 or 32 tokens at a time, fewer where an eighth of K has no room in shared memory for more
+  const int steps = (int)((K + 256 * 8 - 1) / (256 * 8));
+  if (M > 16 && MatvecCfg<FMT, 4>::smem_bytes((int)(M < 32 ? M : 32), steps, GATED) <= kMaxSmem)
+    return matvec_launch<FMT, 4, GATED>(st, tmW, X, Ws, M, N, K, Y, y_dtype, alpha, s);
+  if (M > 8 && MatvecCfg<FMT, 2>::smem_bytes((int)(M < 16 ? M : 16), steps, GATED) <= kMaxSmem)
+    return matvec_launch<FMT, 2, GATED>(st, tmW, X, Ws, M, N, K, Y, y_dtype, alpha, s);
+  return matvec_launch<FMT, 1, GATED>(st, tmW, X, Ws, M, N, K, Y, y_dtype, alpha, s);
 }
 
 // The gated pair of projections on quantized activations: the pair kernel at every number of rows.

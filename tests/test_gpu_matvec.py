@@ -126,6 +126,18 @@ def test_a_token_does_not_depend_on_its_batch(fmt):
     assert torch.equal(matvec(fmt, X[3:4].contiguous(), W, out_dtype=torch.float32), Y[3:4])
 
 
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,K", [(3, 65536), (12, 40960), (20, 28672), (40, 57344)])
+def test_long_contractions(fmt, gated, M, K):
+    """Where fewer tokens go together than otherwise."""
+    g, N = gen(K), 128
+    W = quantized(g, 2 * N if gated else N, K, fmt)
+    X = (heavy(g, M, K) * 0.02).to(torch.bfloat16)
+    Y = matvec(fmt, X, W, gated, out_dtype=torch.float32)
+    (check_gated if gated else check_sums)(Y, X.double(), W[3], matvec_steps(K))
+
+
 def test_stream_argument():
     g = gen(3)
     W = quantized(g, 256, 512, "mxfp4")

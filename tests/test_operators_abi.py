@@ -49,8 +49,8 @@ def test_matvec_argument_errors(fmt, gated):
 
     for k in ("X", "W", "s", "Y"):
         assert call(**{k: None}) == NULL and call(**{k: ODD}) == ALIGN
-    assert call(M=0) == SHAPE and call(M=(1 << 20) + 1) == SHAPE
-    assert call(K=192) == SHAPE and call(K=0) == SHAPE and call(K=1 << 25) == SHAPE
+    assert call(M=0) == SHAPE and call(M=(1 << 18) + 1) == SHAPE
+    assert call(K=192) == SHAPE and call(K=0) == SHAPE and call(K=65536 + 128) == SHAPE and call(K=1 << 25) == SHAPE
     assert call(N=0) == SHAPE and call(N=-128) == SHAPE and call(N=132) == SHAPE and call(N=1 << 30) == SHAPE
     if gated:
         assert call(N=64) == SHAPE and call(N=192) == SHAPE
