@@ -343,27 +343,33 @@ torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void
  * activations that were rotated before): Y[m,n] = sum_k x[m,k] w^[n,k], w^ the dequantized weights.
  *   X [M, K] bf16;  Wq [N, K/2], Ws: the weight operands of torq_mxfp4_gemm / torq_nvfp4_gemm; MXINT4: Wn [N, K/2] in the STORED form
  *   (half the bytes of the operand form torq_mxint4_gemm takes), nibble -8 included;  Y [M, N] of y_dtype
- * Products exact, sums float32: x is widened to float16 after a power of two per token and 128 of K that brings the largest magnitude into
- * [2^14, 2^15), so what is smaller than 2^-31 of that magnitude loses bits (as it would beside it in a float32 sum).  Weights of
- * magnitude 2^100 and more may overflow.  The weights are read once per 32 tokens (16 or 8 where K is long): made for decoding, any M
- * <= 2^18 is served.  K % 128 == 0, K <= 65536, N % 8 == 0.  One launch, no scratch. */
+ *   workspace: torq_matvec_workspace_bytes(M, N, K) bytes, 256-byte aligned; NULL where that is 0 (up to 4 tokens, unless a CTA's range of K
+ *   is long)
+ * Products exact, sums float32.  The tensor cores do not take bfloat16 beside 4-bit weights, so x is split exactly into eight 3-bit digits,
+ * each an FP4 operand, after it has been rounded to a multiple of 2^-21 of the power of two at or below the largest magnitude of its block of
+ * 32 (NVFP4: 16, and a block's counts as 2^-17 of the largest in the token at least): elements down to 2^-14 of the block's largest keep all
+ * their bits, nothing is off by more than 2^-22 of it.  What is smaller than 2^-106 counts as zero in part or whole; MXINT4: magnitudes of 2^125
+ * and more as not a number.
+ * Weights are read from HBM once, for 16 tokens at a time (gated and MXINT4: 8) that find them in the L2: made for decoding, any M <= 2^18 is
+ * served.  K % 128 == 0, K <= 65536, N % 8 == 0.  One launch without a workspace, else two; two calls that may overlap need a workspace each. */
+size_t torq_matvec_workspace_bytes(int64_t M, int64_t N, int64_t K);
 torq_status torq_mxfp4_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
-                              void* stream);
+                              void* workspace, size_t workspace_bytes, void* stream);
 torq_status torq_nvfp4_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K, void* Y,
-                              torq_dtype y_dtype, void* stream);
+                              torq_dtype y_dtype, void* workspace, size_t workspace_bytes, void* stream);
 torq_status torq_mxint4_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
-                               void* stream);
+                               void* workspace, size_t workspace_bytes, void* stream);
 
 /* The gated pair of projections of a feed-forward block, in one launch:
  *   Y[m,n] = silu(g) u,  g = sum_k x[m,k] w^[n,k],  u = sum_k x[m,k] w^[N+n,k],  silu(g) = g / (1 + exp(-g)), float32 up to Y
  * Both projections are one weight matrix of 2 N rows, gate rows first (Wq [2N, K/2], Ws of 2 N rows); Y [M, N] of y_dtype.
  * Otherwise as the products above.  N % 128 == 0. */
 torq_status torq_mxfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
-                                    torq_dtype y_dtype, void* stream);
+                                    torq_dtype y_dtype, void* workspace, size_t workspace_bytes, void* stream);
 torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K,
-                                    void* Y, torq_dtype y_dtype, void* stream);
+                                    void* Y, torq_dtype y_dtype, void* workspace, size_t workspace_bytes, void* stream);
 torq_status torq_mxint4_gated_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
-                                     torq_dtype y_dtype, void* stream);
+                                     torq_dtype y_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The same on quantized activations, the activation and the product in the epilogue of the block-scaled GEMM (M rows, from
  * decoding to prefill): operands as torq_mxfp4_gemm, torq_nvfp4_gemm and torq_mxint4_gemm take them, weights of 2 N rows, gate

@@ -7,8 +7,8 @@
 //   layer(kind, X, R, R_intra, Wq, Ws, Y, workspace, dbg_codes, dbg_scales, stream[, x_scale, w_scale])
 //     -> the library's status, or -1 when an operand is not what the call takes (the caller then finds out which).
 //   set_operator(kind, address)   kind 0..2: torq_{mxfp4,nvfp4,mxint4}_matvec, 3..5: _gated_matvec, 6..8: _gated_gemm, 9, 10:
-//                                 torq_add_rmsnorm, _mxfp8
-//   product(kind, A, As, W, Ws, Y, float32 out, stream, a_scale, w_scale) -> Y, or a status or -1 as above
+//                                 torq_add_rmsnorm, _mxfp8, 11: torq_matvec_workspace_bytes
+//   product(kind, A, As, W, Ws, Y, float32 out, stream, a_scale, w_scale, workspace) -> Y, or a status or -1 as above
 //   norm(mxfp8, X, weight, residual, eps, out, out_scales, residual_out, stream) -> the tuple of results, or a status or -1
 // These two make the results that are None: a call through ctypes takes the host 12 us, and the GPU as little as 2.5.
 // Operands that may be missing are None; stream is None (the current one) or a cudaStream_t as an integer.
@@ -103,7 +103,7 @@ PyObject* layer(PyObject*, PyObject* const* a, Py_ssize_t n) try {
 }
 
 // ---- the operators around the layer ----------------------------------------------------------------------------------
-enum { kNorm = 9, kNormMx = 10, kOperators = 11 };
+enum { kNorm = 9, kNormMx = 10, kMatvecWorkspace = 11, kOperators = 12 };
 void* g_operator[kOperators] = {};
 
 PyObject* set_operator(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -134,8 +134,8 @@ void* stream_of(PyObject* o) { return o == Py_None ? (void*)c10::cuda::getCurren
 
 PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
   HANDLE_TH_ERRORS
-  const long kind = n == 10 ? PyLong_AsLong(a[0]) : -1;
-  if (kind < 0 || kind >= kNorm || !g_operator[kind]) {
+  const long kind = n == 11 ? PyLong_AsLong(a[0]) : -1;
+  if (kind < 0 || kind >= kNorm || !g_operator[kind] || !g_operator[kMatvecWorkspace]) {
     if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "product(): wrong arguments");
     return nullptr;
   }
@@ -159,18 +159,29 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!y || !is_float(*y) || !is_matrix(*y, M, N)) return PyLong_FromLong(-1);
     Y = *y;
   }
+  at::Tensor scratch;
+  size_t scratch_bytes = 0;
+  if (!gemm && a[10] != Py_None) {
+    const at::Tensor* t = plain(a[10], device);
+    if (!t) return PyLong_FromLong(-1);
+    scratch = *t;
+    scratch_bytes = (size_t)t->nbytes();
+  } else if (!gemm) {
+    scratch_bytes = reinterpret_cast<decltype(&torq_matvec_workspace_bytes)>(g_operator[kMatvecWorkspace])(M, N, K);
+    if (scratch_bytes) scratch = at::empty({(int64_t)scratch_bytes}, W->options());
+  }
   void* stream = stream_of(a[7]);
   const float a_scale = nv ? (float)PyFloat_AsDouble(a[8]) : 0.f, w_scale = nv ? (float)PyFloat_AsDouble(a[9]) : 0.f;
   if (PyErr_Occurred()) return nullptr;
   const void *ap = A->data_ptr(), *asp = gemm ? As->data_ptr() : nullptr, *wp = W->data_ptr(), *wsp = Ws->data_ptr();
-  void *yp = Y.data_ptr(), *f = g_operator[kind];
+  void *yp = Y.data_ptr(), *f = g_operator[kind], *sp = scratch.defined() ? scratch.data_ptr() : nullptr;
   const torq_dtype dt = dtype_of(Y);
   torq_status rc;
   Py_BEGIN_ALLOW_THREADS;                                // a launch may wait for room in the stream's queue
   if (gemm && nv) rc = reinterpret_cast<decltype(&torq_nvfp4_gated_gemm)>(f)(ap, asp, a_scale, wp, wsp, w_scale, M, N, K, yp, dt, stream);
   else if (gemm) rc = reinterpret_cast<decltype(&torq_mxfp4_gated_gemm)>(f)(ap, asp, wp, wsp, M, N, K, yp, dt, stream);
-  else if (nv) rc = reinterpret_cast<decltype(&torq_nvfp4_matvec)>(f)(ap, wp, wsp, w_scale, M, N, K, yp, dt, stream);
-  else rc = reinterpret_cast<decltype(&torq_mxfp4_matvec)>(f)(ap, wp, wsp, M, N, K, yp, dt, stream);
+  else if (nv) rc = reinterpret_cast<decltype(&torq_nvfp4_matvec)>(f)(ap, wp, wsp, w_scale, M, N, K, yp, dt, sp, scratch_bytes, stream);
+  else rc = reinterpret_cast<decltype(&torq_mxfp4_matvec)>(f)(ap, wp, wsp, M, N, K, yp, dt, sp, scratch_bytes, stream);
   Py_END_ALLOW_THREADS;
   if (rc != TORQ_OK) return PyLong_FromLong((long)rc);
   if (a[5] == Py_None) return THPVariable_Wrap(std::move(Y));

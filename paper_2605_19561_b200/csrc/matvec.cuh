@@ -1,430 +1,556 @@
 // Products of a few tokens with 4-bit weights, the activations in bfloat16 (not quantized):
 //   y[m, n] = alpha sum_k x[m, k] w^[n, k],   w^ = code * block scale
 // and the gated pair of projections, both stacked in one weight matrix [2 N, K]:
-//   y[m, n] = silu(g) u,  g / u = the product with row n / N + n,  silu(g) = g / (1 + exp(-g)).
-// Streaming the weights from HBM once is the work (K / 2 bytes and K / 32 or K / 16 scale bytes per row).
+//   y[m, n] = silu(g) u,  g / u = the product with row n / N + n.
+// Streaming the weights from HBM once is the work (K / 2 bytes and K / 32 or K / 16 scale bytes per row).  They go to the block-scaled
+// FP4 instruction as they are: widened to float16 in registers for warp-level instructions, they took 146 instructions per
+// 16 x 128 weights and the kernel was bound by those (1 x 5120 -> 5120 7.0 us, now 5.2; 16 tokens 11.5, now 8.0; 32 x 5120 -> 51200 107, now 42).
 //
-// The tensor cores' block-scaled instructions want both operands in few bits, so the codes are widened here: to float16,
-// exactly (e2m1 by the conversion instruction, 41 pairs per clock and SM measured against 22 by masks and shifts; integers by
-// a mask and a subtraction), and contracted by the warp-level mma.m16n8k16 with float32 accumulators: 16 features x 8 tokens.
-// Its rate (1013 multiply-adds per clock and SM measured) is 2.7 times what the weights' stream asks for at 8 tokens.
-//  * x becomes float16 as well, per token and 128 of K scaled by a power of two that puts the largest magnitude into [2^14, 2^15):
-//    bfloat16's 8 bits are kept exactly down to 2^-31 of that magnitude, and what is smaller than 2^-39 of it is lost.  The
-//    power of two comes back in float32 when the 128 products have been added.
-//  * MXFP4 and MXINT4: the sum over one block of 32 is multiplied by the block's power of two in float32.  NVFP4: the E4M3 scale
-//    goes into the codes (e2m1 x e4m3 has 6 significant bits and lies in [2^-10, 2688]: exact in float16).
+// What the instruction cannot take is a bfloat16 activation, so x is written as a sum of numbers that it can.  Per block of 32 (NVFP4: 16)
+// with largest magnitude in [2^E, 2^(E+1)), v = rint(x 2^(21-E)) is an integer of at most 22 bits and a sign; in base 8 with digits
+// -4 ... 3,
+//   v = sum_t d_t 8^(7-t), t = 0 ... 7,   x = sum_t d_t 2^(E-3t),
+// every digit is an e2m1 number and 2^(E-3t) a block scale: a token becomes eight rows of an MXFP4 operand, whose products with a
+// feature add up to the token's.  bfloat16's 8 bits are kept exactly down to 2^-14 of the block's largest magnitude, and nothing is off by more than
+// 2^-22 of it: half a unit of the sum that a float32 accumulator would make of the block.  (NVFP4 scales reach from 2^-9 to 2^8: the scale
+// of a block is taken relative to the token's largest one in this CTA's range of K, 2^(E-R+8), not below 2^(R-17), and the powers 8^-t
+// and 2^(R-8) are multiplied in when the eight sums are added.)
+// The digits cost some 200 instructions per eight elements of x.  Up to FEW_TOK tokens every CTA writes those of its own range of K, once
+// per 128 features, which saves a launch; more tokens have them written once, by a kernel of its own, into the caller's workspace.
 //
-// A CTA has 128 rows of W (gated: 64 of the gate and the 64 of the up projection that belong to them) and a range of K; a CLUSTER of S
-// CTAs shares the rows.  The x of its range is widened ahead of the contraction, by all warps (one of nine doing it stage by stage for
-// the others was what the kernel waited for: 8 tokens, 5120 x 51200, 55.9 us against 39.9).  Then warp 8 fetches W by TMA (256 of K per
-// stage: 128 bytes per row in the 128-byte swizzle, and the scales' 512-byte chunks) and warps 0..7 contract.  Up to 16 tokens such a
-// warp has two instructions' rows (32) and half of the stage's K, which halves what it reads of x; above, 16 rows and all of it.
-// Gated: rows 0..7 of an instruction are gates, 8..15 the ups of the same features, so that both sums of a feature meet in one lane.
-// ldmatrix gives lane (g, t) = (lane / 4, lane % 4) word t of a block of rows g and g + 8: eight elements that stay in their order,
-// so that x is read in its own order, 16 bytes per block.
-// Every warp stores its partial sums straight into the shared memory of the CTA that owns its rows (st.async in a cluster), which adds
-// them in the order of their ranks.
+// MXINT4: a two's-complement nibble n is no e2m1 number, but n = 2 (l + 4 h) with l the e2m1 value of the code n & 3 (0, 1/2, 1, 3/2) and h that of
+// its upper half (0, 4, -8, -4 over 8: codes 0, 1, 10, 9): two operands from one, six logical instructions per eight weights, in shared
+// memory.  Both are multiplied with the same digits, h with scales two powers higher, into one accumulator.
+//
+// Swapped operands as in the few-token GEMM: the instruction's 128 rows are features, its columns the rows of digits.  A CTA has 128
+// features (gated: the 128 gates and the 128 ups of the same features, two accumulators) and a range of K; a CLUSTER of S CTAs shares the
+// features.  Roles: warp 0 fetches W and its scales, warp 1 issues the instructions, warps 2..5 write the digits of every stage (a token
+// each, other ones at the next stage, so that few tokens still keep all four busy) and add up and store at the end.  The partial sums
+// go from registers to the CTA that owns a quarter of the features and 4 tokens (gated: 2), which adds them in the order of their ranks.
 #pragma once
 #include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <type_traits>
 #include "activation.cuh"
 #include "sm100_ptx.cuh"
 
 namespace torq {
 
-template <int FMT, int NT>
-struct MatvecCfg {
-  static constexpr int ROWS = 128;
+template <int FMT, bool GATED>
+struct DigitsCfg {
+  static constexpr bool PLANES = FMT == FMT_MXINT4;
+  static constexpr int BF = 128;                       // features per tile
   static constexpr int BK = 256;                       // elements of K per stage (128 bytes per row)
-  static constexpr int W_BYTES = ROWS * 128;
-  static constexpr int CH = FMT == FMT_NVFP4 ? 4 : 2;  // scale chunks per stage and 128-row tile
-  static constexpr int STAGES = 3;
+  static constexpr int DIGITS = 8;
+  static constexpr int MAX_TOK = GATED || PLANES ? 8 : 16;   // tokens of a CTA
+  static constexpr int FEW_TOK = 4;                    // up to here the product's CTAs may write the digits themselves
+  static constexpr int PER_UNIT = GATED ? 2 : 4;       // tokens of what an epilogue warp adds up at a time
+  static constexpr int TILES = GATED ? 2 : 1;          // of W per stage
+  static constexpr int TILE_BYTES = (PLANES ? 2 : 1) * BF * 128;
+  static constexpr int W_BYTES = TILES * TILE_BYTES;
+  static constexpr int CH = FMT == FMT_NVFP4 ? 4 : 2;  // scale chunks per stage and 128 rows
+  static constexpr int SF_BYTES = CH * 512;
+  static constexpr int SF_SETS = TILES + (PLANES ? 2 : 1);   // of W's tiles and of the digits
+  static constexpr int MAX_STAGES = 4;
+  static constexpr int CTAS_PER_SM = PLANES && GATED ? 1 : 2;
+  static constexpr int MAX_SMEM = CTAS_PER_SM == 2 ? 113 * 1024 : 232448;
+  static constexpr int THREADS = 192;
   static constexpr int MAX_CLUSTER = 8;
-  static constexpr int WARPS = 8;                      // that contract
-  static constexpr int RT = NT > 2 ? 1 : 2;            // instructions' rows per warp: the warps split a stage's K RT ways
-  static constexpr int THREADS = 32 * (WARPS + 1);
-  static constexpr int BAR_BYTES = 128;
-  // what arrives at the owner of 8 / S instructions' rows: 16 bytes per lane and eight tokens from RT warps of S CTAs
-  static constexpr int RECV_BYTES = WARPS * RT * 512 * NT;
-  static constexpr int CTAS_PER_SM = NT == 1 ? 3 : 2;
-  __host__ __device__ static constexpr int stage_bytes(bool gated) { return W_BYTES + (gated ? 2 : 1) * CH * 512; }
-  // float16 row of a token (eight lanes that read 16 bytes of two rows hit all banks), and the powers of two of 8 NT tokens per 128 of K
-  __host__ __device__ static constexpr int x_row(int steps) { return steps * BK * 2 + 64; }
-  __host__ __device__ static constexpr int x_bytes(int tokens, int steps) { return tokens * x_row(steps) + steps * 2 * 32 * NT; }
-  // `tokens` of a group, `steps`: the longest range of K, in stages
-  __host__ __device__ static constexpr int smem_bytes(int tokens, int steps, bool gated) {
-    return 1024 + STAGES * stage_bytes(gated) + x_bytes(tokens, steps) + RECV_BYTES + BAR_BYTES;
+  static constexpr int BAR_BYTES = 256;
+  static constexpr int PART_BYTES = 32 * 16;           // a unit's partial sums from one CTA: 16 bytes per feature
+  __host__ __device__ static constexpr int rows(int tokens) { return (DIGITS * tokens + 15) / 16 * 16; }
+  __host__ __device__ static constexpr int stage_bytes(int r) { return (W_BYTES + r * 128 + SF_SETS * SF_BYTES + 1023) / 1024 * 1024; }
+  __host__ __device__ static constexpr int units(int tokens) { return 4 * ((tokens + PER_UNIT - 1) / PER_UNIT); }
+  __host__ __device__ static constexpr int push_bytes(int tokens) { return (units(tokens) + MAX_CLUSTER - 1) * PART_BYTES; }
+  __host__ __device__ static constexpr int smem_bytes(int tokens, int stages, int S) {
+    return 1024 + stages * stage_bytes(rows(tokens)) + (S > 1 ? push_bytes(tokens) : 0) + BAR_BYTES;
   }
+  // accumulators, then the scale chunks of W and of the digits (4 columns each)
+  __host__ __device__ static constexpr int tmem_cols(int r) {
+    const int n = TILES * r + SF_SETS * 4 * CH;
+    return n <= 32 ? 32 : (n <= 64 ? 64 : (n <= 128 ? 128 : 256));
+  }
+  static_assert(TILES * rows(MAX_TOK) + SF_SETS * 4 * CH <= 256, "two CTAs share an SM's tensor memory");
+  static_assert(smem_bytes(MAX_TOK, 2, MAX_CLUSTER) <= MAX_SMEM, "two stages at least");
 };
 
-__device__ __forceinline__ void mma_16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// Four 8 x 8 matrices of 16-bit pairs: lane l gives the address of row l % 8 of matrix l / 8 and gets word l % 4 of row l / 4 of each.
-__device__ __forceinline__ void ldmatrix_x4(uint32_t a, uint32_t (&r)[4]) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a));
-}
-// The same with nothing to add to.
-__device__ __forceinline__ void mma_16816_f16_first(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
-  return v;
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 v;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
-  return v;
-}
-
-// Eight codes of one word -> four float16 pairs.  e2m1: elements (0,1) (2,3) (4,5) (6,7); integers: (0,4) (1,5) (2,6) (3,7), the
-// order in which a mask finds them (x is stored in the same one).
-template <int FMT>
-__device__ __forceinline__ void widen8(uint32_t w, uint32_t (&p)[4]) {
-  if constexpr (FMT == FMT_MXINT4) {
-    // nibble n of [-8, 8) into float16's mantissa: the bits of 1024 + (n + 8), or of 1024 + 16 (n + 8)
-    auto low = [](uint32_t v) {
-      const uint32_t b = (v & 0x000F000Fu) ^ 0x64086408u;
-      const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&b), __half2half2(__ushort_as_half(0x6408)));          // 1032
-      return *reinterpret_cast<const uint32_t*>(&h);
-    };
-    auto high = [](uint32_t v) {
-      const uint32_t b = (v & 0x00F000F0u) ^ 0x64806480u;
-      const __half2 h = __hfma2(*reinterpret_cast<const __half2*>(&b), __half2half2(__ushort_as_half(0x2C00)),           // 1 / 16
-                                __half2half2(__ushort_as_half(0xD480)));                                                 // -72
-      return *reinterpret_cast<const uint32_t*>(&h);
-    };
-    p[0] = low(w); p[1] = high(w); p[2] = low(w >> 8); p[3] = high(w >> 8);
-  } else {
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-        : "=r"(p[0]), "=r"(p[1]), "=r"(p[2]), "=r"(p[3]) : "r"(w));
+// u_j = v_j + 44444444 (octal) in 24 bits: field t is d_t + 4.  Eight numbers -> eight words, word t the e2m1 codes of the digits t.
+__device__ __forceinline__ void digit_words(const uint32_t (&u)[8], uint32_t (&word)[8]) {
+#pragma unroll
+  for (int t = 0; t < 8; ++t) {
+    uint32_t even = 0, odd = 0;                          // fields of elements 0, 2, 4, 6 and 1, 3, 5, 7, a nibble each
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int from = 21 - 3 * t, to = 4 * (j >> 1);
+      const uint32_t f = (from >= to ? u[j] >> (from - to) : u[j] << (to - from)) & (7u << to);
+      if (j & 1) odd |= f;
+      else even |= f;
+    }
+    // e2m1 codes of -4 ... 3: 14 13 12 10 0 2 4 5
+    word[t] = __byte_perm(0x0A0C0D0Eu, 0x05040200u, even) | __byte_perm(0xA0C0D0E0u, 0x50402000u, odd);
   }
 }
-// Byte `sel & 3` of a word of E4M3 scales, as a float16 pair (sel: the byte's number twice, as __byte_perm takes it).
-__device__ __forceinline__ uint32_t e4m3_pair(uint32_t word, uint32_t sel) {
-  const uint32_t b = __byte_perm(word, 0, sel);
-  uint32_t r;
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, lo;\n\t}" : "=r"(r) : "r"(b));
-  return r;
+
+// The largest of eight magnitudes, as bits of bfloat16 (what is not a number is larger than all others).
+__device__ __forceinline__ uint32_t largest8(const uint4& x) {
+  const uint32_t a = __vmaxu2(__vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
+  return max(a & 0xFFFFu, a >> 16);
 }
-// The four E8M0 bytes of a word as float32 (by way of bfloat16, which has their range: byte 0 is 2^-127).
-__device__ __forceinline__ void e8m0_values(uint32_t word, float (&v)[4]) {
-  uint32_t a, b;
-  asm("{\n\t.reg .b16 lo, hi;\n\tmov.b32 {lo, hi}, %2;\n\tcvt.rn.bf16x2.ue8m0x2 %0, lo;\n\tcvt.rn.bf16x2.ue8m0x2 %1, hi;\n\t}"
-      : "=r"(a), "=r"(b) : "r"(word));
-  v[0] = __uint_as_float(a << 16); v[1] = __uint_as_float(a & 0xFFFF0000u);
-  v[2] = __uint_as_float(b << 16); v[3] = __uint_as_float(b & 0xFFFF0000u);
+constexpr uint32_t kLeastExponent = 21;                  // field of the smallest E: 2^(E - 21) is the smallest E8M0 scale
+constexpr uint32_t kScaleBinades = 17;                   // NVFP4: from the largest scale down to 2^-9
+
+// The digits of 256 elements of K of a token, eight per lane (x): word[t] has the eight codes of digit t.  Returns the scale bytes of the
+// four blocks that this lane's chunk of scales has (32 lanes share two chunks, NVFP4: four), of digit 0.  `ref`, NVFP4: the exponent field
+// that block scales are relative to.  A whole warp calls this.
+template <int FMT>
+__device__ __forceinline__ uint32_t digits_of_256(const uint4& x, uint32_t ref, int lane, uint32_t (&word)[8]) {
+  // exponent field of the block's largest magnitude: of 32 elements in four lanes, or of 16 in two
+  uint32_t ef = largest8(x);
+  ef = max(ef, __shfl_xor_sync(0xFFFFFFFFu, ef, 1));
+  if constexpr (FMT != FMT_NVFP4) ef = max(ef, __shfl_xor_sync(0xFFFFFFFFu, ef, 2));
+  ef >>= 7;
+  uint32_t four;                                         // this lane's block's scale byte, then those of the chunk
+  if constexpr (FMT == FMT_NVFP4) {
+    ef = max(ef, ref - kScaleBinades);
+    const int q = (int)ef - (int)ref + 8;                // -9 ... 8
+    four = (q >= -6 ? (uint32_t)(q + 7) << 3 : 1u << (q + 9)) << (8 * ((lane >> 1) & 3));
+    four |= __shfl_xor_sync(0xFFFFFFFFu, four, 2);
+    four |= __shfl_xor_sync(0xFFFFFFFFu, four, 4);
+  } else {
+    ef = max(ef, kLeastExponent);
+    four = ef << (8 * ((lane >> 2) & 3));                // 255 where something is not a number: so is the scale, and the sum
+    four |= __shfl_xor_sync(0xFFFFFFFFu, four, 4);
+    four |= __shfl_xor_sync(0xFFFFFFFFu, four, 8);
+  }
+  const float f = __uint_as_float((275u - ef) << 23);    // 2^(21 - E)
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t u[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    // 1.5 2^23 + x 2^(21-E): rounded to an integer by the addition, the bits of 1.5 2^23 + v
+    constexpr uint32_t bias = 044444444u - 0x4B400000u;
+    u[2 * i] = __float_as_uint(fmaf(__uint_as_float(w[i] << 16), f, 12582912.f)) + bias;
+    u[2 * i + 1] = __float_as_uint(fmaf(__uint_as_float(w[i] & 0xFFFF0000u), f, 12582912.f)) + bias;
+  }
+  digit_words(u, word);
+  return four;
 }
-__device__ __forceinline__ uint32_t hmul2_bits(uint32_t a, uint32_t b) {
-  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&v);
+// Where this lane stores the word of scale bytes it has of its chunk, if it does: lane t of those that share a chunk has row t of the
+// token's eight.  `token`: in its 128-row scale tile.
+template <int FMT>
+__device__ __forceinline__ bool digit_scales(uint32_t four, int token, int lane, uint32_t& word, uint32_t& chunk, uint32_t& offset) {
+  constexpr int LANES = FMT == FMT_NVFP4 ? 8 : 16;       // that share a chunk
+  const int t = lane & 7;
+  chunk = lane / LANES;
+  offset = ((token & 3) * 8 + t) * 16 + (token >> 2) * 4;
+  word = FMT == FMT_NVFP4 ? four : four - 0x03030303u * t;   // E8M0: 2^(E - 3t); every byte is 21 at least
+  return LANES == 8 || (lane & 8) == 0;
 }
 
-// grid = (row tiles * S in clusters of S along x, groups of 8 NT tokens).  tmW: Wq [rows, K / 2 bytes], box [64 x 128 B].
-template <int FMT, int NT, bool GATED>
-__global__ void __launch_bounds__(MatvecCfg<FMT, NT>::THREADS, MatvecCfg<FMT, NT>::CTAS_PER_SM)
-matvec_kernel(const __grid_constant__ CUtensorMap tmW, const __nv_bfloat16* __restrict__ X, const uint8_t* __restrict__ Ws,
-              void* __restrict__ Y, int y_is_bf16, int M, int N, int K, int S, float alpha, int* err_word) {
-  using C = MatvecCfg<FMT, NT>;
-  constexpr int CH = C::CH, STAGES = C::STAGES, RT = C::RT;
-  constexpr int STAGE_BYTES = C::stage_bytes(GATED);
+// The digits of all tokens, ahead of the product: codes [8 M, K / 2], scales tiled, and for NVFP4 the exponent field of each token's
+// largest magnitude.  grid = M ceil(K / 2048): a warp has 256 elements of a token.
+template <int FMT>
+__global__ void __launch_bounds__(256)
+matvec_split_kernel(const __nv_bfloat16* __restrict__ X, int K, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales,
+                    uint32_t* __restrict__ exponents) {
+  __shared__ uint32_t top_of[8];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int parts = (K + 2047) / 2048;
+  const int64_t m = blockIdx.x / parts;
+  const int k0 = (int)(blockIdx.x % parts) * 2048 + warp * 256, k = k0 + 8 * lane;
+  griddep_launch_dependents();
+  griddep_wait();
+  const uint4* row = reinterpret_cast<const uint4*>(X + m * K);
+  uint32_t ref = 0;
+  if constexpr (FMT == FMT_NVFP4) {
+    uint32_t top = 0;
+    for (int i0 = threadIdx.x; i0 < K / 8; i0 += 8 * 256) {   // eight loads under way: each takes microseconds behind the next kernel's W
+      uint4 x[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = i0 + 256 * j < K / 8 ? __ldg(row + i0 + 256 * j) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = max(top, largest8(x[j]));
+    }
+    top = __reduce_max_sync(0xFFFFFFFFu, top);
+    if (lane == 0) top_of[warp] = top;
+    __syncthreads();
+    for (int i = 0; i < 8; ++i) top = max(top, top_of[i]);
+    ref = max(top >> 7, kLeastExponent + kScaleBinades);
+    if (blockIdx.x % parts == 0 && threadIdx.x == 0) exponents[m] = ref;
+  }
+  if (k0 >= K) return;
+  const uint4 x = k < K ? __ldg(row + k / 8) : make_uint4(0, 0, 0, 0);
+  uint32_t word[8], w, chunk, offset;
+  const uint32_t four = digits_of_256<FMT>(x, ref, lane, word);
+  if (k < K) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) *reinterpret_cast<uint32_t*>(codes + (8 * m + t) * (K / 2) + k / 2) = word[t];
+  }
+  const int kb4 = K / (FMT == FMT_NVFP4 ? 64 : 128);
+  const bool mine = digit_scales<FMT>(four, (int)(m & 15), lane, w, chunk, offset);
+  const int c = k0 / (FMT == FMT_NVFP4 ? 64 : 128) + (int)chunk;
+  if (mine && c < kb4) *reinterpret_cast<uint32_t*>(scales + ((m >> 4) * kb4 + c) * 512 + offset) = w;
+}
+
+// grid: feature tiles x groups of MAX_TOK tokens (the groups of a tile next to one another: W comes from the L2 for all but the first) x S, in
+// clusters of S.  tmW: Wq, box [128 rows x 128 B].  SPLIT: the digits are there already (tmD: codes [8 M, K / 2], box [rows x 128 B];
+// Ds, exponents); otherwise warps 2..5 write them.
+template <int FMT, bool GATED, bool SPLIT>
+__global__ void __launch_bounds__(192, DigitsCfg<FMT, GATED>::CTAS_PER_SM)
+matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmD, const __nv_bfloat16* __restrict__ X,
+                     const uint8_t* __restrict__ Ws, const uint8_t* __restrict__ Ds, const uint32_t* __restrict__ token_exponents,
+                     void* __restrict__ Y, int y_is_bf16, int M, int N, int K, int S, int groups, int nst, float alpha, int* err_word) {
+  using C = DigitsCfg<FMT, GATED>;
+  constexpr int CH = C::CH, PER = C::PER_UNIT;
   extern __shared__ uint8_t smem_raw[];
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const int rank = blockIdx.x % S, tile = blockIdx.x / S;
-  const int m0 = blockIdx.y * 8 * NT;
-  const int mt = M - m0 < 8 * NT ? M - m0 : 8 * NT;      // tokens of this CTA
-  const int k_tiles = (K + C::BK - 1) / C::BK;           // K % 128 == 0: the last stage may be half
-  const int kb4 = K / (CH == 4 ? 64 : 128);              // scale chunks per row tile
-  const int kt0 = (int)((long long)k_tiles * rank / S), kt1 = (int)((long long)k_tiles * (rank + 1) / S);
-  const int steps = kt1 - kt0;                           // one at least
-  const int x_row = C::x_row((k_tiles + S - 1) / S);
-  const uint32_t x_base = base + STAGES * STAGE_BYTES;
-  const uint32_t sx_base = x_base + (uint32_t)((M < 8 * NT ? M : 8 * NT) * x_row);
-  const uint32_t recv_base = sx_base + (uint32_t)((k_tiles + S - 1) / S * 2 * 32 * NT);
-  const uint32_t bar_base = recv_base + C::RECV_BYTES;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+  const int rank = blockIdx.x % S, nt = blockIdx.x / S / groups, group = blockIdx.x / S % groups;
+  const int m0 = group * C::MAX_TOK;
+  const int mt = M - m0 < C::MAX_TOK ? M - m0 : C::MAX_TOK;   // tokens of this CTA
+  const int rows = C::rows(M < C::MAX_TOK ? M : C::MAX_TOK);
+  const int stage_bytes = C::stage_bytes(rows);
+  constexpr bool PLANES = C::PLANES;
+  const uint32_t b_off = C::W_BYTES, sfw_off = b_off + rows * 128, sfb_off = sfw_off + C::TILES * C::SF_BYTES;
+  const uint32_t bar_off = nst * stage_bytes;
+  const uint32_t bar_base = smem_base + bar_off;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };
-  auto empty_bar = [&](int s) { return bar_base + 8u * (STAGES + s); };
-  const uint32_t recv_bar = bar_base + 8u * (2 * STAGES);   // all partial sums that this CTA owns are here
-  volatile int* cta_abort = reinterpret_cast<volatile int*>(smem_raw + (bar_base + 8u * (2 * STAGES + 1) - smem_u32(smem_raw)));
-  const int n0 = tile * (GATED ? 64 : 128), row1 = GATED ? N + n0 : n0 + 64;   // first rows of the two halves of the tile
+  auto empty_bar = [&](int s) { return bar_base + 8u * (C::MAX_STAGES + s); };
+  const uint32_t accf_bar = bar_base + 8u * (2 * C::MAX_STAGES);
+  auto recv_bar = [&](int w) { return accf_bar + 8u + 8u * w; };   // all partials of the units of epilogue warp w are here
+  const uint32_t recv_base = bar_base + C::BAR_BYTES;
+  auto ready_bar = [&](int s) { return bar_base + 208u + 8u * s; };   // MXINT4: W has been taken apart (and the digits written)
+  volatile uint32_t* exponents = reinterpret_cast<volatile uint32_t*>(smem_gen + bar_off + 112);   // NVFP4: of each token's largest magnitude
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + bar_off + 192);
+  volatile int* cta_abort = reinterpret_cast<volatile int*>(smem_gen + bar_off + 200);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int k_tiles = (K + C::BK - 1) / C::BK;           // K % 128 == 0: the last stage may be half
+  const int kb4 = K / (C::BK / CH);                      // scale chunks per row tile
+  const int kt0 = (int)((long long)k_tiles * rank / S), kt1 = (int)((long long)k_tiles * (rank + 1) / S);
+  const int steps = kt1 - kt0;                           // one at least
+  const uint32_t tmem_cols = C::tmem_cols(rows);
+  // unit u = q + 4 c is quarter q of the tile's features and tokens PER c ...; CTA u % S owns it, its epilogue warp u / S % 4
+  // adds and stores it
+  const int units = C::units(mt);
 
   auto fetch = [&](int it, int s) {
     const int kt = kt0 + it;
-    const uint32_t st = base + s * STAGE_BYTES;
+    const uint32_t st = smem_base + s * stage_bytes;
     const uint32_t sf = 512u * (uint32_t)min(CH, kb4 - CH * kt);
-    mbar_arrive_expect_tx(full_bar(s), (uint32_t)C::W_BYTES + (GATED ? 2u : 1u) * sf);
-    tma_load_2d(st, &tmW, kt * 128, n0, full_bar(s));
-    tma_load_2d(st + C::W_BYTES / 2, &tmW, kt * 128, row1, full_bar(s));
-    bulk_load_1d(st + C::W_BYTES, Ws + ((size_t)(n0 >> 7) * kb4 + CH * kt) * 512, sf, full_bar(s));
-    if constexpr (GATED) bulk_load_1d(st + C::W_BYTES + CH * 512, Ws + ((size_t)(row1 >> 7) * kb4 + CH * kt) * 512, sf, full_bar(s));
+    mbar_arrive_expect_tx(full_bar(s), (uint32_t)(C::TILES * C::BF * 128) + C::TILES * sf + (SPLIT ? (uint32_t)rows * 128u + sf : 0u));
+#pragma unroll
+    for (int w = 0; w < C::TILES; ++w) {
+      const int row_tile = nt + w * (N >> 7);            // gated: N % 128 == 0
+      tma_load_2d(st + w * C::TILE_BYTES, &tmW, kt * 128, row_tile * C::BF, full_bar(s));
+      bulk_load_1d(st + sfw_off + w * C::SF_BYTES, Ws + ((size_t)row_tile * kb4 + CH * kt) * 512, sf, full_bar(s));
+    }
+  };
+  auto fetch_digits = [&](int it, int s) {
+    const int kt = kt0 + it;
+    const uint32_t st = smem_base + s * stage_bytes;
+    tma_load_2d(st + b_off, &tmD, kt * 128, 8 * m0, full_bar(s));
+    bulk_load_1d(st + sfb_off, Ds + ((size_t)(m0 >> 4) * kb4 + CH * kt) * 512, 512u * (uint32_t)min(CH, kb4 - CH * kt), full_bar(s));
   };
   // The weights are constants of the layer: their first stages are asked for before anything else.
-  const int pre = steps < STAGES ? steps : STAGES;
-  if (threadIdx.x == 32 * C::WARPS) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), C::WARPS); }
-    mbar_init(recv_bar, 1);
+  const int pre = steps < nst ? steps : nst;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < nst; ++s) { mbar_init(full_bar(s), SPLIT || PLANES ? 1 : 1 + 4); mbar_init(empty_bar(s), 1); mbar_init(ready_bar(s), 4); }
+    mbar_init(accf_bar, 1);
+    for (int w = 0; w < 4; ++w) mbar_init(recv_bar(w), 1);
     *cta_abort = 0;
     fence_mbar_init();
-    fence_proxy_async_smem();
-    if (S > 1) mbar_arrive_expect_tx(recv_bar, (uint32_t)C::RECV_BYTES);
+    fence_proxy_async_smem();                            // the copy engine sees the initialised barriers
     for (int it = 0; it < pre; ++it) fetch(it, it);
+    if (S > 1)
+      for (int w = 0; w < 4 && rank + S * w < units; ++w)
+        mbar_arrive_expect_tx(recv_bar(w), (uint32_t)((units - rank - S * w + 4 * S - 1) / (4 * S) * S * C::PART_BYTES));
   }
+  if (warp == 1) { tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), tmem_cols); tmem_relinquish(); }
+  tc_fence_before_sync();
   __syncthreads();
   if (S > 1) cluster_arrive_relaxed();                   // the wait stands before the first access to another CTA
+  tc_fence_after_sync();
+  const uint32_t tmem_base = *tmem_slot;
   griddep_launch_dependents();
-  griddep_wait();
 
-  // x of this CTA's range: a warp takes 256 of K of a token, four such pieces at a time; a lane has eight elements (16 bytes)
-  {
-    const int pieces = mt * steps;
-    for (int p0 = warp; p0 < pieces; p0 += 4 * (C::WARPS + 1)) {
-      uint4 xr[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p = p0 + i * (C::WARPS + 1), m = p / steps, k = (kt0 + p - m * steps) * C::BK + 8 * lane;
-        xr[i] = p < pieces && k < K ? __ldg(reinterpret_cast<const uint4*>(X + (int64_t)(m0 + m) * K + k)) : make_uint4(0, 0, 0, 0);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int p = p0 + i * (C::WARPS + 1), m = p / steps, it = p - m * steps;
-        if (p < pieces) {                                // the same for the whole warp
-          const uint32_t w[4] = {xr[i].x, xr[i].y, xr[i].z, xr[i].w};
-          float v[8];
-          float amax = 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            v[2 * e] = __uint_as_float(w[e] << 16);
-            v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
-            amax = fmaxf(amax, fmaxf(fabsf(v[2 * e]), fabsf(v[2 * e + 1])));
-          }
-#pragma unroll
-          for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, o));
-          // 2^14 / 2^floor(log2 amax), at most 2^126: exponent field 127 + 14 - (ef - 127)
-          const uint32_t ef = __float_as_uint(amax) >> 23;
-          const uint32_t fe = ef > 15u ? 268u - ef : 253u;
-          const float f = __uint_as_float(fe << 23);
-          uint32_t o4[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float a = FMT == FMT_MXINT4 ? v[e] : v[2 * e], b = FMT == FMT_MXINT4 ? v[e + 4] : v[2 * e + 1];
-            const __half2 h = __floats2half2_rn(a * f, b * f);
-            o4[e] = *reinterpret_cast<const uint32_t*>(&h);
-          }
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(x_base + (uint32_t)(m * x_row + it * (C::BK * 2) + 16 * lane)), "r"(o4[0]),
-                       "r"(o4[1]), "r"(o4[2]), "r"(o4[3]) : "memory");
-          if ((lane & 15) == 0)
-            asm volatile("st.shared.b32 [%0], %1;" ::"r"(sx_base + (uint32_t)((2 * it + (lane >> 4)) * 32 * NT + 4 * m)), "r"((254u - fe) << 23) : "memory");
-        }
-      }
-    }
-  }
-  __syncthreads();
-
-  if (warp == C::WARPS) {
+  if (warp == 0) {
     // ------------------------------------------------------------------ W
+    if constexpr (SPLIT) {
+      griddep_wait();
+      if (elect_one())
+        for (int it = 0; it < pre; ++it) fetch_digits(it, it);
+      __syncwarp();
+    }
     uint32_t s = 0, phase = 0;
     for (int it = pre; it < steps; ++it) {
       if (!mbar_wait_warp(empty_bar(s), phase, cta_abort, err_word, SITE_PRODUCER_EMPTY)) break;
-      if (elect_one()) fetch(it, s);
+      if (elect_one()) {
+        fetch(it, s);
+        if constexpr (SPLIT) fetch_digits(it, s);
+      }
       __syncwarp();
-      if (++s == STAGES) { s = 0; phase ^= 1; }
+      if ((int)++s == nst) { s = 0; phase ^= 1; }
     }
-    if (S > 1) cluster_wait();
-  } else {
-    // ------------------------------------------------------------------ contraction
-    const int g = lane >> 2, t = lane & 3;
-    const int t0 = RT * (RT == 2 ? warp & 3 : warp);     // first of this warp's instructions' row groups, 0..7
-    const int q0 = RT == 2 ? warp >> 2 : 0;              // and its 128 of K of a stage (RT == 1: both)
-    // the row whose address this lane gives ldmatrix (of the first group), and the swizzled address of its first block
-    const int lrow = GATED ? 8 * t0 + (lane & 7) + 64 * ((lane >> 3) & 1) : 16 * t0 + (lane & 15);
-    const uint32_t w_off = (uint32_t)(lrow * 128 + (((lane >> 4) ^ (lane & 7)) << 4));
-    constexpr uint32_t W_GROUP = (GATED ? 8 : 16) * 128;   // from one group to the next
-    uint32_t x_addr[NT];                                 // tokens that there are not read another one's: their sums are not stored
-#pragma unroll
-    for (int j = 0; j < NT; ++j) x_addr[j] = x_base + (uint32_t)(min(8 * j + g, mt - 1) * x_row + 16 * t);
-    const uint32_t sel = (uint32_t)((t >> 1) * 0x11);    // NVFP4: words 0, 1 of a 32 are its first block of 16
-
-    // scale bytes of rows g and g + 8; the halves of a gated tile start at row 0 or 64 of a scale tile
-    auto sf_cell = [](int r) { return (uint32_t)((r & 31) * 16 + ((r & 127) >> 5) * 4); };
-    uint32_t sf0[RT], sf1[RT];
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int a = (GATED ? 8 : 16) * (t0 + r) + g;
-      sf0[r] = C::W_BYTES + sf_cell((GATED ? (n0 & 64) : 0) + a);
-      sf1[r] = GATED ? C::W_BYTES + CH * 512 + sf_cell((row1 & 64) + a) : C::W_BYTES + sf_cell(a + 8);
-    }
-    float acc[RT][NT][4];
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) acc[r][j][e] = 0.f;
-
+    if constexpr (!SPLIT) griddep_wait();
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ MMA issuer
+    griddep_wait();                                      // the waits below count the digits, which wait for the kernel before
     bool ok = true;
+    const uint32_t idesc0 = FMT == FMT_NVFP4 ? idesc_nvf4(128, rows) : idesc_mxf4(128, rows, 0, 0);
+    const uint32_t idesc2 = FMT == FMT_NVFP4 ? idesc_nvf4(128, rows) : idesc_mxf4(128, rows, 2, 2);
+    const uint32_t sfb_t = tmem_base + C::TILES * rows, sfw_t = sfb_t + (PLANES ? 2 : 1) * 4 * CH;   // 4 columns per chunk
+    // a group of eight tokens may have the second half of its scale tile: columns 2 and 3 of each chunk
+    const uint32_t sfb_m = sfb_t + (SPLIT && (m0 & 8) ? 2u : 0u);
     uint32_t s = 0, phase = 0;
     for (int it = 0; it < steps; ++it) {
-      if (!__all_sync(0xFFFFFFFFu, mbar_try_wait(full_bar(s), phase)) &&
-          !mbar_wait_warp(full_bar(s), phase, cta_abort, err_word, SITE_MMA_FULL)) { ok = false; break; }
-      const uint32_t st = base + s * STAGE_BYTES;
+      if (!mbar_wait_warp(full_bar(s), phase, cta_abort, err_word, SITE_MMA_FULL)) { ok = false; break; }
+      if (PLANES && !mbar_wait_warp(ready_bar(s), phase, cta_abort, err_word, SITE_MMA_FULL)) { ok = false; break; }
+      tc_fence_after_sync();
+      const bool two = kb4 - CH * (kt0 + it) >= CH;        // K % 256 == 128: the last stage is half
+      const uint32_t st = smem_base + s * stage_bytes;
+      const uint64_t bdesc = make_desc(st + b_off, 16, 1024, kSwizzle128);
+      const uint64_t sfw_d = make_desc(st + sfw_off, 0, 128, 0), sfb_d = make_desc(st + sfb_off, 0, 128, 0);
+      if (elect_one()) {
 #pragma unroll
-      for (int qq = 0; qq < 3 - RT; ++qq) {            // 128 of K
-        const int q = q0 + qq;
-        if (q == 1 && (kt0 + it) * C::BK + 128 >= K) break;
-        const uint32_t xk = (uint32_t)(it * (C::BK * 2) + q * 256);
-        float part[RT][NT][4];
-        uint32_t nv0[RT][2], nv1[RT][2];               // NVFP4: scale words of this 128
-        float mx0[RT][4], mx1[RT][4];                  // else: block scales
+        for (int c = 0; c < CH; ++c) {
+          if (c < CH / 2 || two) {
+            tmem_cp_32x128b_warpx4(sfb_t + 4 * c, sfb_d + 32 * c);
+            if constexpr (PLANES) tmem_cp_32x128b_warpx4(sfb_t + 4 * (CH + c), sfb_d + 32 * (CH + c));
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-          if constexpr (FMT == FMT_NVFP4) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) { nv0[r][h] = lds32(st + sf0[r] + (2 * q + h) * 512); nv1[r][h] = lds32(st + sf1[r] + (2 * q + h) * 512); }
-          } else {
-            e8m0_values(lds32(st + sf0[r] + q * 512), mx0[r]);
-            e8m0_values(lds32(st + sf1[r] + q * 512), mx1[r]);
+            for (int w = 0; w < C::TILES; ++w) tmem_cp_32x128b_warpx4(sfw_t + 4 * (w * CH + c), sfw_d + 32 * (w * CH + c));
           }
         }
 #pragma unroll
-        for (int pair = 0; pair < 2; ++pair) {         // two blocks of 32
-          const uint32_t wa = (st + w_off) ^ (uint32_t)((2 * q + pair) << 5);
-          uint32_t w[RT][4];
+        for (int w = 0; w < C::TILES; ++w) {
+          const uint32_t acc = tmem_base + w * rows, sfw = sfw_t + 4 * CH * w;
 #pragma unroll
-          for (int r = 0; r < RT; ++r) ldmatrix_x4(wa + r * W_GROUP, w[r]);
+          for (int plane = 0; plane < (PLANES ? 2 : 1); ++plane) {
+            const uint64_t adesc = make_desc(st + w * C::TILE_BYTES + plane * C::BF * 128, 16, 1024, kSwizzle128);
+            const uint32_t sfb = sfb_m + 4 * CH * plane, more = (uint32_t)(it | plane) != 0 ? 1u : 0u;
+            if constexpr (FMT == FMT_NVFP4) {            // one chunk per instruction
 #pragma unroll
-          for (int b = 0; b < 2; ++b) {
-            uint4 x[NT];
-#pragma unroll
-            for (int j = 0; j < NT; ++j) x[j] = lds128(x_addr[j] + xk + (2 * pair + b) * 64);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-              uint32_t a0[4], a1[4];
-              widen8<FMT>(w[r][2 * b], a0);
-              widen8<FMT>(w[r][2 * b + 1], a1);
-              if constexpr (FMT == FMT_NVFP4) {
-                const uint32_t f0 = e4m3_pair(nv0[r][pair], sel + b * 0x22u), f1 = e4m3_pair(nv1[r][pair], sel + b * 0x22u);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) { a0[e] = hmul2_bits(a0[e], f0); a1[e] = hmul2_bits(a1[e], f1); }
-              }
-#pragma unroll
-              for (int j = 0; j < NT; ++j) {
-                if constexpr (FMT == FMT_NVFP4) {
-                  if (pair + b == 0) mma_16816_f16_first(part[r][j], a0[0], a1[0], a0[1], a1[1], x[j].x, x[j].y);
-                  else mma_16816_f16(part[r][j], a0[0], a1[0], a0[1], a1[1], x[j].x, x[j].y);
-                  mma_16816_f16(part[r][j], a0[2], a1[2], a0[3], a1[3], x[j].z, x[j].w);
-                } else {
-                  float d[4];
-                  mma_16816_f16_first(d, a0[0], a1[0], a0[1], a1[1], x[j].x, x[j].y);
-                  mma_16816_f16(d, a0[2], a1[2], a0[3], a1[3], x[j].z, x[j].w);
-                  const float f0 = mx0[r][2 * pair + b], f1 = mx1[r][2 * pair + b];
-                  if (pair + b == 0) {
-                    part[r][j][0] = d[0] * f0; part[r][j][1] = d[1] * f0;
-                    part[r][j][2] = d[2] * f1; part[r][j][3] = d[3] * f1;
-                  } else {
-                    part[r][j][0] = fmaf(d[0], f0, part[r][j][0]);
-                    part[r][j][1] = fmaf(d[1], f0, part[r][j][1]);
-                    part[r][j][2] = fmaf(d[2], f1, part[r][j][2]);
-                    part[r][j][3] = fmaf(d[3], f1, part[r][j][3]);
-                  }
-                }
+              for (int j = 0; j < 4; ++j)
+                if (j < 2 || two) mma_nvf4(acc, adesc + 2 * j, bdesc + 2 * j, idesc0, sfw + 4 * j, sfb + 4 * j, (it | j) != 0);
+            } else {                                     // half a chunk (two scale bytes) per instruction
+              mma_mxf4(acc, adesc, bdesc, idesc0, sfw, sfb, more);
+              mma_mxf4(acc, adesc + 2, bdesc + 2, idesc2, sfw, sfb, 1);
+              if (two) {
+                mma_mxf4(acc, adesc + 4, bdesc + 4, idesc0, sfw + 4, sfb + 4, 1);
+                mma_mxf4(acc, adesc + 6, bdesc + 6, idesc2, sfw + 4, sfb + 4, 1);
               }
             }
           }
         }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {                 // x's power of two: tokens 2 t and 2 t + 1
-          uint32_t f0, f1;
-          asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(f0), "=r"(f1) : "r"(sx_base + (uint32_t)((2 * it + q) * 32 * NT + 4 * (8 * j + 2 * t))));
-#pragma unroll
-          for (int r = 0; r < RT; ++r) {
-            acc[r][j][0] = fmaf(part[r][j][0], __uint_as_float(f0), acc[r][j][0]);
-            acc[r][j][1] = fmaf(part[r][j][1], __uint_as_float(f1), acc[r][j][1]);
-            acc[r][j][2] = fmaf(part[r][j][2], __uint_as_float(f0), acc[r][j][2]);
-            acc[r][j][3] = fmaf(part[r][j][3], __uint_as_float(f1), acc[r][j][3]);
-          }
-        }
+        tc_commit(empty_bar(s));
       }
       __syncwarp();
-      if (lane == 0) mbar_arrive(empty_bar(s));
-      if (++s == STAGES) { s = 0; phase ^= 1; }
+      if ((int)++s == nst) { s = 0; phase ^= 1; }
     }
-
-    // CTA r owns row groups r 8 / S ...: [group of these][source: CTA, warp of the group][eight tokens][lane] 16 bytes
-    const int per = C::WARPS / S;
-    if (S > 1) cluster_wait();
+    if (ok && elect_one()) tc_commit(accf_bar);
+    __syncwarp();
+  } else {
+    // ------------------------------------------------------------------ digits, then the sums (warps 2..5)
+    const int ew = warp - 2;
+    griddep_wait();
+    bool ok = true;
+    // MXINT4: the nibbles of a stage's W -> the two operands, in place and behind it, 16 bytes per thread at a time
+    auto take_apart = [&](uint32_t st) {
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int owner = (t0 + r) / per, slot = (t0 + r) - owner * per;
-      const uint32_t to = recv_base + (uint32_t)(((slot * S + rank) * RT + q0) * NT * 512 + lane * 16);
-      if (S > 1) {
-        const uint32_t far = map_to_cta(to, (uint32_t)owner), far_bar = map_to_cta(recv_bar, (uint32_t)owner);
+      for (int w = 0; w < C::TILES; ++w)
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-          st_async_v4(far + j * 512, __float_as_uint(acc[r][j][0]), __float_as_uint(acc[r][j][1]), __float_as_uint(acc[r][j][2]),
-                      __float_as_uint(acc[r][j][3]), far_bar);
-      } else {                                           // launched without clusters (st.async then faults): plain stores and a barrier
+        for (int i = 0; i < C::BF * 128 / (16 * 128); ++i) {
+          const uint32_t a = st + w * C::TILE_BYTES + i * 2048 + (threadIdx.x - 64) * 16;
+          uint32_t n[4], h[4];
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(n[0]), "=r"(n[1]), "=r"(n[2]), "=r"(n[3]) : "r"(a));
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-          asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to + j * 512), "f"(acc[r][j][0]), "f"(acc[r][j][1]), "f"(acc[r][j][2]),
-                       "f"(acc[r][j][3]) : "memory");
-      }
-    }
-    if (S == 1) named_barrier_sync(1, 32 * C::WARPS);
-    if (warp < per && ok) {
-      if (S > 1) ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(recv_bar, 0, cta_abort, err_word, SITE_EPI_ACC_FULL));
-      if (ok) {
-        const int n = n0 + (rank * per + warp) * (GATED ? 8 : 16) + g;
-#pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          float v[4] = {0.f, 0.f, 0.f, 0.f};
-          for (int r = 0; r < RT * S; ++r) {             // the result does not depend on timing
-            const uint4 p = lds128(recv_base + (uint32_t)(((warp * S * RT + r) * NT + j) * 512 + lane * 16));
-            v[0] += __uint_as_float(p.x); v[1] += __uint_as_float(p.y);
-            v[2] += __uint_as_float(p.z); v[3] += __uint_as_float(p.w);
+          for (int e = 0; e < 4; ++e) {
+            // bits b3 b2 of a nibble -> sign b3, magnitude code 1 if b2, else 2 if b3
+            const uint32_t up2 = n[e] >> 2, up1 = n[e] >> 1;
+            h[e] = (n[e] & 0x88888888u) | (up2 & 0x11111111u) | (up2 & ~up1 & 0x22222222u);
+            n[e] &= 0x33333333u;
           }
-          // lane (g, t) has rows g, g + 8 of tokens 8 j + 2 t, 2 t + 1
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(n[0]), "r"(n[1]), "r"(n[2]), "r"(n[3]) : "memory");
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a + C::BF * 128), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+        }
+    };
+    if constexpr (SPLIT && PLANES) {
+      uint32_t s = 0, phase = 0;
+      for (int it = 0; it < steps; ++it) {
+        if (!mbar_wait_warp(full_bar(s), phase, cta_abort, err_word, SITE_MMA_FULL)) { ok = false; break; }
+        const uint32_t st = smem_base + s * stage_bytes;
+        take_apart(st);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int m = 8 * j + 2 * t + e;
-            auto put = [&](int col, float y) {
-              if (col < N) {
-                const int64_t o = (int64_t)(m0 + m) * N + col;
-                if (y_is_bf16) static_cast<__nv_bfloat16*>(Y)[o] = __float2bfloat16_rn(y);
-                else static_cast<float*>(Y)[o] = y;
-              }
-            };
-            if (m < mt) {
-              if constexpr (GATED) {
-                put(n, silu(v[e] * alpha) * (v[2 + e] * alpha));
-              } else {
-                put(n, v[e] * alpha);
-                put(n + 8, v[2 + e] * alpha);
-              }
+        for (int i = 0; i < C::SF_BYTES / 512; ++i) {    // the digits' scales for the upper halves: two powers higher
+          const uint32_t a = st + sfb_off + i * 512 + (threadIdx.x - 64) * 4;
+          uint32_t v;
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a));
+          asm volatile("st.shared.b32 [%0], %1;" ::"r"(a + C::SF_BYTES), "r"(__vaddus4(v, 0x02020202u)) : "memory");
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(ready_bar(s));
+        if ((int)++s == nst) { s = 0; phase ^= 1; }
+      }
+    } else if constexpr (SPLIT) {
+      if (FMT == FMT_NVFP4 && warp == 2 && lane < mt) exponents[lane] = token_exponents[m0 + lane];
+      if (FMT == FMT_NVFP4) named_barrier_sync(1, 128);
+    } else {
+      // a warp takes 256 of K of a token, a lane eight elements (16 bytes)
+      auto load = [&](int m, int it) {
+        const int k = (kt0 + it) * C::BK + 8 * lane;
+        return m < mt && k < K ? __ldg(reinterpret_cast<const uint4*>(X + (int64_t)(m0 + m) * K + k)) : make_uint4(0, 0, 0, 0);
+      };
+      if constexpr (FMT == FMT_NVFP4) {
+        for (int m = ew; m < mt; m += 4) {
+          uint32_t top = 0;
+          for (int it = 0; it < steps; it += 8) {
+            uint4 x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = it + j < steps ? load(m, it + j) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = max(top, largest8(x[j]));
+          }
+          top = __reduce_max_sync(0xFFFFFFFFu, top);
+          if (lane == 0) exponents[m] = max(top >> 7, kLeastExponent + kScaleBinades);
+        }
+        named_barrier_sync(1, 128);
+      }
+      constexpr int SLOTS = C::FEW_TOK / 4;
+      uint4 next[SLOTS];
+#pragma unroll
+      for (int j = 0; j < SLOTS; ++j) next[j] = load(4 * j + ew, 0);
+      uint32_t s = 0, phase = PLANES ? 0 : 1;
+      for (int it = 0; it < steps; ++it) {
+        uint4 xr[SLOTS];
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) {
+          xr[j] = next[j];
+          if (it + 1 < steps) next[j] = load(4 * j + ((ew - it - 1) & 3), it + 1);
+        }
+        // MXINT4: until W is there, and with it the stage free; else until the stage is free (the first time round the barrier's phase
+        // before its first counts as completed)
+        if (!mbar_wait_warp(PLANES ? full_bar(s) : empty_bar(s), phase, cta_abort, err_word, SITE_PRODUCER_EMPTY)) { ok = false; break; }
+        const uint32_t st = smem_base + s * stage_bytes;
+#pragma unroll
+        for (int j = 0; j < SLOTS; ++j) {
+          const int m = 4 * j + ((ew - it) & 3);
+          if (m < mt) {                                  // the same for the whole warp
+            uint32_t word[8], w, chunk, offset;
+            const uint32_t four = digits_of_256<FMT>(xr[j], FMT == FMT_NVFP4 ? exponents[m] : 0u, lane, word);
+            // row 8 m + t of the operand: 128 bytes in the 128-byte swizzle (8 m + t = t modulo 8)
+            const uint32_t row0 = st + b_off + m * 1024 + (lane & 3) * 4;
+#pragma unroll
+            for (int t = 0; t < 8; ++t)
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(row0 + t * 128 + (((lane >> 2) ^ t) << 4)), "r"(word[t]) : "memory");
+            if (digit_scales<FMT>(four, m, lane, w, chunk, offset)) {
+              asm volatile("st.shared.b32 [%0], %1;" ::"r"(st + sfb_off + chunk * 512 + offset), "r"(w) : "memory");
+              if constexpr (PLANES)
+                asm volatile("st.shared.b32 [%0], %1;" ::"r"(st + sfb_off + C::SF_BYTES + chunk * 512 + offset), "r"(__vaddus4(w, 0x02020202u)) : "memory");
             }
           }
         }
+        if constexpr (PLANES) take_apart(st);
+        fence_proxy_async_smem();                        // the tensor cores see what has been stored
+        __syncwarp();
+        if (lane == 0) mbar_arrive(PLANES ? ready_bar(s) : full_bar(s));
+        if ((int)++s == nst) { s = 0; phase ^= 1; }
       }
     }
+
+    // ---- sums: the accumulator's columns 8 m ... 8 m + 7 are the digits of token m
+    const int q = warp & 3;                              // quarter of the features that this warp can read
+    const uint32_t tacc = tmem_base + ((uint32_t)(q * 32) << 16);
+    ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(accf_bar, 0, cta_abort, err_word, SITE_EPI_ACC_FULL));
+    tc_fence_after_sync();
+    auto add8 = [&](const uint32_t* d, int m) {
+      float y = __uint_as_float(d[7]);                   // from the smallest digit on
+      if constexpr (FMT == FMT_NVFP4) {
+#pragma unroll
+        for (int t = 6; t >= 0; --t) y = fmaf(y, 0.125f, __uint_as_float(d[t]));
+        const uint32_t ref = exponents[m < mt ? m : 0];
+        return y * __uint_as_float(ref == 255u ? 0x7FC00000u : (ref - 8u) << 23);
+      } else {
+#pragma unroll
+        for (int t = 6; t >= 0; --t) y += __uint_as_float(d[t]);
+        return y;
+      }
+    };
+    // the four values of this lane's feature in unit q + 4 c
+    auto partial = [&](int c, float (&p)[4]) {
+      uint32_t d[32];
+      if constexpr (GATED) {
+        tmem_ld_32x32_x16(tacc + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(d));
+        tmem_ld_32x32_x16(tacc + rows + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(d + 16));
+        tmem_ld_wait();
+        p[0] = add8(d, 2 * c); p[1] = add8(d + 16, 2 * c);
+        p[2] = add8(d + 8, 2 * c + 1); p[3] = add8(d + 24, 2 * c + 1);
+      } else {
+        tmem_ld_32x32(tacc + 32 * c, d);
+        tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = add8(d + 8 * i, 4 * c + i);
+      }
+    };
+    auto put = [&](int m, int64_t n, float y) {
+      if (m < mt && n < N) {
+        const int64_t o = (int64_t)(m0 + m) * N + n;
+        if (y_is_bf16) static_cast<__nv_bfloat16*>(Y)[o] = __float2bfloat16_rn(y);
+        else static_cast<float*>(Y)[o] = y;
+      }
+    };
+    auto store = [&](int c, int quarter, const float (&v)[4]) {
+      const int64_t n = (int64_t)nt * C::BF + quarter * 32 + lane;
+      if constexpr (GATED) {
+        put(2 * c, n, silu(v[0] * alpha) * (v[1] * alpha));
+        put(2 * c + 1, n, silu(v[2] * alpha) * (v[3] * alpha));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) put(4 * c + i, n, v[i] * alpha);
+      }
+    };
+    if (S == 1) {
+      if (ok)
+        for (int c = 0; 4 * c < units; ++c) {
+          float p[4];
+          partial(c, p);
+          store(c, q, p);
+        }
+    } else {
+      cluster_wait();
+      if (ok)
+        for (int c = 0; 4 * c < units; ++c) {
+          float p[4];
+          partial(c, p);
+          const int u = q + 4 * c, ui = u / S, owner = u - ui * S;
+          st_async_v4(map_to_cta(recv_base + (uint32_t)((ui * S + rank) * C::PART_BYTES + lane * 16), (uint32_t)owner), __float_as_uint(p[0]),
+                      __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]), map_to_cta(recv_bar(ui & 3), (uint32_t)owner));
+        }
+      if (ok && rank + S * ew < units) {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(recv_bar(ew), 0, cta_abort, err_word, SITE_EPI_ACC_FULL));
+        for (int u = rank + S * ew, ui = ew; u < units && ok; u += 4 * S, ui += 4) {
+          float v[4] = {0.f, 0.f, 0.f, 0.f};             // rank order: the result does not depend on timing
+#pragma unroll
+          for (int r = 0; r < C::MAX_CLUSTER; ++r)
+            if (r < S) {
+              float4 p;
+              asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(p.x), "=f"(p.y), "=f"(p.z), "=f"(p.w)
+                           : "r"(recv_base + (uint32_t)((ui * S + r) * C::PART_BYTES + lane * 16)));
+              v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+            }
+          store(u >> 2, u & 3, v);
+        }
+      }
+    }
+    tc_fence_before_sync();
   }
+  if (S > 1 && warp < 2) cluster_wait();                 // the epilogue warps have waited above
+
+  // ------------------------------------------------------------------ teardown
   __syncthreads();
-  // After a wait has given up, others may still push to this CTA: stay until they have left or given up as well (the
-  // barrier does not count threads that have exited).
-  if (S > 1 && *cta_abort) cluster_sync_all();
+  if (S > 1 && *cta_abort) cluster_sync_all();           // others may still push to this CTA, see the few-token rotation
+  if (warp == 1) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem_base, tmem_cols);
+  }
 }
 
 }  // namespace torq

@@ -104,15 +104,12 @@ static bool opt_in_format() {
          opt_in_smem(gemm_fewtok_kernel<FMT, 1>, few_gemm) && opt_in_smem(gemm_fewtok_kernel<FMT, 2>, few_gemm);
 }
 
-constexpr int kMaxSmem = 232448;             // of a CTA that has its SM to itself
 // The products of few tokens of one format.
-template <int FMT, int NT>
-static bool opt_in_matvec() {
-  return opt_in_smem(matvec_kernel<FMT, NT, false>, kMaxSmem) && opt_in_smem(matvec_kernel<FMT, NT, true>, kMaxSmem);
-}
 template <int FMT>
-static bool opt_in_matvecs() {
-  return opt_in_matvec<FMT, 1>() && opt_in_matvec<FMT, 2>() && opt_in_matvec<FMT, 4>();
+static bool opt_in_digits() {
+  constexpr int plain = DigitsCfg<FMT, false>::MAX_SMEM, gated = DigitsCfg<FMT, true>::MAX_SMEM;
+  return opt_in_smem(matvec_digits_kernel<FMT, false, false>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, false>, gated) &&
+         opt_in_smem(matvec_digits_kernel<FMT, false, true>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, true>, gated);
 }
 
 // CTA pairs of a kernel that fills its SMs.
@@ -149,7 +146,7 @@ static DeviceState* device_state() {
     }
     const bool ok = opt_in_smem(fewtok_fit_kernel, RotFewCfg::max_smem_bytes()) && opt_in_format<FMT_MXFP4>() &&
                     opt_in_format<FMT_NVFP4>() && opt_in_format<FMT_MXINT4>() &&
-                    opt_in_matvecs<FMT_MXFP4>() && opt_in_matvecs<FMT_NVFP4>() && opt_in_matvecs<FMT_MXINT4>() &&
+                    opt_in_digits<FMT_MXFP4>() && opt_in_digits<FMT_NVFP4>() && opt_in_digits<FMT_MXINT4>() &&
                     opt_in_smem(rotate_quantize_kernel<256, FMT_F32OUT>, RotCfg<256>::SMEM_BYTES) &&
                     opt_in_smem(rotate_quantize_pair_kernel<FMT_F32OUT>, RotPairCfg::SMEM_BYTES);
     if (!ok) return nullptr;
@@ -455,6 +452,29 @@ static torq_status quantize_impl(DeviceState* st, const void* Z, torq_dtype dt, 
   return launch_status();
 }
 
+// Whether the digits of x are written ahead of the product, by a kernel of their own: more than FEW_TOK tokens, or a CTA's range of K so long
+// that its own warps would hold up the weights.  (us, MXFP4, product alone / with that kernel: 1 x 5120 -> 5120, 4 steps of 256 5.2 / 5.4, 2
+// tokens 5.6 / 5.5, 4 tokens 6.4 / 5.9; 1 x 14336 -> 4096, 7 steps 7.8 / 8.3; 4 x 4096 -> 1024, 2 steps 3.4 / 4.3; 2 x 5120 -> 51200, 20 steps
+// 30.9 / 28.3; NVFP4 1 x 14336 -> 4096 8.3 / 9.8, 1 x 5120 -> 51200 32.1 / 29.4.)  The steps are counted with the cluster sizes that a part of
+// 148 SMs has room for, so that the answer, which a workspace is sized by, needs no device.
+static bool digits_ahead(int64_t M, int64_t N, int64_t K) {
+  constexpr int fit[9] = {0, 1 << 30, 148, 93, 71, 56, 45, 37, 33};
+  int S = 8;
+  while (S > 1 && (N + 127) / 128 > fit[S]) --S;
+  return M > DigitsCfg<FMT_MXFP4, false>::FEW_TOK || ((K + 255) / 256 + S - 1) / S > 8;
+}
+// Workspace of the few-token products: codes of the digits [8 M, K / 2], their tiled scales, and an exponent per token, each 256-byte
+// aligned; none where the product's CTAs write the digits themselves.
+struct DigitBuffers { size_t scales, exponents, bytes; };
+static DigitBuffers digit_buffers(int fmt, int64_t M, int64_t K) {
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  DigitBuffers b;
+  b.scales = up((size_t)M * 4 * (size_t)K);
+  b.exponents = b.scales + up((size_t)((M + 15) / 16) * (size_t)(K / (fmt == FMT_NVFP4 ? 64 : 128)) * 512);
+  b.bytes = b.exponents + up((size_t)M * 4);
+  return b;
+}
+
 }  // namespace torq
 
 using namespace torq;
@@ -468,6 +488,11 @@ size_t torq_scales_bytes(int64_t rows, int64_t k) {
 
 size_t torq_scale_offset(int64_t row, int64_t kblock, int64_t k) {
   return scale_offset(row, kblock, (k / 32 + 3) / 4);
+}
+
+size_t torq_matvec_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  if (M <= 0 || N <= 0 || K <= 0 || !digits_ahead(M, N, K)) return 0;
+  return digit_buffers(FMT_NVFP4, M, K).bytes;           // the other formats need less
 }
 
 size_t torq_workspace_bytes(int64_t M, int64_t d, int64_t N) {
@@ -1002,48 +1027,55 @@ static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const voi
   return launch_status();
 }
 
-template <int FMT, int NT, bool GATED>
-static torq_status matvec_launch(DeviceState* st, const CUtensorMap& tmW, const void* X, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
-                                 torq_dtype y_dtype, float alpha, cudaStream_t s) {
-  using C = MatvecCfg<FMT, NT>;
-  const int tokens = (int)(M < 8 * NT ? M : 8 * NT), k_tiles = (int)((K + C::BK - 1) / C::BK);
-  const int64_t tiles = GATED ? N / 64 : (N + 127) / 128, groups = (M + 8 * NT - 1) / (8 * NT);
-  // CTAs in a cluster: the most that keep all CTAs resident at once, 8 to 1 (us, S = 1 / 2 / 4 / 8, MXFP4, 1 token: 5120 x 5120 (40 tiles)
-  // 12.6 / 10.6 / 8.9 / 7.1; 5120 x 51200 (400 tiles) 31.8 / 34.1 / 38.9 / 54.5), but not so few that the x of a range leaves room for one CTA
-  // on an SM only (8 tokens, 5120 x 51200, S = 1 / 2 53.8 / 45.3).
+template <int FMT, bool GATED>
+static torq_status matvec_digits(DeviceState* st, const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
+                                 torq_dtype y_dtype, float alpha, void* workspace, cudaStream_t s) {
+  using C = DigitsCfg<FMT, GATED>;
+  CUtensorMap tmW, tmD;
+  const int tokens = (int)(M < C::MAX_TOK ? M : C::MAX_TOK);
+  const int64_t tiles = (N + 127) / 128, groups = (M + C::MAX_TOK - 1) / C::MAX_TOK, k_tiles = (K + C::BK - 1) / C::BK;
+  if (!encode_2d(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(GATED ? 2 * N : N), (uint64_t)(K / 2), C::BF, 128)) return TORQ_ERR_LAUNCH;
+  const bool split = digits_ahead(M, N, K);
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  const DigitBuffers at = digit_buffers(FMT, M, K);
+  if (split) {
+    if (!encode_2d(&tmD, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, ws, (uint64_t)(8 * M), (uint64_t)(K / 2), (uint32_t)C::rows(tokens), 128)) return TORQ_ERR_LAUNCH;
+    launch_tc(matvec_split_kernel<FMT == FMT_NVFP4 ? FMT_NVFP4 : FMT_MXFP4>, 1, dim3((unsigned)((K + 2047) / 2048 * M)), dim3(256), 0, s, static_cast<const __nv_bfloat16*>(X), (int)K, ws,
+              ws + at.scales, reinterpret_cast<uint32_t*>(ws + at.exponents));
+    const torq_status rc = launch_status();
+    if (rc != TORQ_OK) return rc;
+  } else {
+    tmD = tmW;
+  }
+  // Cluster size: the largest whose clusters are all resident at once (us, MXFP4, S = 1 / 2 / 4 / 6 / 8: 1 x 5120 -> 5120 12.6 / 7.8 / 6.2 / 5.8 / 8.7,
+  // 1 x 14336 -> 4096 32.2 / 17.6 / 11.1 / 9.8 / 8.7, 8 x 5120 -> 51200 29.9 / 30.7 / 39.6 / 44.7 / 53.9).
   int S = 8;
-  auto smem_of = [&](int s) { return C::smem_bytes(tokens, (k_tiles + s - 1) / s, GATED); };
-  while (S > 1 && (S > k_tiles || (tiles * groups * S > (int64_t)C::CTAS_PER_SM * st->sm_count && smem_of(S / 2) <= 112 * 1024))) S /= 2;
-  const int smem = smem_of(S);
-  launch_tc(matvec_kernel<FMT, NT, GATED>, S, dim3((unsigned)(tiles * S), (unsigned)groups), dim3(C::THREADS), smem, s, tmW,
-            static_cast<const __nv_bfloat16*>(X), static_cast<const uint8_t*>(Ws), Y, y_dtype == TORQ_BF16 ? 1 : 0, (int)M, (int)N, (int)K, S, alpha,
-            st->err_word);
+  while (S > 1 && (S > k_tiles || tiles * groups > (C::CTAS_PER_SM == 2 ? st->push_fit : st->few_fit)[S])) --S;
+  int nst = C::MAX_STAGES;
+  while (nst > 2 && C::smem_bytes(tokens, nst, S) > C::MAX_SMEM) --nst;
+  launch_tc(split ? matvec_digits_kernel<FMT, GATED, true> : matvec_digits_kernel<FMT, GATED, false>, S, dim3((unsigned)(tiles * groups * S)),
+            dim3(C::THREADS), C::smem_bytes(tokens, nst, S), s, tmW, tmD, static_cast<const __nv_bfloat16*>(X), static_cast<const uint8_t*>(Ws), ws + at.scales,
+            reinterpret_cast<const uint32_t*>(ws + at.exponents), Y, y_dtype == TORQ_BF16 ? 1 : 0, (int)M, (int)N, (int)K, S, (int)groups, nst,
+            C::PLANES ? 2.0f * alpha : alpha, st->err_word);
   return launch_status();
 }
 
-static_assert(MatvecCfg<FMT_NVFP4, 1>::smem_bytes(8, 32, true) <= kMaxSmem, "K of up to 65536");
-
 template <int FMT, bool GATED>
 static torq_status matvec_impl(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
-                               float alpha, void* stream) {
+                               float alpha, void* workspace, size_t workspace_bytes, void* stream) {
   if (!X || !Wq || !Ws || !Y) return TORQ_ERR_NULL;
   if (M < 1 || K < 128 || K % 128 != 0 || M > (1 << 18) || N > (1 << 29) || K > (1 << 16) || (GATED ? N < 128 || N % 128 != 0 : N < 8 || N % 8 != 0))
     return TORQ_ERR_SHAPE;
+  if ((N + 63) / 64 * ((M + 7) / 8) > (1 << 27)) return TORQ_ERR_SHAPE;                         // CTAs are counted in 32 bits
   if (!dtype_ok(y_dtype)) return TORQ_ERR_SHAPE;
   if (!aligned16(X) || !aligned16(Wq) || !aligned16(Ws) || !aligned16(Y)) return TORQ_ERR_ALIGN;
+  const size_t need = torq_matvec_workspace_bytes(M, N, K);
+  if (need && (!workspace || workspace_bytes < need)) return TORQ_ERR_WORKSPACE;
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TORQ_ERR_ALIGN;
   DeviceState* st = device_state();
   if (!st) return TORQ_ERR_LAUNCH;
   if (!st->arch_ok) return TORQ_ERR_ARCH;
-  CUtensorMap tmW;
-  if (!encode_2d(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(GATED ? 2 * N : N), (uint64_t)(K / 2), 64, 128)) return TORQ_ERR_LAUNCH;
-  cudaStream_t s = static_cast<cudaStream_t>(stream);
-  // 8, 16 or 32 tokens at a time, fewer where an eighth of K has no room in shared memory for more
-  const int steps = (int)((K + 256 * 8 - 1) / (256 * 8));
-  if (M > 16 && MatvecCfg<FMT, 4>::smem_bytes((int)(M < 32 ? M : 32), steps, GATED) <= kMaxSmem)
-    return matvec_launch<FMT, 4, GATED>(st, tmW, X, Ws, M, N, K, Y, y_dtype, alpha, s);
-  if (M > 8 && MatvecCfg<FMT, 2>::smem_bytes((int)(M < 16 ? M : 16), steps, GATED) <= kMaxSmem)
-    return matvec_launch<FMT, 2, GATED>(st, tmW, X, Ws, M, N, K, Y, y_dtype, alpha, s);
-  return matvec_launch<FMT, 1, GATED>(st, tmW, X, Ws, M, N, K, Y, y_dtype, alpha, s);
+  return matvec_digits<FMT, GATED>(st, X, Wq, Ws, M, N, K, Y, y_dtype, alpha, workspace, static_cast<cudaStream_t>(stream));
 }
 
 // The gated pair of projections on quantized activations: the pair kernel at every number of rows.
@@ -1566,35 +1598,35 @@ torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void
 }
 
 torq_status torq_mxfp4_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
-                              void* stream) {
-  return matvec_impl<FMT_MXFP4, false>(X, Wq, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  return matvec_impl<FMT_MXFP4, false>(X, Wq, Ws, M, N, K, Y, y_dtype, 1.0f, workspace, workspace_bytes, stream);
 }
 
 torq_status torq_nvfp4_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K, void* Y,
-                              torq_dtype y_dtype, void* stream) {
+                              torq_dtype y_dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (!scale_ok(w_tensor_scale)) return TORQ_ERR_SHAPE;
-  return matvec_impl<FMT_NVFP4, false>(X, Wq, Ws, M, N, K, Y, y_dtype, w_tensor_scale, stream);
+  return matvec_impl<FMT_NVFP4, false>(X, Wq, Ws, M, N, K, Y, y_dtype, w_tensor_scale, workspace, workspace_bytes, stream);
 }
 
 torq_status torq_mxint4_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
-                               void* stream) {
-  return matvec_impl<FMT_MXINT4, false>(X, Wn, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  return matvec_impl<FMT_MXINT4, false>(X, Wn, Ws, M, N, K, Y, y_dtype, 1.0f, workspace, workspace_bytes, stream);
 }
 
-torq_status torq_mxfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
-                                    torq_dtype y_dtype, void* stream) {
-  return matvec_impl<FMT_MXFP4, true>(X, Wq, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+torq_status torq_mxfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
+                                    void* workspace, size_t workspace_bytes, void* stream) {
+  return matvec_impl<FMT_MXFP4, true>(X, Wq, Ws, M, N, K, Y, y_dtype, 1.0f, workspace, workspace_bytes, stream);
 }
 
-torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K,
-                                    void* Y, torq_dtype y_dtype, void* stream) {
+torq_status torq_nvfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, float w_tensor_scale, int64_t M, int64_t N, int64_t K, void* Y,
+                                    torq_dtype y_dtype, void* workspace, size_t workspace_bytes, void* stream) {
   if (!scale_ok(w_tensor_scale)) return TORQ_ERR_SHAPE;
-  return matvec_impl<FMT_NVFP4, true>(X, Wq, Ws, M, N, K, Y, y_dtype, w_tensor_scale, stream);
+  return matvec_impl<FMT_NVFP4, true>(X, Wq, Ws, M, N, K, Y, y_dtype, w_tensor_scale, workspace, workspace_bytes, stream);
 }
 
-torq_status torq_mxint4_gated_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
-                                     torq_dtype y_dtype, void* stream) {
-  return matvec_impl<FMT_MXINT4, true>(X, Wn, Ws, M, N, K, Y, y_dtype, 1.0f, stream);
+torq_status torq_mxint4_gated_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+  return matvec_impl<FMT_MXINT4, true>(X, Wn, Ws, M, N, K, Y, y_dtype, 1.0f, workspace, workspace_bytes, stream);
 }
 
 torq_status torq_mxfp4_gated_gemm(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,

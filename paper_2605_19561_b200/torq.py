@@ -106,10 +106,12 @@ def lib() -> ctypes.CDLL:
     L.torq_add_rmsnorm_mxfp8.argtypes = [vp, ci, vp, vp, ci, vp, f32, i64, i64, vp, vp, vp]
     L.torq_add_rmsnorm_mxfp8.restype = ci
     for name in ("torq_mxfp4_matvec", "torq_mxint4_matvec", "torq_mxfp4_gated_matvec", "torq_mxint4_gated_matvec"):
-        getattr(L, name).argtypes = [vp, vp, vp, i64, i64, i64, vp, ci, vp]
+        getattr(L, name).argtypes = [vp, vp, vp, i64, i64, i64, vp, ci, vp, sz, vp]
         getattr(L, name).restype = ci
+    L.torq_matvec_workspace_bytes.argtypes = [i64, i64, i64]
+    L.torq_matvec_workspace_bytes.restype = sz
     for name in ("torq_nvfp4_matvec", "torq_nvfp4_gated_matvec"):
-        getattr(L, name).argtypes = [vp, vp, vp, f32, i64, i64, i64, vp, ci, vp]
+        getattr(L, name).argtypes = [vp, vp, vp, f32, i64, i64, i64, vp, ci, vp, sz, vp]
         getattr(L, name).restype = ci
     for name in ("torq_mxfp4_gated_gemm", "torq_mxint4_gated_gemm"):
         getattr(L, name).argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, ci, vp]
@@ -145,7 +147,7 @@ _MXFP4, _MXINT4, _STRUCTURED, _NVFP4 = range(4)
 _LAYER_ENTRIES = ("torq_rotated_linear", "torq_rotated_linear_mxint4", "torq_rotated_linear_structured",
                   "torq_rotated_linear_nvfp4")
 _OPERATORS = (*(f"torq_{fmt}_{op}" for op in ("matvec", "gated_matvec", "gated_gemm") for fmt in ("mxfp4", "nvfp4", "mxint4")),
-              "torq_add_rmsnorm", "torq_add_rmsnorm_mxfp8")
+              "torq_add_rmsnorm", "torq_add_rmsnorm_mxfp8", "torq_matvec_workspace_bytes")
 
 
 def _layer(*args):                               # until the first call has put the native function here
@@ -785,10 +787,14 @@ def torq_add_rmsnorm_mxfp8(X, weight, residual=None, eps: float = 1e-6, out_byte
 _IN_BF16 = object()
 
 
-def _product(kind, A, As, Wq, Ws, out_dtype, Y, stream, a_scale=0.0, w_scale=0.0):
+def torq_matvec_workspace_bytes(M: int, N: int, K: int) -> int:
+    return lib().torq_matvec_workspace_bytes(M, N, K)
+
+
+def _product(kind, A, As, Wq, Ws, out_dtype, Y, stream, a_scale=0.0, w_scale=0.0, workspace=None):
     """Y = A W^T of one format and kind (a number in _OPERATORS).  As _IN_BF16: A is bf16 [M,K]; else codes, as Wq's are."""
     if Y is not None or out_dtype in _FLOATS:
-        r = _product_native(kind, A, As, Wq, Ws, Y, out_dtype is torch.float32, _handle(stream), a_scale, w_scale)
+        r = _product_native(kind, A, As, Wq, Ws, Y, out_dtype is torch.float32, _handle(stream), a_scale, w_scale, workspace)
         if r.__class__ is not int:
             return r
         if r > 0:
@@ -815,38 +821,44 @@ def _product(kind, A, As, Wq, Ws, out_dtype, Y, stream, a_scale=0.0, w_scale=0.0
         Y = torch.empty((M, N), dtype=out_dtype, device=A.device)
     _operand(Y, _FLOATS, "Y", (M, N))
     x = (_ptr(A),) if bf16 else (_ptr(A), _ptr(As), *scales[:1])
-    _raise(getattr(lib(), name)(*x, _ptr(Wq), _ptr(Ws), *scales[-1:], M, N, K, _ptr(Y), _dtype_code(Y), _stream(stream)), name)
+    scratch = ()
+    if bf16:
+        if workspace is None:
+            workspace = torch.empty(torq_matvec_workspace_bytes(M, N, K), dtype=torch.uint8, device=A.device)
+        _operand(workspace, (workspace.dtype,), "workspace")
+        scratch = (_ptr(workspace), workspace.nbytes)
+    _raise(getattr(lib(), name)(*x, _ptr(Wq), _ptr(Ws), *scales[-1:], M, N, K, _ptr(Y), _dtype_code(Y), *scratch, _stream(stream)), name)
     return Y
 
 
-def torq_mxfp4_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
+def torq_mxfp4_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, workspace=None, stream=None):
     """X [M,K] bf16 (few tokens) times MXFP4 weights Wq [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product(0, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream)
+    return _product(0, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, workspace=workspace)
 
 
-def torq_nvfp4_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, stream=None):
+def torq_nvfp4_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, workspace=None, stream=None):
     """X [M,K] bf16 (few tokens) times NVFP4 weights Wq [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product(1, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, w_scale=w_tensor_scale)
+    return _product(1, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, w_scale=w_tensor_scale, workspace=workspace)
 
 
-def torq_mxint4_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
+def torq_mxint4_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, workspace=None, stream=None):
     """X [M,K] bf16 (few tokens) times MXINT4 weights in their stored form Wn [N,K/2], Ws tiled -> Y [M,N]."""
-    return _product(2, X, _IN_BF16, Wn, Ws, out_dtype, Y, stream)
+    return _product(2, X, _IN_BF16, Wn, Ws, out_dtype, Y, stream, workspace=workspace)
 
 
-def torq_mxfp4_gated_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
+def torq_mxfp4_gated_matvec(X, Wq, Ws, out_dtype=torch.bfloat16, Y=None, workspace=None, stream=None):
     """silu(X Wg^T) * (X Wu^T) of few tokens, X [M,K] bf16, Wq [2N,K/2] MXFP4 with the gate rows first -> Y [M,N]."""
-    return _product(3, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream)
+    return _product(3, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, workspace=workspace)
 
 
-def torq_nvfp4_gated_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, stream=None):
+def torq_nvfp4_gated_matvec(X, Wq, Ws, w_tensor_scale: float, out_dtype=torch.bfloat16, Y=None, workspace=None, stream=None):
     """The same with NVFP4 weights."""
-    return _product(4, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, w_scale=w_tensor_scale)
+    return _product(4, X, _IN_BF16, Wq, Ws, out_dtype, Y, stream, w_scale=w_tensor_scale, workspace=workspace)
 
 
-def torq_mxint4_gated_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
+def torq_mxint4_gated_matvec(X, Wn, Ws, out_dtype=torch.bfloat16, Y=None, workspace=None, stream=None):
     """The same with MXINT4 weights in their stored form."""
-    return _product(5, X, _IN_BF16, Wn, Ws, out_dtype, Y, stream)
+    return _product(5, X, _IN_BF16, Wn, Ws, out_dtype, Y, stream, workspace=workspace)
 
 
 def torq_mxfp4_gated_gemm(Aq, As, Wq, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):

@@ -110,23 +110,27 @@ def silu(v):
     return v * torch.sigmoid(v)
 
 
-def check_sums(Y, x, w, steps):
+def check_sums(Y, x, w, steps, dx=None):
     """|Y - x w^T| <= steps 2^-22 sum |x| |w| + the rounding of the result.  Products are exact; `steps` additions in float32
     follow one another on the way of a product into the result, each off by at most 2^-23 of the largest partial sum if it
-    truncates; the factor of two leaves room for the power of two that the largest partial sum may exceed the final one by."""
+    truncates; the factor of two leaves room for the power of two that the largest partial sum may exceed the final one by.
+    dx: what x itself is off by."""
     ref, mag = x @ w.t(), x.abs() @ w.abs().t()
     tol = steps * 2.0 ** -22 * mag + HALF_STEP[Y.dtype] * ref.abs() + 1e-40
+    if dx is not None:
+        tol += dx @ w.abs().t()
     assert torch.isfinite(Y).all()
     worst = ((Y.double() - ref).abs() / tol).max().item()
     assert worst <= 1.0, worst
 
 
-def check_gated(Y, x, w, steps):
+def check_gated(Y, x, w, steps, dx=None):
     """The error of both sums as above, through silu(g) u (the derivative of silu is at most 1.1), exp and the quotient at 2^-21."""
     N = w.shape[0] // 2
     g, u = x @ w[:N].t(), x @ w[N:].t()
     e = steps * 2.0 ** -22
-    dg, du = e * (x.abs() @ w[:N].abs().t()), e * (x.abs() @ w[N:].abs().t())
+    dx = e * x.abs() + (0 if dx is None else dx)
+    dg, du = dx @ w[:N].abs().t(), dx @ w[N:].abs().t()
     ref = silu(g) * u
     tol = 1.1 * dg * (u.abs() + du) + silu(g).abs() * du + ref.abs() * (HALF_STEP[Y.dtype] + 2.0 ** -21) + 1e-40
     assert torch.isfinite(Y).all()
@@ -134,9 +138,18 @@ def check_gated(Y, x, w, steps):
     assert worst <= 1.0, worst
 
 
-def matvec_steps(K):
-    """Of the few-token products, in the kernel's order: 8 instructions and 4 block sums per 128 of K, one sum per 128, 8 CTAs."""
-    return 12 + K // 128 + 8
+def matvec_error(fmt, x):
+    """(steps, dx) of the few-token products.  x is rounded to a multiple of 2^-21 of the power of two at or below its block's largest
+    magnitude (NVFP4: a block's counts as 2^-17 of its token's at least); the magnitudes of a number's digits add up to at most
+    three times its own (MXINT4: those of the two halves of a weight to three times its own as well); one instruction per 64 of K
+    (MXINT4: two), what it adds aligned before it is added, then 8 digits and 8 CTAs."""
+    M, K = x.shape
+    block = 16 if fmt == "nvfp4" else 32
+    top = x.abs().view(M, -1, block).amax(-1)
+    if fmt == "nvfp4":
+        top = torch.maximum(top, x.abs().amax(-1, keepdim=True) * 2.0 ** -16)
+    dx = (top * 2.0 ** -22 + 2.0 ** -128).repeat_interleave(block, 1)
+    return (9 * 2 * (K // 32 + 16) if fmt == "mxint4" else 3 * 2 * (K // 64 + 16)), dx
 
 
 def gemm_steps(K):

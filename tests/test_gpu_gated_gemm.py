@@ -3,7 +3,7 @@ against their definitions in 64 bits."""
 import pytest
 import torch
 
-from operator_helpers import (DEV, NORM_REL, check_gated, check_mxfp8, check_sums, gemm_steps, gen, matvec_steps, norm_inputs, norm_ref,
+from operator_helpers import (DEV, NORM_REL, check_gated, check_mxfp8, check_sums, gemm_steps, gen, matvec_error, norm_inputs, norm_ref,
                               quantized, untile, values)
 from paper_2605_19561_b200 import torq
 
@@ -98,8 +98,8 @@ def test_feed_forward_block_decoding(M):
     y, _, z, out = ffn_decode(x, r, w, up, down)
     ref = norm_ref(x, r, w, 1e-6)
     assert ((y.double() - ref).abs() <= (2.0 ** -8 + NORM_REL) * ref.abs()).all()
-    check_gated(z, y.double(), up[3], matvec_steps(d))
-    check_sums(out, z.double(), down[3], matvec_steps(F))
+    check_gated(z, y.double(), up[3], *matvec_error("mxint4", y.double()))
+    check_sums(out, z.double(), down[3], *matvec_error("mxint4", z.double()))
 
 
 @pytest.mark.parametrize("M", [1, 130, 555])

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from operator_helpers import (DEV, check_gated, check_sums, code_values, gen, heavy, matvec_steps, quantized, tile, values)
+from operator_helpers import (DEV, check_gated, check_sums, code_values, gen, heavy, matvec_error, quantized, tile, values)
 from paper_2605_19561_b200 import torq
 
 pytestmark = pytest.mark.gpu
@@ -12,6 +12,10 @@ FMTS = ("mxfp4", "nvfp4", "mxint4")
 def matvec(fmt, X, W, gated=False, **kw):
     f = getattr(torq, f"torq_{fmt}_{'gated_' if gated else ''}matvec")
     return f(X, W[0], W[1], W[2], **kw) if fmt == "nvfp4" else f(X, W[0], W[1], **kw)
+
+
+def launches(M, N, K):
+    return 2 if torq.torq_matvec_workspace_bytes(M, N, K) else 1
 
 
 def tokens(g, M, K):
@@ -26,7 +30,7 @@ def tokens(g, M, K):
 
 
 @pytest.mark.parametrize("fmt", FMTS)
-@pytest.mark.parametrize("N,K", [(8, 128), (136, 256), (200, 384), (1000, 640), (264, 1408), (4096, 1024), (512, 14336)])
+@pytest.mark.parametrize("N,K", [(8, 128), (136, 256), (200, 384), (1000, 640), (264, 1408), (4096, 1024), (512, 14336), (20480, 2304)])
 @pytest.mark.parametrize("M", [1, 2, 7, 8, 9, 16, 17, 33, 70])
 def test_matvec(fmt, M, N, K):
     g = gen(M * 1000 + N)
@@ -36,14 +40,14 @@ def test_matvec(fmt, M, N, K):
     buf = torch.full((M * N + 64,), 7.0, dtype=dtype, device=DEV)
     before = torq.torq_launch_count()
     Y = matvec(fmt, X, W, Y=buf[:M * N].view(M, N))
-    assert torq.torq_launch_count() == before + 1
-    check_sums(Y, X.double(), W[3], matvec_steps(K))
+    assert torq.torq_launch_count() == before + launches(M, N, K)
+    check_sums(Y, X.double(), W[3], *matvec_error(fmt, X.double()))
     assert (buf[M * N:] == 7).all()
     assert torq.torq_last_device_error() == 0
 
 
 @pytest.mark.parametrize("fmt", FMTS)
-@pytest.mark.parametrize("N,K", [(128, 128), (256, 384), (384, 1408), (2048, 4096), (14336, 512)])
+@pytest.mark.parametrize("N,K", [(128, 128), (256, 384), (384, 1408), (2048, 4096), (14336, 512), (25600, 2304)])
 @pytest.mark.parametrize("M", [1, 5, 8, 13, 17, 40])
 def test_gated_matvec(fmt, M, N, K):
     g = gen(M * 1000 + N + 1)
@@ -54,9 +58,9 @@ def test_gated_matvec(fmt, M, N, K):
     buf = torch.full((M * N + 64,), 7.0, dtype=dtype, device=DEV)
     before = torq.torq_launch_count()
     Y = matvec(fmt, X, W, gated=True, Y=buf[:M * N].view(M, N))
-    assert torq.torq_launch_count() == before + 1
+    assert torq.torq_launch_count() == before + launches(M, N, K)
     fine = [m for m in range(M) if m != 4 or M <= 4]     # the product of two huge sums has no float32
-    check_gated(Y[fine], X.double()[fine], W[3], matvec_steps(K))
+    check_gated(Y[fine], X.double()[fine], W[3], *matvec_error(fmt, X.double()[fine]))
     assert (buf[M * N:] == 7).all()
 
 
@@ -70,21 +74,23 @@ def test_block_scales_at_the_ends(fmt):
     X = heavy(g, 3, K).to(torch.bfloat16)
     X[1] = (X[1].double() * 2.0 ** 40).to(torch.bfloat16)
     Y = matvec(fmt, X, (codes, tile(lin), 1.0), out_dtype=torch.float32)
-    check_sums(Y, X.double(), values(codes, lin, fmt), matvec_steps(K))
+    check_sums(Y, X.double(), values(codes, lin, fmt), *matvec_error(fmt, X.double()))
 
 
 @pytest.mark.parametrize("fmt", FMTS)
 def test_small_elements_beside_large_ones(fmt):
-    """Elements down to 2^-30 of their neighbours count in full: the large ones meet codes of zero."""
+    """Elements down to 2^-14 of their block's largest count in full: the large ones meet codes of zero."""
     g, N, K = gen(6), 64, 256
+    large = 2.0 ** 12
     codes, Ws, ts, v = quantized(g, N, K, fmt)
     codes[:, 0] = 0
     v[:, :2] = 0
     X = heavy(g, 2, K).to(torch.bfloat16).clamp(-1, 1)
     X[X.abs() < 0.25] = 0.5
-    X[:, 0] = 2.0 ** 28
+    X[:, 0] = large
     Y = matvec(fmt, X, (codes, Ws, ts), out_dtype=torch.float32)
-    check_sums(Y, torch.cat([X[:, :2] * 0, X[:, 2:]], 1).double(), v, matvec_steps(K))
+    rest = torch.cat([X[:, :2] * 0, X[:, 2:]], 1).double()
+    check_sums(Y, rest, v, matvec_error(fmt, rest)[0])
 
 
 def test_every_code_and_position():
@@ -120,10 +126,31 @@ def test_a_token_does_not_depend_on_its_batch(fmt):
     g, N, K = gen(8), 1024, 2048
     W = quantized(g, N, K, fmt)
     X = heavy(g, 8, K).to(torch.bfloat16)
-    Y = matvec(fmt, X, W, out_dtype=torch.float32)
-    for _ in range(5):
-        assert torch.equal(matvec(fmt, X, W, out_dtype=torch.float32), Y)
-    assert torch.equal(matvec(fmt, X[3:4].contiguous(), W, out_dtype=torch.float32), Y[3:4])
+    for some, one in (((0, 8), 6), ((0, 4), 2)):
+        x = X[some[0]:some[1]].contiguous()
+        Y = matvec(fmt, x, W, out_dtype=torch.float32)
+        for _ in range(5):
+            assert torch.equal(matvec(fmt, x, W, out_dtype=torch.float32), Y)
+        x[one] = X[one + 1 if one > 4 else 0]            # another token changes nothing in the others
+        Z = matvec(fmt, x, W, out_dtype=torch.float32)
+        rest = [m for m in range(x.shape[0]) if m != one]
+        assert torch.equal(Z[rest], Y[rest])
+    assert torch.equal(matvec(fmt, X[3:4].contiguous(), W, out_dtype=torch.float32), matvec(fmt, X[2:4].contiguous(), W, out_dtype=torch.float32)[1:])
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_workspace(fmt):
+    """The caller's own is enough, whatever it held; too small a one is refused."""
+    g, M, N, K = gen(11), 6, 256, 640
+    W = quantized(g, N, K, fmt)
+    X = heavy(g, M, K).to(torch.bfloat16)
+    want = matvec(fmt, X, W)
+    ws = torch.full((torq.torq_matvec_workspace_bytes(M, N, K) + 64,), 0xFF, dtype=torch.uint8, device=DEV)
+    assert torch.equal(matvec(fmt, X, W, workspace=ws[:-64]), want)
+    assert (ws[-64:] == 0xFF).all()
+    with pytest.raises(torq.TorqError) as e:
+        matvec(fmt, X, W, workspace=ws[:256])
+    assert e.value.code == 7
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -135,7 +162,7 @@ def test_long_contractions(fmt, gated, M, K):
     W = quantized(g, 2 * N if gated else N, K, fmt)
     X = (heavy(g, M, K) * 0.02).to(torch.bfloat16)
     Y = matvec(fmt, X, W, gated, out_dtype=torch.float32)
-    (check_gated if gated else check_sums)(Y, X.double(), W[3], matvec_steps(K))
+    (check_gated if gated else check_sums)(Y, X.double(), W[3], *matvec_error(fmt, X.double()))
 
 
 def test_stream_argument():

@@ -8,7 +8,7 @@ import torch
 from paper_2605_19561_b200 import torq
 
 ONE, ODD = ctypes.c_void_p(16), ctypes.c_void_p(24)      # never dereferenced on these paths
-NULL, SHAPE, ALIGN = 1, 2, 3
+NULL, SHAPE, ALIGN, WORKSPACE = 1, 2, 3, 7
 
 
 @pytest.mark.parametrize("mx", [False, True])
@@ -44,8 +44,8 @@ def test_norm_refuses_host_tensors():
 def test_matvec_argument_errors(fmt, gated):
     f = getattr(torq.lib(), f"torq_{fmt}_{'gated_' if gated else ''}matvec")
 
-    def call(X=ONE, W=ONE, s=ONE, ts=1.0, M=3, N=128, K=256, Y=ONE, t=0):
-        return f(X, W, s, *((ts,) if fmt == "nvfp4" else ()), M, N, K, Y, t, None)
+    def call(X=ONE, W=ONE, s=ONE, ts=1.0, M=3, N=128, K=256, Y=ONE, t=0, ws=None, n=0):
+        return f(X, W, s, *((ts,) if fmt == "nvfp4" else ()), M, N, K, Y, t, ws, n, None)
 
     for k in ("X", "W", "s", "Y"):
         assert call(**{k: None}) == NULL and call(**{k: ODD}) == ALIGN
@@ -55,6 +55,12 @@ def test_matvec_argument_errors(fmt, gated):
     if gated:
         assert call(N=64) == SHAPE and call(N=192) == SHAPE
     assert call(t=2) == SHAPE
+    need = torq.torq_matvec_workspace_bytes(5, 128, 256)
+    assert torq.torq_matvec_workspace_bytes(4, 128, 256) == 0 and need >= 5 * 8 * 128 + 512
+    assert torq.torq_matvec_workspace_bytes(1, 51200, 5120) > 0 and torq.torq_matvec_workspace_bytes(0, 128, 256) == 0   # a long range for one CTA
+    big = ctypes.c_void_p(256)
+    assert call(M=5) == WORKSPACE and call(M=5, ws=big, n=need - 1) == WORKSPACE and call(M=5, ws=None, n=need) == WORKSPACE
+    assert call(M=5, ws=ctypes.c_void_p(128), n=need) == ALIGN
     if fmt == "nvfp4":
         assert call(ts=0.0) == SHAPE and call(ts=-1.0) == SHAPE and call(ts=float("inf")) == SHAPE and call(ts=float("nan")) == SHAPE
 
