@@ -40,7 +40,7 @@ struct DigitsCfg {
   static constexpr int BF = 128;                       // features per tile
   static constexpr int BK = 256;                       // elements of K per stage (128 bytes per row)
   static constexpr int DIGITS = 8;
-  static constexpr int MAX_TOK = GATED || PLANES ? 8 : 16;   // tokens of a CTA
+  static constexpr int MAX_TOK = GATED ? 8 : 16;   // tokens of a CTA
   static constexpr int FEW_TOK = 4;                    // up to here the product's CTAs may write the digits themselves
   static constexpr int PER_UNIT = GATED ? 2 : 4;       // tokens of what an epilogue warp adds up at a time
   static constexpr int TILES = GATED ? 2 : 1;          // of W per stage
@@ -59,9 +59,9 @@ struct DigitsCfg {
   __host__ __device__ static constexpr int rows(int tokens) { return (DIGITS * tokens + 15) / 16 * 16; }
   __host__ __device__ static constexpr int stage_bytes(int r) { return (W_BYTES + r * 128 + SF_SETS * SF_BYTES + 1023) / 1024 * 1024; }
   __host__ __device__ static constexpr int units(int tokens) { return 4 * ((tokens + PER_UNIT - 1) / PER_UNIT); }
-  __host__ __device__ static constexpr int push_bytes(int tokens) { return (units(tokens) + MAX_CLUSTER - 1) * PART_BYTES; }
+  __host__ __device__ static constexpr int push_bytes(int tokens, int S) { return S > 1 ? (units(tokens) + S - 1) / S * S * PART_BYTES : 0; }
   __host__ __device__ static constexpr int smem_bytes(int tokens, int stages, int S) {
-    return 1024 + stages * stage_bytes(rows(tokens)) + (S > 1 ? push_bytes(tokens) : 0) + BAR_BYTES;
+    return 1024 + stages * stage_bytes(rows(tokens)) + push_bytes(tokens, S) + BAR_BYTES;
   }
   // accumulators, then the scale chunks of W and of the digits (4 columns each)
   __host__ __device__ static constexpr int tmem_cols(int r) {
@@ -69,7 +69,7 @@ struct DigitsCfg {
     return n <= 32 ? 32 : (n <= 64 ? 64 : (n <= 128 ? 128 : 256));
   }
   static_assert(TILES * rows(MAX_TOK) + SF_SETS * 4 * CH <= 256, "two CTAs share an SM's tensor memory");
-  static_assert(smem_bytes(MAX_TOK, 2, MAX_CLUSTER) <= MAX_SMEM, "two stages at least");
+  static_assert(smem_bytes(MAX_TOK, 2, 1) <= MAX_SMEM, "two stages at least");
 };
 
 // u_j = v_j + 44444444 (octal) in 24 bits: field t is d_t + 4.  Eight numbers -> eight words, word t the e2m1 codes of the digits t.

@@ -1050,7 +1050,7 @@ static torq_status matvec_digits(DeviceState* st, const void* X, const void* Wq,
   // Cluster size: the largest whose clusters are all resident at once (us, MXFP4, S = 1 / 2 / 4 / 6 / 8: 1 x 5120 -> 5120 12.6 / 7.8 / 6.2 / 5.8 / 8.7,
   // 1 x 14336 -> 4096 32.2 / 17.6 / 11.1 / 9.8 / 8.7, 8 x 5120 -> 51200 29.9 / 30.7 / 39.6 / 44.7 / 53.9).
   int S = 8;
-  while (S > 1 && (S > k_tiles || tiles * groups > (C::CTAS_PER_SM == 2 ? st->push_fit : st->few_fit)[S])) --S;
+  while (S > 1 && (S > k_tiles || tiles * groups > (C::CTAS_PER_SM == 2 ? st->push_fit : st->few_fit)[S] || C::smem_bytes(tokens, 2, S) > C::MAX_SMEM)) --S;
   int nst = C::MAX_STAGES;
   while (nst > 2 && C::smem_bytes(tokens, nst, S) > C::MAX_SMEM) --nst;
   launch_tc(split ? matvec_digits_kernel<FMT, GATED, true> : matvec_digits_kernel<FMT, GATED, false>, S, dim3((unsigned)(tiles * groups * S)),
