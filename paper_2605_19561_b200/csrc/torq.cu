@@ -1014,16 +1014,29 @@ static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const voi
     vpt = pieces <= 1024 && M <= 2 * st->sm_count ? 1 : (pieces <= 1024 ? 2 : 4);
     threads = (pieces + 32 * vpt - 1) / (32 * vpt) * 32;
   }
-  const int64_t ctas = (rows + per_cta - 1) / per_cta, per_sm = 2048 / (threads * per_cta) < 16 ? 2048 / (threads * per_cta) : 16;
-  const int64_t most = per_sm * st->sm_count;
-  const dim3 grid((unsigned)(ctas < most ? ctas : most)), block((unsigned)threads, (unsigned)per_cta);
-  const int res = !residual ? RES_NONE : (r_dtype == TORQ_F32 ? RES_F32 : RES_BF16);
+  const int64_t ctas = (rows + per_cta - 1) / per_cta;
   auto launch = [&](auto kernel) {
-    launch_tc(kernel, 1, grid, block, 0, static_cast<cudaStream_t>(stream), X, x_dtype == TORQ_F32 ? 1 : 0, residual, residual_out, res,
-              static_cast<const __nv_bfloat16*>(weight), eps, M, rows, (int)d, out, static_cast<uint8_t*>(out_scales));
+    int per_sm = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads * per_cta, 0) != cudaSuccess || per_sm < 1) per_sm = 1;
+    const int64_t most = (int64_t)per_sm * st->sm_count;
+    launch_tc(kernel, 1, dim3((unsigned)(ctas < most ? ctas : most)), dim3((unsigned)threads, (unsigned)per_cta), 0, static_cast<cudaStream_t>(stream), X, residual,
+              residual_out, static_cast<const __nv_bfloat16*>(weight), eps, M, rows, (int)d, out, static_cast<uint8_t*>(out_scales));
   };
-  if (mx) launch(vpt == 1 ? add_rmsnorm_kernel<1, true> : (vpt == 2 ? add_rmsnorm_kernel<2, true> : add_rmsnorm_kernel<4, true>));
-  else launch(vpt == 1 ? add_rmsnorm_kernel<1, false> : (vpt == 2 ? add_rmsnorm_kernel<2, false> : add_rmsnorm_kernel<4, false>));
+  auto with = [&](auto V, auto MX) {
+    constexpr int v = decltype(V)::value;
+    constexpr bool m = decltype(MX)::value;
+    const bool f32 = x_dtype == TORQ_F32;
+    if (!residual) launch(f32 ? add_rmsnorm_kernel<v, m, true, RES_NONE> : add_rmsnorm_kernel<v, m, false, RES_NONE>);
+    else if (r_dtype == TORQ_F32) launch(f32 ? add_rmsnorm_kernel<v, m, true, RES_F32> : add_rmsnorm_kernel<v, m, false, RES_F32>);
+    else launch(f32 ? add_rmsnorm_kernel<v, m, true, RES_BF16> : add_rmsnorm_kernel<v, m, false, RES_BF16>);
+  };
+  auto pick = [&](auto MX) {
+    if (vpt == 1) with(std::integral_constant<int, 1>{}, MX);
+    else if (vpt == 2) with(std::integral_constant<int, 2>{}, MX);
+    else with(std::integral_constant<int, 4>{}, MX);
+  };
+  if (mx) pick(std::true_type{});
+  else pick(std::false_type{});
   return launch_status();
 }
 
