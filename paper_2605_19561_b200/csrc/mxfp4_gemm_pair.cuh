@@ -330,6 +330,7 @@ mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
       const bool more = accumulator_is_waited_for(tile, npairs, 1, total_tiles);
       if (lane == 0 && more) mbar_arrive_cluster(map_to_cta(acce_bar, 0));   // free again
       if constexpr (GATED) {
+        if (mt * C::BM + q * 32 >= M) continue;            // no row of this warp's is stored
         auto gated = [&](uint32_t g, uint32_t u) {
           const float a = FMT == FMT_NVFP4 ? alpha : 1.0f;
           return __float_as_uint(silu(__uint_as_float(g) * a) * (__uint_as_float(u) * a));
