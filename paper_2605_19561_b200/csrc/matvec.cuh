@@ -34,13 +34,18 @@
 
 namespace torq {
 
-template <int FMT, bool GATED>
+// Where the rows of the second operand come from: digits that warps 2..5 write; digits that were written before, into a workspace; or
+// no digits, the caller's quantized activations, a row per token (the gated GEMM of few tokens).
+enum : int { ROWS_HERE = 0, ROWS_AHEAD = 1, ROWS_QUANTIZED = 2 };
+
+template <int FMT, bool GATED, int ROWS = ROWS_HERE>
 struct DigitsCfg {
   static constexpr bool PLANES = FMT == FMT_MXINT4;
   static constexpr int BF = 128;                       // features per tile
   static constexpr int BK = 256;                       // elements of K per stage (128 bytes per row)
-  static constexpr int DIGITS = 8;
-  static constexpr int MAX_TOK = GATED ? 8 : 16;   // tokens of a CTA
+  static constexpr int DIGITS = ROWS == ROWS_QUANTIZED ? 1 : 8;   // rows per token
+  // tokens of a CTA (quantized: as many as two CTAs have room on an SM for, with their partial sums)
+  static constexpr int MAX_TOK = ROWS == ROWS_QUANTIZED ? (FMT == FMT_NVFP4 ? 24 : 32) : (GATED ? 8 : 16);
   static constexpr int FEW_TOK = 4;                    // up to here the product's CTAs may write the digits themselves
   static constexpr int PER_UNIT = GATED ? 2 : 4;       // tokens of what an epilogue warp adds up at a time
   static constexpr int TILES = GATED ? 2 : 1;          // of W per stage
@@ -191,14 +196,15 @@ matvec_split_kernel(const __nv_bfloat16* __restrict__ X, int K, uint8_t* __restr
 }
 
 // grid: feature tiles x groups of MAX_TOK tokens (the groups of a tile next to one another: W comes from the L2 for all but the first) x S, in
-// clusters of S.  tmW: Wq, box [128 rows x 128 B].  SPLIT: the digits are there already (tmD: codes [8 M, K / 2], box [rows x 128 B];
-// Ds, exponents); otherwise warps 2..5 write them.
-template <int FMT, bool GATED, bool SPLIT>
-__global__ void __launch_bounds__(192, DigitsCfg<FMT, GATED>::CTAS_PER_SM)
+// clusters of S.  tmW: Wq, box [128 rows x 128 B].  tmD, Ds, exponents: the rows where they are there already (codes [8 M or M, K / 2], box
+// [rows x 128 B]; tiled scales); X otherwise.
+template <int FMT, bool GATED, int ROWS>
+__global__ void __launch_bounds__(192, DigitsCfg<FMT, GATED, ROWS>::CTAS_PER_SM)
 matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmD, const __nv_bfloat16* __restrict__ X,
                      const uint8_t* __restrict__ Ws, const uint8_t* __restrict__ Ds, const uint32_t* __restrict__ token_exponents,
                      void* __restrict__ Y, int y_is_bf16, int M, int N, int K, int S, int groups, int nst, float alpha, int* err_word) {
-  using C = DigitsCfg<FMT, GATED>;
+  using C = DigitsCfg<FMT, GATED, ROWS>;
+  constexpr bool SPLIT = ROWS != ROWS_HERE;
   constexpr int CH = C::CH, PER = C::PER_UNIT;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -247,8 +253,8 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
   auto fetch_digits = [&](int it, int s) {
     const int kt = kt0 + it;
     const uint32_t st = smem_base + s * stage_bytes;
-    tma_load_2d(st + b_off, &tmD, kt * 128, 8 * m0, full_bar(s));
-    bulk_load_1d(st + sfb_off, Ds + ((size_t)(m0 >> 4) * kb4 + CH * kt) * 512, 512u * (uint32_t)min(CH, kb4 - CH * kt), full_bar(s));
+    tma_load_2d(st + b_off, &tmD, kt * 128, C::DIGITS * m0, full_bar(s));
+    bulk_load_1d(st + sfb_off, Ds + ((size_t)(C::DIGITS * m0 >> 7) * kb4 + CH * kt) * 512, 512u * (uint32_t)min(CH, kb4 - CH * kt), full_bar(s));
   };
   // The weights are constants of the layer: their first stages are asked for before anything else.
   const int pre = steps < nst ? steps : nst;
@@ -298,8 +304,8 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
     const uint32_t idesc0 = FMT == FMT_NVFP4 ? idesc_nvf4(128, rows) : idesc_mxf4(128, rows, 0, 0);
     const uint32_t idesc2 = FMT == FMT_NVFP4 ? idesc_nvf4(128, rows) : idesc_mxf4(128, rows, 2, 2);
     const uint32_t sfb_t = tmem_base + C::TILES * rows, sfw_t = sfb_t + (PLANES ? 2 : 1) * 4 * CH;   // 4 columns per chunk
-    // a group of eight tokens may have the second half of its scale tile: columns 2 and 3 of each chunk
-    const uint32_t sfb_m = sfb_t + (SPLIT && (m0 & 8) ? 2u : 0u);
+    // a group of 64 rows may have the second half of its scale tile: columns 2 and 3 of each chunk
+    const uint32_t sfb_m = sfb_t + (SPLIT && (C::DIGITS * m0 & 64) ? 2u : 0u);
     uint32_t s = 0, phase = 0;
     for (int it = 0; it < steps; ++it) {
       if (!mbar_wait_warp(full_bar(s), phase, cta_abort, err_word, SITE_MMA_FULL)) { ok = false; break; }
@@ -391,8 +397,10 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         if ((int)++s == nst) { s = 0; phase ^= 1; }
       }
     } else if constexpr (SPLIT) {
-      if (FMT == FMT_NVFP4 && warp == 2 && lane < mt) exponents[lane] = token_exponents[m0 + lane];
-      if (FMT == FMT_NVFP4) named_barrier_sync(1, 128);
+      if (FMT == FMT_NVFP4 && ROWS == ROWS_AHEAD) {
+        if (warp == 2 && lane < mt) exponents[lane] = token_exponents[m0 + lane];
+        named_barrier_sync(1, 128);
+      }
     } else {
       // a warp takes 256 of K of a token, a lane eight elements (16 bytes)
       auto load = [&](int m, int it) {
@@ -474,20 +482,39 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         return y;
       }
     };
-    // the four values of this lane's feature in unit q + 4 c
-    auto partial = [&](int c, float (&p)[4]) {
-      uint32_t d[32];
-      if constexpr (GATED) {
-        tmem_ld_32x32_x16(tacc + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(d));
-        tmem_ld_32x32_x16(tacc + rows + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(d + 16));
-        tmem_ld_wait();
-        p[0] = add8(d, 2 * c); p[1] = add8(d + 16, 2 * c);
-        p[2] = add8(d + 8, 2 * c + 1); p[3] = add8(d + 24, 2 * c + 1);
-      } else {
-        tmem_ld_32x32(tacc + 32 * c, d);
-        tmem_ld_wait();
+    // calls f(c, the four values of this lane's feature in unit q + 4 c) for every c
+    auto units_of_quarter = [&](auto f) {
+      if constexpr (ROWS == ROWS_QUANTIZED) {
+        static_assert(GATED, "the GEMM of one projection has kernels of its own");
+        for (int c0 = 0; 4 * c0 < units; c0 += 16 / PER) {
+          uint32_t d[2][16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = add8(d + 8 * i, 4 * c + i);
+          for (int w = 0; w < 2; ++w) tmem_ld_32x32_x16(tacc + w * rows + PER * c0, d[w]);
+          tmem_ld_wait();
+#pragma unroll
+          for (int i = 0; i < 16 / PER; ++i) {
+            const float p[4] = {__uint_as_float(d[0][2 * i]), __uint_as_float(d[1][2 * i]), __uint_as_float(d[0][2 * i + 1]), __uint_as_float(d[1][2 * i + 1])};
+            if (4 * (c0 + i) < units) f(c0 + i, p);
+          }
+        }
+      } else {
+        for (int c = 0; 4 * c < units; ++c) {
+          uint32_t d[32];
+          float p[4];
+          if constexpr (GATED) {
+            tmem_ld_32x32_x16(tacc + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(d));
+            tmem_ld_32x32_x16(tacc + rows + 16 * c, *reinterpret_cast<uint32_t(*)[16]>(d + 16));
+            tmem_ld_wait();
+            p[0] = add8(d, 2 * c); p[1] = add8(d + 16, 2 * c);
+            p[2] = add8(d + 8, 2 * c + 1); p[3] = add8(d + 24, 2 * c + 1);
+          } else {
+            tmem_ld_32x32(tacc + 32 * c, d);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[i] = add8(d + 8 * i, 4 * c + i);
+          }
+          f(c, p);
+        }
       }
     };
     auto put = [&](int m, int64_t n, float y) {
@@ -508,22 +535,15 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
       }
     };
     if (S == 1) {
-      if (ok)
-        for (int c = 0; 4 * c < units; ++c) {
-          float p[4];
-          partial(c, p);
-          store(c, q, p);
-        }
+      if (ok) units_of_quarter([&](int c, const float (&p)[4]) { store(c, q, p); });
     } else {
       cluster_wait();
       if (ok)
-        for (int c = 0; 4 * c < units; ++c) {
-          float p[4];
-          partial(c, p);
+        units_of_quarter([&](int c, const float (&p)[4]) {
           const int u = q + 4 * c, ui = u / S, owner = u - ui * S;
           st_async_v4(map_to_cta(recv_base + (uint32_t)((ui * S + rank) * C::PART_BYTES + lane * 16), (uint32_t)owner), __float_as_uint(p[0]),
                       __float_as_uint(p[1]), __float_as_uint(p[2]), __float_as_uint(p[3]), map_to_cta(recv_bar(ui & 3), (uint32_t)owner));
-        }
+        });
       if (ok && rank + S * ew < units) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait_cluster(recv_bar(ew), 0, cta_abort, err_word, SITE_EPI_ACC_FULL));
         for (int u = rank + S * ew, ui = ew; u < units && ok; u += 4 * S, ui += 4) {

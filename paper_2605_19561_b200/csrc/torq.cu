@@ -108,8 +108,10 @@ static bool opt_in_format() {
 template <int FMT>
 static bool opt_in_digits() {
   constexpr int plain = DigitsCfg<FMT, false>::MAX_SMEM, gated = DigitsCfg<FMT, true>::MAX_SMEM;
-  return opt_in_smem(matvec_digits_kernel<FMT, false, false>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, false>, gated) &&
-         opt_in_smem(matvec_digits_kernel<FMT, false, true>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, true>, gated);
+  if constexpr (FMT != FMT_MXINT4)
+    if (!opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_QUANTIZED>, gated)) return false;
+  return opt_in_smem(matvec_digits_kernel<FMT, false, ROWS_HERE>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_HERE>, gated) &&
+         opt_in_smem(matvec_digits_kernel<FMT, false, ROWS_AHEAD>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_AHEAD>, gated);
 }
 
 // CTA pairs of a kernel that fills its SMs.
@@ -1040,13 +1042,30 @@ static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const voi
   return launch_status();
 }
 
+template <int FMT, bool GATED, int ROWS>
+static torq_status digits_launch(DeviceState* st, const CUtensorMap& tmW, const CUtensorMap& tmD, const void* X, const void* Ws, const void* Ds,
+                                 const uint32_t* exponents, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype, float alpha, cudaStream_t s) {
+  using C = DigitsCfg<FMT, GATED, ROWS>;
+  const int tokens = (int)(M < C::MAX_TOK ? M : C::MAX_TOK);
+  const int64_t tiles = (N + 127) / 128, groups = (M + C::MAX_TOK - 1) / C::MAX_TOK, k_tiles = (K + C::BK - 1) / C::BK;
+  // Cluster size: the largest whose clusters are all resident at once (us, MXFP4, S = 1 / 2 / 4 / 6 / 8: 1 x 5120 -> 5120 12.6 / 7.8 / 6.2 / 5.8 / 8.7,
+  // 1 x 14336 -> 4096 32.2 / 17.6 / 11.1 / 9.8 / 8.7, 8 x 5120 -> 51200 29.9 / 30.7 / 39.6 / 44.7 / 53.9).
+  int S = C::MAX_CLUSTER;
+  while (S > 1 && (S > k_tiles || tiles * groups > (C::CTAS_PER_SM == 2 ? st->push_fit : st->few_fit)[S] || C::smem_bytes(tokens, 2, S) > C::MAX_SMEM)) --S;
+  int nst = C::MAX_STAGES;
+  while (nst > 2 && C::smem_bytes(tokens, nst, S) > C::MAX_SMEM) --nst;
+  launch_tc(matvec_digits_kernel<FMT, GATED, ROWS>, S, dim3((unsigned)(tiles * groups * S)), dim3(C::THREADS), C::smem_bytes(tokens, nst, S), s, tmW, tmD,
+            static_cast<const __nv_bfloat16*>(X), static_cast<const uint8_t*>(Ws), static_cast<const uint8_t*>(Ds), exponents, Y, y_dtype == TORQ_BF16 ? 1 : 0,
+            (int)M, (int)N, (int)K, S, (int)groups, nst, C::PLANES ? 2.0f * alpha : alpha, st->err_word);
+  return launch_status();
+}
+
 template <int FMT, bool GATED>
 static torq_status matvec_digits(DeviceState* st, const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
                                  torq_dtype y_dtype, float alpha, void* workspace, cudaStream_t s) {
   using C = DigitsCfg<FMT, GATED>;
   CUtensorMap tmW, tmD;
   const int tokens = (int)(M < C::MAX_TOK ? M : C::MAX_TOK);
-  const int64_t tiles = (N + 127) / 128, groups = (M + C::MAX_TOK - 1) / C::MAX_TOK, k_tiles = (K + C::BK - 1) / C::BK;
   if (!encode_2d(&tmW, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(GATED ? 2 * N : N), (uint64_t)(K / 2), C::BF, 128)) return TORQ_ERR_LAUNCH;
   const bool split = digits_ahead(M, N, K);
   uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -1057,20 +1076,11 @@ static torq_status matvec_digits(DeviceState* st, const void* X, const void* Wq,
               ws + at.scales, reinterpret_cast<uint32_t*>(ws + at.exponents));
     const torq_status rc = launch_status();
     if (rc != TORQ_OK) return rc;
-  } else {
-    tmD = tmW;
   }
-  // Cluster size: the largest whose clusters are all resident at once (us, MXFP4, S = 1 / 2 / 4 / 6 / 8: 1 x 5120 -> 5120 12.6 / 7.8 / 6.2 / 5.8 / 8.7,
-  // 1 x 14336 -> 4096 32.2 / 17.6 / 11.1 / 9.8 / 8.7, 8 x 5120 -> 51200 29.9 / 30.7 / 39.6 / 44.7 / 53.9).
-  int S = 8;
-  while (S > 1 && (S > k_tiles || tiles * groups > (C::CTAS_PER_SM == 2 ? st->push_fit : st->few_fit)[S] || C::smem_bytes(tokens, 2, S) > C::MAX_SMEM)) --S;
-  int nst = C::MAX_STAGES;
-  while (nst > 2 && C::smem_bytes(tokens, nst, S) > C::MAX_SMEM) --nst;
-  launch_tc(split ? matvec_digits_kernel<FMT, GATED, true> : matvec_digits_kernel<FMT, GATED, false>, S, dim3((unsigned)(tiles * groups * S)),
-            dim3(C::THREADS), C::smem_bytes(tokens, nst, S), s, tmW, tmD, static_cast<const __nv_bfloat16*>(X), static_cast<const uint8_t*>(Ws), ws + at.scales,
-            reinterpret_cast<const uint32_t*>(ws + at.exponents), Y, y_dtype == TORQ_BF16 ? 1 : 0, (int)M, (int)N, (int)K, S, (int)groups, nst,
-            C::PLANES ? 2.0f * alpha : alpha, st->err_word);
-  return launch_status();
+  if (split)
+    return digits_launch<FMT, GATED, ROWS_AHEAD>(st, tmW, tmD, nullptr, Ws, ws + at.scales, reinterpret_cast<uint32_t*>(ws + at.exponents), M, N, K, Y,
+                                                 y_dtype, alpha, s);
+  return digits_launch<FMT, GATED, ROWS_HERE>(st, tmW, tmW, X, Ws, nullptr, nullptr, M, N, K, Y, y_dtype, alpha, s);
 }
 
 template <int FMT, bool GATED>
@@ -1091,7 +1101,7 @@ static torq_status matvec_impl(const void* X, const void* Wq, const void* Ws, in
   return matvec_digits<FMT, GATED>(st, X, Wq, Ws, M, N, K, Y, y_dtype, alpha, workspace, static_cast<cudaStream_t>(stream));
 }
 
-// The gated pair of projections on quantized activations: the pair kernel at every number of rows.
+// The gated pair of projections on quantized activations.
 template <int FMT>
 static torq_status gated_gemm_impl(const void* Aq, const void* As, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
                                    torq_dtype y_dtype, float alpha, void* stream) {
@@ -1107,6 +1117,18 @@ static torq_status gated_gemm_impl(const void* Aq, const void* As, const void* W
   const uint64_t krow = (uint64_t)(FMT == FMT_MXINT4 ? K : K / 2), kb4 = (uint64_t)(K / (FMT == FMT_NVFP4 ? 64 : 128));
   const bool ybf = y_dtype == TORQ_BF16;
   CUtensorMap tmA, tmB, tmSFA, tmSFB, tmY;
+  if constexpr (FMT != FMT_MXINT4) {
+    using D = DigitsCfg<FMT, true, ROWS_QUANTIZED>;
+    // Few tokens: the kernel of the few-token products, with the quantized activations in the place of digits (us, this / pair kernel, 1, 16
+    // and 32 tokens, MXFP4: 5120 -> 25600 25.3 / 39.6, 26.0 / 33.7 and 28.7 / 34.7; 2048 -> 5632 4.4 / 8.2, 5.6 / 7.4 and 6.8 / 7.4; beyond, 48
+    // tokens 4096 -> 14336 20.1 / 17.6; NVFP4 32 tokens 4096 -> 14336 19.1 / 18.2).
+    if (M <= D::MAX_TOK) {
+      if (!encode_2d(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(2 * N), krow, D::BF, 128) ||
+          !encode_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Aq, (uint64_t)M, krow, (uint32_t)D::rows((int)M), 128))
+        return TORQ_ERR_LAUNCH;
+      return digits_launch<FMT, true, ROWS_QUANTIZED>(st, tmB, tmA, nullptr, Ws, As, nullptr, M, N, K, Y, y_dtype, alpha, static_cast<cudaStream_t>(stream));
+    }
+  }
   if (!encode_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Aq, (uint64_t)M, krow, 128, 128) ||
       !encode_2d(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(2 * N), krow, 128, 128) ||
       !encode_2d(&tmSFA, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, As, (uint64_t)((M + 127) / 128), kb4 * 128, 1, C::SF_BOX_WORDS,

@@ -29,7 +29,7 @@ def operands(g, M, N, K, fmt):
 
 @pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4", "mxint4", "w4a8"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("M,N,K", [(1, 128, 128), (3, 256, 384), (128, 128, 256), (129, 384, 640), (256, 1024, 2048), (300, 2176, 1152),
+@pytest.mark.parametrize("M,N,K", [(1, 128, 128), (3, 256, 384), (8, 25600, 640), (17, 384, 2304), (24, 5632, 1024), (25, 256, 896), (32, 1024, 512), (33, 128, 256), (128, 128, 256), (129, 384, 640), (256, 1024, 2048), (300, 2176, 1152),
                                    (777, 5504, 1024), (2600, 5632, 512)])
 def test_gated_gemm(fmt, dtype, M, N, K):
     A, W = operands(gen(M + N), M, N, K, fmt)
