@@ -20,19 +20,45 @@ __device__ __forceinline__ uint4 load_once(const void* p) {
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
   return v;
 }
-__device__ __forceinline__ void bf16x8_to_float(const uint4& a, float (&v)[8]) {
+// Two float32 in a 64-bit register: one instruction for both, each rounded by itself as the scalar one.
+__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
+  uint64_t p;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi));
+  return p;
+}
+__device__ __forceinline__ uint64_t pair_of(float v) { return pair_of(__float_as_uint(v), __float_as_uint(v)); }
+__device__ __forceinline__ float2 halves(uint64_t p) {
+  uint32_t lo, hi;
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(p));
+  return make_float2(__uint_as_float(lo), __uint_as_float(hi));
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+// Eight bfloat16 <-> four pairs of float32.
+__device__ __forceinline__ void bf16x8_to_pairs(const uint4& a, uint64_t (&v)[4]) {
   const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  }
+  for (int i = 0; i < 4; ++i) v[i] = pair_of(w[i] << 16, w[i] & 0xFFFF0000u);
 }
-__device__ __forceinline__ uint4 float_to_bf16x8(const float (&v)[8]) {
+__device__ __forceinline__ uint4 pairs_to_bf16x8(const uint64_t (&v)[4]) {
   uint32_t w[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    const float2 f = halves(v[i]);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(f.x, f.y);
     w[i] = *reinterpret_cast<const uint32_t*>(&h);
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
@@ -50,12 +76,12 @@ struct Raw8 {
     v[0] = make_uint4(0, 0, 0, 0);
     if constexpr (F32) v[1] = v[0];
   }
-  __device__ __forceinline__ void values(float (&f)[8]) const {
+  __device__ __forceinline__ void values(uint64_t (&f)[4]) const {
     if constexpr (F32) {
-      f[0] = __uint_as_float(v[0].x); f[1] = __uint_as_float(v[0].y); f[2] = __uint_as_float(v[0].z); f[3] = __uint_as_float(v[0].w);
-      f[4] = __uint_as_float(v[1].x); f[5] = __uint_as_float(v[1].y); f[6] = __uint_as_float(v[1].z); f[7] = __uint_as_float(v[1].w);
+      f[0] = pair_of(v[0].x, v[0].y); f[1] = pair_of(v[0].z, v[0].w);
+      f[2] = pair_of(v[1].x, v[1].y); f[3] = pair_of(v[1].z, v[1].w);
     } else {
-      bf16x8_to_float(v[0], f);
+      bf16x8_to_pairs(v[0], f);
     }
   }
 };
@@ -107,20 +133,20 @@ add_rmsnorm_kernel(const void* X, const void* R, void* R_out, const __nv_bfloat1
       continue;
     }
     const int64_t base = row * d;
-    float h[VPT][8];
-    float sum = 0.f;
+    uint64_t h[VPT][4], squares = 0;
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
       x[k].values(h[k]);
       if constexpr (RES != RES_NONE) {
-        float a[8];
+        uint64_t a[4];
         r[k].values(a);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[k][i] += a[i];
+        for (int i = 0; i < 4; ++i) h[k][i] = add2(h[k][i], a[i]);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum = fmaf(h[k][i], h[k][i], sum);
+      for (int i = 0; i < 4; ++i) squares = fma2(h[k][i], h[k][i], squares);
     }
+    float sum = halves(squares).x + halves(squares).y;
     if (row + step < M) load(row + step);
     if constexpr (RES != RES_NONE) {
 #pragma unroll
@@ -128,11 +154,11 @@ add_rmsnorm_kernel(const void* X, const void* R, void* R_out, const __nv_bfloat1
         const int p = tid + k * nt;
         if (p < pieces) {
           if constexpr (RES == RES_F32) {
-            float4* o = reinterpret_cast<float4*>(static_cast<float*>(R_out) + base + 8 * p);
-            o[0] = make_float4(h[k][0], h[k][1], h[k][2], h[k][3]);
-            o[1] = make_float4(h[k][4], h[k][5], h[k][6], h[k][7]);
+            ulonglong2* o = reinterpret_cast<ulonglong2*>(static_cast<float*>(R_out) + base + 8 * p);
+            o[0] = make_ulonglong2(h[k][0], h[k][1]);
+            o[1] = make_ulonglong2(h[k][2], h[k][3]);
           } else {
-            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(R_out) + base + 8 * p) = float_to_bf16x8(h[k]);
+            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(R_out) + base + 8 * p) = pairs_to_bf16x8(h[k]);
           }
         }
       }
@@ -147,28 +173,32 @@ add_rmsnorm_kernel(const void* X, const void* R, void* R_out, const __nv_bfloat1
       for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
       turn ^= 1;
     }
-    const float rstd = 1.0f / sqrtf(sum / (float)d + eps);
+    const uint64_t rstd = pair_of(1.0f / sqrtf(sum / (float)d + eps));
 #pragma unroll
     for (int k = 0; k < VPT; ++k) {
       const int p = tid + k * nt;
-      float wv[8], y[8];
-      bf16x8_to_float(w[k], wv);
+      uint64_t y[4];
+      bf16x8_to_pairs(w[k], y);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = h[k][i] * rstd * wv[i];
+      for (int i = 0; i < 4; ++i) y[i] = mul2(mul2(h[k][i], rstd), y[i]);
       if constexpr (!MX) {
-        if (p < pieces) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + base + 8 * p) = float_to_bf16x8(y);
+        if (p < pieces) *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(out) + base + 8 * p) = pairs_to_bf16x8(y);
       } else {
         // four lanes share a block of 32, sixteen a word of four scale bytes
         float amax = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) amax = fmaxf(amax, fabsf(y[i]));
+        for (int i = 0; i < 4; ++i) amax = fmaxf(amax, fmaxf(fabsf(halves(y[i]).x), fabsf(halves(y[i]).y)));
         amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
         amax = fmaxf(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
         const uint32_t ef = __float_as_uint(amax) >> 23, sbyte = ef > 8u ? ef - 8u : 0u;
-        const float inv = __uint_as_float((254u - sbyte) << 23);
-        if (p < pieces)
+        const uint64_t inv = pair_of((254u - sbyte) << 23, (254u - sbyte) << 23);
+        if (p < pieces) {
+          float2 q[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) q[i] = halves(mul2(y[i], inv));
           *reinterpret_cast<uint2*>(static_cast<uint8_t*>(out) + base + 8 * p) =
-              make_uint2(pack4_e4m3(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), pack4_e4m3(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
+              make_uint2(pack4_e4m3(q[0].x, q[0].y, q[1].x, q[1].y), pack4_e4m3(q[2].x, q[2].y, q[3].x, q[3].y));
+        }
         uint32_t word = sbyte << (8 * ((lane >> 2) & 3));
         word |= __shfl_xor_sync(0xFFFFFFFFu, word, 4);
         word |= __shfl_xor_sync(0xFFFFFFFFu, word, 8);
