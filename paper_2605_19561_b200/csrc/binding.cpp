@@ -130,6 +130,10 @@ torq_dtype dtype_of(const at::Tensor& t) { return t.scalar_type() == at::kFloat 
 bool is_matrix(const at::Tensor& t, int64_t rows, int64_t cols) { return t.dim() == 2 && t.size(0) == rows && t.size(1) == cols; }
 // Scale bytes of [rows, k] with `block` elements to a scale, in whole tiles.
 int64_t scale_bytes(int64_t rows, int64_t k, int64_t block) { return (rows + 127) / 128 * ((k / block + 3) / 4) * 512; }
+// What a call makes belongs to the current stream's pool; where another stream is given, the allocator has to know that it uses it.
+void used_by(const at::Tensor& t, PyObject* stream, void* handle) {
+  if (stream != Py_None && t.defined()) t.record_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(handle), t.device().index()));
+}
 void* stream_of(PyObject* o) { return o == Py_None ? (void*)c10::cuda::getCurrentCUDAStream().stream() : PyLong_AsVoidPtr(o); }
 
 PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -171,6 +175,9 @@ PyObject* product(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (scratch_bytes) scratch = at::empty({(int64_t)scratch_bytes}, W->options());
   }
   void* stream = stream_of(a[7]);
+  if (PyErr_Occurred()) return nullptr;
+  used_by(scratch, a[7], stream);
+  if (a[5] == Py_None) used_by(Y, a[7], stream);
   const float a_scale = nv ? (float)PyFloat_AsDouble(a[8]) : 0.f, w_scale = nv ? (float)PyFloat_AsDouble(a[9]) : 0.f;
   if (PyErr_Occurred()) return nullptr;
   const void *ap = A->data_ptr(), *asp = gemm ? As->data_ptr() : nullptr, *wp = W->data_ptr(), *wsp = Ws->data_ptr();
@@ -230,6 +237,9 @@ PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
   const float eps = (float)PyFloat_AsDouble(a[4]);
   void* stream = stream_of(a[8]);
   if (PyErr_Occurred()) return nullptr;
+  if (a[5] == Py_None) used_by(out, a[8], stream);
+  if (mx && a[6] == Py_None) used_by(sf, a[8], stream);
+  if (R && a[7] == Py_None) used_by(h, a[8], stream);
   const void *xp = X->data_ptr(), *wp = w->data_ptr(), *rp = R ? R->data_ptr() : nullptr;
   void *op = out.data_ptr(), *sp = mx ? sf.data_ptr() : nullptr, *hp = R ? h.data_ptr() : nullptr;
   const torq_dtype xt = dtype_of(*X), rt = R ? dtype_of(*R) : TORQ_BF16;

@@ -1017,20 +1017,26 @@ static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const voi
     threads = (pieces + 32 * vpt - 1) / (32 * vpt) * 32;
   }
   const int64_t ctas = (rows + per_cta - 1) / per_cta;
-  auto launch = [&](auto kernel) {
-    int per_sm = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kernel, threads * per_cta, 0) != cudaSuccess || per_sm < 1) per_sm = 1;
-    const int64_t most = (int64_t)per_sm * st->sm_count;
+  auto launch = [&](auto V, auto MX, auto F32, auto RES) {
+    constexpr auto kernel = add_rmsnorm_kernel<decltype(V)::value, decltype(MX)::value, decltype(F32)::value, decltype(RES)::value>;
+    static const int regs = [] {                           // asked once: the runtime's own count of resident CTAs costs 0.8 us a call
+      cudaFuncAttributes a;
+      return cudaFuncGetAttributes(&a, kernel) == cudaSuccess ? (a.numRegs + 7) / 8 * 8 : 128;
+    }();
+    const int warps = threads * per_cta / 32, by_regs = 4 * (16384 / (regs * 32)) / warps, by_warps = 64 / warps;   // registers are a quarter SM's
+    const int64_t per_sm = by_regs < by_warps ? (by_regs < 1 ? 1 : by_regs) : (by_warps < 32 ? by_warps : 32), most = per_sm * st->sm_count;
     launch_tc(kernel, 1, dim3((unsigned)(ctas < most ? ctas : most)), dim3((unsigned)threads, (unsigned)per_cta), 0, static_cast<cudaStream_t>(stream), X, residual,
               residual_out, static_cast<const __nv_bfloat16*>(weight), eps, M, rows, (int)d, out, static_cast<uint8_t*>(out_scales));
   };
   auto with = [&](auto V, auto MX) {
-    constexpr int v = decltype(V)::value;
-    constexpr bool m = decltype(MX)::value;
-    const bool f32 = x_dtype == TORQ_F32;
-    if (!residual) launch(f32 ? add_rmsnorm_kernel<v, m, true, RES_NONE> : add_rmsnorm_kernel<v, m, false, RES_NONE>);
-    else if (r_dtype == TORQ_F32) launch(f32 ? add_rmsnorm_kernel<v, m, true, RES_F32> : add_rmsnorm_kernel<v, m, false, RES_F32>);
-    else launch(f32 ? add_rmsnorm_kernel<v, m, true, RES_BF16> : add_rmsnorm_kernel<v, m, false, RES_BF16>);
+    using std::integral_constant;
+    auto typed = [&](auto F32) {
+      if (!residual) launch(V, MX, F32, integral_constant<int, RES_NONE>{});
+      else if (r_dtype == TORQ_F32) launch(V, MX, F32, integral_constant<int, RES_F32>{});
+      else launch(V, MX, F32, integral_constant<int, RES_BF16>{});
+    };
+    if (x_dtype == TORQ_F32) typed(std::true_type{});
+    else typed(std::false_type{});
   };
   auto pick = [&](auto MX) {
     if (vpt == 1) with(std::integral_constant<int, 1>{}, MX);

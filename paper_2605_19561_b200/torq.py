@@ -705,6 +705,13 @@ def _operand(t, dtypes, name, shape=None, at_least=None):
         raise ValueError(f"{name}: expected room for {at_least} elements, got {tuple(t.shape)}")
 
 
+def _used_by(stream, *tensors):
+    """Tensors made for a call on another stream than the current one: the allocator has to know that it uses them."""
+    if stream is not None:
+        for t in tensors:
+            t.record_stream(stream)
+
+
 _FLOATS = (torch.float32, torch.bfloat16)
 _BYTES = (torch.uint8,)
 
@@ -713,7 +720,7 @@ def _dtype_code(t):
     return TORQ_F32 if t.dtype is torch.float32 else TORQ_BF16
 
 
-def _norm_operands(X, weight, residual, residual_out):
+def _norm_operands(X, weight, residual, residual_out, stream):
     _operand(X, _FLOATS, "X")
     if X.dim() != 2:
         raise ValueError(f"X: expected two dimensions, got {tuple(X.shape)}")
@@ -726,6 +733,7 @@ def _norm_operands(X, weight, residual, residual_out):
     _operand(residual, _FLOATS, "residual", (M, d))
     if residual_out is None:
         residual_out = torch.empty_like(residual)
+        _used_by(stream, residual_out)
     _operand(residual_out, (residual.dtype,), "residual_out", (M, d))
     return M, d, residual_out, _dtype_code(residual)
 
@@ -746,9 +754,10 @@ def _norm_native(*args):
 
 def _norm(mx, X, weight, residual, eps, out, out_scales, residual_out, stream):
     """The norm through ctypes, with reasons for what it refuses: the tuple of results."""
-    M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out)
+    M, d, h, r_dtype = _norm_operands(X, weight, residual, residual_out, stream)
     if out is None:
         out = torch.empty((M, d), dtype=torch.uint8 if mx else torch.bfloat16, device=X.device)
+        _used_by(stream, out)
     _operand(out, _BYTES if mx else (torch.bfloat16,), "out_bytes" if mx else "out", (M, d))
     args = (_ptr(X), _dtype_code(X), _ptr(residual), _ptr(h), r_dtype, _ptr(weight), eps, M, d, _ptr(out))
     if not mx:
@@ -756,6 +765,7 @@ def _norm(mx, X, weight, residual, eps, out, out_scales, residual_out, stream):
         return (out,) if h is None else (out, h)
     if out_scales is None:
         out_scales = torch.empty(torq_scales_bytes(M, d), dtype=torch.uint8, device=X.device)
+        _used_by(stream, out_scales)
     _operand(out_scales, _BYTES, "out_scales", at_least=torq_scales_bytes(M, d))
     _raise(lib().torq_add_rmsnorm_mxfp8(*args, _ptr(out_scales), _stream(stream)), "torq_add_rmsnorm_mxfp8")
     return (out, out_scales) if h is None else (out, out_scales, h)
@@ -819,12 +829,14 @@ def _product(kind, A, As, Wq, Ws, out_dtype, Y, stream, a_scale=0.0, w_scale=0.0
     N = rows // 2 if gated else rows
     if Y is None:
         Y = torch.empty((M, N), dtype=out_dtype, device=A.device)
+        _used_by(stream, Y)
     _operand(Y, _FLOATS, "Y", (M, N))
     x = (_ptr(A),) if bf16 else (_ptr(A), _ptr(As), *scales[:1])
     scratch = ()
     if bf16:
         if workspace is None:
             workspace = torch.empty(torq_matvec_workspace_bytes(M, N, K), dtype=torch.uint8, device=A.device)
+            _used_by(stream, workspace)
         _operand(workspace, (workspace.dtype,), "workspace")
         scratch = (_ptr(workspace), workspace.nbytes)
     _raise(getattr(lib(), name)(*x, _ptr(Wq), _ptr(Ws), *scales[-1:], M, N, K, _ptr(Y), _dtype_code(Y), *scratch, _stream(stream)), name)

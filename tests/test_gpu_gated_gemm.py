@@ -113,8 +113,9 @@ def test_feed_forward_block_prefill(M):
     check_sums(out, values(q, untile(qs, M, F // 32), "w4a8"), down[3], gemm_steps(F))
 
 
-def test_feed_forward_block_captured_and_on_another_stream():
-    d, F, M = 512, 1408, 4
+@pytest.mark.parametrize("M", [4, 6, 40])
+def test_feed_forward_block_captured_and_on_another_stream(M):
+    d, F = 512, 1408
     up, down = ffn_weights(gen(0), d, F)
     x, r, w = norm_inputs(M, d, torch.bfloat16, torch.bfloat16)
 
@@ -157,3 +158,23 @@ def test_calls_through_ctypes_are_the_same(monkeypatch):
     monkeypatch.setattr(torq, "_product_native", lambda *a: -1)
     monkeypatch.setattr(torq, "_norm_native", lambda *a: -1)
     assert all(torch.equal(a, b) and a.dtype is b.dtype for a, b in zip(both(), want, strict=True))
+
+
+def test_two_graphs_replayed_in_turn():
+    """Each has its own workspace and results, whatever the other does in between."""
+    d, F = 512, 1408
+    up, down = ffn_weights(gen(0), d, F)
+    graphs = []
+    for M in (6, 9):
+        x, r, w = norm_inputs(M, d, torch.bfloat16, torch.bfloat16, seed=M)
+        want = [t.clone() for t in ffn_decode(x, r, w, up, down)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            got = ffn_decode(x, r, w, up, down)
+        graphs.append((graph, got, want, x, r, w))
+    for _ in range(3):
+        for graph, *_ in graphs:
+            graph.replay()
+    torch.cuda.synchronize()
+    for _, got, want, *_ in graphs:
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

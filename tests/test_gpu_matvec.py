@@ -165,18 +165,25 @@ def test_long_contractions(fmt, gated, M, K):
     (check_gated if gated else check_sums)(Y, X.double(), W[3], *matvec_error(fmt, X.double()))
 
 
-def test_stream_argument():
-    g = gen(3)
-    W = quantized(g, 256, 512, "mxfp4")
-    X = heavy(g, 3, 512).to(torch.bfloat16)
+@pytest.mark.parametrize("native", [True, False])
+def test_stream_argument(native, monkeypatch):
+    """A call on another stream than the current one, its workspace taken from the current one's pool: calls on both at once, with
+    the memory that the first has given back taken and overwritten at once."""
+    if not native:
+        monkeypatch.setattr(torq, "_product_native", lambda *a: -1)
+    g, M = gen(3), 7
+    W = quantized(g, 4096, 4096, "mxfp4")
+    X = heavy(g, M, 4096).to(torch.bfloat16)
     want = matvec("mxfp4", X, W)
     s = torch.cuda.Stream()
-    s.wait_stream(torch.cuda.current_stream())
-    Y = torch.zeros_like(want)
     torch.cuda.synchronize()
-    matvec("mxfp4", X, W, Y=Y, stream=s)
-    s.synchronize()
-    assert torch.equal(Y, want)
+    size = torq.torq_matvec_workspace_bytes(M, 4096, 4096)
+    for _ in range(20):
+        got = [matvec("mxfp4", X, W, stream=s) for _ in range(3)]
+        torch.full((size,), 0x55, dtype=torch.uint8, device=DEV)
+        also = matvec("mxfp4", X, W)
+        torch.cuda.synchronize()
+        assert all(torch.equal(y, want) for y in (*got, also))
 
 
 def test_refusals():

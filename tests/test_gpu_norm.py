@@ -102,3 +102,17 @@ def test_refusals():
             f()
         assert e.value.code == code
     assert torq.torq_launch_count() == before
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_stream_argument(native, monkeypatch):
+    if not native:
+        monkeypatch.setattr(torq, "_norm_native", lambda *a: -1)
+    x, r, w = norm_inputs(64, 2048, torch.bfloat16, torch.bfloat16)
+    want = torq.torq_add_rmsnorm_mxfp8(x, w, r)
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = torq.torq_add_rmsnorm_mxfp8(x, w, r, stream=s)
+        s.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
