@@ -40,9 +40,10 @@ enum : int { ROWS_HERE = 0, ROWS_AHEAD = 1, ROWS_QUANTIZED = 2 };
 
 template <int FMT, bool GATED, int ROWS = ROWS_HERE>
 struct DigitsCfg {
-  static constexpr bool PLANES = FMT == FMT_MXINT4;
+  // MXINT4: two operands from one in front of digits; beside quantized activations operand bytes, a byte per element (kind::mxf8f6f4)
+  static constexpr bool BYTES = FMT == FMT_MXINT4 && ROWS == ROWS_QUANTIZED, PLANES = FMT == FMT_MXINT4 && !BYTES;
   static constexpr int BF = 128;                       // features per tile
-  static constexpr int BK = 256;                       // elements of K per stage (128 bytes per row)
+  static constexpr int BK = BYTES ? 128 : 256;         // elements of K per stage (128 bytes per row)
   static constexpr int DIGITS = ROWS == ROWS_QUANTIZED ? 1 : 8;   // rows per token
   // tokens of a CTA (quantized: as many as two CTAs have room on an SM for, with their partial sums)
   static constexpr int MAX_TOK = ROWS == ROWS_QUANTIZED ? (FMT == FMT_NVFP4 ? 24 : 32) : (GATED ? 8 : 16);
@@ -51,7 +52,7 @@ struct DigitsCfg {
   static constexpr int TILES = GATED ? 2 : 1;          // of W per stage
   static constexpr int TILE_BYTES = (PLANES ? 2 : 1) * BF * 128;
   static constexpr int W_BYTES = TILES * TILE_BYTES;
-  static constexpr int CH = FMT == FMT_NVFP4 ? 4 : 2;  // scale chunks per stage and 128 rows
+  static constexpr int CH = FMT == FMT_NVFP4 ? 4 : (BYTES ? 1 : 2);   // scale chunks per stage and 128 rows
   static constexpr int SF_BYTES = CH * 512;
   static constexpr int SF_SETS = TILES + (PLANES ? 2 : 1);   // of W's tiles and of the digits
   static constexpr int MAX_STAGES = 4;
@@ -336,6 +337,9 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
 #pragma unroll
               for (int j = 0; j < 4; ++j)
                 if (j < 2 || two) mma_nvf4(acc, adesc + 2 * j, bdesc + 2 * j, idesc0, sfw + 4 * j, sfb + 4 * j, (it | j) != 0);
+            } else if constexpr (C::BYTES) {                // a scale byte per instruction
+#pragma unroll
+              for (int j = 0; j < 4; ++j) mma_mxf8(acc, adesc + 2 * j, bdesc + 2 * j, idesc_mxf8(128, rows, j), sfw, sfb, (it | j) != 0);
             } else {                                     // half a chunk (two scale bytes) per instruction
               mma_mxf4(acc, adesc, bdesc, idesc0, sfw, sfb, more);
               mma_mxf4(acc, adesc + 2, bdesc + 2, idesc2, sfw, sfb, 1);

@@ -108,9 +108,8 @@ static bool opt_in_format() {
 template <int FMT>
 static bool opt_in_digits() {
   constexpr int plain = DigitsCfg<FMT, false>::MAX_SMEM, gated = DigitsCfg<FMT, true>::MAX_SMEM;
-  if constexpr (FMT != FMT_MXINT4)
-    if (!opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_QUANTIZED>, gated)) return false;
-  return opt_in_smem(matvec_digits_kernel<FMT, false, ROWS_HERE>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_HERE>, gated) &&
+  return opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_QUANTIZED>, DigitsCfg<FMT, true, ROWS_QUANTIZED>::MAX_SMEM) &&
+         opt_in_smem(matvec_digits_kernel<FMT, false, ROWS_HERE>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_HERE>, gated) &&
          opt_in_smem(matvec_digits_kernel<FMT, false, ROWS_AHEAD>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_AHEAD>, gated);
 }
 
@@ -1123,17 +1122,16 @@ static torq_status gated_gemm_impl(const void* Aq, const void* As, const void* W
   const uint64_t krow = (uint64_t)(FMT == FMT_MXINT4 ? K : K / 2), kb4 = (uint64_t)(K / (FMT == FMT_NVFP4 ? 64 : 128));
   const bool ybf = y_dtype == TORQ_BF16;
   CUtensorMap tmA, tmB, tmSFA, tmSFB, tmY;
-  if constexpr (FMT != FMT_MXINT4) {
-    using D = DigitsCfg<FMT, true, ROWS_QUANTIZED>;
-    // Few tokens: the kernel of the few-token products, with the quantized activations in the place of digits (us, this / pair kernel, 1, 16
-    // and 32 tokens, MXFP4: 5120 -> 25600 25.3 / 39.6, 26.0 / 33.7 and 28.7 / 34.7; 2048 -> 5632 4.4 / 8.2, 5.6 / 7.4 and 6.8 / 7.4; beyond, 48
-    // tokens 4096 -> 14336 20.1 / 17.6; NVFP4 32 tokens 4096 -> 14336 19.1 / 18.2).
-    if (M <= D::MAX_TOK) {
-      if (!encode_2d(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(2 * N), krow, D::BF, 128) ||
-          !encode_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Aq, (uint64_t)M, krow, (uint32_t)D::rows((int)M), 128))
-        return TORQ_ERR_LAUNCH;
-      return digits_launch<FMT, true, ROWS_QUANTIZED>(st, tmB, tmA, nullptr, Ws, As, nullptr, M, N, K, Y, y_dtype, alpha, static_cast<cudaStream_t>(stream));
-    }
+  using D = DigitsCfg<FMT, true, ROWS_QUANTIZED>;
+  // Few tokens: the kernel of the few-token products, with the quantized activations in the place of digits (us, this / pair kernel, 1, 16
+  // and 32 tokens, MXFP4: 5120 -> 25600 25.3 / 39.6, 26.0 / 33.7 and 28.7 / 34.7; 2048 -> 5632 4.4 / 8.2, 5.6 / 7.4 and 6.8 / 7.4; beyond, 48
+  // tokens 4096 -> 14336 20.1 / 17.6; NVFP4 32 tokens 4096 -> 14336 19.1 / 18.2; operand bytes 5120 -> 25600 44.4 / 72.3, 45.8 / 64.7 and
+  // 50.2 / 53.4, 2048 -> 5632 6.2 / 13.1, 7.7 / 10.9 and 8.9 / 10.9).
+  if (M <= D::MAX_TOK) {
+    if (!encode_2d(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(2 * N), krow, D::BF, 128) ||
+        !encode_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Aq, (uint64_t)M, krow, (uint32_t)D::rows((int)M), 128))
+      return TORQ_ERR_LAUNCH;
+    return digits_launch<FMT, true, ROWS_QUANTIZED>(st, tmB, tmA, nullptr, Ws, As, nullptr, M, N, K, Y, y_dtype, alpha, static_cast<cudaStream_t>(stream));
   }
   if (!encode_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Aq, (uint64_t)M, krow, 128, 128) ||
       !encode_2d(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)(2 * N), krow, 128, 128) ||
