@@ -162,9 +162,11 @@ matvec_split_kernel(const __nv_bfloat16* __restrict__ X, int K, uint8_t* __restr
   const int parts = (K + 2047) / 2048;
   const int64_t m = blockIdx.x / parts;
   const int k0 = (int)(blockIdx.x % parts) * 2048 + warp * 256, k = k0 + 8 * lane;
+  const uint4* row = reinterpret_cast<const uint4*>(X + m * K);
+  // Into the L2 ahead of the product's W, which would stand before it in memory's queue.  Only that: the kernel before may still be writing x.
+  if (k < K) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + k / 8));
   griddep_launch_dependents();
   griddep_wait();
-  const uint4* row = reinterpret_cast<const uint4*>(X + m * K);
   uint32_t ref = 0;
   if constexpr (FMT == FMT_NVFP4) {
     uint32_t top = 0;
