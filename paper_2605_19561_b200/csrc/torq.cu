@@ -1005,7 +1005,8 @@ static torq_status add_rmsnorm_impl(const void* X, torq_dtype x_dtype, const voi
   const int pieces = (int)(d / 8);
   const int64_t rows = mx ? (M + 127) / 128 * 128 : M;
   // Up to 1024 columns a row is one warp's, four rows to a CTA.  Above, a CTA's: one piece of eight per thread while the rows
-  // are few, two or four where a CTA has several.
+  // are few, two or four where a CTA has several (us, 1 / 2 / 4 pieces: 64 x 5120 bfloat16 out 2.05 / 2.36, 296 x 5120 3.41 / 3.32,
+  // 300 x 5120 4.0 / 3.9 / 4.0, 200 x 8192 float32 to MXFP8 6.5 / 6.9, 8192 x 5120 bfloat16 to MXFP8 66.6 / 53.6 / 52.8).
   int vpt, threads, per_cta = 1;
   if (pieces <= 128) {
     vpt = pieces <= 32 ? 1 : (pieces <= 64 ? 2 : 4);
