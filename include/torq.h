@@ -350,8 +350,7 @@ torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void
  * 32 (NVFP4: 16, and a block's counts as 2^-17 of the largest in the token at least): elements down to 2^-14 of the block's largest keep all
  * their bits, nothing is off by more than 2^-22 of it.  What is smaller than 2^-106 counts as zero in part or whole; MXINT4: magnitudes of 2^125
  * and more as not a number.
- * Weights are read from HBM once, for 16 tokens at a time (gated: 8) that find them in the L2: made for decoding, any M <= 2^18 is
- * served.  K % 128 == 0, K <= 65536, N % 8 == 0.  One launch without a workspace, else two; two calls that may overlap need a workspace
+ * Weights are read from HBM once, for 8 to 32 tokens at a time, the others finding them in the L2: made for decoding, any M <= 2^18 is served.  K % 128 == 0, K <= 65536, N % 8 == 0.  One launch without a workspace, else two; two calls that may overlap need a workspace
  * each.  Y and the workspace overlap no operand and not each other, here and in the entry points below. */
 size_t torq_matvec_workspace_bytes(int64_t M, int64_t N, int64_t K);
 torq_status torq_mxfp4_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,

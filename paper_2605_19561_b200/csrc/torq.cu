@@ -108,6 +108,10 @@ static bool opt_in_format() {
 template <int FMT>
 static bool opt_in_digits() {
   constexpr int plain = DigitsCfg<FMT, false>::MAX_SMEM, gated = DigitsCfg<FMT, true>::MAX_SMEM;
+  if constexpr (FMT != FMT_MXINT4)
+    if (!opt_in_smem(mxfp4_gemm_pair_kernel<FMT, false, true>, GemmPairCfgT<FMT>::SMEM_BYTES) ||
+        !opt_in_smem(mxfp4_gemm_pair_kernel<FMT, true, true>, GemmPairCfgT<FMT>::SMEM_BYTES))
+      return false;
   return opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_QUANTIZED>, DigitsCfg<FMT, true, ROWS_QUANTIZED>::MAX_SMEM) &&
          opt_in_smem(matvec_digits_kernel<FMT, false, ROWS_HERE>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_HERE>, gated) &&
          opt_in_smem(matvec_digits_kernel<FMT, false, ROWS_AHEAD>, plain) && opt_in_smem(matvec_digits_kernel<FMT, true, ROWS_AHEAD>, gated);
@@ -982,7 +986,7 @@ static torq_status gemm_impl(const void* Aq, const void* As, const void* Wq, con
   const MixedTiles list = plan_gemm_tiles(M, N, krow, max_pairs);
   const int pairs = list.total < max_pairs ? list.total : max_pairs;
   launch_tc(mxfp4_gemm_pair_kernel<FMT>, 2, 2 * pairs, GemmPairCfgT<FMT>::THREADS, GemmPairCfgT<FMT>::SMEM_BYTES, s,
-            tmA, tmB, tmSFA, tmSFB, tmY, tmBn, list, ybf ? 1 : 0, (int)M, (int)N, (int)K, alpha, st->err_word);
+            tmA, tmB, tmSFA, tmSFB, tmY, tmBn, list, ybf ? 1 : 0, (int)M, (int)N, (int)K, alpha, st->err_word, static_cast<void*>(nullptr), static_cast<const uint32_t*>(nullptr));
   return launch_status();
 }
 
@@ -1066,6 +1070,45 @@ static torq_status digits_launch(DeviceState* st, const CUtensorMap& tmW, const 
   return launch_status();
 }
 
+// The digits as the A operand of the GEMM on CTA pairs: 32 tokens to a tile of 256 rows, each W tile read once for them.
+template <int FMT, bool GATED>
+static torq_status digits_pair_launch(DeviceState* st, const void* D, const void* Ds, const uint32_t* exponents, const void* Wq, const void* Ws, int64_t M,
+                                      int64_t N, int64_t K, void* Y, torq_dtype y_dtype, float alpha, cudaStream_t s) {
+  using C = GemmPairCfgT<FMT>;
+  const int64_t rows = 8 * M, features = GATED ? 2 * N : N;
+  const uint64_t krow = (uint64_t)(K / 2), kb4 = (uint64_t)(K / (FMT == FMT_NVFP4 ? 64 : 128));
+  CUtensorMap tmA, tmB, tmBn, tmSFA, tmSFB;
+  if (!encode_2d(&tmA, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, D, (uint64_t)rows, krow, 128, 128) ||
+      !encode_2d(&tmB, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)features, krow, 128, 128) ||
+      !encode_2d(&tmBn, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, Wq, (uint64_t)features, krow, kNarrowCols / 2, 128) ||
+      !encode_2d(&tmSFA, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, Ds, (uint64_t)((rows + 127) / 128), kb4 * 128, 1, C::SF_BOX_WORDS,
+                 CU_TENSOR_MAP_SWIZZLE_NONE) ||
+      !encode_2d(&tmSFB, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, Ws, (uint64_t)((features + 127) / 128), kb4 * 128, GATED ? 1 : 2, C::SF_BOX_WORDS,
+                 CU_TENSOR_MAP_SWIZZLE_NONE))
+    return TORQ_ERR_LAUNCH;
+  MixedTiles list = plan_gemm_tiles(rows, features, krow, st->gemm_pairs);
+  if (GATED) {                                           // whole tiles only
+    const int group = list.group;
+    list = mixed_tiles_make((int)((rows + 255) / 256), (int)(N / 128), 0);
+    list.group = group;
+  }
+  const int pairs = list.total < st->gemm_pairs ? list.total : st->gemm_pairs;
+  launch_tc(mxfp4_gemm_pair_kernel<FMT, GATED, true>, 2, 2 * pairs, C::THREADS, C::SMEM_BYTES, s, tmA, tmB, tmSFA, tmSFB, tmA, tmBn, list,
+            y_dtype == TORQ_BF16 ? 1 : 0, (int)rows, (int)N, (int)K, alpha, st->err_word, Y, exponents);
+  return launch_status();
+}
+// Whether that is faster than groups of 16 tokens (gated: 8), each with its own pass over W.  More than 16 tokens: where the pairs have enough
+// tiles; gated, from 9: where two groups are more than a wave (us, pairs / groups, MXFP4, 17, 32, 64 and 128 tokens: 5120 -> 25600 21.0 / 23.9,
+// 21.1 / 25.1, 26.7 / 36.9 and 46 / 69; 2048 -> 10240 7.6 / 7.8, 7.6 / 8.0, 12.2 / 13.1 and 14.9 / 19.7; 24 and 48 tiles, 4096 -> 6144, 32, 48 and 64
+// tokens: 9.1 / 8.9, 11.3 / 9.2 and 11.6 / 12.0; 32 tiles, 14336 -> 4096, 64 tokens 24.5 / 18.5.  Gated 5120 -> 25600 31.3 / 50, 31.5 / 53, 50 / 97 and
+// 86 / 172; 32 tiles, 14336 -> 4096, 17 tokens 22.5 / 26.0; 12 tokens 5120 -> 25600 31.4 / 38.2, but 4096 -> 14336 20.7 / 18.8.)
+template <bool GATED>
+static bool digits_in_pairs(const DeviceState* st, int64_t M, int64_t N) {
+  const int64_t tiles = (M + 31) / 32 * (((GATED ? 2 * N : N) + 255) / 256);
+  if (!GATED) return M > 16 && 10 * tiles >= 7 * st->gemm_pairs;
+  return M > 16 ? 5 * tiles >= 2 * st->gemm_pairs : M > 8 && 2 * (N / 128) > 2 * st->sm_count;
+}
+
 template <int FMT, bool GATED>
 static torq_status matvec_digits(DeviceState* st, const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
                                  torq_dtype y_dtype, float alpha, void* workspace, cudaStream_t s) {
@@ -1083,6 +1126,9 @@ static torq_status matvec_digits(DeviceState* st, const void* X, const void* Wq,
     const torq_status rc = launch_status();
     if (rc != TORQ_OK) return rc;
   }
+  if constexpr (FMT != FMT_MXINT4)                       // whose weights have to be taken apart on the way
+    if (split && digits_in_pairs<GATED>(st, M, N))
+      return digits_pair_launch<FMT, GATED>(st, ws, ws + at.scales, reinterpret_cast<uint32_t*>(ws + at.exponents), Wq, Ws, M, N, K, Y, y_dtype, alpha, s);
   if (split)
     return digits_launch<FMT, GATED, ROWS_AHEAD>(st, tmW, tmD, nullptr, Ws, ws + at.scales, reinterpret_cast<uint32_t*>(ws + at.exponents), M, N, K, Y,
                                                  y_dtype, alpha, s);
@@ -1147,7 +1193,7 @@ static torq_status gated_gemm_impl(const void* Aq, const void* As, const void* W
   list.group = plan_gemm_tiles(M, 2 * N, krow, st->gemm_pairs).group;
   const int pairs = list.total < st->gemm_pairs ? list.total : st->gemm_pairs;
   launch_tc(mxfp4_gemm_pair_kernel<FMT, true>, 2, 2 * pairs, C::THREADS, C::SMEM_BYTES, static_cast<cudaStream_t>(stream), tmA, tmB, tmSFA, tmSFB,
-            tmY, tmB, list, ybf ? 1 : 0, (int)M, (int)N, (int)K, alpha, st->err_word);
+            tmY, tmB, list, ybf ? 1 : 0, (int)M, (int)N, (int)K, alpha, st->err_word, static_cast<void*>(nullptr), static_cast<const uint32_t*>(nullptr));
   return launch_status();
 }
 

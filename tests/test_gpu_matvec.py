@@ -214,3 +214,34 @@ def test_refusals():
             f()
         assert e.value.code == code
     assert torq.torq_launch_count() == before
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("gated,M,N,K", [(False, 17, 13320, 128), (False, 32, 13832, 640), (False, 33, 6920, 1408), (False, 64, 20480, 384), (False, 100, 3336, 2048),
+                                         (False, 513, 1000, 384), (False, 2085, 136, 128), (True, 9, 19072, 128), (True, 17, 3840, 640), (True, 31, 5632, 1152),
+                                         (True, 100, 1024, 2048), (True, 257, 384, 384), (True, 1027, 128, 128)])
+def test_more_tokens(fmt, gated, M, N, K):
+    """Where 32 tokens share a tile: workspaces and padding scales that hold no numbers, nothing written behind Y, a token that is not a
+    number, a captured call."""
+    g = gen(M + N + K)
+    W = quantized(g, 2 * N if gated else N, K, fmt, pad=0xFF)
+    X = (heavy(g, M, K) * 0.1).to(torch.bfloat16)
+    X[2] = 0
+    buf = torch.full((M * N + 64,), 7.0, dtype=torch.float32 if M % 2 else torch.bfloat16, device=DEV)
+    Y = buf[:M * N].view(M, N)
+    ws = torch.full((torq.torq_matvec_workspace_bytes(M, N, K),), 0xFF, dtype=torch.uint8, device=DEV)
+    matvec(fmt, X, W, gated, Y=Y, workspace=ws)
+    (check_gated if gated else check_sums)(Y, X.double(), W[3], *matvec_error(fmt, X.double()))
+    clean = Y.clone()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        matvec(fmt, X, W, gated, Y=Y, workspace=ws)
+    X[M - 2, K // 2] = float("nan")
+    Y.zero_()
+    graph.replay()
+    rest = [m for m in range(M) if m != M - 2]
+    assert not torch.isfinite(Y[M - 2]).any() and torch.equal(Y[rest], clean[rest])
+    assert (buf[M * N:] == 7).all()
+    assert torq.torq_last_device_error() == 0
