@@ -17,6 +17,7 @@
 // and 2^(R-8) are multiplied in when the eight sums are added.)
 // The digits cost some 200 instructions per eight elements of x.  Up to FEW_TOK tokens every CTA writes those of its own range of K, once
 // per 128 features, which saves a launch; more tokens have them written once, by a kernel of its own, into the caller's workspace.
+// From 17 tokens on (gated: 9) the GEMM on CTA pairs may take the digits instead, where it has enough tiles for them.
 //
 // MXINT4: a two's-complement nibble n is no e2m1 number, but n = 2 (l + 4 h) with l the e2m1 value of the code n & 3 (0, 1/2, 1, 3/2) and h that of
 // its upper half (0, 4, -8, -4 over 8: codes 0, 1, 10, 9): two operands from one, six logical instructions per eight weights, in shared
@@ -45,8 +46,9 @@ struct DigitsCfg {
   static constexpr int BF = 128;                       // features per tile
   static constexpr int BK = BYTES ? 128 : 256;         // elements of K per stage (128 bytes per row)
   static constexpr int DIGITS = ROWS == ROWS_QUANTIZED ? 1 : 8;   // rows per token
-  // tokens of a CTA (quantized: as many as two CTAs have room on an SM for, with their partial sums)
-  static constexpr int MAX_TOK = ROWS == ROWS_QUANTIZED ? (FMT == FMT_NVFP4 ? 24 : 32) : (GATED ? 8 : 16);
+  // tokens of a CTA (quantized: as many as two CTAs have room on an SM for, with their partial sums; gated MXINT4: one CTA has an SM's tensor
+  // memory to itself: 4096 -> 14336 45.9 us for 16 tokens in two groups of 8, 28.8 in one)
+  static constexpr int MAX_TOK = ROWS == ROWS_QUANTIZED ? (FMT == FMT_NVFP4 ? 24 : 32) : (GATED && !PLANES ? 8 : 16);
   static constexpr int FEW_TOK = 4;                    // up to here the product's CTAs may write the digits themselves
   static constexpr int PER_UNIT = GATED ? 2 : 4;       // tokens of what an epilogue warp adds up at a time
   static constexpr int TILES = GATED ? 2 : 1;          // of W per stage
@@ -72,9 +74,9 @@ struct DigitsCfg {
   // accumulators, then the scale chunks of W and of the digits (4 columns each)
   __host__ __device__ static constexpr int tmem_cols(int r) {
     const int n = TILES * r + SF_SETS * 4 * CH;
-    return n <= 32 ? 32 : (n <= 64 ? 64 : (n <= 128 ? 128 : 256));
+    return n <= 32 ? 32 : (n <= 64 ? 64 : (n <= 128 ? 128 : (n <= 256 ? 256 : 512)));
   }
-  static_assert(TILES * rows(MAX_TOK) + SF_SETS * 4 * CH <= 256, "two CTAs share an SM's tensor memory");
+  static_assert(TILES * rows(MAX_TOK) + SF_SETS * 4 * CH <= 512 / CTAS_PER_SM, "the CTAs of an SM share its tensor memory");
   static_assert(smem_bytes(MAX_TOK, 2, 1) <= MAX_SMEM, "two stages at least");
 };
 
