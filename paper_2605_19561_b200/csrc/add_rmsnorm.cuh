@@ -99,8 +99,7 @@ add_rmsnorm_kernel(const void* X, const void* R, void* R_out, const __nv_bfloat1
   __shared__ float part[2][32];
   const int tid = threadIdx.x, nt = blockDim.x, lane = tid & 31;
   const int pieces = d / 8;
-  griddep_launch_dependents();
-  griddep_wait();
+  griddep_launch_and_wait();
   Raw8<XF32> x[VPT];
   Raw8<RES == RES_F32> r[VPT];
   auto load = [&](int64_t row) {

@@ -167,8 +167,7 @@ matvec_split_kernel(const __nv_bfloat16* __restrict__ X, int K, uint8_t* __restr
   const uint4* row = reinterpret_cast<const uint4*>(X + m * K);
   // Into the L2 ahead of the product's W, which would stand before it in memory's queue.  Only that: the kernel before may still be writing x.
   if (k < K) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + k / 8));
-  griddep_launch_dependents();
-  griddep_wait();
+  griddep_launch_and_wait();
   uint32_t ref = 0;
   if constexpr (FMT == FMT_NVFP4) {
     uint32_t top = 0;
@@ -285,8 +284,8 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
 
   if (warp == 0) {
     // ------------------------------------------------------------------ W
+    griddep_wait();                                      // the stages are freed behind products that wait for the kernel before
     if constexpr (SPLIT) {
-      griddep_wait();
       if (elect_one())
         for (int it = 0; it < pre; ++it) fetch_digits(it, it);
       __syncwarp();
@@ -301,7 +300,6 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
       __syncwarp();
       if ((int)++s == nst) { s = 0; phase ^= 1; }
     }
-    if constexpr (!SPLIT) griddep_wait();
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer
     griddep_wait();                                      // the waits below count the digits, which wait for the kernel before

@@ -38,6 +38,8 @@ __device__ __forceinline__ void griddep_wait() {
 __device__ __forceinline__ void griddep_launch_dependents() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
+// Both, for a kernel that has nothing to do before and no bounded waits.
+__device__ __forceinline__ void griddep_launch_and_wait() { griddep_launch_dependents(); griddep_wait(); }
 
 // ---- mbarrier --------------------------------------------------------------------------------
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {

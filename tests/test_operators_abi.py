@@ -1,12 +1,15 @@
 """The operators around the layer, what needs no GPU: argument errors of the C entry points are status codes before anything
 touches a device, and the Python calls refuse tensors that are not the current GPU's."""
 import ctypes
+import os
+import re
 
 import pytest
 import torch
 
 from paper_2605_19561_b200 import torq
 
+CSRC = os.path.join(os.path.dirname(torq.__file__), "csrc")
 ONE, ODD = ctypes.c_void_p(16), ctypes.c_void_p(24)      # never dereferenced on these paths
 NULL, SHAPE, ALIGN, WORKSPACE = 1, 2, 3, 7
 
@@ -94,3 +97,20 @@ def test_gated_gemm_refuses_host_tensors():
     for f in (torq.torq_mxfp4_gated_gemm, torq.torq_mxint4_gated_gemm):
         with pytest.raises(ValueError):
             f(w, s, w, s)
+
+
+def test_every_role_waits_for_the_kernel_before_in_every_instance():
+    """The few-token kernel's roles pass griddepcontrol.wait before their first wait that has a limit, and not only in some instances of
+    the template."""
+    body = re.sub(r"//.*", "", open(os.path.join(CSRC, "matvec.cuh")).read())
+    body = body[re.search(r"^  griddep_launch_dependents\(\);", body, re.M).start():]
+    while (m := re.search(r"(?:else )?if constexpr \([^{;]*\) \{", body)):
+        end, depth = m.end(), 1
+        while depth:
+            depth += {"{": 1, "}": -1}.get(body[end], 0)
+            end += 1
+        body = body[:m.start()] + body[end:]
+    roles = re.split(r"^  (?:if \(warp == \d+\) \{|\} else if \(warp == \d+\) \{|\} else \{)$", body, flags=re.M)[1:4]   # behind them the teardown
+    assert len(roles) == 3
+    for role in roles:
+        assert "griddep_wait();" in role[:role.index("mbar_wait")]
