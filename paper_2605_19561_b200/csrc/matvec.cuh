@@ -442,7 +442,8 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
         }
         // MXINT4: until W is there, and with it the stage free; else until the stage is free (the first time round the barrier's phase
         // before its first counts as completed)
-        if (!mbar_wait_warp(PLANES ? full_bar(s) : empty_bar(s), phase, cta_abort, err_word, SITE_PRODUCER_EMPTY)) { ok = false; break; }
+        if (!mbar_wait_warp(PLANES ? full_bar(s) : empty_bar(s), phase, cta_abort, err_word,
+                            PLANES ? SITE_MMA_FULL : SITE_PRODUCER_EMPTY)) { ok = false; break; }
         const uint32_t st = smem_base + s * stage_bytes;
 #pragma unroll
         for (int j = 0; j < SLOTS; ++j) {
