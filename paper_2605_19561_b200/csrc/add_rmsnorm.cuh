@@ -14,12 +14,6 @@ namespace torq {
 
 enum : int { RES_NONE = 0, RES_BF16 = 1, RES_F32 = 2 };
 
-// Plain loads (the residual may be updated in place), kept out of the L1: every element is read once.
-__device__ __forceinline__ uint4 load_once(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
-  return v;
-}
 // Two float32 in a 64-bit register: one instruction for both, each rounded by itself as the scalar one.
 __device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
   uint64_t p;
@@ -123,7 +117,7 @@ add_rmsnorm_kernel(const void* X, const void* R, void* R_out, const __nv_bfloat1
 #pragma unroll
   for (int k = 0; k < VPT; ++k) {
     const int p = tid + k * nt;
-    w[k] = p < pieces ? __ldg(reinterpret_cast<const uint4*>(weight) + p) : make_uint4(0, 0, 0, 0);
+    w[k] = p < pieces ? load_once(reinterpret_cast<const uint4*>(weight) + p) : make_uint4(0, 0, 0, 0);
   }
   const int kb4 = (d / 32 + 3) / 4;
   int turn = 0;

@@ -169,14 +169,20 @@ matvec_split_kernel(const __nv_bfloat16* __restrict__ X, int K, uint8_t* __restr
   if (k < K) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + k / 8));
   griddep_launch_and_wait();
   uint32_t ref = 0;
+  uint4 own = make_uint4(0, 0, 0, 0);
   if constexpr (FMT == FMT_NVFP4) {
     uint32_t top = 0;
-    for (int i0 = threadIdx.x; i0 < K / 8; i0 += 8 * 256) {   // eight loads under way: each takes microseconds behind the next kernel's W
+    for (int p0 = 0; p0 < K / 8; p0 += 8 * 256) {        // eight loads under way: each takes microseconds behind the next kernel's W
       uint4 x[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = i0 + 256 * j < K / 8 ? __ldg(row + i0 + 256 * j) : make_uint4(0, 0, 0, 0);
+      for (int j = 0; j < 8; ++j)
+        if (p0 + 256 * j < K / 8) x[j] = load_once(row + min(p0 + 256 * j + (int)threadIdx.x, K / 8 - 1));
 #pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, largest8(x[j]));
+      for (int j = 0; j < 8; ++j)
+        if (p0 + 256 * j < K / 8) {
+          top = max(top, largest8(x[j]));
+          if (p0 / 256 + j == (int)(blockIdx.x % parts)) own = x[j];   // piece k / 8
+        }
     }
     top = __reduce_max_sync(0xFFFFFFFFu, top);
     if (lane == 0) top_of[warp] = top;
@@ -184,11 +190,12 @@ matvec_split_kernel(const __nv_bfloat16* __restrict__ X, int K, uint8_t* __restr
     for (int i = 0; i < 8; ++i) top = max(top, top_of[i]);
     ref = max(top >> 7, kLeastExponent + kScaleBinades);
     if (blockIdx.x % parts == 0 && threadIdx.x == 0) exponents[m] = ref;
+  } else if (k < K) {
+    own = load_once(row + k / 8);
   }
   if (k0 >= K) return;
-  const uint4 x = k < K ? __ldg(row + k / 8) : make_uint4(0, 0, 0, 0);
   uint32_t word[8], w, chunk, offset;
-  const uint32_t four = digits_of_256<FMT>(x, ref, lane, word);
+  const uint32_t four = digits_of_256<FMT>(own, ref, lane, word);
   if (k < K) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) *reinterpret_cast<uint32_t*>(codes + (8 * m + t) * (K / 2) + k / 2) = word[t];
@@ -205,7 +212,7 @@ matvec_split_kernel(const __nv_bfloat16* __restrict__ X, int K, uint8_t* __restr
 template <int FMT, bool GATED, int ROWS>
 __global__ void __launch_bounds__(192, DigitsCfg<FMT, GATED, ROWS>::CTAS_PER_SM)
 matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmD, const __nv_bfloat16* __restrict__ X,
-                     const uint8_t* __restrict__ Ws, const uint8_t* __restrict__ Ds, const uint32_t* __restrict__ token_exponents,
+                     const uint8_t* __restrict__ Ws, const uint8_t* __restrict__ Ds, const uint32_t* token_exponents,
                      void* __restrict__ Y, int y_is_bf16, int M, int N, int K, int S, int groups, int nst, float alpha, int* err_word) {
   using C = DigitsCfg<FMT, GATED, ROWS>;
   constexpr bool SPLIT = ROWS != ROWS_HERE;
@@ -411,7 +418,7 @@ matvec_digits_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_const
       // a warp takes 256 of K of a token, a lane eight elements (16 bytes)
       auto load = [&](int m, int it) {
         const int k = (kt0 + it) * C::BK + 8 * lane;
-        return m < mt && k < K ? __ldg(reinterpret_cast<const uint4*>(X + (int64_t)(m0 + m) * K + k)) : make_uint4(0, 0, 0, 0);
+        return m < mt && k < K ? load_once(X + (int64_t)(m0 + m) * K + k) : make_uint4(0, 0, 0, 0);
       };
       if constexpr (FMT == FMT_NVFP4) {
         for (int m = ew; m < mt; m += 4) {

@@ -95,7 +95,7 @@ mxfp4_gemm_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_con
                        const __grid_constant__ CUtensorMap tmSFA, const __grid_constant__ CUtensorMap tmSFB,
                        const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmBn,
                        const MixedTiles tiles, int y_is_bf16, int M, int N, int K, float alpha, int* err_word, void* Y,
-                       const uint32_t* __restrict__ token_exponents) {
+                       const uint32_t* token_exponents) {
   using C = GemmPairCfgT<FMT>;
   constexpr int CH = C::CH;
   constexpr int BN = C::BN;

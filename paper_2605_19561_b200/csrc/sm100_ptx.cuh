@@ -41,6 +41,14 @@ __device__ __forceinline__ void griddep_launch_dependents() {
 // Both, for a kernel that has nothing to do before and no bounded waits.
 __device__ __forceinline__ void griddep_launch_and_wait() { griddep_launch_dependents(); griddep_wait(); }
 
+// An operand that the kernel before may have written, 16 bytes, read once.  Not through the read-only path (__ldg): this kernel may have been
+// started before those writes, and what that path has once fetched or the compiler has moved need not see them.
+__device__ __forceinline__ uint4 load_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
 // ---- mbarrier --------------------------------------------------------------------------------
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");

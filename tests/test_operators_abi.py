@@ -114,3 +114,12 @@ def test_every_role_waits_for_the_kernel_before_in_every_instance():
     assert len(roles) == 3
     for role in roles:
         assert "griddep_wait();" in role[:role.index("mbar_wait")]
+
+
+@pytest.mark.parametrize("name", ["add_rmsnorm.cuh", "matvec.cuh", "mxfp4_gemm_pair.cuh"])
+def test_nothing_that_the_kernel_before_may_write_is_read_as_read_only(name):
+    """These kernels may start before the one in front has written their operands: no load of the read-only path, by name or by a
+    pointer that the compiler may take for one."""
+    code = re.sub(r"//.*", "", open(os.path.join(CSRC, name)).read())
+    assert "__ldg" not in code and "ld.global.nc" not in code
+    assert not re.search(r"const uint32_t\* __restrict__", code)
