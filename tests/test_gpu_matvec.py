@@ -245,3 +245,35 @@ def test_more_tokens(fmt, gated, M, N, K):
     assert not torch.isfinite(Y[M - 2]).any() and torch.equal(Y[rest], clean[rest])
     assert (buf[M * N:] == 7).all()
     assert torq.torq_last_device_error() == 0
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("M,N,K", [(1, 256, 512), (4, 128, 1024), (6, 256, 512), (24, 13824, 512), (17, 3840, 512)])
+def test_calls_in_a_row_share_memory(fmt, gated, M, N, K):
+    """Launches overlap: a norm writes x while the product before it may still run and the one behind it has been started, all on one x
+    and one workspace.  Each gives what it gives alone."""
+    g, calls = gen(M + N), 40
+    W = quantized(g, 2 * N if gated else N, K, fmt)
+    X = (heavy(g, calls, M, K) * 3).to(torch.bfloat16)
+    weight = torch.ones(K, dtype=torch.bfloat16, device=DEV)
+    x = torch.empty(M, K, dtype=torch.bfloat16, device=DEV)
+    ws = torch.empty(torq.torq_matvec_workspace_bytes(M, N, K), dtype=torch.uint8, device=DEV)
+    Y = torch.empty(2, calls, M, N, dtype=torch.bfloat16, device=DEV)
+
+    def both(i, y):
+        torq.torq_add_rmsnorm(X[i], weight, out=x)
+        matvec(fmt, x, W, gated, Y=y[i], workspace=ws)
+
+    for i in range(calls):
+        both(i, Y[0])
+        torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()                       # without the host between them
+    with torch.cuda.graph(graph):
+        for i in range(calls):
+            both(i, Y[1])
+    for _ in range(3):
+        Y[1].zero_()
+        graph.replay()
+        assert torch.equal(Y[0], Y[1])
+    assert torq.torq_last_device_error() == 0
