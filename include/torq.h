@@ -362,6 +362,7 @@ torq_status torq_mxint4_matvec(const void* X, const void* Wn, const void* Ws, in
 
 /* The gated pair of projections of a feed-forward block, in one launch:
  *   Y[m,n] = silu(g) u,  g = sum_k x[m,k] w^[n,k],  u = sum_k x[m,k] w^[N+n,k],  silu(g) = g / (1 + exp(-g)), float32 up to Y
+ * (a gate below -87.3, whose silu lies between -1.1e-36 and 0, counts as zero).
  * Both projections are one weight matrix of 2 N rows, gate rows first (Wq [2N, K/2], Ws of 2 N rows); Y [M, N] of y_dtype.
  * Otherwise as the products above.  N % 128 == 0. */
 torq_status torq_mxfp4_gated_matvec(const void* X, const void* Wq, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y,
