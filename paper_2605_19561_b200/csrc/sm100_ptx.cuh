@@ -40,6 +40,9 @@ __device__ __forceinline__ void griddep_launch_dependents() {
 }
 // Both, for a kernel that has nothing to do before and no bounded waits.
 __device__ __forceinline__ void griddep_launch_and_wait() { griddep_launch_dependents(); griddep_wait(); }
+// In this order the kernel keeps its neighbours apart: the next one cannot start before the one in front has completed, so what it reads ahead of
+// its own wait (weights) may have been written there.
+__device__ __forceinline__ void griddep_wait_and_launch() { griddep_wait(); griddep_launch_dependents(); }
 
 // An operand that the kernel before may have written, 16 bytes, read once.  Not through the read-only path (__ldg): this kernel may have been
 // started before those writes, and what that path has once fetched or the compiler has moved need not see them.

@@ -123,3 +123,16 @@ def test_nothing_that_the_kernel_before_may_write_is_read_as_read_only(name):
     code = re.sub(r"//.*", "", open(os.path.join(CSRC, name)).read())
     assert "__ldg" not in code and "ld.global.nc" not in code
     assert not re.search(r"const uint32_t\* __restrict__", code)
+
+
+def test_the_norm_lets_the_next_kernel_start_behind_the_kernel_before():
+    """What stands behind a norm reads its weights ahead of its wait: the norm, which may be all that is between it and what wrote them,
+    passes griddepcontrol.wait first."""
+    norm, ptx = (re.sub(r"//.*", "", open(os.path.join(CSRC, f)).read()) for f in ("add_rmsnorm.cuh", "sm100_ptx.cuh"))
+    kernel = norm[norm.index("add_rmsnorm_kernel("):]
+    calls = re.findall(r"griddep_\w+|griddepcontrol\.\w+", kernel)
+    order = []
+    for c in calls:
+        body = re.search(r"void " + c + r"\(\) \{(.*?)\n?\}", ptx, re.S).group(1)
+        order += re.findall(r"griddep_wait|griddep_launch_dependents", body) if "asm" not in body else [c]
+    assert order == ["griddep_wait", "griddep_launch_dependents"]
