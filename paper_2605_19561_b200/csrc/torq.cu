@@ -420,10 +420,16 @@ static MixedTiles plan_pair_tiles(int rows, int64_t cols, int max_pairs, double 
 // 207, 4096 x 16384, K = 2048 69.1 / 68.6, 4096 x 10240, K = 8192 133 / 130, 8192 x 10240, K = 4096 139.3 / 139.0, x 8192, K = 8192 215.0 /
 // 213.4.  Fewer columns or smaller weights lose: x 9216, K = 4096 125.0 / 125.3, 4500 x 8448 66.7 / 67.3, 8192 x 4096, K = 14336 179 /
 // 181, x 28672, K = 256 102 / 103; the rotation loses too (d = 14336, 8192 tokens, the layer 2886 / 3062).
-static MixedTiles plan_gemm_tiles(int64_t M, int64_t N, uint64_t w_row_bytes, int max_pairs) {
-  MixedTiles t = plan_pair_tiles((int)((M + 255) / 256), N, max_pairs, kNarrowTileCost);
+static MixedTiles group_gemm_tiles(MixedTiles t, int64_t N, uint64_t w_row_bytes) {
   if (N >= 8192 && (uint64_t)N * w_row_bytes >= (N >= 10240 ? 16u << 20 : 32u << 20)) t.group = 16;
   return t;
+}
+static MixedTiles plan_gemm_tiles(int64_t M, int64_t N, uint64_t w_row_bytes, int max_pairs) {
+  return group_gemm_tiles(plan_pair_tiles((int)((M + 255) / 256), N, max_pairs, kNarrowTileCost), N, w_row_bytes);
+}
+// Gates and ups of N features each, stacked: whole tiles only, each with 128 features of both.
+static MixedTiles plan_gated_tiles(int64_t M, int64_t N, uint64_t w_row_bytes) {
+  return group_gemm_tiles(mixed_tiles_make((int)((M + 255) / 256), (int)(N / 128), 0), 2 * N, w_row_bytes);
 }
 
 static int64_t write_tile_list(const MixedTiles& t, int32_t* out, int64_t cap) {
@@ -1086,12 +1092,7 @@ static torq_status digits_pair_launch(DeviceState* st, const void* D, const void
       !encode_2d(&tmSFB, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, Ws, (uint64_t)((features + 127) / 128), kb4 * 128, GATED ? 1 : 2, C::SF_BOX_WORDS,
                  CU_TENSOR_MAP_SWIZZLE_NONE))
     return TORQ_ERR_LAUNCH;
-  MixedTiles list = plan_gemm_tiles(rows, features, krow, st->gemm_pairs);
-  if (GATED) {                                           // whole tiles only
-    const int group = list.group;
-    list = mixed_tiles_make((int)((rows + 255) / 256), (int)(N / 128), 0);
-    list.group = group;
-  }
+  const MixedTiles list = GATED ? plan_gated_tiles(rows, N, krow) : plan_gemm_tiles(rows, N, krow, st->gemm_pairs);
   const int pairs = list.total < st->gemm_pairs ? list.total : st->gemm_pairs;
   launch_tc(mxfp4_gemm_pair_kernel<FMT, GATED, true>, 2, 2 * pairs, C::THREADS, C::SMEM_BYTES, s, tmA, tmB, tmSFA, tmSFB, tmA, tmBn, list,
             y_dtype == TORQ_BF16 ? 1 : 0, (int)rows, (int)N, (int)K, alpha, st->err_word, Y, exponents);
@@ -1189,8 +1190,7 @@ static torq_status gated_gemm_impl(const void* Aq, const void* As, const void* W
       !encode_2d(&tmY, ybf ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, ybf ? 2 : 4, Y, (uint64_t)M, (uint64_t)N, 32,
                  ybf ? 64 : 32))
     return TORQ_ERR_LAUNCH;
-  MixedTiles list = mixed_tiles_make((int)((M + 255) / 256), (int)(N / 128), 0);
-  list.group = plan_gemm_tiles(M, 2 * N, krow, st->gemm_pairs).group;
+  const MixedTiles list = plan_gated_tiles(M, N, krow);
   const int pairs = list.total < st->gemm_pairs ? list.total : st->gemm_pairs;
   launch_tc(mxfp4_gemm_pair_kernel<FMT, true>, 2, 2 * pairs, C::THREADS, C::SMEM_BYTES, static_cast<cudaStream_t>(stream), tmA, tmB, tmSFA, tmSFB,
             tmY, tmB, list, ybf ? 1 : 0, (int)M, (int)N, (int)K, alpha, st->err_word, static_cast<void*>(nullptr), static_cast<const uint32_t*>(nullptr));
