@@ -352,8 +352,10 @@ torq_status torq_add_rmsnorm_mxfp8(const void* X, torq_dtype x_dtype, const void
  * Products exact, sums float32.  The tensor cores do not take bfloat16 beside 4-bit weights, so x is split exactly into eight 3-bit digits,
  * each an FP4 operand, after it has been rounded to a multiple of 2^-21 of the power of two at or below the largest magnitude of its block of
  * 32 (NVFP4: 16, and a block's counts as 2^-17 of the largest in the token at least): elements down to 2^-14 of the block's largest keep all
- * their bits, nothing is off by more than 2^-22 of it.  What is smaller than 2^-106 counts as zero in part or whole; MXINT4: magnitudes of 2^125
- * and more as not a number.
+ * their bits, nothing is off by more than 2^-22 of it (which is more than a float32 sum loses where the large element meets a weight of zero:
+ * 2^-6 beside one of 2^16).  What is smaller than 2^-106 counts as zero in part or whole; MXINT4: a token with a magnitude of 2^126 or more
+ * is not a number.  The digits' magnitudes add up to at most three times (MXINT4: nine times) those of the products they stand for: sums
+ * of magnitudes that come as near as that to float32's largest may overflow.
  * Weights are read from HBM once, for 8 to 32 tokens at a time, the others finding them in the L2: made for decoding, any M <= 2^18 is served.  K % 128 == 0, K <= 65536, N % 8 == 0.  One launch without a workspace, else two; two calls that may overlap need a workspace
  * each.  Y and the workspace overlap no operand and not each other, here and in the entry points below. */
 size_t torq_matvec_workspace_bytes(int64_t M, int64_t N, int64_t K);
@@ -364,7 +366,7 @@ torq_status torq_nvfp4_matvec(const void* X, const void* Wq, const void* Ws, flo
 torq_status torq_mxint4_matvec(const void* X, const void* Wn, const void* Ws, int64_t M, int64_t N, int64_t K, void* Y, torq_dtype y_dtype,
                                void* workspace, size_t workspace_bytes, void* stream);
 
-/* The gated pair of projections of a feed-forward block, in one launch:
+/* The gated pair of projections of a feed-forward block, in one call:
  *   Y[m,n] = silu(g) u,  g = sum_k x[m,k] w^[n,k],  u = sum_k x[m,k] w^[N+n,k],  silu(g) = g / (1 + exp(-g)), float32 up to Y
  * (a gate below -87.3, whose silu lies between -1.1e-36 and 0, counts as zero).
  * Both projections are one weight matrix of 2 N rows, gate rows first (Wq [2N, K/2], Ws of 2 N rows); Y [M, N] of y_dtype.

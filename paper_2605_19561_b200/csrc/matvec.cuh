@@ -12,7 +12,8 @@
 //   v = sum_t d_t 8^(7-t), t = 0 ... 7,   x = sum_t d_t 2^(E-3t),
 // every digit is an e2m1 number and 2^(E-3t) a block scale: a token becomes eight rows of an MXFP4 operand, whose products with a
 // feature add up to the token's.  bfloat16's 8 bits are kept exactly down to 2^-14 of the block's largest magnitude, and nothing is off by more than
-// 2^-22 of it: half a unit of the sum that a float32 accumulator would make of the block.  (NVFP4 scales reach from 2^-9 to 2^8: the scale
+// 2^-22 of it: half a unit of the sum that a float32 accumulator would make of the block, if the large element enters it.  Where its weight is
+// zero the sum is small and the error is not (beside an element of 2^16 up to 2^-6).  (NVFP4 scales reach from 2^-9 to 2^8: the scale
 // of a block is taken relative to the token's largest one in this CTA's range of K, 2^(E-R+8), not below 2^(R-17), and the powers 8^-t
 // and 2^(R-8) are multiplied in when the eight sums are added.)
 // The digits cost some 200 instructions per eight elements of x.  Up to FEW_TOK tokens every CTA writes those of its own range of K, once

@@ -90,3 +90,18 @@ def test_every_code_and_position_in_the_pair_gemm(fmt, gated):
     codes = codes[:, None].expand(-1, K // 2).contiguous()
     X = torch.eye(K, dtype=torch.bfloat16, device=DEV)
     check(product(fmt, X, codes, 0, gated), X.double(), code_values(codes, fmt), gated)
+
+
+@pytest.mark.parametrize("M", [1, 3, 8, 20])
+def test_mxint4_takes_magnitudes_below_two_to_the_126(M):
+    N, K = 128, 256
+    codes = (torch.arange(N, device=DEV) % 16 * 0x11).to(torch.uint8)[:, None].expand(-1, K // 2).contiguous()
+    X = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+    X[:, 5] = 1.9921875 * 2.0 ** 125
+    X[:, 40] = -1.5
+    v = code_values(codes, "mxint4") * 2.0 ** -60
+    Y = product("mxint4", X, codes, -60, False)
+    assert torch.equal(Y, (X.double() @ v.t()).float())
+    X[M - 1, 5] = 2.0 ** 126                             # its scale for the upper halves has no byte
+    Z = product("mxint4", X, codes, -60, False)
+    assert Z[M - 1].isnan().all() and torch.equal(Z[:M - 1], Y[:M - 1])
