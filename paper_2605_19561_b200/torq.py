@@ -828,6 +828,8 @@ def _product(kind, A, As, Wq, Ws, out_dtype, Y, stream, a_scale=0.0, w_scale=0.0
         raise ValueError(f"{name}: W has gate and up rows, got an odd number of them")
     N = rows // 2 if gated else rows
     if Y is None:
+        if out_dtype not in _FLOATS:
+            raise ValueError(f"{name}: expected an out_dtype of {' or '.join(str(d) for d in _FLOATS)}, got {out_dtype}")
         Y = torch.empty((M, N), dtype=out_dtype, device=A.device)
         _used_by(stream, Y)
     _operand(Y, _FLOATS, "Y", (M, N))
@@ -837,7 +839,7 @@ def _product(kind, A, As, Wq, Ws, out_dtype, Y, stream, a_scale=0.0, w_scale=0.0
         if workspace is None:
             workspace = torch.empty(torq_matvec_workspace_bytes(M, N, K), dtype=torch.uint8, device=A.device)
             _used_by(stream, workspace)
-        _operand(workspace, (workspace.dtype,), "workspace")
+        _operand(workspace, (getattr(workspace, "dtype", "any type"),), "workspace")
         scratch = (_ptr(workspace), workspace.nbytes)
     _raise(getattr(lib(), name)(*x, _ptr(Wq), _ptr(Ws), *scales[-1:], M, N, K, _ptr(Y), _dtype_code(Y), *scratch, _stream(stream)), name)
     return Y
