@@ -336,6 +336,7 @@ torq_status torq_rotated_linear_mxint4(const void* X, const void* R_inter, const
  * layout, one E8M0 byte per 32 elements: byte = e + 127, e = clamp(floor(log2 amax) - 8, -127, 127) (amax == 0 -> byte 0), codes
  * E4M3(y / 2^e) to nearest even, saturating at 448, padding bytes 0x00: the A operand that torq_mxint4_gemm and
  * torq_mxint4_gated_gemm take (any E4M3 bytes with E8M0 scales are).  The squares of a row must sum to less than float32's largest value.
+ * Squares below 2^-126 lose bits: a row whose mean square and eps are as small as that is not normalised (zeros with eps = 0: not a number).
  * 32 <= d <= 16384, d % 32 == 0.  One launch.  Apart from residual_out the outputs overlap nothing. */
 torq_status torq_add_rmsnorm(const void* X, torq_dtype x_dtype, const void* residual, void* residual_out, torq_dtype r_dtype,
                              const void* weight, float eps, int64_t M, int64_t d, void* out, void* stream);

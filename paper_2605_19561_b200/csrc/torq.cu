@@ -466,8 +466,11 @@ static torq_status quantize_impl(DeviceState* st, const void* Z, torq_dtype dt, 
 // Whether the digits of x are written ahead of the product, by a kernel of their own: more than FEW_TOK tokens, or a CTA's range of K so long
 // that its own warps would hold up the weights.  (us, MXFP4, product alone / with that kernel: 1 x 5120 -> 5120, 4 steps of 256 5.2 / 5.4, 2
 // tokens 5.6 / 5.5, 4 tokens 6.4 / 5.9; 1 x 14336 -> 4096, 7 steps 7.8 / 8.3; 4 x 4096 -> 1024, 2 steps 3.4 / 4.3; 2 x 5120 -> 51200, 20 steps
-// 30.9 / 28.3; NVFP4 1 x 14336 -> 4096 8.3 / 9.8, 1 x 5120 -> 51200 32.1 / 29.4.)  The steps are counted with the cluster sizes that a part of
-// 148 SMs has room for, so that the answer, which a workspace is sized by, needs no device.
+// 30.9 / 28.3; NVFP4 1 x 14336 -> 4096 8.3 / 9.8, 1 x 5120 -> 51200 32.1 / 29.4.  The steps are counted with the cluster sizes that two CTAs
+// per SM leave room for on a part of 148 SMs, whatever the format, so that the answer, which a workspace is sized by, needs neither device nor format.
+// The gated MXINT4 product has one CTA per SM and up to twice the steps that are counted: 1 token is the same on both sides (us, product alone / with
+// that kernel: 10240 -> 5120 17.9 / 17.8, 14336 -> 4096 18.3 / 18.5, 4096 -> 14336 19.3 / 19.3), 4 tokens lose by up to 14 % (21.0 / 18.6, 21.8 / 19.4,
+// 22.7 / 19.9; 4096 -> 4096 9.75 / 8.95, 1024 -> 2816 4.70 / 4.83) where the rule has them written by the product.)
 static bool digits_ahead(int64_t M, int64_t N, int64_t K) {
   constexpr int fit[9] = {0, 1 << 30, 148, 93, 71, 56, 45, 37, 33};
   int S = 8;
