@@ -4,7 +4,7 @@
 //   y[m, n] = silu(g) u,  g / u = the product with row n / N + n.
 // Streaming the weights from HBM once is the work (K / 2 bytes and K / 32 or K / 16 scale bytes per row).  They go to the block-scaled
 // FP4 instruction as they are: widened to float16 in registers for warp-level instructions, they took 146 instructions per
-// 16 x 128 weights and the kernel was bound by those (1 x 5120 -> 5120 7.0 us, now 5.2; 16 tokens 11.5, now 8.0; 32 x 5120 -> 51200 107, now 42).
+// 16 x 128 weights and the kernel was bound by those (1 x 5120 -> 5120 7.0 us, now 5.1; 16 tokens 11.5, now 7.0; 32 x 5120 -> 51200 107, 42 in this kernel).
 //
 // What the instruction cannot take is a bfloat16 activation, so x is written as a sum of numbers that it can.  Per block of 32 (NVFP4: 16)
 // with largest magnitude in [2^E, 2^(E+1)), v = rint(x 2^(21-E)) is an integer of at most 22 bits and a sign; in base 8 with digits
