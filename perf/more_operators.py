@@ -5,6 +5,8 @@ One case is one call as a serving program makes it.  The cache lies in pages of 
 a table; every sequence has a length of its own.  A call's query tokens are the last of their sequences, `starts` says
 where each sequence's begin in the batch (absent: one token each).
 
+A page of one head holds, for its tokens, the codes of the keys, their scale bytes, the codes of the values, their scale bytes.
+
   append      new keys and values (columns of the rows of a fused projection) quantized into their slots, and read back
   attention   softmax(cap(scale q k) + bias) v over the cached tokens that a query may see, and the logarithm of the sum:
               causal, optionally a window, a prefix seen by all, a first token of each query's document, scores capped by a
@@ -144,212 +146,207 @@ def _dequantize(codes, sf, fmt, tensor_scale):
     return torch.ldexp(v, sf.int().unsqueeze(-1) - 127).flatten(-2)
 
 
-def _pages_of(s, b, table="table"):
-    length = s["lens"][b] if table == "table" else s["new_lens"][b]
-    return s[table][b, :-(-length // s["page"])].long(), length
-
-
-def _tokens(s, name, b):
-    """What the pages of sequence b hold under `name`, [kv_heads, length, ...]."""
-    pages, length = _pages_of(s, b)
-    return s[name][pages].transpose(0, 1).flatten(1, 2)[:, :length]
-
-
-def _fill(s, K, V):
-    """The cache of a program that has run so far: K and V [pages, kv_heads, page, dim]."""
-    for name, x in (("k", K), ("v", V)):
-        s[name + "_codes"], s[name + "_scales"] = _quantize(x, s["fmt"], s[name + "_scale"])
-    if not own:
-        return
-    from paper_2605_19561_b200 import torq
-    s["cache"] = _empty_cache(s)
-    for b, length in enumerate(s["lens"]):
-        if length:
-            pages, _ = _pages_of(s, b)
-            k, v = (x[pages].transpose(1, 2).flatten(0, 1)[:length].contiguous() for x in (K, V))
-            torq.torq_kv_append(s["cache"], s["table"][b:b + 1], s["lengths"][b:b + 1], k, v, starts=_starts([length]))
-
-
-def _empty_cache(s):
-    from paper_2605_19561_b200 import torq
-    return torq.torq_kv_cache(s["fmt"], s["pages"], s["page"], s["kv_heads"], s["dim"], s["k_scale"], s["v_scale"])
-
-
-def _starts(counts):
-    return torch.tensor([sum(counts[:i]) for i in range(len(counts) + 1)], dtype=torch.int32, device="cuda")
+def _page_parts(pages, fmt, dim):
+    """The parts of pages [pages, kv_heads, bytes]: of the keys and of the values, codes [.., page, dim / 2] and scale bytes [.., page, blocks]."""
+    code, sf = dim // 2, dim // (16 if fmt == "nvfp4" else 32)
+    page = pages.shape[2] // (2 * (code + sf))
+    parts, at = [], 0
+    for n in (code, sf, code, sf):
+        parts.append(pages[:, :, at:at + page * n].unflatten(2, (page, n)))
+        at += page * n
+    return parts
 
 
 def prepare(case, seed):
     g = torch.Generator(device="cuda").manual_seed(seed)
     s = dict(case)
-    H, D, P, B = case["kv_heads"], case["dim"], case["page"], case["batch"]
+    H, D, P, B, fmt = case["kv_heads"], case["dim"], case["page"], case["batch"], case["fmt"]
     s["lens"], s["news"] = _lengths(case)
-    s["new_lens"] = [min(n, case["keep"]) for n in s["lens"]]
-    counts = [-(-n // P) for n in s["lens"]]
-    more = [-(-n // P) for n in s["new_lens"]]
-    s["pages"] = sum(counts) + sum(more) + 3
-    order = torch.randperm(s["pages"], generator=g, device="cuda").to(torch.int32)
-    for name, c, at in (("table", counts, 0), ("new_table", more, sum(counts))):
-        s[name] = torch.zeros(B, max(1, max(c)), dtype=torch.int32, device="cuda")
-        for b, n in enumerate(c):
-            s[name][b, :n] = order[at:at + n]
-            at += n
+    s["kept"] = [min(n, case["keep"]) for n in s["lens"]]
+    counts, more = [-(-n // P) for n in s["lens"]], [-(-n // P) for n in s["kept"]]
+    total = sum(counts) + sum(more) + 3
+    order = torch.randperm(total, generator=g, device="cuda").to(torch.int32)
+    s["table"], s["new_table"] = _table(counts, order), _table(more, order[sum(counts):])
     s["lengths"] = torch.tensor(s["lens"], dtype=torch.int32, device="cuda")
-    T = sum(s["news"])
+    s["tokens"] = T = sum(s["news"])
     s["starts"] = None if case["new"] == 1 else _starts(s["news"])
-    nv = case["fmt"] == "nvfp4"
-    s["k_scale"], s["v_scale"] = (80.0 / (6 * 448), 5.0 / (6 * 448)) if nv else (1.0, 1.0)   # calibrated ahead of time
+    s["scales"] = (80.0 / (6 * 448), 5.0 / (6 * 448)) if fmt == "nvfp4" else ()              # calibrated ahead of time
     loud = torch.where(torch.rand(H, D, generator=g, device="cuda") < 0.02, 8.0, 1.0)        # a few channels of the keys
-    if case["op"] == "append":
-        q = case["group"] * H
-        rows = _gaussian(g, T, q + 2 * H, D)
-        rows[:, q:q + H] *= loud
-        s["rows"] = rows.to(torch.bfloat16)
-        s["K"], s["V"] = s["rows"][:, q:q + H], s["rows"][:, q + H:]
-        for name in ("k", "v"):
-            s[name + "_codes"] = torch.zeros(s["pages"], H, P, D // 2, dtype=torch.uint8, device="cuda")
-            s[name + "_scales"] = torch.zeros(s["pages"], H, P, D // (16 if nv else 32), dtype=torch.uint8, device="cuda")
-        if own:
-            s["cache"] = _empty_cache(s)
-        return s
-    _fill(s, (_gaussian(g, s["pages"], H, P, D) * loud.unsqueeze(1)).to(torch.bfloat16), _gaussian(g, s["pages"], H, P, D).to(torch.bfloat16))
-    if case["op"] == "evict":
-        w = _gaussian(g, s["pages"], H, P).mul_(2.0).exp_()
-        s["weights"] = torch.where(torch.rand(w.shape, generator=g, device="cuda") < 0.1, 0.0, w)    # and some that nobody looked at
-        s["new_starts"] = _starts(s["new_lens"])
-        return s
-    s["Q"] = (1.5 * _gaussian(g, T, H * case["group"], D) / (1.0 + 0.4 * loud.repeat_interleave(case["group"], 0))).to(torch.bfloat16)
-    s["factor"] = D ** -0.5
     heads = H * case["group"]
+    if case["op"] == "append":
+        rows = _gaussian(g, T, heads + 2 * H, D)
+        rows[:, heads:heads + H] *= loud
+        s["K"], s["V"] = rows.to(torch.bfloat16).split([heads, H, H], dim=1)[1:]
+        s["pages"] = torch.zeros(total, H, 2 * P * (D // 2 + D // (16 if fmt == "nvfp4" else 32)), dtype=torch.uint8, device="cuda")
+        return s
+    K, V = (_gaussian(g, total, H, P, D) * loud.unsqueeze(1)).to(torch.bfloat16), _gaussian(g, total, H, P, D).to(torch.bfloat16)
+    s["pages"] = torch.cat([x.flatten(2) for x in (*_quantize(K, fmt, _scale(s, 0)), *_quantize(V, fmt, _scale(s, 1)))], dim=2)
+    if case["op"] == "evict":
+        w = _gaussian(g, total, H, P).mul_(2.0).exp_()
+        s["weights"] = torch.where(torch.rand(w.shape, generator=g, device="cuda") < 0.1, 0.0, w)    # and some that nobody looked at
+        s["new_starts"], s["new_tokens"] = _starts(s["kept"]), sum(s["kept"])
+        return s
+    s["Q"] = (1.5 * _gaussian(g, T, heads, D) / (1.0 + 0.4 * loud.repeat_interleave(case["group"], 0))).to(torch.bfloat16)
+    s["factor"] = D ** -0.5
     s["slopes"] = torch.exp2(-8.0 * torch.arange(1, heads + 1, device="cuda") / heads) if case["bias"] else None
     s["prefixes"] = (s["lengths"] // 3).to(torch.int32) if case["prefix"] else None
     s["first"] = None
     if case["documents"]:                                  # two documents: the later half of the new tokens starts another one
-        s["first"] = torch.cat([torch.where(torch.arange(n, device="cuda") < n // 2, 0, length - n + n // 2)
-                                for n, length in zip(s["news"], s["lens"])]).to(torch.int32)
+        seq, slot = _places(s)
+        middle = s["lengths"][seq] - torch.tensor([n - n // 2 for n in s["news"]], device="cuda")[seq]
+        s["first"] = torch.where(slot < middle, 0, middle).to(torch.int32)
     if case["op"] == "weights":
-        s["weights"] = _gaussian(g, s["pages"], H, P).abs_()
+        s["weights"] = _gaussian(g, total, H, P).abs_()
         s["out"] = torch.zeros_like(s["weights"])
-        s["lse"] = torch.cat([_scores(s, b).double().logsumexp(-1).float().permute(2, 0, 1).flatten(1)
-                              for b in range(B) if s["news"][b]])
+        s["lse"] = _unpadded(s, _scores(s).double().logsumexp(-1).float().permute(0, 3, 1, 2)).flatten(1)
     return s
 
 
+def _table(counts, order):
+    """A row of page numbers for each sequence, taken one after the other from `order`; zeros behind them."""
+    c = torch.tensor(counts, device="cuda").unsqueeze(1)
+    at = c.cumsum(0) - c + torch.arange(max(1, max(counts)), device="cuda")
+    return torch.where(at < c.cumsum(0), order[at.clamp(max=order.numel() - 1)], 0).to(torch.int32)
+
+
+def _starts(counts):
+    return torch.tensor([0] + counts, device="cuda").cumsum(0).to(torch.int32)
+
+
+def _scale(s, i):
+    return s["scales"][i] if s["scales"] else 1.0
+
+
 # ---- plain forms ----------------------------------------------------------------------------------------------
-def _begin(s, b):
-    return sum(s["news"][:b])
+def _places(s, lengths=None, starts=None, tokens=None):
+    """Of each new token its sequence and its place in that, in the order of the batch."""
+    lengths = s["lengths"] if lengths is None else lengths
+    starts = s["starts"] if starts is None else starts
+    if starts is None:
+        starts = torch.arange(s["batch"] + 1, device="cuda")
+    i = torch.arange(s["tokens"] if tokens is None else tokens, device="cuda")
+    seq = torch.bucketize(i, starts[1:], right=True)
+    return seq, lengths[seq] - starts[seq + 1] + i
 
 
-def _scores(s, b):
-    """Scores of the queries of sequence b with its tokens, [kv_heads, group, new, length], -inf where a query may not look."""
-    n, length, H, D = s["news"][b], s["lens"][b], s["kv_heads"], s["dim"]
-    at = _begin(s, b)
-    q = s["Q"][at:at + n].float().view(n, H, -1, D).permute(1, 2, 0, 3)
-    k = _dequantize(_tokens(s, "k_codes", b), _tokens(s, "k_scales", b), s["fmt"], s["k_scale"])
-    x = (q.flatten(1, 2) @ k.transpose(1, 2)).view(H, -1, n, length).mul_(s["factor"])
+def _padded(s, x):
+    """[tokens, ...] -> [batch, most new tokens of a sequence, ...], what is not there repeats some token."""
+    starts = torch.arange(s["batch"] + 1, device="cuda") if s["starts"] is None else s["starts"]
+    i = starts[:-1].unsqueeze(1) + torch.arange(max(s["news"]), device="cuda")
+    return x[i.clamp(max=s["tokens"] - 1)]
+
+
+def _unpadded(s, x):
+    seq, slot = _places(s)
+    first = s["lengths"] - (1 if s["starts"] is None else s["starts"].diff())
+    return x[seq, slot - first[seq]]
+
+
+def _cached(s, i):
+    """The keys (0) or values (1) of all sequences, [batch, kv_heads, longest, dim] in 32 bits."""
+    codes, sf = _page_parts(s["pages"], s["fmt"], s["dim"])[2 * i:2 * i + 2]
+    codes, sf = (x[s["table"].long()].transpose(1, 2).flatten(2, 3)[:, :, :s["longest"]] for x in (codes, sf))
+    return _dequantize(codes, sf, s["fmt"], _scale(s, i))
+
+
+def _scores(s):
+    """Scores of all queries with the tokens of their sequence, [batch, kv_heads, group, new, longest], -inf where a query may not look."""
+    B, H, n = s["batch"], s["kv_heads"], max(s["news"])
+    q = _padded(s, s["Q"]).float().view(B, n, H, s["group"], s["dim"]).permute(0, 2, 3, 1, 4)
+    x = (q.flatten(2, 3) @ _cached(s, 0).transpose(2, 3)).view(B, H, s["group"], n, -1).mul_(s["factor"])
     if s["softcap"]:
         x = x.div_(s["softcap"]).tanh_().mul_(s["softcap"])
-    j = torch.arange(length, device="cuda")
-    p = torch.arange(length - n, length, device="cuda").unsqueeze(1)
+    j = torch.arange(s["longest"], device="cuda")
+    p = _padded(s, _places(s)[1]).unsqueeze(2)
     if s["slopes"] is not None:
-        x -= s["slopes"].view(H, -1, 1, 1) * (p - j).abs()
-    seen = j <= p if s["prefixes"] is None else (j <= p) | (j < s["prefixes"][b])
+        x -= s["slopes"].view(H, -1, 1, 1) * (p - j).abs().view(B, 1, 1, n, -1)
+    seen = j <= p if s["prefixes"] is None else (j <= p) | (j < s["prefixes"].view(B, 1, 1))
     if s["window"]:
         seen = seen & (j > p - s["window"])
     if s["first"] is not None:
-        seen = seen & (j >= s["first"][at:at + n].unsqueeze(1))
-    return x.masked_fill_(~seen, -math.inf)
+        seen = seen & (j >= _padded(s, s["first"]).unsqueeze(2))
+    seen = seen & (j < s["lengths"].view(B, 1, 1))
+    return x.masked_fill_(~seen.view(B, 1, 1, n, -1), -math.inf)
+
+
+def _plain_read(s, table, lengths, starts, tokens):
+    seq, slot = _places(s, lengths, starts, tokens)
+    page = table[seq, slot // s["page"]].long()
+    parts = [x[page, :, slot % s["page"]] for x in _page_parts(s["pages"], s["fmt"], s["dim"])]
+    return tuple(_dequantize(*parts[2 * i:2 * i + 2], s["fmt"], _scale(s, i)).to(torch.bfloat16) for i in (0, 1))
 
 
 def _plain_append(s):
-    for b, n in enumerate(s["news"]):
-        if n:
-            slot = torch.arange(s["lens"][b] - n, s["lens"][b], device="cuda")
-            page = s["table"][b].long()[slot // s["page"]]
-            at = _begin(s, b)
-            for name, x in (("k", s["K"]), ("v", s["V"])):
-                codes, sf = _quantize(x[at:at + n], s["fmt"], s[name + "_scale"])
-                s[name + "_codes"][page, :, slot % s["page"]] = codes
-                s[name + "_scales"][page, :, slot % s["page"]] = sf
-    return tuple(_plain_read(s, name, "table", s["lens"], s["news"]) for name in ("k", "v"))
-
-
-def _plain_read(s, name, table, lens, news):
-    parts = []
-    for b, n in enumerate(news):
-        slot = torch.arange(lens[b] - n, lens[b], device="cuda")
-        page, slot = s[table][b].long()[slot // s["page"]], slot % s["page"]
-        parts.append(_dequantize(s[name + "_codes"][page, :, slot], s[name + "_scales"][page, :, slot], s["fmt"], s[name + "_scale"]))
-    return torch.cat(parts).to(torch.bfloat16)
+    seq, slot = _places(s)
+    page = s["table"][seq, slot // s["page"]].long()
+    new = (*_quantize(s["K"], s["fmt"], _scale(s, 0)), *_quantize(s["V"], s["fmt"], _scale(s, 1)))
+    for part, x in zip(_page_parts(s["pages"], s["fmt"], s["dim"]), new):
+        part[page, :, slot % s["page"]] = x
+    return _plain_read(s, s["table"], s["lengths"], s["starts"], s["tokens"])
 
 
 def _plain_attention(s):
-    out = torch.zeros(s["Q"].shape, dtype=torch.bfloat16, device="cuda")
-    lse = torch.full(s["Q"].shape[:2], -math.inf, device="cuda")
-    for b, n in enumerate(s["news"]):
-        if not n or not s["lens"][b]:
-            continue
-        x = _scores(s, b)
-        m = x.amax(-1, keepdim=True).clamp_(min=-1e30)
-        x = x.sub_(m).exp_()
-        total = x.sum(-1, keepdim=True)
-        v = _dequantize(_tokens(s, "v_codes", b), _tokens(s, "v_scales", b), s["fmt"], s["v_scale"])
-        o = (x.flatten(1, 2) @ v).view(*x.shape[:3], -1) / total.clamp(min=1e-30)
-        at = _begin(s, b)
-        out[at:at + n] = o.permute(2, 0, 1, 3).flatten(1, 2).to(torch.bfloat16)
-        lse[at:at + n] = (m + total.log()).squeeze(-1).permute(2, 0, 1).flatten(1)
-    return out, lse
+    x = _scores(s)
+    m = x.amax(-1, keepdim=True).clamp_(min=-1e30)
+    x = x.sub_(m).exp_()
+    total = x.sum(-1, keepdim=True)
+    o = (x.flatten(2, 3) @ _cached(s, 1)).view(*x.shape[:4], -1) / total.clamp(min=1e-30)
+    lse = (m + total.log()).squeeze(-1)
+    return _unpadded(s, o.permute(0, 3, 1, 2, 4)).flatten(1, 2).to(torch.bfloat16), _unpadded(s, lse.permute(0, 3, 1, 2)).flatten(1)
 
 
 def _plain_weights(s):
+    B, j = s["batch"], torch.arange(s["longest"], device="cuda")
+    new = 1 if s["starts"] is None else s["starts"].diff().view(B, 1, 1)
+    lse = _padded(s, s["lse"]).view(B, -1, s["kv_heads"], s["group"]).permute(0, 2, 3, 1).unsqueeze(-1)
+    there = (lse > -math.inf) & (torch.arange(max(s["news"]), device="cuda").unsqueeze(1) < torch.as_tensor(new, device="cuda").view(-1, 1, 1, 1, 1))
+    w = torch.where(there, (_scores(s) - lse).exp_(), 0.0).sum((2, 3))
+    lengths = s["lengths"].view(B, 1, 1)
+    old = s["weights"][s["table"].long()].transpose(1, 2).flatten(2, 3)[:, :, :s["longest"]]
+    w += torch.where(j < lengths - new, old, 0.0)
     out = torch.zeros_like(s["weights"])
-    for b, n in enumerate(s["news"]):
-        length = s["lens"][b]
-        if not n or not length:
-            continue
-        at = _begin(s, b)
-        lse = s["lse"][at:at + n].view(n, s["kv_heads"], -1).permute(1, 2, 0).unsqueeze(-1)
-        w = torch.where(lse > -math.inf, (_scores(s, b) - lse).exp_(), 0.0).sum((1, 2))
-        w[:, :length - n] += _tokens(s, "weights", b)[:, :length - n]
-        slot = torch.arange(length, device="cuda")
-        out[s["table"][b].long()[slot // s["page"]], :, slot % s["page"]] = w.t()
+    seq, slot = (j < lengths.squeeze(1)).nonzero(as_tuple=True)
+    out[s["table"][seq, slot // s["page"]].long(), :, slot % s["page"]] = w[seq, :, slot]
     return out
 
 
 def _plain_evict(s):
-    H, P = s["kv_heads"], s["page"]
-    kept = torch.full((s["batch"], H, s["keep"]), -1, dtype=torch.int32, device="cuda")
-    for b, (length, n) in enumerate(zip(s["lens"], s["new_lens"])):
-        recent = min(s["recent"], n)
-        w = _tokens(s, "weights", b)[:, :length - recent]
-        best = torch.sort(w, dim=1, descending=True, stable=True).indices[:, :n - recent]
-        src = torch.cat((best.sort(dim=1).values, torch.arange(length - recent, length, device="cuda").expand(H, -1)), dim=1)
-        kept[b, :, :n] = src.to(torch.int32)
-        from_page, head = s["table"][b].long()[src // P], torch.arange(H, device="cuda").unsqueeze(1)
-        slot = torch.arange(n, device="cuda")
-        to_page = s["new_table"][b].long()[slot // P].expand(H, -1)
-        for name in ("k_codes", "k_scales", "v_codes", "v_scales", "weights"):
-            s[name][to_page, head, (slot % P).expand(H, -1)] = s[name][from_page, head, src % P]
-    lengths = s["lengths"].clamp(max=s["keep"])
-    return (lengths, kept, s["weights"]) + tuple(_plain_read(s, name, "new_table", s["new_lens"], s["new_lens"]) for name in ("k", "v"))
+    B, H, P, keep = s["batch"], s["kv_heads"], s["page"], s["keep"]
+    lengths = s["lengths"].clamp(max=keep)
+    n, old, j = lengths.view(B, 1, 1), s["lengths"].view(B, 1, 1), torch.arange(s["longest"], device="cuda")
+    w = s["weights"][s["table"].long()].transpose(1, 2).flatten(2, 3)[:, :, :s["longest"]]
+    w = torch.where(j >= old - n.clamp(max=s["recent"]), math.inf, w).masked_fill_(j >= old, -math.inf)
+    order = torch.sort(w, dim=2, descending=True, stable=True).indices
+    rank = torch.empty_like(order).scatter_(2, order, j.expand_as(order))
+    src = torch.where(rank < n, j, s["longest"]).sort(dim=2).values[:, :, :keep]
+    to = torch.arange(src.shape[2], device="cuda")
+    kept = torch.full((B, H, keep), -1, dtype=torch.int32, device="cuda")
+    kept[:, :, :src.shape[2]] = torch.where(to < n, src, -1)
+    b, h, to = (to < n).expand_as(src).nonzero(as_tuple=True)
+    src = src[b, h, to]
+    from_page, to_page = s["table"][b, src // P].long(), s["new_table"][b, to // P].long()
+    for part in (*_page_parts(s["pages"], s["fmt"], s["dim"]), s["weights"]):
+        part[to_page, h, to % P] = part[from_page, h, src % P]
+    return (lengths, kept, s["weights"]) + _plain_read(s, s["new_table"], lengths, s["new_starts"], s["new_tokens"])
 
 
 def run(s):
     if not own:
         return {"append": _plain_append, "attention": _plain_attention, "weights": _plain_weights, "evict": _plain_evict}[s["op"]](s)
     from paper_2605_19561_b200 import torq
+    call = lambda name: getattr(torq, f"torq_{s['fmt']}_kv_{name}")
     if s["op"] == "append":
-        torq.torq_kv_append(s["cache"], s["table"], s["lengths"], s["K"], s["V"], starts=s["starts"])
-        return torq.torq_kv_read(s["cache"], s["table"], s["lengths"], sum(s["news"]), starts=s["starts"])
+        call("append")(s["pages"], s["table"], s["lengths"], s["K"], s["V"], *s["scales"], starts=s["starts"])
+        return call("read")(s["pages"], s["table"], s["lengths"], s["dim"], s["tokens"], *s["scales"], starts=s["starts"])
     if s["op"] == "evict":
-        lengths, kept = torq.torq_kv_evict(s["cache"], s["table"], s["lengths"], s["weights"], s["new_table"], s["keep"], s["recent"])
-        return (lengths, kept, s["weights"]) + tuple(
-            torq.torq_kv_read(s["cache"], s["new_table"], lengths, sum(s["new_lens"]), starts=s["new_starts"]))
+        lengths, kept = call("evict")(s["pages"], s["table"], s["lengths"], s["dim"], s["weights"], s["new_table"], s["keep"], s["recent"])
+        return (lengths, kept, s["weights"]) + call("read")(
+            s["pages"], s["new_table"], lengths, s["dim"], s["new_tokens"], *s["scales"], starts=s["new_starts"])
     options = {"starts": s["starts"], "scale": s["factor"], "softcap": s["softcap"], "slopes": s["slopes"], "window": s["window"],
                "prefix": s["prefixes"], "first": s["first"]}
     if s["op"] == "attention":
-        return torq.torq_kv_attention(s["cache"], s["table"], s["lengths"], s["Q"], return_lse=True, **options)
-    return torq.torq_kv_weights(s["cache"], s["table"], s["lengths"], s["Q"], s["lse"], s["weights"], weights_out=s["out"], **options)
+        return call("attention")(s["pages"], s["table"], s["lengths"], s["Q"], *s["scales"], return_lse=True, **options)
+    return call("weights")(s["pages"], s["table"], s["lengths"], s["Q"], s["lse"], s["weights"], *s["scales"][:1], weights_out=s["out"], **options)
 
 
 def work(case):
@@ -416,28 +413,28 @@ def _rounded(x, fmt, tensor_scale):
     return (q * scale).view_as(x)
 
 
-def _gathered(s, name, b, h, slots, table="table"):
-    return s[name][s[table][b].long()[slots // s["page"]], h, slots % s["page"]]
+def _gathered(s, part, b, h, slots, table="table"):
+    return part[s[table][b].long()[slots // s["page"]], h, slots % s["page"]]
 
 
-def _read_exact(s, b, h, slots, table="table"):
-    return [_number(_gathered(s, n + "_codes", b, h, slots, table), _gathered(s, n + "_scales", b, h, slots, table), s["fmt"], s[n + "_scale"])
-            for n in ("k", "v")]
+def _read_exact(s, b, h, slots):
+    p = [_gathered(s, x, b, h, slots) for x in _page_parts(s["pages"], s["fmt"], s["dim"])]
+    return _number(p[0], p[1], s["fmt"], _scale(s, 0)), _number(p[2], p[3], s["fmt"], _scale(s, 1))
 
 
 def exact(case, seed):
     s = prepare(case, seed)
     H, G, D, fmt = case["kv_heads"], case["group"], case["dim"], case["fmt"]
     if case["op"] == "append":
-        return tuple(_rounded(s[n].double().reshape(-1, D), fmt, s[n.lower() + "_scale"]).view(s[n].shape) for n in ("K", "V"))
+        return tuple(_rounded(s[n].double().reshape(-1, D), fmt, _scale(s, i)).view(s[n].shape) for i, n in enumerate(("K", "V")))
     if case["op"] == "evict":
         kept = torch.full((case["batch"], H, case["keep"]), -1, dtype=torch.int64, device="cuda")
         weights, parts = s["weights"].double().clone(), ([], [])
-        for b, (length, n) in enumerate(zip(s["lens"], s["new_lens"])):
+        for b, (length, n) in enumerate(zip(s["lens"], s["kept"])):
             slots, rows = torch.arange(length, device="cuda"), ([], [])
             recent = min(case["recent"], n)
             for h in range(H):
-                w = _gathered(s, "weights", b, h, slots).double()
+                w = _gathered(s, s["weights"], b, h, slots).double()
                 w[length - recent:] = math.inf
                 # kept: how many come before a token, by weight and then by place, is less than the room
                 rank = torch.empty_like(slots)
@@ -445,18 +442,18 @@ def exact(case, seed):
                 src = slots[rank < n]
                 kept[b, h, :n] = src
                 to = slots[:n]
-                weights[s["new_table"][b].long()[to // s["page"]], h, to % s["page"]] = _gathered(s, "weights", b, h, src).double()
+                weights[s["new_table"][b].long()[to // s["page"]], h, to % s["page"]] = _gathered(s, s["weights"], b, h, src).double()
                 for r, x in zip(rows, _read_exact(s, b, h, src)):
                     r.append(x)
             for p, r in zip(parts, rows):
                 p.append(torch.stack(r, dim=1))
-        return (torch.tensor(s["new_lens"], device="cuda"), kept, weights, torch.cat(parts[0]), torch.cat(parts[1]))
+        return (torch.tensor(s["kept"], device="cuda"), kept, weights, torch.cat(parts[0]), torch.cat(parts[1]))
     if sum(n * length for n, length in zip(s["news"], s["lens"])) * H * G * D > _MAX_PRODUCTS:
         return None
     T = sum(s["news"])
     out = torch.zeros(T, H * G, D, dtype=torch.float64, device="cuda")
     lse = torch.full((T, H * G), -math.inf, dtype=torch.float64, device="cuda")
-    account, at = torch.zeros(s["pages"], H, case["page"], dtype=torch.float64, device="cuda"), 0
+    account, at = torch.zeros(s["weights"].shape if case["op"] == "weights" else 0, dtype=torch.float64, device="cuda"), 0
     for b, (n, length) in enumerate(zip(s["news"], s["lens"])):
         slots = torch.arange(length, device="cuda")
         place = torch.arange(n, device="cuda").unsqueeze(1) + (length - n)
@@ -486,7 +483,7 @@ def exact(case, seed):
                 lse[at:at + n, q] = y
                 out[at:at + n, q] = torch.where(torch.isinf(y).unsqueeze(1), 0.0, torch.exp(x - y.unsqueeze(1))) @ v
             if case["op"] == "weights":
-                old = _gathered(s, "weights", b, h, slots).double()
+                old = _gathered(s, s["weights"], b, h, slots).double()
                 account[s["table"][b].long()[slots // case["page"]], h, slots % case["page"]] = total + torch.where(slots < length - n, old, 0.0)
         at += n
     return account if case["op"] == "weights" else (out, lse)
