@@ -52,7 +52,8 @@ typedef enum {
   TORQ_ERR_ARCH = 4,       /* current device is not compute capability 10.x */
   TORQ_ERR_LAUNCH = 5,     /* CUDA reported an error while encoding descriptors or launching */
   TORQ_ERR_TIMEOUT = 6,    /* (device error word) a bounded wait inside a kernel ran out */
-  TORQ_ERR_WORKSPACE = 7   /* workspace missing or smaller than torq_workspace_bytes() */
+  TORQ_ERR_WORKSPACE = 7,  /* workspace missing or smaller than torq_workspace_bytes() */
+  TORQ_ERR_PAGE = 8        /* (device error word) a page number or a length of a key/value cache is out of range */
 } torq_status;
 
 typedef enum { TORQ_F32 = 0, TORQ_BF16 = 1 } torq_dtype;
@@ -436,7 +437,7 @@ torq_status torq_selftest_wait_timeout(uint64_t limit_ns, void* result_u64x3, vo
 const char* torq_status_string(torq_status s);
 
 /* Synchronises `stream`, then returns and clears the device error word of the current device:
- * 0, or TORQ_ERR_TIMEOUT in the low byte with the id of the wait that gave up in bits 8..15. */
+ * 0, or TORQ_ERR_TIMEOUT in the low byte with the id of the wait that gave up in bits 8..15, or TORQ_ERR_PAGE. */
 int torq_last_device_error(void* stream);
 
 /* Host helper (no device work): the list of output tiles that the CTA-pair kernels (more than
@@ -462,6 +463,97 @@ int64_t torq_gemm_tile_list(int64_t M, int64_t N, int64_t w_row_bytes, int32_t p
 
 /* Number of kernels this library has launched since load (all devices, all streams). */
 int64_t torq_launch_count(void);
+
+/* ---- a key/value cache in 4 bits --------------------------------------------------------------------------------------------------------
+ * The cache of an attention layer lies in pages of page_tokens tokens (a power of two from 16 to 1024) that all sequences share; table[b][i] is
+ * the page of the tokens i page_tokens ... of sequence b.  A page holds, for one key/value head after the other,
+ *   key codes [page_tokens][D/2] | key scale bytes [page_tokens][D/B] | value codes [page_tokens][D/2] | value scale bytes [page_tokens][D/B]
+ * with D = head_dim (64, 128 or 256), B = 32 (MXFP4, MXINT4) or 16 (NVFP4): codes and scale bytes by the rules of torq_quantize_*, MXINT4 in its
+ * stored form, scale bytes row by row.  NVFP4 caches have a float32 tensor scale for the keys and one for the values.
+ * lengths[b] counts the tokens of sequence b, the new ones included.  The new tokens of a call are rows of one batch: rows starts[b] to
+ * starts[b+1] - 1 are the last ones of sequence b (0 <= starts[0], ascending, starts[batch] <= tokens); starts == NULL: one row per sequence,
+ * tokens == batch.  A row that no sequence has, or more new rows than a length, is a row without a place: nothing is stored for it, and its
+ * results are zeros (lse: minus infinity).  table, lengths, starts are int32 and 4-byte aligned, and are read on the device: one captured call
+ * serves every step.  A page number that a call needs and that lies outside [0, num_pages), or a length that the table has no room for, latches
+ * TORQ_ERR_PAGE in the device error word; nothing is read or written there, and the results of that sequence are unspecified.
+ * Entries of table behind a sequence's length and what pages hold there are never looked at, so they may hold anything.
+ * Sizes: batch <= 65536, kv_heads <= 1024, table_width page_tokens <= 2^30, tokens <= 2^24. */
+typedef struct {
+  void* pages;               /* [num_pages][kv_heads][torq_kv_page_bytes()], 16-byte aligned */
+  const int32_t* table;      /* [batch][table_width] */
+  const int32_t* lengths;    /* [batch] */
+  int64_t num_pages, page_tokens, kv_heads, head_dim, batch, table_width;
+  float k_tensor_scale, v_tensor_scale;   /* NVFP4; the others do not look at them */
+} torq_kv_cache;
+
+/* Bytes of one head's page; scale_block: 32, NVFP4 16.  0 for sizes that make none. */
+size_t torq_kv_page_bytes(int64_t scale_block, int64_t page_tokens, int64_t head_dim);
+
+/* New keys and values, quantized into their slots.  K, V [tokens][kv_heads][D] of `dtype`, rows k_stride and v_stride elements apart (columns of
+ * a fused projection; 16-byte aligned, strides a multiple of 16 bytes).  Everything else in the pages stays as it is.  One launch. */
+torq_status torq_mxfp4_kv_append(const torq_kv_cache* cache, const void* K, const void* V, torq_dtype dtype, int64_t k_stride, int64_t v_stride,
+                                 const int32_t* starts, int64_t tokens, void* stream);
+torq_status torq_nvfp4_kv_append(const torq_kv_cache* cache, const void* K, const void* V, torq_dtype dtype, int64_t k_stride, int64_t v_stride,
+                                 const int32_t* starts, int64_t tokens, void* stream);
+torq_status torq_mxint4_kv_append(const torq_kv_cache* cache, const void* K, const void* V, torq_dtype dtype, int64_t k_stride, int64_t v_stride,
+                                  const int32_t* starts, int64_t tokens, void* stream);
+
+/* The values that the same slots stand for, K and V [tokens][kv_heads][D] dense, float32 or rounded once to bfloat16 (exact but for NVFP4).
+ * With starts the sums of all lengths this is the whole cache.  One launch. */
+torq_status torq_mxfp4_kv_read(const torq_kv_cache* cache, const int32_t* starts, int64_t tokens, void* K, void* V, torq_dtype dtype, void* stream);
+torq_status torq_nvfp4_kv_read(const torq_kv_cache* cache, const int32_t* starts, int64_t tokens, void* K, void* V, torq_dtype dtype, void* stream);
+torq_status torq_mxint4_kv_read(const torq_kv_cache* cache, const int32_t* starts, int64_t tokens, void* K, void* V, torq_dtype dtype, void* stream);
+
+/* How a query at place p of its sequence (its last new row is at length - 1) scores and sees the token at place j:
+ *   x_j = cap(scale q k_j) - slopes[head] |p - j|,   cap(x) = softcap tanh(x / softcap), or x where softcap is 0
+ *   p - window < j (window > 0),   j <= max(p, prefix[b] - 1),   first[row] <= j < length
+ * slopes [heads] float32, prefix [batch] and first [tokens] int32, each or all NULL: no bias by distance, causal, from the beginning. */
+typedef struct {
+  float scale, softcap;
+  const float* slopes;
+  int64_t window;
+  const int32_t* prefix;
+  const int32_t* first;
+} torq_kv_scoring;
+
+/* Attention of the new rows over the cache (append them first):  out = sum_j exp(x_j - lse) v_j,  lse = log sum_j exp(x_j), the sums over what
+ * a row sees; zeros and minus infinity for a row that sees nothing.
+ *   Q [tokens][heads][D] bf16, rows q_stride elements apart; heads % kv_heads == 0, query heads h G ... h G + G - 1 share key/value head h
+ *   out [tokens][heads][D] bf16;  lse [tokens][heads] float32, natural logarithm, or NULL
+ *   workspace: torq_kv_attention_workspace_bytes() bytes, 256-byte aligned; two calls that may overlap need one each
+ * Scores, sums and the running maximum are float32.  Outputs overlap no operand. */
+size_t torq_kv_attention_workspace_bytes(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t head_dim);
+torq_status torq_mxfp4_kv_attention(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
+                                    const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+torq_status torq_nvfp4_kv_attention(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
+                                    const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+torq_status torq_mxint4_kv_attention(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
+                                     const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The account of the cache: what attention gave to each cached token, summed over the new rows and the query heads that share its head.
+ *   weights_out[page][h][slot] = (weights[page][h][slot] of a token that is not new, else 0) + sum over rows and heads of exp(x_j - lse)
+ * weights, weights_out [num_pages][kv_heads][page_tokens] float32 (16-byte aligned; they may be the same); only slots of the sequences' tokens are
+ * written.  Q, scoring and starts as the attention call had them, lse [tokens][heads] what it gave.  The order of the sums is fixed.  One launch. */
+torq_status torq_mxfp4_kv_weights(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
+                                  const int32_t* starts, int64_t tokens, const float* lse, const float* weights, float* weights_out, void* stream);
+torq_status torq_nvfp4_kv_weights(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
+                                  const int32_t* starts, int64_t tokens, const float* lse, const float* weights, float* weights_out, void* stream);
+torq_status torq_mxint4_kv_weights(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
+                                   const int32_t* starts, int64_t tokens, const float* lse, const float* weights, float* weights_out, void* stream);
+
+/* Eviction by account: of each sequence and key/value head the `recent` newest tokens and, of the others, those with the largest weights stay, `keep`
+ * in all (equal weights: the lower place stays; a sequence of at most `keep` tokens stays whole).  Codes, scale bytes and weights of what stays
+ * are copied, in their order, to the pages of new_table [batch][new_width], which are no pages of the sequences.  Places count anew there: a
+ * bias by distance or a window then counts what is left.
+ *   new_lengths [batch] int32 = min(length, keep);  kept [batch][kv_heads][keep] int32: the places of what stayed, -1 behind them
+ * new_width page_tokens >= min(keep, table_width page_tokens); batch kv_heads <= 65535.  Weights that are no numbers are outside the contract.
+ * Two launches. */
+torq_status torq_mxfp4_kv_evict(const torq_kv_cache* cache, float* weights, const int32_t* new_table, int64_t new_width, int64_t keep, int64_t recent,
+                                int32_t* new_lengths, int32_t* kept, void* stream);
+torq_status torq_nvfp4_kv_evict(const torq_kv_cache* cache, float* weights, const int32_t* new_table, int64_t new_width, int64_t keep, int64_t recent,
+                                int32_t* new_lengths, int32_t* kept, void* stream);
+torq_status torq_mxint4_kv_evict(const torq_kv_cache* cache, float* weights, const int32_t* new_table, int64_t new_width, int64_t keep, int64_t recent,
+                                 int32_t* new_lengths, int32_t* kept, void* stream);
 
 #ifdef __cplusplus
 }

@@ -9,7 +9,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libtorq_b200.so")
-SOURCES = [os.path.join(CSRC, "torq.cu")]
+SOURCES = [os.path.join(CSRC, "torq.cu"), os.path.join(CSRC, "kv.cu")]
 BINDING_SOURCE = os.path.join(CSRC, "binding.cpp")
 
 
@@ -76,7 +76,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         return LIB_PATH
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
-           "-Xcompiler", "-fPIC", "-shared"] + SOURCES
+           "-Xcompiler", "-fPIC", "-shared", "--threads", "2"] + SOURCES
     if verbose:
         cmd[1:1] = ["-Xptxas", "-v"]
     return _compile(cmd, LIB_PATH, verbose)

@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(256) mxint4_quantize_kernel(const T* __restric
 }
 
 // Stored form -> operand form: `words` 32-bit words of eight nibbles each -> eight E4M3 bytes each.
-__global__ void __launch_bounds__(256) mxint4_expand_kernel(const uint32_t* __restrict__ packed, int64_t words,
+static __global__ void __launch_bounds__(256) mxint4_expand_kernel(const uint32_t* __restrict__ packed, int64_t words,
                                                             uint2* __restrict__ out) {
   for (int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; t < words;
        t += (int64_t)gridDim.x * blockDim.x) {

@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(256) nv_quantize_kernel(const T* __restrict__ 
 // [d/16, 16, 16] intra-block rotations -> the same linear map written with 32-wide blocks
 // [d/32, 32, 32]: blocks 2b and 2b+1 on the diagonal of block b, zeros elsewhere (what the rotation
 // kernels, which work on 32 columns per thread, take).
-__global__ void expand_intra16_kernel(const __nv_bfloat16* __restrict__ r16, int64_t nb32,
+static __global__ void expand_intra16_kernel(const __nv_bfloat16* __restrict__ r16, int64_t nb32,
                                       __nv_bfloat16* __restrict__ r32) {
   const int64_t total = nb32 * 1024;
   for (int64_t t = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; t < total;

@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(256) quantize_kernel(const T* __restrict__ Z, 
 
 // Intra-block rotation (Algorithm 3 step 3) followed by quantization, without the inter-block
 // step: one thread per (row, block).  Used when the caller passes no R_inter.
-__global__ void __launch_bounds__(128) intra_quantize_kernel(
+static __global__ void __launch_bounds__(128) intra_quantize_kernel(
     const __nv_bfloat16* __restrict__ X, const __nv_bfloat16* __restrict__ R_intra, int64_t M,
     int64_t d, uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
   const int64_t nb = d / 32;
@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(128) intra_quantize_kernel(
 }
 
 // Plain [rows, kb] scale bytes -> tiled layout; padding := 0.
-__global__ void swizzle_scales_kernel(const uint8_t* __restrict__ lin, int64_t rows, int64_t kb,
+static __global__ void swizzle_scales_kernel(const uint8_t* __restrict__ lin, int64_t rows, int64_t kb,
                                       uint8_t* __restrict__ out) {
   const int64_t kb4 = (kb + 3) / 4;
   const int64_t mpad = (rows + 127) / 128 * 128;

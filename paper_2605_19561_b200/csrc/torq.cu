@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "../../include/torq.h"
+#include "host_launch.cuh"
 #include "mxfp4_gemm_pair.cuh"
 #include "mxfp4_gemm_wide.cuh"
 #include "quantize.cuh"
@@ -43,7 +44,7 @@ struct DeviceState {
 };
 static DeviceState g_dev[kMaxDevices];
 static std::mutex g_mutex;
-static std::atomic<int64_t> g_launches{0};
+std::atomic<int64_t> g_launches{0};
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,
                                    const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -171,6 +172,15 @@ static DeviceState* device_state() {
   return &st;
 }
 
+torq_status current_device(int* sm_count, int** err_word) {
+  DeviceState* st = device_state();
+  if (!st) return TORQ_ERR_LAUNCH;
+  if (!st->arch_ok) return TORQ_ERR_ARCH;
+  *sm_count = st->sm_count;
+  *err_word = st->err_word;
+  return TORQ_OK;
+}
+
 // 2-D row-major tensor [rows, cols] of `elem_bytes`-byte elements, box [box_rows, box_cols],
 // 128-byte swizzle, zero fill outside the tensor.
 static bool encode_2d(CUtensorMap* map, CUtensorMapDataType dt, int elem_bytes, const void* base,
@@ -209,39 +219,10 @@ static bool encode_x_slabs_3d(CUtensorMap* map, const void* base, uint64_t M, ui
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static inline int ew_grid(int64_t items, int per_block, int sm_count) {
   int64_t blocks = (items + per_block - 1) / per_block;
   int64_t cap = (int64_t)sm_count * 16;
   return (int)(blocks < 1 ? 1 : (blocks > cap ? cap : blocks));
-}
-static inline torq_status launch_status() {
-  g_launches.fetch_add(1, std::memory_order_relaxed);
-  return cudaGetLastError() == cudaSuccess ? TORQ_OK : TORQ_ERR_LAUNCH;
-}
-
-// Launch of a persistent tensor-core kernel: `cluster` CTAs per cluster along x (1 or 2; the grid
-// is a multiple of it) and programmatic stream serialization, so that the launch processing of
-// this kernel overlaps the tail of the kernel before it (the kernel itself waits for that kernel
-// to complete before it touches global memory).
-template <typename... KArgs, typename... Args>
-static void launch_tc(void (*kernel)(KArgs...), int cluster, dim3 grid, dim3 threads, int smem, cudaStream_t s,
-                      Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = threads;
-  cfg.dynamicSmemBytes = (size_t)smem;
-  cfg.stream = s;
-  cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = (unsigned)cluster;
-  attr[1].val.clusterDim.y = 1;
-  attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = cluster > 1 ? 2 : 1;
-  cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
 
 // What the workspace holds beyond the quantized activations: room that a rotation split over the SMs needs for its fp32
@@ -525,6 +506,7 @@ const char* torq_status_string(torq_status s) {
     case TORQ_ERR_LAUNCH: return "CUDA launch or descriptor error";
     case TORQ_ERR_TIMEOUT: return "a bounded device wait ran out";
     case TORQ_ERR_WORKSPACE: return "workspace missing or too small";
+    case TORQ_ERR_PAGE: return "a page or a length of a key/value cache is out of range";
   }
   return "unknown";
 }

@@ -14,8 +14,19 @@ from . import build as _build
 
 TORQ_F32, TORQ_BF16 = 0, 1
 _STATUS = {0: "TORQ_OK", 1: "TORQ_ERR_NULL", 2: "TORQ_ERR_SHAPE", 3: "TORQ_ERR_ALIGN", 4: "TORQ_ERR_ARCH",
-           5: "TORQ_ERR_LAUNCH", 6: "TORQ_ERR_TIMEOUT", 7: "TORQ_ERR_WORKSPACE"}
+           5: "TORQ_ERR_LAUNCH", 6: "TORQ_ERR_TIMEOUT", 7: "TORQ_ERR_WORKSPACE", 8: "TORQ_ERR_PAGE"}
 _lib_handle = None
+
+
+class _KvCache(ctypes.Structure):                # torq_kv_cache
+    _fields_ = [("pages", ctypes.c_void_p), ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                *((n, ctypes.c_int64) for n in ("num_pages", "page_tokens", "kv_heads", "head_dim", "batch", "table_width")),
+                ("k_tensor_scale", ctypes.c_float), ("v_tensor_scale", ctypes.c_float)]
+
+
+class _KvScoring(ctypes.Structure):              # torq_kv_scoring
+    _fields_ = [("scale", ctypes.c_float), ("softcap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("window", ctypes.c_int64),
+                ("prefix", ctypes.c_void_p), ("first", ctypes.c_void_p)]
 
 
 class TorqError(RuntimeError):
@@ -118,6 +129,17 @@ def lib() -> ctypes.CDLL:
         getattr(L, name).restype = ci
     L.torq_nvfp4_gated_gemm.argtypes = [vp, vp, f32, vp, vp, f32, i64, i64, i64, vp, ci, vp]
     L.torq_nvfp4_gated_gemm.restype = ci
+    kc, ks = ctypes.POINTER(_KvCache), ctypes.POINTER(_KvScoring)
+    for fmt in ("mxfp4", "nvfp4", "mxint4"):
+        for name, args in (("append", [kc, vp, vp, ci, i64, i64, vp, i64, vp]), ("read", [kc, vp, i64, vp, vp, ci, vp]),
+                           ("attention", [kc, ks, vp, i64, i64, vp, i64, vp, vp, vp, sz, vp]),
+                           ("weights", [kc, ks, vp, i64, i64, vp, i64, vp, vp, vp, vp]), ("evict", [kc, vp, vp, i64, i64, i64, vp, vp, vp])):
+            f = getattr(L, f"torq_{fmt}_kv_{name}")
+            f.argtypes, f.restype = args, ci
+    L.torq_kv_page_bytes.argtypes = [i64, i64, i64]
+    L.torq_kv_page_bytes.restype = sz
+    L.torq_kv_attention_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    L.torq_kv_attention_workspace_bytes.restype = sz
     L.torq_block_covariance.argtypes = [vp, i64, i64, vp, vp]
     L.torq_block_covariance.restype = ci
     L.torq_givens_equalize.argtypes = [vp, i64, ctypes.c_double, vp, vp, vp, vp]
@@ -889,6 +911,241 @@ def torq_nvfp4_gated_gemm(Aq, As, a_tensor_scale: float, Wq, Ws, w_tensor_scale:
 def torq_mxint4_gated_gemm(A8, As, W8, Ws, out_dtype=torch.bfloat16, Y=None, stream=None):
     """The same on operand bytes: A8 [M,K] E4M3 with E8M0 scales (MXINT4 or torq_add_rmsnorm_mxfp8's), W8 [2N,K]."""
     return _product(8, A8, As, W8, Ws, out_dtype, Y, stream)
+
+
+# ---- a key/value cache in 4 bits -----------------------------------------------------------------------
+# pages [num_pages, kv_heads, bytes] uint8, table [batch, width], lengths [batch] and starts [batch + 1] int32; see torq_kv_cache in the
+# header for the layout of a page and for what a call's rows are.
+_INTS = (torch.int32,)
+
+
+def torq_kv_page_bytes(fmt: str, page_tokens: int, head_dim: int) -> int:
+    """Bytes of one head's page: the last dimension of pages.  fmt: "mxfp4", "nvfp4" or "mxint4"."""
+    return int(lib().torq_kv_page_bytes(16 if fmt == "nvfp4" else 32, page_tokens, head_dim))
+
+
+def torq_kv_attention_workspace_bytes(tokens: int, batch: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return int(lib().torq_kv_attention_workspace_bytes(tokens, batch, heads, kv_heads, head_dim))
+
+
+def _kv_rows(t, dtypes, name):
+    """[tokens, heads, dim] with dense rows that may lie apart: the distance between rows."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or not t.is_cuda or t.dim() != 3:
+        what = f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else type(t).__name__
+        raise ValueError(f"{name}: expected a CUDA tensor [tokens, heads, dim] of {' or '.join(str(d) for d in dtypes)}, got {what}")
+    _here(t, name)
+    tokens, heads, dim = t.shape
+    if t.stride(2) != 1 and dim > 1 or t.stride(1) != dim and heads > 1 or t.stride(0) < heads * dim and tokens > 1:
+        raise ValueError(f"{name}: the heads of a row have to lie one behind the other, got strides {t.stride()}")
+    return t.stride(0) if tokens > 1 else heads * dim
+
+
+def _here(t, name):
+    if t.device.index != torch._C._cuda_getDevice():
+        raise ValueError(f"{name}: is on {t.device}, the call goes to the current device, cuda:{torch._C._cuda_getDevice()}")
+
+
+def _kv_cache(fmt, pages, table, lengths, dim, scales, starts, tokens):
+    _operand(pages, _BYTES, "pages")
+    _operand(table, _INTS, "table")
+    if pages.dim() != 3 or table.dim() != 2:
+        raise ValueError(f"expected pages [num_pages, kv_heads, bytes] and table [batch, width], got {tuple(pages.shape)} and {tuple(table.shape)}")
+    batch = table.shape[0]
+    _operand(lengths, _INTS, "lengths", (batch,))
+    if starts is not None:
+        _operand(starts, _INTS, "starts", (batch + 1,))
+    elif tokens != batch:
+        raise ValueError(f"{tokens} tokens of {batch} sequences: starts says which are whose")
+    one = torq_kv_page_bytes(fmt, 1, dim)
+    if dim not in (64, 128, 256) or pages.shape[2] % one:
+        raise ValueError(f"pages: {pages.shape[2]} bytes of a head are no whole tokens of head dimension {dim}")
+    return _KvCache(_ptr(pages), _ptr(table), _ptr(lengths), pages.shape[0], pages.shape[2] // one, pages.shape[1], dim, batch,
+                    table.shape[1], *(scales or (1.0, 1.0)))
+
+
+def _kv_scoring(scale, softcap, slopes, window, prefix, first, dim, heads, batch, tokens):
+    if slopes is not None:
+        _operand(slopes, (torch.float32,), "slopes", (heads,))
+    if prefix is not None:
+        _operand(prefix, _INTS, "prefix", (batch,))
+    if first is not None:
+        _operand(first, _INTS, "first", (tokens,))
+    return _KvScoring(dim ** -0.5 if scale is None else scale, softcap, _ptr(slopes), window, _ptr(prefix), _ptr(first))
+
+
+def _kv_append(fmt, pages, table, lengths, K, V, scales, starts, stream):
+    strides = _kv_rows(K, _FLOATS, "K"), _kv_rows(V, (getattr(K, "dtype", None),), "V")
+    cache = _kv_cache(fmt, pages, table, lengths, K.shape[2], scales, starts, K.shape[0])
+    if K.shape != V.shape or K.shape[1] != pages.shape[1]:
+        raise ValueError(f"K and V: {tuple(K.shape)} and {tuple(V.shape)} do not fit {pages.shape[1]} heads")
+    name = f"torq_{fmt}_kv_append"
+    _raise(getattr(lib(), name)(cache, _ptr(K), _ptr(V), _dtype_code(K), *strides, _ptr(starts), K.shape[0], _stream(stream)), name)
+
+
+def _kv_read(fmt, pages, table, lengths, head_dim, tokens, scales, starts, out_dtype, stream):
+    cache = _kv_cache(fmt, pages, table, lengths, head_dim, scales, starts, tokens)
+    name = f"torq_{fmt}_kv_read"
+    if out_dtype not in _FLOATS:
+        raise ValueError(f"{name}: expected an out_dtype of {' or '.join(str(d) for d in _FLOATS)}, got {out_dtype}")
+    K, V = (torch.empty((tokens, pages.shape[1], head_dim), dtype=out_dtype, device=pages.device) for _ in range(2))
+    _used_by(stream, K, V)
+    _raise(getattr(lib(), name)(cache, _ptr(starts), tokens, _ptr(K), _ptr(V), _dtype_code(K), _stream(stream)), name)
+    return K, V
+
+
+def _kv_queries(fmt, pages, table, lengths, Q, scales, starts):
+    stride = _kv_rows(Q, (torch.bfloat16,), "Q")
+    tokens, heads, dim = Q.shape
+    cache = _kv_cache(fmt, pages, table, lengths, dim, scales, starts, tokens)
+    if heads % pages.shape[1]:
+        raise ValueError(f"Q: {heads} heads do not share {pages.shape[1]} key/value heads evenly")
+    return cache, stride, tokens, heads, dim
+
+
+def _kv_attention(fmt, pages, table, lengths, Q, scales, starts, scale, softcap, slopes, window, prefix, first, out, return_lse, workspace,
+                  stream):
+    cache, stride, tokens, heads, dim = _kv_queries(fmt, pages, table, lengths, Q, scales, starts)
+    scoring = _kv_scoring(scale, softcap, slopes, window, prefix, first, dim, heads, cache.batch, tokens)
+    if out is None:
+        out = torch.empty((tokens, heads, dim), dtype=torch.bfloat16, device=Q.device)
+        _used_by(stream, out)
+    _operand(out, (torch.bfloat16,), "out", (tokens, heads, dim))
+    lse = None
+    if return_lse:
+        lse = torch.empty((tokens, heads), dtype=torch.float32, device=Q.device)
+        _used_by(stream, lse)
+    if workspace is None:
+        workspace = torch.empty(torq_kv_attention_workspace_bytes(tokens, cache.batch, heads, cache.kv_heads, dim), dtype=torch.uint8, device=Q.device)
+        _used_by(stream, workspace)
+    _operand(workspace, (getattr(workspace, "dtype", "any type"),), "workspace")
+    name = f"torq_{fmt}_kv_attention"
+    _raise(getattr(lib(), name)(cache, scoring, _ptr(Q), stride, heads, _ptr(starts), tokens, _ptr(out), _ptr(lse), _ptr(workspace),
+                                workspace.nbytes, _stream(stream)), name)
+    return (out, lse) if return_lse else out
+
+
+def _kv_weights(fmt, pages, table, lengths, Q, lse, weights, scales, starts, scale, softcap, slopes, window, prefix, first, weights_out, stream):
+    cache, stride, tokens, heads, dim = _kv_queries(fmt, pages, table, lengths, Q, scales, starts)
+    scoring = _kv_scoring(scale, softcap, slopes, window, prefix, first, dim, heads, cache.batch, tokens)
+    _operand(lse, (torch.float32,), "lse", (tokens, heads))
+    shape = (cache.num_pages, cache.kv_heads, cache.page_tokens)
+    _operand(weights, (torch.float32,), "weights", shape)
+    if weights_out is None:
+        weights_out = weights
+    _operand(weights_out, (torch.float32,), "weights_out", shape)
+    name = f"torq_{fmt}_kv_weights"
+    _raise(getattr(lib(), name)(cache, scoring, _ptr(Q), stride, heads, _ptr(starts), tokens, _ptr(lse), _ptr(weights), _ptr(weights_out),
+                                _stream(stream)), name)
+    return weights_out
+
+
+def _kv_evict(fmt, pages, table, lengths, head_dim, weights, new_table, keep, recent, stream):
+    cache = _kv_cache(fmt, pages, table, lengths, head_dim, (1.0, 1.0), None, table.shape[0] if isinstance(table, torch.Tensor) else 0)
+    _operand(weights, (torch.float32,), "weights", (cache.num_pages, cache.kv_heads, cache.page_tokens))
+    _operand(new_table, _INTS, "new_table")
+    if new_table.dim() != 2 or new_table.shape[0] != cache.batch:
+        raise ValueError(f"new_table: expected a row for each of {cache.batch} sequences, got {tuple(new_table.shape)}")
+    name = f"torq_{fmt}_kv_evict"
+    if keep < 1:
+        raise ValueError(f"{name}: keep has to be positive, got {keep}")
+    new_lengths = torch.empty(cache.batch, dtype=torch.int32, device=pages.device)
+    kept = torch.empty((cache.batch, cache.kv_heads, keep), dtype=torch.int32, device=pages.device)
+    _used_by(stream, new_lengths, kept)
+    _raise(getattr(lib(), name)(cache, _ptr(weights), _ptr(new_table), new_table.shape[1], keep, recent, _ptr(new_lengths), _ptr(kept),
+                                _stream(stream)), name)
+    return new_lengths, kept
+
+
+def torq_mxfp4_kv_append(pages, table, lengths, K, V, starts=None, stream=None):
+    """New keys and values K, V [tokens, kv_heads, dim] float32 or bfloat16 (rows may lie apart) into their slots in pages."""
+    _kv_append("mxfp4", pages, table, lengths, K, V, None, starts, stream)
+
+
+def torq_nvfp4_kv_append(pages, table, lengths, K, V, k_tensor_scale: float, v_tensor_scale: float, starts=None, stream=None):
+    """The same in NVFP4."""
+    _kv_append("nvfp4", pages, table, lengths, K, V, (k_tensor_scale, v_tensor_scale), starts, stream)
+
+
+def torq_mxint4_kv_append(pages, table, lengths, K, V, starts=None, stream=None):
+    """The same in MXINT4."""
+    _kv_append("mxint4", pages, table, lengths, K, V, None, starts, stream)
+
+
+def torq_mxfp4_kv_read(pages, table, lengths, head_dim: int, tokens: int, starts=None, out_dtype=torch.bfloat16, stream=None):
+    """The last `tokens` tokens of the sequences (one of each, or as starts says): (K, V) [tokens, kv_heads, dim]."""
+    return _kv_read("mxfp4", pages, table, lengths, head_dim, tokens, None, starts, out_dtype, stream)
+
+
+def torq_nvfp4_kv_read(pages, table, lengths, head_dim: int, tokens: int, k_tensor_scale: float, v_tensor_scale: float, starts=None,
+                       out_dtype=torch.bfloat16, stream=None):
+    """The same from NVFP4."""
+    return _kv_read("nvfp4", pages, table, lengths, head_dim, tokens, (k_tensor_scale, v_tensor_scale), starts, out_dtype, stream)
+
+
+def torq_mxint4_kv_read(pages, table, lengths, head_dim: int, tokens: int, starts=None, out_dtype=torch.bfloat16, stream=None):
+    """The same from MXINT4."""
+    return _kv_read("mxint4", pages, table, lengths, head_dim, tokens, None, starts, out_dtype, stream)
+
+
+def torq_mxfp4_kv_attention(pages, table, lengths, Q, starts=None, scale=None, softcap: float = 0.0, slopes=None, window: int = 0, prefix=None,
+                            first=None, out=None, return_lse: bool = False, workspace=None, stream=None):
+    """Attention of Q [tokens, heads, dim] bf16 over the cached tokens of its sequences -> out [tokens, heads, dim] bf16, or (out, lse).
+    scale: dim ** -0.5; softcap, slopes, window, prefix, first: torq_kv_scoring."""
+    return _kv_attention("mxfp4", pages, table, lengths, Q, None, starts, scale, softcap, slopes, window, prefix, first, out, return_lse,
+                         workspace, stream)
+
+
+def torq_nvfp4_kv_attention(pages, table, lengths, Q, k_tensor_scale: float, v_tensor_scale: float, starts=None, scale=None,
+                            softcap: float = 0.0, slopes=None, window: int = 0, prefix=None, first=None, out=None, return_lse: bool = False,
+                            workspace=None, stream=None):
+    """The same over an NVFP4 cache."""
+    return _kv_attention("nvfp4", pages, table, lengths, Q, (k_tensor_scale, v_tensor_scale), starts, scale, softcap, slopes, window, prefix,
+                         first, out, return_lse, workspace, stream)
+
+
+def torq_mxint4_kv_attention(pages, table, lengths, Q, starts=None, scale=None, softcap: float = 0.0, slopes=None, window: int = 0,
+                             prefix=None, first=None, out=None, return_lse: bool = False, workspace=None, stream=None):
+    """The same over an MXINT4 cache."""
+    return _kv_attention("mxint4", pages, table, lengths, Q, None, starts, scale, softcap, slopes, window, prefix, first, out, return_lse,
+                         workspace, stream)
+
+
+def torq_mxfp4_kv_weights(pages, table, lengths, Q, lse, weights, starts=None, scale=None, softcap: float = 0.0, slopes=None,
+                          window: int = 0, prefix=None, first=None, weights_out=None, stream=None):
+    """What attention (same arguments, its lse) gave to each cached token, added to weights [num_pages, kv_heads, page_tokens] float32
+    (a new token's starts at zero): in place, or to weights_out."""
+    return _kv_weights("mxfp4", pages, table, lengths, Q, lse, weights, None, starts, scale, softcap, slopes, window, prefix, first,
+                       weights_out, stream)
+
+
+def torq_nvfp4_kv_weights(pages, table, lengths, Q, lse, weights, k_tensor_scale: float, starts=None, scale=None, softcap: float = 0.0,
+                          slopes=None, window: int = 0, prefix=None, first=None, weights_out=None, stream=None):
+    """The same of an NVFP4 cache."""
+    return _kv_weights("nvfp4", pages, table, lengths, Q, lse, weights, (k_tensor_scale, 1.0), starts, scale, softcap, slopes, window,
+                       prefix, first, weights_out, stream)
+
+
+def torq_mxint4_kv_weights(pages, table, lengths, Q, lse, weights, starts=None, scale=None, softcap: float = 0.0, slopes=None,
+                           window: int = 0, prefix=None, first=None, weights_out=None, stream=None):
+    """The same of an MXINT4 cache."""
+    return _kv_weights("mxint4", pages, table, lengths, Q, lse, weights, None, starts, scale, softcap, slopes, window, prefix, first,
+                       weights_out, stream)
+
+
+def torq_mxfp4_kv_evict(pages, table, lengths, head_dim: int, weights, new_table, keep: int, recent: int = 0, stream=None):
+    """The `recent` newest tokens of each sequence and head and those of the others with the largest weights, `keep` in all, moved to the
+    pages of new_table [batch, width], their weights with them -> (new lengths [batch], places that stayed [batch, kv_heads, keep])."""
+    return _kv_evict("mxfp4", pages, table, lengths, head_dim, weights, new_table, keep, recent, stream)
+
+
+def torq_nvfp4_kv_evict(pages, table, lengths, head_dim: int, weights, new_table, keep: int, recent: int = 0, stream=None):
+    """The same of an NVFP4 cache."""
+    return _kv_evict("nvfp4", pages, table, lengths, head_dim, weights, new_table, keep, recent, stream)
+
+
+def torq_mxint4_kv_evict(pages, table, lengths, head_dim: int, weights, new_table, keep: int, recent: int = 0, stream=None):
+    """The same of an MXINT4 cache."""
+    return _kv_evict("mxint4", pages, table, lengths, head_dim, weights, new_table, keep, recent, stream)
 
 
 # ---- calibration of the inter-block rotation (Section 5.1, Algorithm 1; offline) -----------------------
