@@ -121,6 +121,34 @@ static torq_status read_impl(const torq_kv_cache* cache, const int32_t* starts, 
   return launch_status();
 }
 
+// ---- few queries per sequence
+constexpr int kMaxCtas = 480;            // of the streaming kernel: the workspace does not depend on the device
+static int decode_groups(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads) {
+  return (tokens + batch - 1) / batch * (heads / kv_heads) <= 8 ? 1 : 2;
+}
+static size_t decode_partials_at() { return kMaxCtas * sizeof(KvOwner); }
+static size_t decode_workspace(int groups, int64_t dim) { return decode_partials_at() + (size_t)kMaxCtas * 2 * 8 * groups * (size_t)(dim + 2) * sizeof(float); }
+
+template <int FMT, int D, int NT>
+static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, const void* Q, int64_t q_stride, int heads, void* out, float* lse,
+                                 void* workspace, cudaStream_t s) {
+  using C = KvDecodeCfg<FMT, D, NT>;
+  using J = KvJoinCfg<D, NT>;
+  constexpr auto kernel = kv_decode_kernel<C>;
+  constexpr auto join = kv_join_kernel<D, NT>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return TORQ_ERR_LAUNCH;
+  const int most = sms * C::CTAS, ctas = most < kMaxCtas ? most : kMaxCtas;
+  KvOwner* owners = static_cast<KvOwner*>(workspace);
+  float* partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + decode_partials_at());
+  launch_tc(kernel, 1, dim3((unsigned)ctas), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads,
+            static_cast<__nv_bfloat16*>(out), lse, owners, partials);
+  const torq_status rc = launch_status();
+  if (rc != TORQ_OK) return rc;
+  launch_tc(join, 1, dim3((unsigned)ctas), dim3(J::THREADS), 0, s, ctas, heads, heads / v.heads, static_cast<const KvOwner*>(owners),
+            static_cast<const float*>(partials), static_cast<__nv_bfloat16*>(out), lse);
+  return launch_status();
+}
+
 template <int FMT>
 static torq_status attention_impl(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
                                   const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
@@ -137,11 +165,13 @@ static torq_status attention_impl(const torq_kv_cache* cache, const torq_kv_scor
   if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return TORQ_ERR_ALIGN;
   int sms;
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
+  cudaStream_t stm = static_cast<cudaStream_t>(stream);
+  const bool one = decode_groups(tokens, cache->batch, heads, v.heads) == 1;
   with_dim(v.dim, [&](auto D) {
-    launch_tc(kv_attention_simple_kernel<FMT, decltype(D)::value>, 1, dim3((unsigned)((tokens * heads + 3) / 4)), dim3(128), 0,
-              static_cast<cudaStream_t>(stream), v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, (int)heads, static_cast<__nv_bfloat16*>(out), lse);
+    rc = one ? decode_launch<FMT, decltype(D)::value, 1>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm)
+             : decode_launch<FMT, decltype(D)::value, 2>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
   });
-  return launch_status();
+  return rc;
 }
 
 template <int FMT>
@@ -202,8 +232,8 @@ size_t torq_kv_page_bytes(int64_t scale_block, int64_t page_tokens, int64_t head
 }
 
 size_t torq_kv_attention_workspace_bytes(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t head_dim) {
-  (void)tokens; (void)batch; (void)heads; (void)kv_heads; (void)head_dim;
-  return 0;
+  if (tokens < 1 || batch < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || head_dim < 1) return 0;
+  return decode_workspace(decode_groups(tokens, batch, heads, kv_heads), head_dim);
 }
 
 #define TORQ_KV_ENTRIES(name, FMT)                                                                                                                   \
