@@ -122,30 +122,31 @@ static torq_status read_impl(const torq_kv_cache* cache, const int32_t* starts, 
 }
 
 // ---- few queries per sequence
-constexpr int kMaxCtas = 480;            // of the streaming kernel: the workspace does not depend on the device
+constexpr int kMaxRanges = 2560;         // warps of the streaming kernel: the workspace does not depend on the device
 static int decode_groups(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads) {
   return (tokens + batch - 1) / batch * (heads / kv_heads) <= 8 ? 1 : 2;
 }
-static size_t decode_partials_at() { return kMaxCtas * sizeof(KvOwner); }
-static size_t decode_workspace(int groups, int64_t dim) { return decode_partials_at() + (size_t)kMaxCtas * 2 * 8 * groups * (size_t)(dim + 2) * sizeof(float); }
+static size_t decode_workspace(int groups, int64_t dim) { return (size_t)kMaxRanges * 2 * 8 * groups * (size_t)(dim + 2) * sizeof(float); }
 
 template <int FMT, int D, int NT>
 static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, const void* Q, int64_t q_stride, int heads, void* out, float* lse,
                                  void* workspace, cudaStream_t s) {
   using C = KvDecodeCfg<FMT, D, NT>;
-  using J = KvJoinCfg<D, NT>;
   constexpr auto kernel = kv_decode_kernel<C>;
-  constexpr auto join = kv_join_kernel<D, NT>;
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return TORQ_ERR_LAUNCH;
-  const int most = sms * C::CTAS, ctas = most < kMaxCtas ? most : kMaxCtas;
-  KvOwner* owners = static_cast<KvOwner*>(workspace);
-  float* partials = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + decode_partials_at());
-  launch_tc(kernel, 1, dim3((unsigned)ctas), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads,
-            static_cast<__nv_bfloat16*>(out), lse, owners, partials);
+  const int most = sms * C::CTAS, ctas = most < kMaxRanges / C::WARPS ? most : kMaxRanges / C::WARPS, group = heads / v.heads;
+  float* partials = static_cast<float*>(workspace);
+  __nv_bfloat16* y = static_cast<__nv_bfloat16*>(out);
+  launch_tc(kernel, 1, dim3((unsigned)ctas), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads, y, lse, partials);
   const torq_status rc = launch_status();
   if (rc != TORQ_OK) return rc;
-  launch_tc(join, 1, dim3((unsigned)ctas), dim3(J::THREADS), 0, s, ctas, heads, heads / v.heads, static_cast<const KvOwner*>(owners),
-            static_cast<const float*>(partials), static_cast<__nv_bfloat16*>(out), lse);
+  // items at most: every sequence may have a group that is not full.  Few items: a row to each CTA, with the ranges shared among its warps
+  const int64_t items = ((int64_t)v.tokens * group / C::ROWS + (v.tokens < v.batch ? v.tokens : v.batch)) * v.heads;
+  if (items > INT32_MAX) return TORQ_ERR_SHAPE;
+  if (items <= 64)
+    launch_tc(kv_join_kernel<D, NT, 8>, 1, dim3((unsigned)items, C::ROWS), dim3(256), 0, s, v, a, ctas * C::WARPS, heads, static_cast<const float*>(partials), y, lse);
+  else
+    launch_tc(kv_join_kernel<D, NT, 1>, 1, dim3((unsigned)items, NT), dim3(256), 0, s, v, a, ctas * C::WARPS, heads, static_cast<const float*>(partials), y, lse);
   return launch_status();
 }
 
@@ -187,13 +188,18 @@ static torq_status weights_impl(const torq_kv_cache* cache, const torq_kv_scorin
   if (!aligned4(lse) || !aligned16(weights) || !aligned16(weights_out)) return TORQ_ERR_ALIGN;
   int sms;
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
-  if ((int64_t)v.batch * v.heads > 65535) return TORQ_ERR_SHAPE;
-  const unsigned x = grid_of((int64_t)v.width << v.page_shift, 4, 512);
   with_dim(v.dim, [&](auto D) {
-    launch_tc(kv_weights_simple_kernel<FMT, decltype(D)::value>, 1, dim3(x, (unsigned)(v.batch * v.heads)), dim3(128), 0, static_cast<cudaStream_t>(stream),
-              v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, (int)heads, lse, weights, weights_out);
+    using C = KvWeightsCfg<FMT, decltype(D)::value>;
+    constexpr auto kernel = kv_weights_kernel<C>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) {
+      rc = TORQ_ERR_LAUNCH;
+      return;
+    }
+    launch_tc(kernel, 1, dim3((unsigned)(sms * C::CTAS)), dim3(C::THREADS), C::SMEM, static_cast<cudaStream_t>(stream), v, a,
+              static_cast<const __nv_bfloat16*>(Q), q_stride, (int)heads, lse, weights, weights_out);
+    rc = launch_status();
   });
-  return launch_status();
+  return rc;
 }
 
 template <int FMT>

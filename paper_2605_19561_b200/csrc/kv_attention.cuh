@@ -39,154 +39,202 @@ __device__ __forceinline__ float kv_score(float x, float softcap, float slope, i
 
 
 // ---- few queries per sequence -----------------------------------------------------------------------------------------------------------------
-// The cache is streamed once, by all SMs alike: the work is a list of units of UNIT cached tokens (sequence after sequence, key/value head after head,
-// group of 8 NT rows after group), cut into as many equal ranges as there are CTAs, whatever the lengths are.  Lengths are known on the device
-// alone, so every CTA counts the units itself.  An item (sequence, head, group) that lies in one range is finished by its CTA; of one that crosses a
-// border each CTA leaves sums, maximum and a partial result, and a second kernel joins them in the order of the ranges.
+// The cache is streamed once, by all warps alike: the work is a list of steps of 32 cached tokens (sequence after sequence, key/value head after head,
+// group of 8 NT rows after group), cut into as many equal ranges as there are warps, whatever the lengths are.  Lengths are known on the device
+// alone, so every warp counts the steps itself.  An item (sequence, head, group) that lies in one range is finished by its warp; of one that crosses a
+// border each warp leaves sums, maximum and a partial result, and a second kernel joins them in the order of the ranges.  A warp works alone, through a
+// ring of its own filled by cp.async: there is no barrier in the kernel.  (Ranges for CTAs of four warps that share an item and meet at its end:
+// 32 sequences of up to 8192 tokens 73.6 us, SMs idle for a quarter of it, since a CTA with more items in its range took longer.)
 //
-// Inside a CTA each of four warps takes 32 tokens of a unit by itself, through a ring of its own filled by cp.async: no barrier until the item ends.
 // A warp keeps a maximum m of its scores in powers of two that is raised only when a score exceeds it by 3, so weights are exp2(x - m + 12) <= 2^15 in
 // float16; they keep 11 bits down to 2^-26 of the largest.  The same goes for the values' scales (see kv_fragments.cuh).
 template <int FMT_, int D_, int NT_>
 struct KvDecodeCfg {
   static constexpr int FMT = FMT_, D = D_, NT = NT_;
-  static constexpr int WARPS = 4, THREADS = 32 * WARPS, STEP = 32, UNIT = WARPS * STEP, ROWS = 8 * NT;
+  static constexpr int WARPS = 4, THREADS = 32 * WARPS, STEP = 32, ROWS = 8 * NT;
   static constexpr int CH = D / 32, SB = D / kv_block(FMT);
   static constexpr int K_BYTES = STEP * D / 2, S_BYTES = STEP * SB, STAGE = 2 * (K_BYTES + S_BYTES);      // keys, values, their scales
-  static constexpr int CTAS = D == 256 || NT == 2 ? 2 : 3;                 // per SM
-  static constexpr int STAGES = D == 256 ? 3 : (D == 128 ? 4 : 6);
-  static constexpr int RING = WARPS * STAGES * STAGE;
-  static constexpr int JOIN = WARPS * ROWS * D * 4;                        // the warps' results, in the ring's place
-  static constexpr int SMEM = (RING > JOIN ? RING : JOIN) + 1024;
+  static constexpr int CTAS = D == 256 || NT == 2 ? 2 : 4;                 // per SM
+  static constexpr int STAGES = D == 64 ? 4 : 3 - (FMT == FMT_NVFP4 ? 1 : 0);
+  static constexpr int ROOM = KvScaleRoom<FMT, D>::BYTES;                  // scales made ready, per warp
+  static constexpr int SMEM = WARPS * (STAGES * STAGE + ROOM);
   static constexpr int PARTIAL = ROWS * (D + 2);                           // floats: results, maxima, sums
 };
-struct KvOwner {                         // written by every CTA: the item that it begins and does not finish
-  int32_t rows, first_row, first_token, head;                              // of the group (0: none), its first of its sequence's, of the batch; key/value head
-  long long end, units;                                                    // of the item's units, one behind the last; units in all
-};
 
-// What one warp's rows are, for its columns 2t and 2t + 1 of each group of eight.
+// An item: `rows` rows of sequence b from its first_row on (count * group in all), a key/value head, and cached tokens [lo, hi) that any row of the
+// sequence sees; base = lo / 32 * 32.
 struct KvItem {
-  int b, head, first_token, count, length, first_row, rows;                // of the sequence; of the group: its first row among count * group, how many
-  int lo, base, hi;                                                        // cached tokens [lo, hi) that any row of the sequence sees; base = lo / 32 * 32
+  int b, head, first_token, count, length, first_row, rows, lo, base, hi;
 };
 
-__device__ __forceinline__ long long kv_range_begin(long long units, int cta, int ctas) { return units * cta / ctas; }
+__device__ __forceinline__ long long kv_range_begin(long long units, int which, int ranges) { return units * which / ranges; }
 
-// Of sequence b: groups of ROWS rows, units per group and head.
-template <int ROWS, int UNIT>
-__device__ __forceinline__ void kv_sequence_units(const KvView& c, const KvScoring& a, int b, int group, KvItem& it, int& groups, int& units) {
+// Of sequence b: groups of ROWS rows, steps per group and head.
+template <int ROWS>
+__device__ __forceinline__ void kv_sequence_steps(const KvView& c, const KvScoring& a, int b, int group, KvItem& it, int& groups, int& per) {
   it.b = b;
   kv_new_tokens(c, b, it.first_token, it.count);
   it.length = kv_length(c, b);
   groups = (it.count * group + ROWS - 1) / ROWS;
   const int p0 = it.length - it.count;
-  int lo = 0, hi = it.length;
-  if (a.window > 0 && p0 - a.window + 1 > 0) lo = p0 - a.window + 1;
-  it.lo = lo;
-  it.base = lo & ~31;
-  it.hi = hi;
-  units = hi > it.base ? (hi - it.base + UNIT - 1) / UNIT : 1;             // rows that see nothing are an item all the same
+  it.lo = a.window > 0 && p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
+  it.hi = it.length;
+  it.base = it.lo & ~31;
+  per = (it.hi - it.base + 31) / 32;
+  if (it.length == 0) groups = 0;
+}
+__device__ __forceinline__ long long warp_scan(long long v, int lane) {    // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long x = __shfl_up_sync(0xFFFFFFFFu, v, o);
+    if (lane >= o) v += x;
+  }
+  return v;
+}
+__device__ __forceinline__ int64_t kv_out_row(const KvItem& it, int r, int heads, int group) {
+  const int rr = it.first_row + r;
+  return (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
 }
 
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const KvView c, const KvScoring a, const __nv_bfloat16* Q, int64_t q_stride, int heads,
-                                                                        __nv_bfloat16* out, float* lse, KvOwner* owners, float* partials) {
+                                                                        __nv_bfloat16* out, float* lse, float* partials) {
   constexpr int FMT = C::FMT, D = C::D, NT = C::NT, CH = C::CH, SB = C::SB, ROWS = C::ROWS;
   extern __shared__ __align__(128) uint8_t smem[];
-  __shared__ long long scan[C::WARPS + 1];
-  __shared__ float row_m[C::WARPS][ROWS], row_l[C::WARPS][ROWS];
   griddep_wait_and_launch();
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3, group = heads / c.heads;
-  const int cta = blockIdx.x, ctas = gridDim.x;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, group = heads / c.heads;
+  const int range = blockIdx.x * C::WARPS + warp, ranges = gridDim.x * C::WARPS;
 
-  // rows of the batch that no sequence has
+  // rows of the batch that no sequence has, or an empty one
+  auto nothing = [&](int i) {
+    const int64_t row = (int64_t)i * heads;
+    for (int e = lane; e < heads * D / 8; e += 32) reinterpret_cast<uint4*>(out + row * D)[e] = make_uint4(0, 0, 0, 0);
+    if (lse)
+      for (int e = lane; e < heads; e += 32) lse[row + e] = -INFINITY;
+  };
   if (c.starts) {
     const int before = min(max(c.starts[0], 0), c.tokens), behind = min(max(c.starts[c.batch], before), c.tokens), none = before + c.tokens - behind;
-    for (int i = cta; i < none; i += ctas) {
-      const int64_t row = (int64_t)(i < before ? i : behind + i - before) * heads;
-      for (int e = tid; e < heads * D / 8; e += C::THREADS) reinterpret_cast<uint4*>(out + row * D)[e] = make_uint4(0, 0, 0, 0);
-      if (lse)
-        for (int e = tid; e < heads; e += C::THREADS) lse[row + e] = -INFINITY;
-    }
+    for (int i = range; i < none; i += ranges) nothing(i < before ? i : behind + i - before);
   }
+  for (int b = range; b < c.batch; b += ranges)
+    if (c.lengths[b] <= 0) {
+      int first, count;
+      kv_new_tokens(c, b, first, count);
+      for (int i = 0; i < count; ++i) nothing(first + i);
+    }
 
-  // units in all, then where this CTA's range begins
+  // steps in all, then where this warp's range begins
   KvItem it;
   int groups, per;
-  auto units_of = [&](int b) -> long long {
+  auto steps_of = [&](int b) -> long long {
     if (b >= c.batch) return 0;
-    kv_sequence_units<ROWS, C::UNIT>(c, a, b, group, it, groups, per);
+    kv_sequence_steps<ROWS>(c, a, b, group, it, groups, per);
     return (long long)groups * c.heads * per;
   };
-  auto block_scan = [&](long long v, long long& total) {                   // exclusive
-    long long s = v;
+  const long long mine = steps_of(lane);
+  long long units = mine;
+#pragma unroll 4
+  for (int b0 = 32; b0 < c.batch; b0 += 32) units += steps_of(b0 + lane);
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long x = __shfl_up_sync(0xFFFFFFFFu, s, o);
-      if (lane >= o) s += x;
-    }
-    __syncthreads();
-    if (lane == 31) scan[warp] = s;
-    __syncthreads();
-    long long before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < C::WARPS; ++w) {
-      if (w < warp) before += scan[w];
-      total += scan[w];
-    }
-    return before + s - v;
-  };
-  long long units = 0, total;
-  __shared__ long long found[2];
-  const long long mine = units_of(tid), mine_before = block_scan(mine, units);
-  for (int b = C::THREADS; b < c.batch; b += C::THREADS) {
-    block_scan(units_of(b + tid), total);
-    units += total;
-  }
-  const long long begin = kv_range_begin(units, cta, ctas), end = kv_range_begin(units, cta + 1, ctas);
-  if (tid == 0) owners[cta].rows = 0;
+  for (int o = 16; o; o >>= 1) units += __shfl_xor_sync(0xFFFFFFFFu, units, o);
+  const long long begin = kv_range_begin(units, range, ranges), end = kv_range_begin(units, range + 1, ranges);
   if (begin >= end) return;
-  {
-    long long before = mine_before, v = mine, base = 0;
-    for (int b = 0;; b += C::THREADS) {                                    // ends: begin < units
-      if (b) {
-        v = units_of(b + tid);
-        before = base + block_scan(v, total);
-      } else {
-        total = 0;
-        for (int w = 0; w < C::WARPS; ++w) total += scan[w];
-        if (c.batch > C::THREADS) block_scan(mine, total);                 // `scan` has been overwritten
-      }
-      if (before <= begin && begin < before + v) {
-        found[0] = b + tid;
-        found[1] = before;
-      }
-      base += total;
-      if (begin < base) break;
+  int b = 0;
+  long long sequence_begin = 0;
+  for (int b0 = 0;; b0 += 32) {                                            // ends, since begin < units
+    const long long v = b0 ? steps_of(b0 + lane) : mine, sum = warp_scan(v, lane);
+    const uint32_t here = __ballot_sync(0xFFFFFFFFu, begin < sequence_begin + sum);
+    if (here) {
+      const int first = __ffs(here) - 1;
+      b = b0 + first;
+      sequence_begin += __shfl_sync(0xFFFFFFFFu, sum - v, first);
+      break;
     }
-    __syncthreads();
+    sequence_begin += __shfl_sync(0xFFFFFFFFu, sum, 31);
   }
-  int b = (int)found[0];
-  long long at = begin, sequence_begin = found[1], sequence_units = units_of(b);
+  long long at = begin, sequence_units = steps_of(b);
 
   const uint32_t ring = smem_u32(smem) + warp * C::STAGES * C::STAGE;
-  uint8_t* ring_p = smem + warp * C::STAGES * C::STAGE;
+  uint8_t *ring_p = smem + warp * C::STAGES * C::STAGE, *room = smem + C::WARPS * C::STAGES * C::STAGE + warp * C::ROOM;
+  uint8_t* v_room = room + KvScaleRoom<FMT, D>::KEYS;
   const int row_of = lane & 15, chunk_of = lane >> 4;
+  // Where a lane's pieces of 16 bytes come from and go to.  The codes of 16 tokens are dense in their page; a lane takes every 32nd chunk of them.
+  constexpr int PER_GROUP = CH / 2;                                        // copies of a lane for the codes of 16 tokens
+  uint32_t to_chunk[CH == 8 ? 2 : 1];
+#pragma unroll
+  for (int i = 0; i < (CH == 8 ? 2 : 1); ++i) to_chunk[i] = 16 * kv_swizzled<D>((32 * i + lane) / CH, lane % CH) - 512 * i;
+  constexpr int PIECES = 16 * SB / 16;                                     // of the scale bytes of 16 tokens, of keys or of values
+  const int my_piece = lane % PIECES, my_group = lane / PIECES & 1, my_half = lane / (2 * PIECES);   // keys, values
+  const int scale_from = (my_half ? c.v_scales : c.k_scales) + my_piece * 16;
 
   while (at < end) {
-    while (at >= sequence_begin + sequence_units) {                        // sequences without rows have no units
+    while (at >= sequence_begin + sequence_units) {                        // sequences without rows have no steps
       sequence_begin += sequence_units;
-      sequence_units = units_of(++b);
+      sequence_units = steps_of(++b);
     }
-    const int local = (int)((at - sequence_begin) / per), unit0 = (int)((at - sequence_begin) % per);   // (head, group) of the sequence; its unit
+    const int local = (int)((at - sequence_begin) / per), step0 = (int)((at - sequence_begin) - (long long)local * per);   // (head, group) of the sequence; its step
     const long long left = end - at;
-    const int unit1 = (int)(left < per - unit0 ? unit0 + left : per);
+    const int steps = (int)(left < per - step0 ? left : per - step0);
     it.head = local / groups;
     it.first_row = local % groups * ROWS;
     it.rows = min(ROWS, it.count * group - it.first_row);
-    at += unit1 - unit0;
+    at += steps;
+
+    const int first = it.base + step0 * C::STEP;
+    const int32_t* table = c.table + (int64_t)b * c.width;
+    const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
+    const int mask = (1 << c.page_shift) - 1;
+    int64_t page[2];                                                       // where the pages of the next step's two groups of 16 tokens begin
+    bool there[2];
+    auto look_up = [&](int k) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j = first + k * C::STEP + 16 * i;
+        there[i] = k < steps && j < it.hi && j + 16 > it.lo;
+        page[i] = 0;
+        if (there[i]) {
+          const int p = table[j >> c.page_shift];
+          there[i] = (unsigned)p < (unsigned)c.num_pages;
+          if (there[i]) page[i] = p * c.page_bytes;
+          else kv_bad_page(c);
+        }
+      }
+    };
+    uint32_t dst = ring;                                                   // the stage that is filled next
+    auto fetch = [&](int k) {
+      const int j0 = first + k * C::STEP;
+      if (k < steps) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int slot = (j0 + 16 * i) & mask;
+          const uint8_t* src = head_pages + page[i] + slot * (D / 2) + lane * 16;
+          const int bytes = there[i] ? 16 : 0;
+#pragma unroll
+          for (int x = 0; x < PER_GROUP; ++x) {
+            const int y = i * PER_GROUP + x;
+            cp_async_16(dst + to_chunk[CH == 8 ? y & 1 : 0] + 512 * y, src + 512 * x, bytes);
+            cp_async_16(dst + C::K_BYTES + to_chunk[CH == 8 ? y & 1 : 0] + 512 * y, src + c.v_codes + 512 * x, bytes);
+          }
+        }
+        const bool mine = my_group ? there[1] : there[0];
+        const uint8_t* src = head_pages + (my_group ? page[1] : page[0]) + ((j0 + 16 * my_group) & mask) * SB + scale_from;
+        const uint32_t to = dst + 2 * C::K_BYTES + my_half * C::S_BYTES + (my_group * PIECES + my_piece) * 16;
+        if constexpr (4 * PIECES <= 32) {
+          if (lane < 4 * PIECES) cp_async_16(to, src, mine ? 16 : 0);
+        } else {
+          cp_async_16(to, src, mine ? 16 : 0);
+          cp_async_16(to + C::S_BYTES, src + (c.v_scales - c.k_scales), mine ? 16 : 0);
+        }
+      }
+      cp_async_commit();
+      dst = dst == ring + (C::STAGES - 1) * C::STAGE ? ring : dst + C::STAGE;
+    };
+    look_up(0);
+#pragma unroll
+    for (int k = 0; k < C::STAGES - 1; ++k) {
+      fetch(k);
+      look_up(k + 1);
+    }
 
     // the queries, and what each row sees
     KvQuery<D> q[NT];
@@ -227,84 +275,79 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
 #pragma unroll
       for (int i = 0; i < CH * 8; ++i) o[n][i / 8][i / 4 % 2][i % 4] = 0.f;
     int top_scale[CH];                                                     // MXFP4, MXINT4: E of each chunk
-    uint32_t top_pair[CH / 2], shift[CH];                                  // the same, chunks i and i + 2 (bytes apart) in halves; 27 - E twice
+    uint32_t top_pair[CH / 2];                                             // the same in halves: chunks i and i + 2 of four (CH = 2: both)
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
       top_scale[i] = 27;
-      shift[i] = 0;
       top_pair[i / 2] = 0x001B001Bu;
     }
 
-    const int steps = unit1 - unit0, first = it.base + unit0 * C::UNIT + warp * C::STEP;
-    const int32_t* table = c.table + (int64_t)b * c.width;
-    int page[2];
-    auto look_up = [&](int k) {                                            // pages of step k's two groups of 16 tokens; -1: nothing there
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int j = first + k * C::UNIT + 16 * i;
-        page[i] = -1;
-        if (k < steps && j < it.hi && j + 16 > it.lo) {
-          page[i] = table[j >> c.page_shift];
-          if ((unsigned)page[i] >= (unsigned)c.num_pages) {
-            kv_bad_page(c);
-            page[i] = -1;
-          }
-        }
-      }
-    };
-    auto fetch = [&](int k) {
-      const int j0 = first + k * C::UNIT, mask = (1 << c.page_shift) - 1;
-      const uint32_t dst = ring + (k % C::STAGES) * C::STAGE;
-      if (k < steps) {
-#pragma unroll
-        for (int i = 0; i < 2 * CH; ++i) {                                 // chunks of keys, then of values
-          const int id = i % CH * 32 + lane, row = id / CH, chunk = id % CH, p = page[row >> 4];
-          const uint8_t* src = kv_head_page(c, p < 0 ? 0 : p, it.head) + (i < CH ? 0 : c.v_codes) + ((j0 + row) & mask) * (D / 2) + chunk * 16;
-          cp_async_16(dst + (i < CH ? 0 : C::K_BYTES) + 16 * kv_swizzled<D>(row, chunk), src, p < 0 ? 0 : 16);
-        }
-        constexpr int PIECES = C::S_BYTES / 16;                            // of the keys' scales, and of the values'
-#pragma unroll
-        for (int i = 0; i < (2 * PIECES + 31) / 32; ++i) {
-          const int id = i * 32 + lane, piece = id % PIECES;
-          if (id < 2 * PIECES) {
-            const int row = piece * 16 / SB, p = page[row >> 4];
-            const uint8_t* src = kv_head_page(c, p < 0 ? 0 : p, it.head) + (id < PIECES ? c.k_scales : c.v_scales) + ((j0 + row) & mask) * SB +
-                                 (piece * 16 - row * SB);
-            cp_async_16(dst + 2 * C::K_BYTES + id * 16, src, p < 0 ? 0 : 16);
-          }
-        }
-      }
-      cp_async_commit();
-    };
-    look_up(0);
-#pragma unroll
-    for (int k = 0; k < C::STAGES - 1; ++k) {
-      fetch(k);
-      look_up(k + 1);
-    }
-
+    uint32_t stage = ring;
     for (int k = 0; k < steps; ++k) {
       cp_async_wait<C::STAGES - 2>();
       __syncwarp();
       fetch(k + C::STAGES - 1);                                            // into the stage that the last step has left
       look_up(k + C::STAGES);
-      const int j0 = first + k * C::UNIT;
-      if (j0 >= it.hi) continue;
-      const uint32_t stage = ring + (k % C::STAGES) * C::STAGE;
-      uint8_t* stage_p = ring_p + (k % C::STAGES) * C::STAGE;
-      uint8_t* v_scales = stage_p + 2 * C::K_BYTES + C::S_BYTES;
+      const int j0 = first + k * C::STEP;
+      const uint8_t* scales = ring_p + (stage - ring) + 2 * C::K_BYTES;
       const bool border = j0 < all_lo || j0 + C::STEP > all_hi;
-      if (border && (j0 + lane >= it.hi || j0 + lane < it.base)) {         // what lies there may be no numbers
+
+      // scales of the 32 tokens; behind the last token may lie what is no number
+      kv_ready_key_scales<FMT, D>(scales, lane, room);
+      {
+        uint32_t w[(SB + 3) / 4];
+        kv_scale_words<SB>(scales + C::S_BYTES + lane * SB, w);
+        if (border && j0 + lane >= it.hi) {
 #pragma unroll
-        for (int i = 0; i < SB; i += 2) *reinterpret_cast<uint16_t*>(v_scales + lane * SB + i) = 0;
+          for (int i = 0; i < (SB + 3) / 4; ++i) w[i] = 0;
+        }
+        uint16_t* to = reinterpret_cast<uint16_t*>(v_room) + kv_value_order(lane);
+        if constexpr (FMT == FMT_NVFP4) {
+#pragma unroll
+          for (int i = 0; i < SB; i += 2) {
+            const uint32_t f = e4m3x2_f16x2(w[i / 4] >> (8 * (i & 2)));
+            to[32 * i] = (uint16_t)f;
+            to[32 * (i + 1)] = (uint16_t)(f >> 16);
+          }
+        } else {
+          uint32_t pair[CH / 2];                                           // chunks i and i + 2 of four
+          bool above = false;
+#pragma unroll
+          for (int i = 0; i < CH / 2; ++i) {
+            if constexpr (CH == 2) pair[i] = (w[0] & 0xFFu) | (w[0] & 0xFF00u) << 8;
+            else pair[i] = (w[i / 2] >> (8 * (i % 2))) & 0x00FF00FFu;
+            above |= __vmaxu2(pair[i], top_pair[i]) != top_pair[i];
+          }
+          if (__any_sync(0xFFFFFFFFu, above)) {
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+              const int word = CH == 2 ? 0 : i / 4 * 2 + i % 2, half = CH == 2 ? i : i % 4 / 2;
+              const int top = max(top_scale[i], (int)__reduce_max_sync(0xFFFFFFFFu, pair[word] >> (16 * half) & 0xFFFFu));
+              const float old = top - top_scale[i] > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (top - top_scale[i])) << 23);
+              top_scale[i] = top;
+              top_pair[word] = half ? (top_pair[word] & 0xFFFFu) | (uint32_t)top << 16 : (top_pair[word] & 0xFFFF0000u) | (uint32_t)top;
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int x = 0; x < 8; ++x) o[n][i][x / 4][x % 4] *= old;
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < CH / 2; ++i) {
+            const uint32_t f = __viaddmax_s16x2_relu(pair[i], __vsub2(0x001B001Bu, top_pair[i]), 0u) << 10;
+            const int low = CH == 2 ? 0 : i / 2 * 4 + i % 2, high = CH == 2 ? 1 : low + 2;
+            to[32 * low] = (uint16_t)f;
+            to[32 * high] = (uint16_t)(f >> 16);
+          }
+        }
       }
-      if (border) __syncwarp();
+      __syncwarp();
 
       // scores, weights
       uint32_t p[NT][2][2];
       float s[2][NT][4];
 #pragma unroll
-      for (int u = 0; u < 2; ++u) kv_tile_scores<FMT, D, NT>(stage, stage_p + 2 * C::K_BYTES, 16 * u, lane, q, s[u]);
+      for (int u = 0; u < 2; ++u) kv_tile_scores<FMT, D, NT>(stage, room, 16 * u, lane, q, s[u]);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         float f[2] = {factor[n][0], factor[n][1]};
@@ -357,38 +400,8 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
       }
 
       // values
-      if constexpr (FMT != FMT_NVFP4) {
-        uint32_t w[(SB + 3) / 4], pair[CH / 2];
-        kv_scale_words<SB>(v_scales + lane * SB, w);                       // a token's each
-        bool above = false;
-#pragma unroll
-        for (int i = 0; i < CH / 2; ++i) {
-          if constexpr (CH == 2) pair[i] = (w[0] & 0xFFu) | (w[0] & 0xFF00u) << 8;
-          else pair[i] = (w[i / 2] >> (8 * (i % 2))) & 0x00FF00FFu;
-          above |= __vmaxu2(pair[i], top_pair[i]) != top_pair[i];
-        }
-        if (__any_sync(0xFFFFFFFFu, above)) {
-#pragma unroll
-          for (int i = 0; i < CH; ++i) {
-            const int word = CH == 2 ? 0 : i / 4 * 2 + i % 2, half = CH == 2 ? i : i % 4 / 2;
-            const int top = max(top_scale[i], (int)__reduce_max_sync(0xFFFFFFFFu, pair[word] >> (16 * half) & 0xFFFFu));
-            const float old = top - top_scale[i] > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (top - top_scale[i])) << 23);
-            top_scale[i] = top;
-            top_pair[word] = half ? (top_pair[word] & 0xFFFFu) | (uint32_t)top << 16 : (top_pair[word] & 0xFFFF0000u) | (uint32_t)top;
-            shift[i] = (uint32_t)(27 - top) & 0xFFFFu;
-            shift[i] |= shift[i] << 16;
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-              for (int x = 0; x < 8; ++x) o[n][i][x / 4][x % 4] *= old;
-          }
-        }
-      }
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        uint32_t w[4][(SB + 3) / 4];                                       // scales of tokens 2t, 2t + 1, 2t + 8, 2t + 9
-#pragma unroll
-        for (int i = 0; i < 4; ++i) kv_scale_words<SB>(v_scales + (16 * u + 2 * t + (i & 1) + 8 * (i >> 1)) * SB, w[i]);
 #pragma unroll
         for (int c2 = 0; c2 < CH; c2 += 2) {
           uint32_t raw[4];
@@ -396,20 +409,14 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             const int ch = c2 + e;
+            const int blk = FMT == FMT_NVFP4 ? 2 * ch + (g >> 2) : ch;
+            const uint2 f = *reinterpret_cast<const uint2*>(v_room + 64 * blk + 32 * u + 8 * t);   // tokens 2t, 2t + 1; 2t + 8, 2t + 9
             uint32_t v[2][4];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-              uint32_t f;
-              if constexpr (FMT == FMT_NVFP4) {
-                const uint32_t at_byte = 2 * (ch & 1) + (g >> 2);
-                f = e4m3x2_f16x2(__byte_perm(w[2 * i][ch / 2], w[2 * i + 1][ch / 2], at_byte | (at_byte + 4) << 4));
-              } else {
-                const uint32_t x = __byte_perm(w[2 * i][ch / 4], w[2 * i + 1][ch / 4], (ch % 4) | (ch % 4 + 4) << 8) & 0x00FF00FFu;
-                f = __viaddmax_s16x2_relu(x, shift[ch], 0u) << 10;
-              }
               kv_value_pairs<FMT>(raw[2 * e + i], v[i]);
 #pragma unroll
-              for (int x = 0; x < 4; ++x) v[i][x] = mul_f16x2(v[i][x], f);
+              for (int x = 0; x < 4; ++x) v[i][x] = mul_f16x2(v[i][x], i ? f.y : f.x);
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
@@ -419,129 +426,113 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
           }
         }
       }
+      stage = stage == ring + (C::STAGES - 1) * C::STAGE ? ring : stage + C::STAGE;
     }
     cp_async_wait<0>();
+    __syncwarp();                                                          // before the ring is filled again
 
-    // the warps' results together
+    const bool begins = step0 == 0, whole = begins && steps == per;
+    float* part = partials + (int64_t)(2 * range + (begins ? 1 : 0)) * C::PARTIAL;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], x);
-        if (g == 0) {
-          row_m[warp][8 * n + 2 * t + e] = m[n][e];
-          row_l[warp][8 * n + 2 * t + e] = l[n][e];
-        }
-      }
-    __syncthreads();                                                       // and the ring is free
-    float* join = reinterpret_cast<float*>(smem);
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
         const int r = 8 * n + 2 * t + e;
-        float top = row_m[0][r];
-#pragma unroll
-        for (int w = 1; w < C::WARPS; ++w) top = fmaxf(top, row_m[w][r]);
-        const float f = ex2(m[n][e] - top);
+        if (r >= it.rows) continue;
+        const float inv = whole ? (l[n][e] > 0.f ? 1.f / l[n][e] : 0.f) : 1.f;
+        const int64_t row = kv_out_row(it, r, heads, group);
 #pragma unroll
         for (int ch = 0; ch < CH; ++ch) {
-          const float fs = FMT == FMT_NVFP4 ? f * c.v_ts : f * __uint_as_float((uint32_t)(top_scale[ch] - 12) << 23);
-          *reinterpret_cast<float4*>(join + (warp * ROWS + r) * D + 32 * ch + 4 * g) =
-              make_float4(o[n][ch][0][e] * fs, o[n][ch][0][e + 2] * fs, o[n][ch][1][e] * fs, o[n][ch][1][e + 2] * fs);
+          const float fs = FMT == FMT_NVFP4 ? inv * c.v_ts : inv * __uint_as_float((uint32_t)(top_scale[ch] - 12) << 23);
+          const float4 v = make_float4(o[n][ch][0][e] * fs, o[n][ch][0][e + 2] * fs, o[n][ch][1][e] * fs, o[n][ch][1][e + 2] * fs);
+          if (whole) {
+            uint2 y;
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y.x) : "f"(v.y), "f"(v.x));
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y.y) : "f"(v.w), "f"(v.z));
+            *reinterpret_cast<uint2*>(out + row * D + 32 * ch + 4 * g) = y;
+          } else {
+            *reinterpret_cast<float4*>(part + r * D + 32 * ch + 4 * g) = v;
+          }
+        }
+        if (g) continue;
+        if (!whole) {
+          part[ROWS * D + r] = m[n][e];
+          part[ROWS * D + ROWS + r] = l[n][e];
+        } else if (lse) {
+          lse[row] = l[n][e] > 0.f ? (m[n][e] - 12.f + log2f(l[n][e])) * kLn2 : -INFINITY;
         }
       }
-    __syncthreads();
-    const bool begins = unit0 == 0, whole = begins && unit1 == per;
-    float* part = partials + (int64_t)(2 * cta + (begins ? 1 : 0)) * C::PARTIAL;
-    for (int i = tid; i < ROWS * D / 4; i += C::THREADS) {
-      const int r = i / (D / 4), d = i % (D / 4) * 4;
-      float4 v = make_float4(0, 0, 0, 0);
-      float top = row_m[0][r], sum = 0.f;
-#pragma unroll
-      for (int w = 1; w < C::WARPS; ++w) top = fmaxf(top, row_m[w][r]);
-#pragma unroll
-      for (int w = 0; w < C::WARPS; ++w) {
-        const float4 x = *reinterpret_cast<const float4*>(join + (w * ROWS + r) * D + d);
-        v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-        sum += row_l[w][r] * ex2(row_m[w][r] - top);
-      }
-      if (whole) {
-        if (r < it.rows) {
-          const float inv = sum > 0.f ? 1.f / sum : 0.f;
-          const int rr = it.first_row + r;
-          const int64_t row = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
-          uint2 y;
-          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y.x) : "f"(v.y * inv), "f"(v.x * inv));
-          asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y.y) : "f"(v.w * inv), "f"(v.z * inv));
-          *reinterpret_cast<uint2*>(out + row * D + d) = y;
-          if (lse && d == 0) lse[row] = sum > 0.f ? (top - 12.f + log2f(sum)) * kLn2 : -INFINITY;
-        }
-      } else {
-        *reinterpret_cast<float4*>(part + r * D + d) = v;
-        if (d == 0) {
-          part[ROWS * D + r] = top;
-          part[ROWS * D + ROWS + r] = sum;
-        }
-      }
-    }
-    if (begins && !whole && tid == 0) {
-      KvOwner w;
-      w.rows = it.rows;
-      w.first_row = it.first_row;
-      w.first_token = it.first_token;
-      w.head = it.head;
-      w.end = sequence_begin + (long long)local * per + per;
-      w.units = units;
-      owners[cta] = w;
-    }
-    __syncthreads();                                                       // before the ring is filled again
   }
 }
 
-// The CTA of an item's first range joins the ranges' results; SPLIT warps to a row, each with its share of the ranges.
-template <int D, int NT>
-struct KvJoinCfg {
-  static constexpr int ROWS = 8 * NT, SPLIT = NT == 1 ? 4 : 2, THREADS = 32 * ROWS * SPLIT, EACH = D / 32;       // elements per lane
-  static constexpr int PARTIAL = ROWS * (D + 2);
-};
-template <int D, int NT>
-__global__ void __launch_bounds__(KvJoinCfg<D, NT>::THREADS) kv_join_kernel(int ctas, int heads, int group, const KvOwner* owners, const float* partials,
-                                                                         __nv_bfloat16* out, float* lse) {
-  using J = KvJoinCfg<D, NT>;
-  constexpr int ROWS = J::ROWS;
-  __shared__ float parts[J::SPLIT][ROWS][D + 2];
-  griddep_wait_and_launch();
-  const int cta = blockIdx.x, lane = threadIdx.x & 31, r = (threadIdx.x >> 5) / J::SPLIT, which = (threadIdx.x >> 5) % J::SPLIT;
-  const KvOwner w = owners[cta];
-  if (w.rows == 0) return;
-  int last = cta;                        // the CTA of unit end - 1: the last whose range begins before `end`
-  {
-    long long x = (w.end * ctas - 1) / w.units;                            // about there
-    if (x > ctas - 1) x = ctas - 1;
-    while (kv_range_begin(w.units, (int)x, ctas) >= w.end) --x;
-    while (x + 1 < ctas && kv_range_begin(w.units, (int)x + 1, ctas) < w.end) ++x;
-    last = (int)x;
+// Joins the results of an item that more than one warp has worked on.  CTA (i, j): item i of the list, its rows from j (8 / SPLIT) on; SPLIT warps to a
+// row, each with its share of the ranges.  The list is counted before the wait for the streaming kernel: that one has waited for all before it.
+template <int D, int NT, int SPLIT>
+__global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvScoring a, int ranges, int heads, const float* partials, __nv_bfloat16* out,
+                                                      float* lse) {
+  constexpr int ROWS = 8 * NT, PARTIAL = ROWS * (D + 2), EACH = D / 32;
+  __shared__ float parts[SPLIT == 1 ? 1 : 8][D + 2];
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = warp % SPLIT, group = heads / c.heads;
+  const int r = blockIdx.y * (8 / SPLIT) + warp / SPLIT;
+  KvItem it;
+  int groups = 0, per = 1;
+  auto steps_of = [&](int b, long long& items) -> long long {
+    items = 0;
+    if (b >= c.batch) return 0;
+    kv_sequence_steps<ROWS>(c, a, b, group, it, groups, per);
+    items = (long long)groups * c.heads;
+    return items * per;
+  };
+  long long units = 0, items_before = 0, begin = -1;
+  int found_b = -1, local = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += 32) {
+    long long items;
+    const long long v = steps_of(b0 + lane, items), sum = warp_scan(v, lane), item_sum = warp_scan(items, lane);
+    const uint32_t here = __ballot_sync(0xFFFFFFFFu, (long long)blockIdx.x < items_before + item_sum);
+    if (here && begin < 0) {
+      const int first = __ffs(here) - 1;
+      found_b = b0 + first;
+      local = (int)((long long)blockIdx.x - items_before - __shfl_sync(0xFFFFFFFFu, item_sum - items, first));
+      begin = units + __shfl_sync(0xFFFFFFFFu, sum - v, first) + (long long)local * __shfl_sync(0xFFFFFFFFu, per, first);
+    }
+    units += __shfl_sync(0xFFFFFFFFu, sum, 31);
+    items_before += __shfl_sync(0xFFFFFFFFu, item_sum, 31);
   }
-  float m = -1e30f, l = 0.f, o[J::EACH] = {};
-  auto part_of = [&](int i) { return partials + (int64_t)(2 * i + (i == cta ? 1 : 0)) * J::PARTIAL; };
+  if (found_b < 0) return griddep_wait();                                  // every CTA waits: what stands behind this kernel relies on that
+  long long items;
+  steps_of(found_b, items);
+  it.head = local / groups;
+  it.first_row = local % groups * ROWS;
+  it.rows = min(ROWS, it.count * group - it.first_row);
+  const long long end = begin + per;
+  // the range that has this step: the last that begins at or before it
+  auto range_of = [&](long long unit) { return (int)(((unit + 1) * ranges + units - 1) / units) - 1; };
+  const int from = range_of(begin), to = range_of(end - 1);
+  griddep_wait();
+  if (from == to) return;                                                  // finished
+  float m = -1e30f, l = 0.f, o[EACH] = {};
   constexpr int BATCH = 4;
-  for (int i = cta + which; i <= last; i += J::SPLIT * BATCH) {
-    float pm[BATCH], pl[BATCH], v[BATCH][J::EACH];
+  const bool dense = units >= ranges;                                      // else a range has one step at most, and most have none
+  const int parts_n = dense ? to - from + 1 : per;
+  for (int i = which; i < parts_n && r < it.rows; i += SPLIT * BATCH) {
+    float pm[BATCH], pl[BATCH], v[BATCH][EACH];
 #pragma unroll
     for (int x = 0; x < BATCH; ++x) {
-      const int at = i + x * J::SPLIT;
+      const int k = i + x * SPLIT;
       pm[x] = -1e30f;
       pl[x] = 0.f;
 #pragma unroll
-      for (int e = 0; e < J::EACH; ++e) v[x][e] = 0.f;
-      if (at <= last && kv_range_begin(w.units, at, ctas) < kv_range_begin(w.units, at + 1, ctas)) {       // CTAs without units left nothing
-        const float* p = part_of(at);
+      for (int e = 0; e < EACH; ++e) v[x][e] = 0.f;
+      if (k < parts_n) {
+        const int at = dense ? from + k : range_of(begin + k);
+        const float* p = partials + (int64_t)(2 * at + (at == from ? 1 : 0)) * PARTIAL;
         pm[x] = p[ROWS * D + r];
         pl[x] = p[ROWS * D + ROWS + r];
 #pragma unroll
-        for (int e = 0; e < J::EACH; ++e) v[x][e] = p[r * D + e * 32 + lane];
+        for (int e = 0; e < EACH; ++e) v[x][e] = p[r * D + e * 32 + lane];
       }
     }
     float top = m;
@@ -550,93 +541,311 @@ __global__ void __launch_bounds__(KvJoinCfg<D, NT>::THREADS) kv_join_kernel(int 
     const float old = ex2(m - top);
     l *= old;
 #pragma unroll
-    for (int e = 0; e < J::EACH; ++e) o[e] *= old;
+    for (int e = 0; e < EACH; ++e) o[e] *= old;
 #pragma unroll
     for (int x = 0; x < BATCH; ++x) {
       const float f = ex2(pm[x] - top);
       l += pl[x] * f;
 #pragma unroll
-      for (int e = 0; e < J::EACH; ++e) o[e] += v[x][e] * f;
+      for (int e = 0; e < EACH; ++e) o[e] += v[x][e] * f;
     }
     m = top;
   }
+  if constexpr (SPLIT > 1) {
 #pragma unroll
-  for (int e = 0; e < J::EACH; ++e) parts[which][r][e * 32 + lane] = o[e];
-  if (lane == 0) {
-    parts[which][r][D] = m;
-    parts[which][r][D + 1] = l;
+    for (int e = 0; e < EACH; ++e) parts[warp][e * 32 + lane] = o[e];
+    if (lane == 0) {
+      parts[warp][D] = m;
+      parts[warp][D + 1] = l;
+    }
+    __syncthreads();
+    if (which) return;
+    float top = m;
+#pragma unroll
+    for (int x = 1; x < SPLIT; ++x) top = fmaxf(top, parts[warp + x][D]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int x = 0; x < SPLIT; ++x) {
+      const float f = ex2(parts[warp + x][D] - top);
+      l += parts[warp + x][D + 1] * f;
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) o[e] += parts[warp + x][e * 32 + lane] * f;
+    }
+    m = top;
   }
-  __syncthreads();
-  if (which || r >= w.rows) return;
-  float top = m;
-#pragma unroll
-  for (int x = 1; x < J::SPLIT; ++x) top = fmaxf(top, parts[x][r][D]);
-  l = 0.f;
-#pragma unroll
-  for (int e = 0; e < J::EACH; ++e) o[e] = 0.f;
-#pragma unroll
-  for (int x = 0; x < J::SPLIT; ++x) {
-    const float f = ex2(parts[x][r][D] - top);
-    l += parts[x][r][D + 1] * f;
-#pragma unroll
-    for (int e = 0; e < J::EACH; ++e) o[e] += parts[x][r][e * 32 + lane] * f;
-  }
-  const int rr = w.first_row + r;
-  const int64_t row = (int64_t)(w.first_token + rr / group) * heads + w.head * group + rr % group;
+  if (r >= it.rows) return;
+  const int64_t row = kv_out_row(it, r, heads, group);
   const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-  for (int e = 0; e < J::EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
-  if (lse && lane == 0) lse[row] = l > 0.f ? (top - 12.f + log2f(l)) * kLn2 : -INFINITY;
+  for (int e = 0; e < EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
+  if (lse && lane == 0) lse[row] = l > 0.f ? (m - 12.f + log2f(l)) * kLn2 : -INFINITY;
 }
 
-// A lane's share of a row: DPL consecutive elements.
-template <int FMT, int DPL>
-__device__ __forceinline__ void kv_row_share(const uint8_t* codes, const uint8_t* scales, int lane, float ts, float (&v)[DPL]) {
-  const float s = kv_scale<FMT>(scales[lane * DPL / kv_block(FMT)], ts);
-  const int at = lane * (DPL / 2);
-  const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + (at & ~3)) >> (8 * (at & 3));
-  float all[8];
-  kv_codes8<FMT>(w, all);
-#pragma unroll
-  for (int i = 0; i < DPL; ++i) v[i] = all[i] * s;
-}
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-  return v;
-}
+// ---- the account ------------------------------------------------------------------------------------------------------------------------------
+// weights_out[token] = (old or, of a new token, 0) + sum over the rows of its sequence and the heads of its group of exp2(x log2 e - lse log2 e).
+// Only keys are read.  The list of steps of 32 cached tokens is cut into equal ranges for warps as above, a step counting as often as its sequence
+// has groups of eight rows; a step belongs to the range that it begins in, so every slot is written once and the order of its sum is fixed.  A warp holds
+// the keys of a step as operands (D = 256: of half a step) and goes through the groups.
+template <int FMT_, int D_>
+struct KvWeightsCfg {
+  static constexpr int FMT = FMT_, D = D_, WARPS = 4, THREADS = 128, CH = D / 32, SB = D / kv_block(FMT), CTAS = D == 64 ? 4 : 3;
+  static constexpr int K_BYTES = 16 * D, S_BYTES = 32 * SB, STAGE = K_BYTES + S_BYTES, STAGES = D == 256 ? 3 : 4;
+  static constexpr int ROOM = KvScaleRoom<FMT, D>::KEYS, SMEM = WARPS * (STAGES * STAGE + ROOM), TILES = D == 256 ? 1 : 2;
+};
 
-// One warp per cached token and head: what the queries of its sequence gave it, added to what it had (new tokens had nothing).
-template <int FMT, int D>
-__global__ void __launch_bounds__(128) kv_weights_simple_kernel(const KvView c, const KvScoring a, const __nv_bfloat16* Q, int64_t q_stride, int heads,
-                                                                const float* lse, const float* weights, float* weights_out) {
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const KvView c, const KvScoring a, const __nv_bfloat16* Q, int64_t q_stride, int heads,
+                                                                         const float* lse, const float* weights, float* weights_out) {
+  constexpr int FMT = C::FMT, D = C::D, CH = C::CH, SB = C::SB, TILES = C::TILES;
+  extern __shared__ __align__(128) uint8_t smem[];
   griddep_wait_and_launch();
-  constexpr int DPL = D / 32;
-  const int lane = threadIdx.x & 31, kvh = blockIdx.y % c.heads, b = blockIdx.y / c.heads, group = heads / c.heads;
-  const int length = kv_length(c, b);
-  int first, count;
-  kv_new_tokens(c, b, first, count);
-  for (int j = blockIdx.x * 4 + (threadIdx.x >> 5); j < length; j += gridDim.x * 4) {
-    const int page = kv_page(c, c.table, c.width, b, j);
-    if (page < 0) continue;
-    const uint8_t* at = kv_head_page(c, page, kvh);
-    const int slot = j & ((1 << c.page_shift) - 1);
-    float k[DPL], sum = 0.f;
-    kv_row_share<FMT, DPL>(at + slot * (D / 2), at + c.k_scales + slot * (D / kv_block(FMT)), lane, c.k_ts, k);
-    for (int r = 0; r < count * group; ++r) {
-      const int i = first + r / group, h = kvh * group + r % group, p = length - count + r / group;
-      int lo, hi;
-      kv_range(a, b, i, p, length, lo, hi);
-      const float y = lse[(int64_t)i * heads + h];
-      if (j < lo || j >= hi || y == -INFINITY) continue;
-      float x = 0.f;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, group = heads / c.heads;
+  const int range = blockIdx.x * C::WARPS + warp, ranges = gridDim.x * C::WARPS;
+  KvItem it;
+  int groups, cost, per;                                                   // groups of rows; what a step counts; steps of a head
+  auto units_of = [&](int b) -> long long {
+    if (b >= c.batch) return 0;
+    it.b = b;
+    kv_new_tokens(c, b, it.first_token, it.count);
+    it.length = kv_length(c, b);
+    groups = (it.count * group + 7) / 8;
+    cost = groups > 1 ? groups : 1;
+    per = (it.length + 31) / 32;
+    const int p0 = it.length - it.count;
+    it.lo = a.window > 0 && p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
+    return (long long)cost * c.heads * per;
+  };
+  const long long mine = units_of(lane);
+  long long units = mine;
+#pragma unroll 4
+  for (int b0 = 32; b0 < c.batch; b0 += 32) units += units_of(b0 + lane);
 #pragma unroll
-      for (int e = 0; e < DPL; ++e) x += __bfloat162float(Q[i * q_stride + h * D + lane * DPL + e]) * k[e];
-      x = kv_score(warp_sum(x) * a.scale, a.softcap, a.slopes ? a.slopes[h] : 0.f, abs(p - j));
-      sum += exp2f(x - y * kLog2e);
+  for (int o = 16; o; o >>= 1) units += __shfl_xor_sync(0xFFFFFFFFu, units, o);
+  const long long begin = kv_range_begin(units, range, ranges), end = kv_range_begin(units, range + 1, ranges);
+  if (begin >= end) return;
+  int b = 0;
+  long long sequence_begin = 0;
+  for (int b0 = 0;; b0 += 32) {                                            // ends, since begin < units
+    const long long v = b0 ? units_of(b0 + lane) : mine, sum = warp_scan(v, lane);
+    const uint32_t here = __ballot_sync(0xFFFFFFFFu, begin < sequence_begin + sum);
+    if (here) {
+      const int first = __ffs(here) - 1;
+      b = b0 + first;
+      sequence_begin += __shfl_sync(0xFFFFFFFFu, sum - v, first);
+      break;
     }
-    const int64_t w = (((int64_t)page * c.heads + kvh) << c.page_shift) + slot;
-    if (lane == 0) weights_out[w] = sum + (j < length - count ? weights[w] : 0.f);
+    sequence_begin += __shfl_sync(0xFFFFFFFFu, sum, 31);
+  }
+  long long sequence_units = units_of(b);
+  long long at = (begin - sequence_begin + cost - 1) / cost * cost + sequence_begin;       // the first step that begins in the range
+
+  const uint32_t ring = smem_u32(smem) + warp * C::STAGES * C::STAGE;
+  uint8_t *ring_p = smem + warp * C::STAGES * C::STAGE, *room = smem + C::WARPS * C::STAGES * C::STAGE + warp * C::ROOM;
+  const int row_of = lane & 15, chunk_of = lane >> 4, mask = (1 << c.page_shift) - 1;
+  constexpr int PER_GROUP = CH / 2;
+  uint32_t to_chunk[CH == 8 ? 2 : 1];
+#pragma unroll
+  for (int i = 0; i < (CH == 8 ? 2 : 1); ++i) to_chunk[i] = 16 * kv_swizzled<D>((32 * i + lane) / CH, lane % CH) - 512 * i;
+  constexpr int PIECES = SB;                                               // of 16 bytes: the scale bytes of 16 tokens
+  const int my_piece = lane % PIECES, my_group = lane / PIECES & 1;
+
+  while (at < end) {
+    while (at >= sequence_begin + sequence_units) {
+      sequence_begin += sequence_units;
+      sequence_units = units_of(++b);
+    }
+    const int step_of = (int)((at - sequence_begin) / cost);
+    it.head = step_of / per;
+    const int step0 = step_of - it.head * per;
+    const long long left = (end - at + cost - 1) / cost;                   // steps that begin in the range
+    const int steps = (int)(left < per - step0 ? left : per - step0);
+    at += (long long)steps * cost;
+
+    const int first = 32 * step0;
+    const int32_t* table = c.table + (int64_t)b * c.width;
+    const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
+    int64_t page[2];
+    bool there[2];
+    auto look_up = [&](int k) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int j = first + 32 * k + 16 * i;
+        there[i] = k < steps && j < it.length && j + 16 > it.lo;
+        page[i] = 0;
+        if (there[i]) {
+          const int p = table[j >> c.page_shift];
+          there[i] = (unsigned)p < (unsigned)c.num_pages;
+          if (there[i]) page[i] = p * c.page_bytes;
+          else kv_bad_page(c);
+        }
+      }
+    };
+    uint32_t dst = ring;
+    auto fetch = [&](int k) {
+      const int j0 = first + 32 * k;
+      if (k < steps) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint8_t* src = head_pages + page[i] + ((j0 + 16 * i) & mask) * (D / 2) + lane * 16;
+#pragma unroll
+          for (int x = 0; x < PER_GROUP; ++x) {
+            const int y = i * PER_GROUP + x;
+            cp_async_16(dst + to_chunk[CH == 8 ? y & 1 : 0] + 512 * y, src + 512 * x, there[i] ? 16 : 0);
+          }
+        }
+        if (lane < 2 * PIECES) {
+          const bool have = my_group ? there[1] : there[0];
+          cp_async_16(dst + C::K_BYTES + lane * 16, head_pages + (my_group ? page[1] : page[0]) + c.k_scales + ((j0 + 16 * my_group) & mask) * SB + my_piece * 16,
+                      have ? 16 : 0);
+        }
+      }
+      cp_async_commit();
+      dst = dst == ring + (C::STAGES - 1) * C::STAGE ? ring : dst + C::STAGE;
+    };
+    look_up(0);
+#pragma unroll
+    for (int k = 0; k < C::STAGES - 1; ++k) {
+      fetch(k);
+      look_up(k + 1);
+    }
+
+    // eight rows: their operand, factors to powers of two, ranges.  A row that is not there, or that saw nothing, counts exp2(-inf).
+    KvQuery<D> q[1];
+    float factor[2], off[2], slope[2];
+    int place[2], lo[2], hi[2], all_lo, all_hi;
+    auto load_rows = [&](int n) {
+      const int r = 8 * n + g, rows = it.count * group;
+      const float back = kv_load_query<FMT, D>(r < rows ? Q + (it.first_token + r / group) * q_stride + (it.head * group + r % group) * D : nullptr, t, q[0]);
+      all_lo = 0;
+      all_hi = INT32_MAX;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rr = 8 * n + 2 * t + e;
+        factor[e] = __shfl_sync(0xFFFFFFFFu, back, 8 * t + 4 * e) * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e);
+        lo[e] = hi[e] = place[e] = 0;
+        slope[e] = 0.f;
+        off[e] = -INFINITY;
+        if (rr < rows) {
+          const int i = it.first_token + rr / group, h = it.head * group + rr % group;
+          const float y = lse[(int64_t)i * heads + h];
+          place[e] = it.length - it.count + rr / group;
+          if (y != -INFINITY) {
+            off[e] = -y * kLog2e;
+            kv_range(a, it.b, i, place[e], it.length, lo[e], hi[e]);
+            all_lo = max(all_lo, lo[e]);
+            all_hi = min(all_hi, hi[e]);
+          }
+          if (a.slopes) slope[e] = a.slopes[h];
+        }
+      }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1) {
+        all_lo = max(all_lo, __shfl_xor_sync(0xFFFFFFFFu, all_lo, o));
+        all_hi = min(all_hi, __shfl_xor_sync(0xFFFFFFFFu, all_hi, o));
+      }
+    };
+    if (groups == 1) load_rows(0);
+    const bool special = a.softcap > 0.f || a.slopes;
+
+    uint32_t stage = ring;
+    for (int k = 0; k < steps; ++k) {
+      cp_async_wait<C::STAGES - 2>();
+      __syncwarp();
+      fetch(k + C::STAGES - 1);
+      look_up(k + C::STAGES);
+      const int j0 = first + 32 * k, mine_j = j0 + lane;
+      // this lane's slot in the account
+      int64_t slot = -1;
+      float old = 0.f;
+      if (mine_j < it.length) {
+        const int p = table[mine_j >> c.page_shift];
+        if ((unsigned)p < (unsigned)c.num_pages) {
+          slot = (((int64_t)p * c.heads + it.head) << c.page_shift) + (mine_j & mask);
+          if (mine_j < it.length - it.count) old = weights[slot];
+        }
+      }
+      float sum[2][2] = {};                                                // tokens g, g + 8, g + 16, g + 24, of this lane's columns
+      if (groups > 0 && j0 + 32 > it.lo) {
+        kv_ready_key_scales<FMT, D>(ring_p + (stage - ring) + C::K_BYTES, lane, room);
+        __syncwarp();
+#pragma unroll 1
+        for (int u0 = 0; u0 < 2; u0 += TILES) {
+          uint32_t keys[TILES][CH][2][4], scale[TILES][2][CH];
+          float part[TILES][2] = {};
+#pragma unroll
+          for (int u = 0; u < TILES; ++u) {
+            kv_key_scales<FMT, D>(room, 16 * (u0 + u) + g, t, scale[u][0]);
+            kv_key_scales<FMT, D>(room, 16 * (u0 + u) + g + 8, t, scale[u][1]);
+#pragma unroll
+            for (int c2 = 0; c2 < CH; c2 += 2) {
+              uint32_t raw[4];
+              ldmatrix_x4(stage + 16 * kv_swizzled<D>(16 * (u0 + u) + row_of, c2 + chunk_of), raw);
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                kv_key_pairs<FMT>(raw[x], keys[u][c2 + x / 2][x & 1]);
+                if constexpr (FMT == FMT_NVFP4) {
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) keys[u][c2 + x / 2][x & 1][i] = mul_f16x2(keys[u][c2 + x / 2][x & 1][i], scale[u][x & 1][c2 + x / 2]);
+                }
+              }
+            }
+          }
+#pragma unroll 1
+          for (int n = 0; n < groups; ++n) {
+            if (groups > 1) load_rows(n);
+            const bool border = j0 < all_lo || j0 + 32 > all_hi;
+#pragma unroll
+            for (int u = 0; u < TILES; ++u) {
+              float s[4] = {};
+              const float zero[4] = {};
+#pragma unroll
+              for (int ch = 0; ch < CH; ++ch) {
+                const uint32_t(&x)[2][4] = keys[u][ch];
+                if constexpr (FMT == FMT_NVFP4) {
+                  mma_f16(s, x[0][0], x[1][0], x[0][1], x[1][1], q[0].q[ch][0], q[0].q[ch][1], s);
+                  mma_f16(s, x[0][2], x[1][2], x[0][3], x[1][3], q[0].q[ch][2], q[0].q[ch][3], s);
+                } else {
+                  float y[4];
+                  mma_f16(y, x[0][0], x[1][0], x[0][1], x[1][1], q[0].q[ch][0], q[0].q[ch][1], zero);
+                  mma_f16(y, x[0][2], x[1][2], x[0][3], x[1][3], q[0].q[ch][2], q[0].q[ch][3], y);
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) s[i] = fmaf(y[i], __uint_as_float(scale[u][i >> 1][ch]), s[i]);
+                }
+              }
+              if (special || border) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const int e = i & 1, j = j0 + 16 * (u0 + u) + g + 8 * (i >> 1);
+                  float x = s[i] * factor[e];
+                  if (special) x = kv_score(x * kLn2, a.softcap, slope[e], abs(place[e] - j));
+                  part[u][i >> 1] += j >= lo[e] && j < hi[e] ? ex2(x + off[e]) : 0.f;
+                }
+              } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) part[u][i >> 1] += ex2(fmaf(s[i], factor[i & 1], off[i & 1]));
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            if (TILES == 2 || u0 == 0) sum[0][i] = part[0][i];
+            if (TILES == 2 || u0 == 1) sum[1][i] = part[TILES - 1][i];
+          }
+        }
+      }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum[i >> 1][i & 1] += __shfl_xor_sync(0xFFFFFFFFu, sum[i >> 1][i & 1], o);
+      const float own = t & 2 ? (t & 1 ? sum[1][1] : sum[1][0]) : (t & 1 ? sum[0][1] : sum[0][0]);         // token g + 8 t
+      const float w = __shfl_sync(0xFFFFFFFFu, own, (lane & 7) * 4 + (lane >> 3));
+      if (slot >= 0) weights_out[slot] = old + w;
+      stage = stage == ring + (C::STAGES - 1) * C::STAGE ? ring : stage + C::STAGE;
+    }
+    cp_async_wait<0>();
+    __syncwarp();
   }
 }
 

@@ -106,10 +106,10 @@ __device__ __forceinline__ void kv_value_pairs(uint32_t u, uint32_t (&o)[4]) {
   if constexpr (FMT == FMT_MXINT4) {
     int4_pairs(u, o);
   } else {
-    const uint32_t x = u & 0x0F0F0F0Fu, y = (u >> 4) & 0x0F0F0F0Fu;      // codes 0, 2 and 1, 3 of both, a byte each
-    const uint32_t even = x | (x >> 12), odd = y | (y >> 12);            // low two bytes: both tokens' code in one byte
+    // byte 2 gets code 0 (odd: code 1) of both tokens, byte 3 code 2 (3); by products, since shifts run where the conversions do
+    const uint32_t even = (u & 0x0F0F0F0Fu) * 0x00010010u, odd = (u & 0xF0F0F0F0u) * 0x00001001u;
     asm("{\n\t.reg .b8 b0, b1, b2, b3, c0, c1, c2, c3;\n\tmov.b32 {b0, b1, b2, b3}, %4;\n\tmov.b32 {c0, c1, c2, c3}, %5;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\tcvt.rn.f16x2.e2m1x2 %1, c0;\n\tcvt.rn.f16x2.e2m1x2 %2, b1;\n\tcvt.rn.f16x2.e2m1x2 %3, c1;\n\t}"
+        "cvt.rn.f16x2.e2m1x2 %0, b2;\n\tcvt.rn.f16x2.e2m1x2 %1, c2;\n\tcvt.rn.f16x2.e2m1x2 %2, b3;\n\tcvt.rn.f16x2.e2m1x2 %3, c3;\n\t}"
         : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]) : "r"(even), "r"(odd));
   }
 }
@@ -128,12 +128,63 @@ __device__ __forceinline__ void kv_scale_words(const uint8_t* p, uint32_t (&w)[(
     w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
   }
 }
-// Byte `i` of the words as the exponent of a float32: 2^(byte - 127), zero for byte 0.
-__device__ __forceinline__ float e8m0_float(const uint32_t* words, int i) {
-  const uint32_t w = words[i / 4];
-  const int at = 8 * (i % 4);
-  return __uint_as_float((at < 24 ? w << (23 - at) : w >> 1) & 0x7F800000u);
+// Scales are made ready once per token, by the lane that has its number, instead of by every lane that needs them (eight for a value's, four for a
+// key's), and kept beside the ring.  Keys: float32 per chunk; NVFP4: a pair of equal float16 per block, the blocks of even and of odd
+// number apart (lane (g, t) needs block 2 c + t / 2).  Values: float16, tokens in the order 0 1 8 9 2 3 10 11 ... of every sixteen: the pairs that a
+// lane needs lie together.
+template <int FMT, int D>
+struct KvScaleRoom {
+  static constexpr int CH = D / 32, SB = D / kv_block(FMT);
+  static constexpr int KEYS = 32 * SB * 4, VALUES = 32 * SB * 2, BYTES = KEYS + VALUES;
+};
+template <int N>
+__device__ __forceinline__ void store_words(uint8_t* p, const uint32_t* w) {
+  if constexpr (N == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
 }
+template <int N>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
+  if constexpr (N == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+    const uint4 v = *reinterpret_cast<const uint4*>(p);
+    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+  }
+}
+// The scale bytes of key `token` of the 32 (E8M0 byte 0 counts as zero).
+template <int FMT, int D>
+__device__ __forceinline__ void kv_ready_key_scales(const uint8_t* scales, int token, uint8_t* room) {
+  constexpr int CH = D / 32, SB = D / kv_block(FMT), V = CH < 4 ? CH : 4;
+  uint32_t w[(SB + 3) / 4];
+  kv_scale_words<SB>(scales + token * SB, w);
+  uint32_t even[CH], odd[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if constexpr (FMT == FMT_NVFP4) {
+      const uint32_t f = e4m3x2_f16x2(w[c / 2] >> (16 * (c & 1)));
+      even[c] = __byte_perm(f, 0, 0x1010);
+      odd[c] = __byte_perm(f, 0, 0x3232);
+    } else {
+      const int at = 8 * (c % 4);
+      even[c] = (at < 24 ? w[c / 4] << (23 - at) : w[c / 4] >> 1) & 0x7F800000u;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < CH; c += V) {
+    store_words<V>(room + (c / V * 32 + token) * (4 * V), even + c);
+    if constexpr (FMT == FMT_NVFP4) store_words<V>(room + KvScaleRoom<FMT, D>::KEYS / 2 + (c / V * 32 + token) * (4 * V), odd + c);
+  }
+}
+// ... as lane t needs them.
+template <int FMT, int D>
+__device__ __forceinline__ void kv_key_scales(const uint8_t* room, int token, int t, uint32_t (&f)[D / 32]) {
+  constexpr int CH = D / 32, V = CH < 4 ? CH : 4;
+  if (FMT == FMT_NVFP4) room += (t >> 1) * (KvScaleRoom<FMT, D>::KEYS / 2);
+#pragma unroll
+  for (int c = 0; c < CH; c += V) load_words<V>(room + (c / V * 32 + token) * (4 * V), f + c);
+}
+__device__ __forceinline__ int kv_value_order(int token) { return (token & 16) | (token & 6) << 1 | (token & 8) >> 2 | (token & 1); }
 
 // The queries' operand of a warp: lane (g, t) holds of row g the elements 32 c + 8 t ... + 7 of every chunk, as four registers.
 template <int D>
@@ -173,15 +224,15 @@ __device__ __forceinline__ float kv_load_query(const __nv_bfloat16* p, int t, Kv
   return __uint_as_float((254u - field) << 23);
 }
 
-// Scores of 16 cached tokens (rows first_row ... of the tile at `keys`, scale bytes at `scales`) with NT groups of eight queries:
+// Scores of 16 cached tokens (rows first_row ... of the tile at `keys`, their scales made ready in `room`) with NT groups of eight queries:
 // s[n][0, 1] token g, queries 2t and 2t + 1 of group n; s[n][2, 3] token g + 8.
 template <int FMT, int D, int NT>
-__device__ __forceinline__ void kv_tile_scores(uint32_t keys, const uint8_t* scales, int first_row, int lane, const KvQuery<D> (&q)[NT], float (&s)[NT][4]) {
-  constexpr int CH = D / 32, SB = D / kv_block(FMT);
+__device__ __forceinline__ void kv_tile_scores(uint32_t keys, const uint8_t* room, int first_row, int lane, const KvQuery<D> (&q)[NT], float (&s)[NT][4]) {
+  constexpr int CH = D / 32;
   const int g = lane >> 2, t = lane & 3;
-  uint32_t w0[(SB + 3) / 4], w1[(SB + 3) / 4];
-  kv_scale_words<SB>(scales + (first_row + g) * SB, w0);
-  kv_scale_words<SB>(scales + (first_row + g + 8) * SB, w1);
+  uint32_t fa[CH], fb[CH];
+  kv_key_scales<FMT, D>(room, first_row + g, t, fa);
+  kv_key_scales<FMT, D>(room, first_row + g + 8, t, fb);
   const float zero[4] = {};
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -198,12 +249,10 @@ __device__ __forceinline__ void kv_tile_scores(uint32_t keys, const uint8_t* sca
       kv_key_pairs<FMT>(raw[2 * e], a);
       kv_key_pairs<FMT>(raw[2 * e + 1], b);
       if constexpr (FMT == FMT_NVFP4) {
-        const uint32_t pick = t & 2 ? 0x3232u : 0x1010u;
-        const uint32_t fa = __byte_perm(e4m3x2_f16x2(w0[c / 2] >> (16 * (c & 1))), 0, pick), fb = __byte_perm(e4m3x2_f16x2(w1[c / 2] >> (16 * (c & 1))), 0, pick);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          a[i] = mul_f16x2(a[i], fa);
-          b[i] = mul_f16x2(b[i], fb);
+          a[i] = mul_f16x2(a[i], fa[c]);
+          b[i] = mul_f16x2(b[i], fb[c]);
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -211,16 +260,15 @@ __device__ __forceinline__ void kv_tile_scores(uint32_t keys, const uint8_t* sca
           mma_f16(s[n], a[2], b[2], a[3], b[3], q[n].q[c][2], q[n].q[c][3], s[n]);
         }
       } else {
-        const float fa = e8m0_float(w0, c), fb = e8m0_float(w1, c);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
           float x[4];
           mma_f16(x, a[0], b[0], a[1], b[1], q[n].q[c][0], q[n].q[c][1], zero);
           mma_f16(x, a[2], b[2], a[3], b[3], q[n].q[c][2], q[n].q[c][3], x);
-          s[n][0] += x[0] * fa;
-          s[n][1] += x[1] * fa;
-          s[n][2] += x[2] * fb;
-          s[n][3] += x[3] * fb;
+          s[n][0] += x[0] * __uint_as_float(fa[c]);
+          s[n][1] += x[1] * __uint_as_float(fa[c]);
+          s[n][2] += x[2] * __uint_as_float(fb[c]);
+          s[n][3] += x[3] * __uint_as_float(fb[c]);
         }
       }
     }
