@@ -7,6 +7,7 @@
 #include "kv_attention.cuh"
 #include "kv_cache.cuh"
 #include "kv_evict.cuh"
+#include "kv_prefill.cuh"
 
 namespace torq {
 
@@ -150,6 +151,21 @@ static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, c
   return launch_status();
 }
 
+// ---- many queries per sequence
+template <int FMT, int D>
+static torq_status prefill_launch(const KvView& v, const KvScoring& a, int sms, const void* Q, int64_t q_stride, int heads, void* out, float* lse,
+                                  cudaStream_t s) {
+  using C = KvPrefillCfg<FMT, D>;
+  constexpr auto kernel = kv_prefill_kernel<C>;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return TORQ_ERR_LAUNCH;
+  launch_tc(kernel, 1, dim3((unsigned)sms), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads,
+            static_cast<__nv_bfloat16*>(out), lse);
+  return launch_status();
+}
+static bool many_rows(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads) {
+  return tokens / batch * (heads / kv_heads) >= 64;
+}
+
 template <int FMT>
 static torq_status attention_impl(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
                                   const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
@@ -167,9 +183,10 @@ static torq_status attention_impl(const torq_kv_cache* cache, const torq_kv_scor
   int sms;
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
   cudaStream_t stm = static_cast<cudaStream_t>(stream);
-  const bool one = decode_groups(tokens, cache->batch, heads, v.heads) == 1;
+  const bool one = decode_groups(tokens, cache->batch, heads, v.heads) == 1, many = many_rows(tokens, cache->batch, heads, v.heads);
   with_dim(v.dim, [&](auto D) {
-    rc = one ? decode_launch<FMT, decltype(D)::value, 1>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm)
+    rc = many ? prefill_launch<FMT, decltype(D)::value>(v, a, sms, Q, q_stride, (int)heads, out, lse, stm)
+         : one ? decode_launch<FMT, decltype(D)::value, 1>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm)
              : decode_launch<FMT, decltype(D)::value, 2>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
   });
   return rc;
