@@ -14,33 +14,6 @@ namespace torq {
 
 enum : int { RES_NONE = 0, RES_BF16 = 1, RES_F32 = 2 };
 
-// Two float32 in a 64-bit register: one instruction for both, each rounded by itself as the scalar one.
-__device__ __forceinline__ uint64_t pair_of(uint32_t lo, uint32_t hi) {
-  uint64_t p;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "r"(lo), "r"(hi));
-  return p;
-}
-__device__ __forceinline__ uint64_t pair_of(float v) { return pair_of(__float_as_uint(v), __float_as_uint(v)); }
-__device__ __forceinline__ float2 halves(uint64_t p) {
-  uint32_t lo, hi;
-  asm("mov.b64 {%0, %1}, %2;" : "=r"(lo), "=r"(hi) : "l"(p));
-  return make_float2(__uint_as_float(lo), __uint_as_float(hi));
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
 // Eight bfloat16 <-> four pairs of float32.
 __device__ __forceinline__ void bf16x8_to_pairs(const uint4& a, uint64_t (&v)[4]) {
   const uint32_t w[4] = {a.x, a.y, a.z, a.w};

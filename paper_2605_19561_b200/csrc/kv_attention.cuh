@@ -17,6 +17,8 @@ struct KvScoring {
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// Weights are exp2(x - m + kShift), m raised when a score exceeds it by kSlack: in float16 they are at most 2^15, and those of 2^-14 - kShift keep 11 bits.
+constexpr float kShift = 10.f, kSlack = 5.f;
 
 // The range [lo, hi) of cached tokens that row `i`, place p of sequence b with `length` tokens, sees.
 __device__ __forceinline__ void kv_range(const KvScoring& a, int b, int i, int p, int length, int& lo, int& hi) {
@@ -46,8 +48,8 @@ __device__ __forceinline__ float kv_score(float x, float softcap, float slope, i
 // ring of its own filled by cp.async: there is no barrier in the kernel.  (Ranges for CTAs of four warps that share an item and meet at its end:
 // 32 sequences of up to 8192 tokens 73.6 us, SMs idle for a quarter of it, since a CTA with more items in its range took longer.)
 //
-// A warp keeps a maximum m of its scores in powers of two that is raised only when a score exceeds it by 3, so weights are exp2(x - m + 12) <= 2^15 in
-// float16; they keep 11 bits down to 2^-26 of the largest.  The same goes for the values' scales (see kv_fragments.cuh).
+// A warp keeps a maximum m of its scores in powers of two that is raised only when a score exceeds it by 5, so weights are exp2(x - m + 10) <= 2^15 in
+// float16; they keep 11 bits down to 2^-24 of the largest.  The same goes for the values' scales (see kv_fragments.cuh).
 template <int FMT_, int D_, int NT_>
 struct KvDecodeCfg {
   static constexpr int FMT = FMT_, D = D_, NT = NT_;
@@ -368,7 +370,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           most[e] = fmaxf(fmaxf(s[0][n][e], s[0][n][e + 2]), fmaxf(s[1][n][e], s[1][n][e + 2])) * f[e];
-          raise |= most[e] > m[n][e] + 3.f;
+          raise |= most[e] > m[n][e] + kSlack;
         }
         if (__any_sync(0xFFFFFFFFu, raise)) {
 #pragma unroll
@@ -386,7 +388,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
             }
           }
         }
-        const float off[2] = {12.f - m[n][0], 12.f - m[n][1]};
+        const float off[2] = {kShift - m[n][0], kShift - m[n][1]};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -461,7 +463,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
           part[ROWS * D + r] = m[n][e];
           part[ROWS * D + ROWS + r] = l[n][e];
         } else if (lse) {
-          lse[row] = l[n][e] > 0.f ? (m[n][e] - 12.f + log2f(l[n][e])) * kLn2 : -INFINITY;
+          lse[row] = l[n][e] > 0.f ? (m[n][e] - kShift + log2f(l[n][e])) * kLn2 : -INFINITY;
         }
       }
   }
@@ -580,7 +582,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
   const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
   for (int e = 0; e < EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
-  if (lse && lane == 0) lse[row] = l > 0.f ? (m - 12.f + log2f(l)) * kLn2 : -INFINITY;
+  if (lse && lane == 0) lse[row] = l > 0.f ? (m - kShift + log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ---- the account ------------------------------------------------------------------------------------------------------------------------------

@@ -5,15 +5,17 @@
 //   O += P V         P from tensor memory, V from shared memory
 // Keys and values are widened to float16 once per CTA and tile, whatever the number of rows: codes are exact there, with the scales as follows.
 // NVFP4: code times E4M3 scale, exact.  MXFP4, MXINT4: code times 2^(e - E + 12), E the largest exponent in the tile (keys and values apart), exact for
-// scales down to 2^-35 of that; 2^E of the keys goes into the scores' factor, that of the values into the weights: P = exp2(x - m + 12 + E - E_max), E_max the
+// scales down to 2^-35 of that; 2^E of the keys goes into the scores' factor, that of the values into the weights: P = exp2(x - m + 10 + E - E_max), E_max the
 // largest E so far, so a tile with smaller values has smaller weights.  What is summed for the softmax does not have it.
 //
 // Warp-specialised, one CTA per SM, persistent over the items (sequence, head, tiles of rows):
 //   warps 0 - 3, 4 - 7   softmax of the first and second tile, a row to each thread: loads its query, keeps maximum and sum, corrects O when the maximum has
-//                        grown by more than 2^3 (seldom), writes the result
-//   warps 8 - 11         cached tokens: cp.async of the codes one tile ahead, widening into a ring of three tiles (K, V, K, ...)
-//   warp 12              issues the products: for every tile of tokens P V of the one before and then the next S, of the first tile of rows, then of the
-//                        second, so that one tile's softmax runs beside the other's products
+//                        grown by more than 2^5 (seldom), writes the result
+//   warps 8 - 11         cached tokens: codes 128 tokens ahead in registers, widened into a ring of tiles of 64 (K, K, V, V, ...)
+//   warps 12, 13         issue the products of the first and second tile: P V of a tile of tokens and then S of the one after the next
+// Each tile of rows has two buffers for S, so its softmax goes from one tile of tokens to the next without waiting for the products of its own weights.
+// (One buffer and tiles of 128 tokens: a softmax of 2600 cycles, then its products' 1400, then the next; 327 to 391 us for 2048 tokens behind 6144,
+// whether one thread had a row or two, whether one warp issued the products or two.)
 #pragma once
 #include "kv_attention.cuh"
 
@@ -21,17 +23,23 @@ namespace torq {
 
 template <int FMT_, int D_>
 struct KvPrefillCfg {
-  static constexpr int FMT = FMT_, D = D_, TILES = D == 256 ? 1 : 2, ROWS = 128 * TILES, TOK = D == 256 ? 64 : 128;
-  static constexpr int CH = D / 32, SB = D / kv_block(FMT), THREADS = 416, GROUPS = TOK / 16;
-  static constexpr int Q_BYTES = 128 * D * 2, KV_BYTES = TOK * D * 2, STAGES = 3;
-  static constexpr int CODES = TOK * D / 2, SCALES = TOK * SB, RAW = 2 * (CODES + SCALES);
-  static constexpr int RAW_AT = TILES * Q_BYTES + STAGES * KV_BYTES, INFO_AT = RAW_AT + 2 * RAW, SMEM = INFO_AT + 512 + 1024;
+  static constexpr int FMT = FMT_, D = D_, TILES = D == 256 ? 1 : 2, ROWS = 128 * TILES, TOK = 64;
+  static constexpr int CH = D / 32, SB = D / kv_block(FMT), THREADS = 512;
+  static constexpr int Q_BYTES = 128 * D * 2, KV_BYTES = TOK * D * 2, STAGES = D == 256 ? 5 : 8;
+  static constexpr int INFO_AT = TILES * Q_BYTES + STAGES * KV_BYTES, SMEM = INFO_AT + 256 + 1024;
   static constexpr int O_COL = 256;
   static_assert(SMEM <= 232448, "shared memory");
 };
 // kind::f16 with float16 operands, as idesc_bf16.
 __host__ __device__ constexpr uint32_t idesc_f16(int M, int N, bool a_mn_major, bool b_mn_major) {
   return idesc_bf16(M, N, a_mn_major, b_mn_major) & ~((1u << 7) | (1u << 10));
+}
+
+// The larger of three.
+__device__ __forceinline__ float max3(float x, float y, float z) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
+  return r;
 }
 
 struct KvPrefillItem {
@@ -79,7 +87,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
                                                                    __nv_bfloat16* out, float* lse) {
   constexpr int FMT = C::FMT, D = C::D, CH = C::CH, SB = C::SB, TOK = C::TOK;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t bars[16];
+  __shared__ __align__(8) uint64_t bars[2 * C::STAGES + 10];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -87,26 +95,25 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
   volatile int* cta_abort = &abort_flag;
   const uint32_t bar = smem_u32(bars);
   auto kv_full = [&](uint32_t i) { return bar + 8 * (i % C::STAGES); };
-  auto kv_empty = [&](uint32_t i) { return bar + 24 + 8 * (i % C::STAGES); };
-  auto s_full = [&](int t) { return bar + 48 + 8 * t; };
-  auto p_full = [&](int t) { return bar + 64 + 8 * t; };
-  auto q_full = [&](int t) { return bar + 80 + 8 * t; };
-  auto o_full = [&](int t) { return bar + 96 + 8 * t; };
+  auto kv_empty = [&](uint32_t i) { return bar + 8 * (C::STAGES + i % C::STAGES); };
+  auto s_full = [&](int t, int buffer) { return bar + 8 * (2 * C::STAGES + 2 * t + buffer); };
+  auto p_full = [&](int t, int buffer) { return bar + 8 * (2 * C::STAGES + 4 + 2 * t + buffer); };
+  auto q_full = [&](int t) { return bar + 8 * (2 * C::STAGES + 8 + t); };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = heads / c.heads;
-  volatile int* tile_top = reinterpret_cast<volatile int*>(smem_p + C::INFO_AT);                   // [4][2]: E of the keys and of the values
-  int64_t* page_at = reinterpret_cast<int64_t*>(smem_p + C::INFO_AT + 64);                         // [2][GROUPS], -1: nothing there
-  int* warp_top = reinterpret_cast<int*>(smem_p + C::INFO_AT + 64 + 2 * 8 * C::GROUPS);            // [2][4][2]
+  volatile int* tile_top = reinterpret_cast<volatile int*>(smem_p + C::INFO_AT);                   // [8][2]: E of the keys and of the values of 128 tokens
+  int* warp_top = reinterpret_cast<int*>(smem_p + C::INFO_AT + 64);                                // [2][4][2]
 
   if (tid == 0) {
     for (int i = 0; i < C::STAGES; ++i) {
       mbar_init(bar + 8 * i, 128);
-      mbar_init(bar + 24 + 8 * i, 1);
+      mbar_init(bar + 8 * (C::STAGES + i), C::TILES);
     }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(s_full(t), 1);
-      mbar_init(p_full(t), 128);
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(s_full(t, i), 1);
+        mbar_init(p_full(t, i), 128);
+      }
       mbar_init(q_full(t), 128);
-      mbar_init(o_full(t), 1);
     }
     abort_flag = 0;
     fence_mbar_init();
@@ -144,21 +151,27 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         for (int i = 0; i < count; ++i) nothing(first + i);
       }
 
-    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, s_at = tmem + lanes + t * TOK, o_at = tmem + lanes + C::O_COL + t * D;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, o_at = tmem + lanes + C::O_COL + t * D;
     const bool special = a.softcap > 0.f || a.slopes;
-    uint32_t s_count = 0, o_count = 0, tile_no = 0;
+    uint32_t phases[2] = {0, 0}, group_no = 0;                             // of s_full; of 128 tokens, over all items
     bool ok = true;
     for (long long index = blockIdx.x; ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
-      const uint32_t first_tile = tile_no;
-      tile_no += it.tiles;
+      const uint32_t first_group = group_no;
+      group_no += (it.tiles + 1) / 2;
       if (128 * t >= it.rows) continue;
+      // S of tile k, or what comes after the last ones, is number k of its item on s_full: at k it is there, and P V of tile k - 2 is done
+      auto wait_s = [&](int k) {
+        ok = ok && mbar_wait_warp(s_full(t, k & 1), (phases[k & 1] + (k >> 1)) & 1, cta_abort, c.err_word, SITE_EPI_ACC_FULL);
+        return ok;
+      };
       const int rr = it.first_row + 128 * t + row;
       const bool there = 128 * t + row < it.rows;
-      const int token = it.first_token + rr / group, h = it.head * group + rr % group, place = it.length - it.count + rr / group;
-      int lo = 0, hi = 0;
+      int lo = 0, hi = 0, place;
       float factor, slope = 0.f;
       {
         // the query: float16 times a power of two, as kv_load_query
+        const int token = it.first_token + rr / group, h = it.head * group + rr % group;
+        place = it.length - it.count + rr / group;
         const __nv_bfloat16* p = Q + token * q_stride + h * D;
         uint32_t top = 0;
 #pragma unroll 4
@@ -195,17 +208,17 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
 
       float m = -1e30f, l = 0.f;
       int e_max = 27;
-      for (int k = 0; k < it.tiles; ++k, ++s_count) {
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(s_full(t), s_count & 1, cta_abort, c.err_word, SITE_EPI_ACC_FULL));
-        if (!ok) break;
+      for (int k = 0; k < it.tiles; ++k) {
+        if (!wait_s(k)) break;
         tc_fence_after_sync();
         const int j0 = it.base + k * TOK;
-        const bool masked = __any_sync(0xFFFFFFFFu, there && (j0 < lo || j0 + TOK > hi));
+        const uint32_t s_at = tmem + lanes + (2 * t + (k & 1)) * TOK;
         float f = factor;
         int e_tile = 27;
         if constexpr (FMT != FMT_NVFP4) {
-          f *= __uint_as_float((uint32_t)(tile_top[2 * ((first_tile + k) & 3)] - 12) << 23);
-          e_tile = tile_top[2 * ((first_tile + k) & 3) + 1];
+          const volatile int* tops = tile_top + 2 * ((first_group + (k >> 1)) & 7);
+          f *= __uint_as_float((uint32_t)(tops[0] - 12) << 23);
+          e_tile = tops[1];
         }
         auto score = [&](float s, int col) {                               // where there is more to a score than its factor
           const int j = j0 + col;
@@ -213,127 +226,120 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           if (special) x = kv_score(x * kLn2, a.softcap, slope, abs(place - j));
           return j >= lo && j < hi ? x : -INFINITY;
         };
-        const bool slow = masked || special;
-        // Two buffers, so that a load from tensor memory runs beside the work on the one before.  What is seldom needed has loops of its own: in
-        // one loop with the plain case it made the warps wait for instructions (2048 tokens behind 6144: 1530 us).
-        uint32_t va[32], vb[32];
-        float top = -INFINITY;
-        if (!slow) {
-          float top2 = -INFINITY;
-          tmem_ld_32x32(s_at, va);
-#pragma unroll 1
-          for (int x = 0; x < TOK; x += 64) {
-            tmem_ld_wait();
-            tmem_ld_32x32(s_at + x + 32, vb);
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              top = fmaxf(top, __uint_as_float(va[i]));
-              top2 = fmaxf(top2, __uint_as_float(va[i + 1]));
-            }
-            tmem_ld_wait();
-            if (x + 64 < TOK) tmem_ld_32x32(s_at + x + 64, va);
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              top = fmaxf(top, __uint_as_float(vb[i]));
-              top2 = fmaxf(top2, __uint_as_float(vb[i + 1]));
-            }
-          }
-          top = fmaxf(top, top2) * f;
-        } else {
-#pragma unroll 1
-          for (int x = 0; x < TOK; x += 32) {
-            tmem_ld_32x32(s_at + x, va);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) top = fmaxf(top, score(__uint_as_float(va[i]), x + i));
-          }
-        }
-        float fix = 1.f;
-        __syncwarp();
-        if (top > m + 3.f) {
-          fix = ex2(m - top);
-          m = top;
-          l *= fix;
-        }
-        if (e_tile > e_max) {
-          fix *= e_tile - e_max > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (e_tile - e_max)) << 23);
-          e_max = e_tile;
-        }
-        if (k > 0 && __any_sync(0xFFFFFFFFu, fix != 1.f)) {
-#pragma unroll 1
-          for (int x = 0; x < D; x += 16) {
-            uint32_t w[16];
-            tmem_ld_32x32_x16(o_at + x, w);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * fix);
-            tmem_st_32x32_x16(o_at + x, w);
-          }
-        }
+        const bool slow = special || __any_sync(0xFFFFFFFFu, there && (j0 < lo || j0 + TOK > hi));
+        const int e_old = e_max;
+        e_max = max(e_max, e_tile);
         const int down = e_max - e_tile;                                   // this tile's values are smaller: so are its weights
         const bool faint = down > 40;                                      // too small to matter, but they count in the sum
-        const float off = 12.f - m - (faint ? 0.f : (float)down);
-        float sum = 0.f, sum2 = 0.f;
-        if (!slow) {
-          auto weigh = [&](const uint32_t (&v)[32], int x) {
-            uint32_t w[16];
+        float fix = e_max - e_old > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (e_max - e_old)) << 23);      // of O
+        const float off0 = kShift - (faint ? 0.f : (float)down);
+        auto raised = [&](float top) {                                     // m is no longer near enough to the largest score
+          if (top <= m + kSlack) return;
+          const float old = ex2(m - top);
+          m = top;
+          l *= old;
+          fix *= old;
+        };
+        // In one pass with the maximum so far; a second one where a score turns out to exceed it by too much (the first tiles).  P stays in
+        // registers until it may take the place of S.  What is seldom needed has loops of its own: in one loop with the plain case it
+        // made the warps wait for instructions (1530 us).
+        uint32_t w[2][16];
+        float sum = 0.f, top = -INFINITY;
+        auto weigh = [&]() {
+          const uint64_t f2 = pair_of(f), off2 = pair_of(off0 - m);
+          uint64_t sums = 0;
+          float tops[2] = {-INFINITY, -INFINITY};
+          uint32_t v[2][32];
+          tmem_ld_32x32(s_at, v[0]);
+          tmem_ld_wait();
+          tmem_ld_32x32(s_at + 32, v[1]);
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            if (x) tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              const float p = ex2(fmaf(__uint_as_float(v[i]), f, off)), p2 = ex2(fmaf(__uint_as_float(v[i + 1]), f, off));
-              sum += p;
-              sum2 += p2;
-              w[i / 2] = pack_f16(p, p2);
+              tops[i / 2 & 1] = max3(tops[i / 2 & 1], __uint_as_float(v[x][i]), __uint_as_float(v[x][i + 1]));
+              const float2 z = halves(fma2(pair_of(v[x][i], v[x][i + 1]), f2, off2));
+              const float p = ex2(z.x), p2 = ex2(z.y);
+              sums = add2(sums, pair_of(__float_as_uint(p), __float_as_uint(p2)));
+              w[x][i / 2] = pack_f16(p, p2);
             }
-            if (faint) {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) w[i] = 0;
-            }
-            tmem_st_32x32_x16(s_at + x / 2, w);
-          };
-          tmem_ld_32x32(s_at, va);
-#pragma unroll 1
-          for (int x = 0; x < TOK; x += 64) {
-            tmem_ld_wait();
-            tmem_ld_32x32(s_at + x + 32, vb);
-            weigh(va, x);
-            tmem_ld_wait();
-            if (x + 64 < TOK) tmem_ld_32x32(s_at + x + 64, va);
-            weigh(vb, x + 32);
+          }
+          sum = halves(sums).x + halves(sums).y;
+          top = fmaxf(tops[0], tops[1]) * f;
+        };
+        if (!slow) {
+          weigh();
+          if (__any_sync(0xFFFFFFFFu, top > m + kSlack)) {
+            raised(top);
+            __syncwarp();
+            weigh();
           }
         } else {
 #pragma unroll 1
           for (int x = 0; x < TOK; x += 32) {
-            tmem_ld_32x32(s_at + x, va);
+            uint32_t v[32];
+            tmem_ld_32x32(s_at + x, v);
             tmem_ld_wait();
-            uint32_t w[16];
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-              const float p = ex2(score(__uint_as_float(va[i]), x + i) + off), p2 = ex2(score(__uint_as_float(va[i + 1]), x + i + 1) + off);
-              sum += p;
-              sum2 += p2;
-              w[i / 2] = faint ? 0u : pack_f16(p, p2);
-            }
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, score(__uint_as_float(v[i]), x + i));
             __syncwarp();
-            tmem_st_32x32_x16(s_at + x / 2, w);
+          }
+          raised(top);
+          __syncwarp();
+        }
+        if (k > 0 && __any_sync(0xFFFFFFFFu, fix != 1.f)) {
+          if (!wait_s(k + 1)) break;                                       // the products of the tile before are done
+          tc_fence_after_sync();
+#pragma unroll 1
+          for (int x = 0; x < D; x += 16) {
+            uint32_t v[16];
+            tmem_ld_32x32_x16(o_at + x, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * fix);
+            tmem_st_32x32_x16(o_at + x, v);
           }
         }
-        sum += sum2;
+        if (slow) {
+          sum = 0.f;
+#pragma unroll 1
+          for (int x = 0; x < TOK; x += 32) {
+            uint32_t v[32], y[16];
+            tmem_ld_32x32(s_at + x, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+              const float p = ex2(score(__uint_as_float(v[i]), x + i) + (off0 - m)), p2 = ex2(score(__uint_as_float(v[i + 1]), x + i + 1) + (off0 - m));
+              sum += p + p2;
+              y[i / 2] = faint ? 0u : pack_f16(p, p2);
+            }
+            __syncwarp();
+            tmem_st_32x32_x16(s_at + x / 2, y);
+          }
+        } else {
+          if (faint) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) w[i / 16][i % 16] = 0;
+          }
+          tmem_st_32x32_x16(s_at, w[0]);
+          tmem_st_32x32_x16(s_at + 16, w[1]);
+        }
         l += sum * (faint ? 1.f : __uint_as_float((uint32_t)(127 + down) << 23));
         tmem_st_wait();
         tc_fence_before_sync();
-        mbar_arrive(p_full(t));
+        mbar_arrive(p_full(t, k & 1));
       }
-      if (!ok) break;
-      ok = __all_sync(0xFFFFFFFFu, mbar_wait(o_full(t), o_count & 1, cta_abort, c.err_word, SITE_EPI_ACC_FULL));
-      ++o_count;
-      if (!ok) break;
+      if (!ok || !wait_s(it.tiles + 1)) break;
+      phases[0] += (it.tiles + 3) / 2;
+      phases[1] += (it.tiles + 2) / 2;
       tc_fence_after_sync();
       const float inv = (l > 0.f ? 1.f / l : 0.f) * (FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(e_max - 12) << 23));
-      const int64_t to = (int64_t)token * heads + h;
+      const int64_t to = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
 #pragma unroll 1
       for (int x = 0; x < D; x += 16) {
-        uint32_t w[16];
-        tmem_ld_32x32_x16(o_at + x, w);
+        uint32_t v[16];
+        tmem_ld_32x32_x16(o_at + x, v);
         tmem_ld_wait();
 #pragma unroll
         for (int e = 0; e < 16; e += 8) {
@@ -341,187 +347,186 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
 #pragma unroll
           for (int i = 0; i < 4; ++i) {                                    // MXINT4: the elements lie in the order of kv_query_order
             constexpr auto column = [](int el) { return FMT == FMT_MXINT4 ? (el < 4 ? 2 * el : 2 * (el - 4) + 1) : el; };
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"((&y.x)[i]) : "f"(__uint_as_float(w[e + column(2 * i + 1)]) * inv),
-                "f"(__uint_as_float(w[e + column(2 * i)]) * inv));
+            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"((&y.x)[i]) : "f"(__uint_as_float(v[e + column(2 * i + 1)]) * inv),
+                "f"(__uint_as_float(v[e + column(2 * i)]) * inv));
           }
           if (there) *reinterpret_cast<uint4*>(out + to * D + x + e) = y;
         }
         __syncwarp();
       }
-      if (there && lse) lse[to] = l > 0.f ? (m - 12.f + log2f(l)) * kLn2 : -INFINITY;
+      if (there && lse) lse[to] = l > 0.f ? (m - kShift + log2f(l)) * kLn2 : -INFINITY;
       tc_fence_before_sync();
     }
   } else if (warp < 12) {
     // ------------------------------------------------------------------ cached tokens
-    // The named barriers are executed by every one of these threads for every tile, also after a wait has given up, so that no warp is left in one.
+    // In groups of two tiles, 128 tokens, keys before values.  A thread takes every 128th chunk of 16 bytes (32 codes of a token), with its scale byte, from
+    // global memory into registers, the next group's while it widens this one's.  The named barrier is executed by every one of these threads for
+    // every group, also after a wait has given up, so that no warp is left in one.
     const int dt = tid - 256, dw = warp - 8, mask = (1 << c.page_shift) - 1;
-    uint32_t fill = 0, tile_no = 0;
+    constexpr int N = CH;                                                  // chunks of keys, and of values, the first half of them of the first tile
+    const int ch = dt % CH, row0 = dt / CH;                                // of chunk i: row row0 + i 128 / CH of the group
+    uint32_t fill = 0, group_no = 0;
     bool ok = true;
     for (long long index = blockIdx.x; kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
       const int32_t* table = c.table + (int64_t)it.b * c.width;
       const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
-      auto look_up = [&](int k) {                                          // where the pages of tile k's groups of 16 tokens begin
-        if (dt < C::GROUPS) {
-          const int j = it.base + k * TOK + 16 * dt;
-          int64_t at = -1;
-          if (k < it.tiles && j < it.hi) {
-            const int p = table[j >> c.page_shift];
-            if ((unsigned)p < (unsigned)c.num_pages) at = p * c.page_bytes;
-            else kv_bad_page(c);
-          }
-          page_at[(k & 1) * C::GROUPS + dt] = at;
-        }
-      };
-      auto fetch = [&](int k) {
-        if (ok && k < it.tiles) {
-          const uint32_t dst = smem + C::RAW_AT + (k & 1) * C::RAW;
-          constexpr int PER = TOK * CH / 128;                              // chunks of codes of a thread, of keys and of values
+      const int groups = (it.tiles + 1) / 2;
+      int page[N];                                                         // of the next group's chunks; -1: nothing there
+      auto look_up = [&](int g) {
 #pragma unroll
-          for (int i = 0; i < PER; ++i) {
-            const int id = i * 128 + dt, r = id / CH;
-            const int64_t at = page_at[(k & 1) * C::GROUPS + r / 16];
-            const uint8_t* src = head_pages + (at < 0 ? 0 : at) + ((it.base + k * TOK + r) & mask) * (D / 2) + (id % CH) * 16;
-            cp_async_16(dst + id * 16, src, at < 0 ? 0 : 16);
-            cp_async_16(dst + C::CODES + id * 16, src + c.v_codes, at < 0 ? 0 : 16);
-          }
-          constexpr int PIECES = TOK * SB / 16;                            // of scale bytes
-#pragma unroll
-          for (int i = 0; i < (PIECES + 127) / 128; ++i) {
-            const int id = i * 128 + dt;
-            if (id < PIECES) {
-              const int g16 = id / SB;
-              const int64_t at = page_at[(k & 1) * C::GROUPS + g16];
-              const uint8_t* src = head_pages + (at < 0 ? 0 : at) + c.k_scales + ((it.base + k * TOK + 16 * g16) & mask) * SB + (id % SB) * 16;
-              cp_async_16(dst + 2 * C::CODES + id * 16, src, at < 0 ? 0 : 16);
-              cp_async_16(dst + 2 * C::CODES + C::SCALES + id * 16, src + (c.v_scales - c.k_scales), at < 0 ? 0 : 16);
+        for (int i = 0; i < N; ++i) {
+          const int j = it.base + g * 128 + row0 + i * (128 / CH);
+          page[i] = -1;
+          if (g < groups && j < it.hi) {
+            page[i] = table[j >> c.page_shift];
+            if ((unsigned)page[i] >= (unsigned)c.num_pages) {
+              kv_bad_page(c);
+              page[i] = -1;
             }
           }
         }
-        cp_async_commit();
       };
-      named_barrier_sync(1, 128);                                          // the item before has been read
+      uint4 codes[2][N];
+      uint32_t scale[2][N], next_scale[N];                                 // zero where there is nothing; the values' of the next group
+      auto load_scale = [&](int g, int half, int i) -> uint32_t {
+        if (page[i] < 0) return 0;
+        const int slot = (it.base + g * 128 + row0 + i * (128 / CH)) & mask;
+        const uint8_t* p = head_pages + page[i] * c.page_bytes + (half ? c.v_scales : c.k_scales) + slot * SB;
+        return FMT == FMT_NVFP4 ? *reinterpret_cast<const uint16_t*>(p + 2 * ch) : p[ch];
+      };
+      auto load_codes = [&](int g, int half) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int slot = (it.base + g * 128 + row0 + i * (128 / CH)) & mask;
+          codes[half][i] = make_uint4(0, 0, 0, 0);
+          if (page[i] >= 0) codes[half][i] = load_once(head_pages + page[i] * c.page_bytes + (half ? c.v_codes : 0) + slot * (D / 2) + ch * 16);
+        }
+      };
+      // E of a group needs the scale bytes of both, so the values' come with the keys, a group ahead of their codes
+      auto load_keys = [&](int g) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          scale[0][i] = load_scale(g, 0, i);
+          next_scale[i] = load_scale(g, 1, i);
+        }
+        load_codes(g, 0);
+      };
+      auto load_values = [&](int g) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) scale[1][i] = next_scale[i];
+        load_codes(g, 1);
+      };
       look_up(0);
-      named_barrier_sync(1, 128);
-      fetch(0);
+      load_keys(0);
+      load_values(0);
       look_up(1);
-      for (int k = 0; k < it.tiles; ++k, ++tile_no) {
-        cp_async_wait<0>();
-        named_barrier_sync(1, 128);                                        // the tile is there, and the next one's pages; the one before has been read
-        fetch(k + 1);
-        const int j0 = it.base + k * TOK;
-        const uint8_t* raw = smem_p + C::RAW_AT + (k & 1) * C::RAW;
-        const uint8_t *k_scales = raw + 2 * C::CODES, *v_scales = k_scales + C::SCALES;
+      for (int g = 0; g < groups; ++g, ++group_no) {
         int down[2] = {0, 0};                                              // 27 - E
         if constexpr (FMT != FMT_NVFP4) {
-          int top[2] = {27, 27};
-          if (dt < TOK && j0 + dt < it.hi) {
 #pragma unroll
-            for (int i = 0; i < SB; ++i) {
-              top[0] = max(top[0], (int)k_scales[dt * SB + i]);
-              top[1] = max(top[1], (int)v_scales[dt * SB + i]);
-            }
-          }
+          for (int half = 0; half < 2; ++half) {
+            uint32_t top = 27;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            top[i] = __reduce_max_sync(0xFFFFFFFFu, top[i]);
-            if (lane == 0) warp_top[(k & 1) * 8 + dw * 2 + i] = top[i];
+            for (int i = 0; i < N; ++i) top = max(top, scale[half][i]);
+            top = __reduce_max_sync(0xFFFFFFFFu, top);
+            if (lane == 0) warp_top[(group_no & 1) * 8 + dw * 2 + half] = (int)top;
           }
           named_barrier_sync(1, 128);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int* w = warp_top + (k & 1) * 8 + i;
+          for (int half = 0; half < 2; ++half) {
+            const int* w = warp_top + (group_no & 1) * 8 + half;
             const int most = max(max(w[0], w[2]), max(w[4], w[6]));
-            down[i] = 27 - most;
-            if (dt == 0) tile_top[2 * (tile_no & 3) + i] = most;
+            down[half] = 27 - most;
+            if (dt == 0) tile_top[2 * (group_no & 7) + half] = most;
           }
         }
-        look_up(k + 2);
-#pragma unroll 1
-        for (int half = 0; half < 2; ++half, ++fill) {                     // keys, values
-          if (ok) ok = mbar_wait_warp(kv_empty(fill), ((fill / C::STAGES) & 1) ^ 1, cta_abort, c.err_word, SITE_PRODUCER_EMPTY);
-          if (!ok) continue;
-          uint8_t* dst = smem_p + C::TILES * C::Q_BYTES + (fill % C::STAGES) * C::KV_BYTES;
-          const uint8_t *codes = raw + half * C::CODES, *scales = half ? v_scales : k_scales;
-#pragma unroll 2
-          for (int i = 0; i < TOK * CH / 128; ++i) {
-            const int id = i * 128 + dt, r = id / CH, ch = id % CH;
-            const uint4 w = *reinterpret_cast<const uint4*>(codes + id * 16);
-            uint32_t f[2];                                                 // of the first and last 16 codes
-            if constexpr (FMT == FMT_NVFP4) {
-              const uint32_t two = e4m3x2_f16x2(*reinterpret_cast<const uint16_t*>(scales + r * SB + 2 * ch));
-              f[0] = __byte_perm(two, 0, 0x1010);
-              f[1] = __byte_perm(two, 0, 0x3232);
-            } else {
-              f[0] = f[1] = (uint32_t)max((int)scales[r * SB + ch] + (half ? down[1] : down[0]), 0) * 0x04000400u;
-            }
-            if (j0 + r >= it.hi) f[0] = f[1] = 0;                          // what lies there may be no number
-            uint8_t* to = dst + (ch >> 1) * (TOK * 128) + r * 128;
+        const int tiles = min(2, it.tiles - 2 * g);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              uint32_t o[4];
-              kv_key_pairs<FMT>((&w.x)[x], o);
-              uint4 y;
+        for (int half = 0; half < 2; ++half) {                             // keys, values
 #pragma unroll
-              for (int e = 0; e < 4; ++e) (&y.x)[e] = mul_f16x2(o[e], f[x >> 1]);
-              *reinterpret_cast<uint4*>(to + ((((ch & 1) * 4 + x) ^ (r & 7)) << 4)) = y;
+          for (int tile = 0; tile < 2; ++tile) {
+            if (tile < tiles) {
+              if (ok) ok = mbar_wait_warp(kv_empty(fill), ((fill / C::STAGES) & 1) ^ 1, cta_abort, c.err_word, SITE_PRODUCER_EMPTY);
+              if (ok) {
+                uint8_t* dst = smem_p + C::TILES * C::Q_BYTES + (fill % C::STAGES) * C::KV_BYTES + (ch >> 1) * (TOK * 128);
+#pragma unroll
+                for (int i = tile * (N / 2); i < (tile + 1) * (N / 2); ++i) {
+                  const int r = (row0 + i * (128 / CH)) & (TOK - 1);
+                  uint32_t f[2];                                           // of the first and last 16 codes
+                  if constexpr (FMT == FMT_NVFP4) {
+                    const uint32_t two = e4m3x2_f16x2(scale[half][i]);
+                    f[0] = __byte_perm(two, 0, 0x1010);
+                    f[1] = __byte_perm(two, 0, 0x3232);
+                  } else {
+                    f[0] = f[1] = (uint32_t)max((int)scale[half][i] + down[half], 0) * 0x04000400u;
+                  }
+#pragma unroll
+                  for (int x = 0; x < 4; ++x) {
+                    uint32_t o[4];
+                    kv_key_pairs<FMT>((&codes[half][i].x)[x], o);
+                    uint4 y;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) (&y.x)[e] = mul_f16x2(o[e], f[x >> 1]);
+                    *reinterpret_cast<uint4*>(dst + r * 128 + ((((ch & 1) * 4 + x) ^ (r & 7)) << 4)) = y;
+                  }
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(kv_full(fill));
+              }
+              ++fill;
             }
           }
-          fence_proxy_async_smem();
-          mbar_arrive(kv_full(fill));
+          if (half == 0) load_keys(g + 1);
+          else load_values(g + 1);
         }
+        look_up(g + 2);
       }
-      cp_async_wait<0>();
     }
   } else {
     // ------------------------------------------------------------------ products
     constexpr uint32_t idesc_s = idesc_f16(128, TOK, false, false), idesc_o = idesc_f16(128, D, false, true);
-    uint32_t fill = 0, p_count[2] = {0, 0}, q_count[2] = {0, 0};
+    uint32_t fill = 0, p_count[2] = {0, 0}, q_count = 0;
     bool ok = true;
-    for (long long index = blockIdx.x; ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
-      const int active = it.rows > 128 ? 2 : 1;
-      for (int k = 0; k <= it.tiles && ok; ++k) {
-        const uint32_t kf = fill + 2 * k, vf = kf - 1;
-        if (k > 0) ok = mbar_wait_warp(kv_full(vf), (vf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
-        if (ok && k < it.tiles) ok = mbar_wait_warp(kv_full(kf), (kf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
-        for (int t = 0; t < active && ok; ++t) {
-          if (k == 0) {
-            ok = mbar_wait_warp(q_full(t), q_count[t] & 1, cta_abort, c.err_word, SITE_MMA_ACC_EMPTY);
-            ++q_count[t];
-          } else {
-            ok = mbar_wait_warp(p_full(t), p_count[t] & 1, cta_abort, c.err_word, SITE_MMA_ACC_EMPTY);
-            ++p_count[t];
-          }
-          if (!ok) break;
-          tc_fence_after_sync();
-          const uint32_t s_at = tmem + t * TOK, o_at = tmem + C::O_COL + t * D;
-          if (elect_one()) {
-            if (k > 0) {
-              const uint64_t v = make_desc(smem + C::TILES * C::Q_BYTES + (vf % C::STAGES) * C::KV_BYTES, TOK * 128, 1024, kSwizzle128);
-#pragma unroll
-              for (int i = 0; i < TOK / 16; ++i)           // 16 tokens: 8 columns of P, 16 rows of V (2 KiB)
-                mma_bf16_tmem_a(o_at, s_at + 8 * i, v + 128 * i, idesc_o, k > 1 || i > 0);
-            }
-            if (k < it.tiles) {
-              const uint64_t q = make_desc(smem + t * C::Q_BYTES, 16, 1024, kSwizzle128);
-              const uint64_t x = make_desc(smem + C::TILES * C::Q_BYTES + (kf % C::STAGES) * C::KV_BYTES, 16, 1024, kSwizzle128);
-#pragma unroll
-              for (int i = 0; i < D / 16; ++i)             // 16 elements: 32 bytes of a row of 128
-                mma_bf16(s_at, q + (i >> 2) * (128 * 128 / 16) + 2 * (i & 3), x + (i >> 2) * (TOK * 128 / 16) + 2 * (i & 3), idesc_s, i > 0);
-              tc_commit(s_full(t));
-            } else {
-              tc_commit(o_full(t));
-            }
-          }
-          __syncwarp();
-        }
+    // What goes into the products' descriptors has to lie in uniform registers (from others an instruction takes 75 cycles to issue: 330 us), and the
+    // result of a reduction does.
+    const int t = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)warp) - 12;                  // the tile of rows
+    const uint32_t tm = __reduce_max_sync(0xFFFFFFFFu, tmem), sm = __reduce_max_sync(0xFFFFFFFFu, smem);
+    for (long long index = blockIdx.x; t < C::TILES && ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
+      const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)it.tiles);
+      const bool active = 128 * t < (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)it.rows);
+      const uint32_t o_at = tm + C::O_COL + t * D;
+      if (active) ok = mbar_wait_warp(q_full(t), q_count++ & 1, cta_abort, c.err_word, SITE_MMA_ACC_EMPTY);
+      // number i: P V of tile i - 2, then S of tile i into the place of that P
+      for (int i = 0; i < tiles + 2 && ok; ++i) {
+        const int k = i - 2;
+        const uint32_t kf = fill + 4 * (i >> 1) + (i & 1), vf = fill + 4 * (k >> 1) + min(2, tiles - (k & ~1)) + (k & 1);
+        if (k >= 0) ok = mbar_wait_warp(kv_full(vf), (vf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
+        if (ok && i < tiles) ok = mbar_wait_warp(kv_full(kf), (kf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
+        if (ok && active && k >= 0) ok = mbar_wait_warp(p_full(t, i & 1), p_count[i & 1]++ & 1, cta_abort, c.err_word, SITE_MMA_ACC_EMPTY);
         if (!ok) break;
+        tc_fence_after_sync();
+        const uint32_t s_at = tm + (2 * t + (i & 1)) * TOK;
         if (elect_one()) {
-          if (k > 0) tc_commit(kv_empty(vf));
-          if (k < it.tiles) tc_commit(kv_empty(kf));
+          if (active && k >= 0) {
+            const uint64_t v = make_desc(sm + C::TILES * C::Q_BYTES + (vf % C::STAGES) * C::KV_BYTES, TOK * 128, 1024, kSwizzle128);
+#pragma unroll
+            for (int x = 0; x < TOK / 16; ++x)             // 16 tokens: 8 columns of P, 16 rows of V (2 KiB)
+              mma_bf16_tmem_a(o_at, s_at + 8 * x, v + 128 * x, idesc_o, k > 0 || x > 0);
+          }
+          if (active && i < tiles) {
+            const uint64_t q = make_desc(sm + t * C::Q_BYTES, 16, 1024, kSwizzle128);
+            const uint64_t y = make_desc(sm + C::TILES * C::Q_BYTES + (kf % C::STAGES) * C::KV_BYTES, 16, 1024, kSwizzle128);
+#pragma unroll
+            for (int x = 0; x < D / 16; ++x)               // 16 elements: 32 bytes of a row of 128
+              mma_bf16(s_at, q + (x >> 2) * (128 * 128 / 16) + 2 * (x & 3), y + (x >> 2) * (TOK * 128 / 16) + 2 * (x & 3), idesc_s, x > 0);
+          }
+          if (active) tc_commit(s_full(t, i & 1));
+          if (k >= 0) tc_commit(kv_empty(vf));             // a tile of rows that is not there gives the tokens back as they come
+          if (i < tiles) tc_commit(kv_empty(kf));
         }
         __syncwarp();
       }
-      fill += 2 * it.tiles;
+      fill += 2 * tiles;
     }
   }
 
