@@ -1,5 +1,6 @@
 // C-ABI entry points of the 4-bit key/value cache (see include/torq.h): argument validation, kernel selection and launch.
 #include <cuda_runtime.h>
+#include <atomic>
 #include <type_traits>
 
 #include "../../include/torq.h"
@@ -73,6 +74,18 @@ static inline unsigned grid_of(int64_t threads, int per_cta, int64_t most) {
   return (unsigned)(n < 1 ? 1 : (n > most ? most : n));
 }
 
+// Opts a kernel in to `bytes` of dynamic shared memory, once per device (asked every time it costs the host 0.4 us a call).
+template <auto KERNEL>
+static bool opt_in(int bytes) {
+  static std::atomic<uint64_t> done{0};
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev > 63) return false;
+  if (done.load(std::memory_order_relaxed) >> dev & 1) return true;
+  if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+  done.fetch_or(1ull << dev, std::memory_order_relaxed);
+  return true;
+}
+
 template <typename F>
 static void with_dim(int dim, F f) {
   if (dim == 64) f(std::integral_constant<int, 64>{});
@@ -134,7 +147,7 @@ static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, c
                                  void* workspace, cudaStream_t s) {
   using C = KvDecodeCfg<FMT, D, NT>;
   constexpr auto kernel = kv_decode_kernel<C>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return TORQ_ERR_LAUNCH;
+  if (!opt_in<kernel>(C::SMEM)) return TORQ_ERR_LAUNCH;
   const int most = sms * C::CTAS, ctas = most < kMaxRanges / C::WARPS ? most : kMaxRanges / C::WARPS, group = heads / v.heads;
   float* partials = static_cast<float*>(workspace);
   __nv_bfloat16* y = static_cast<__nv_bfloat16*>(out);
@@ -157,7 +170,7 @@ static torq_status prefill_launch(const KvView& v, const KvScoring& a, int sms, 
                                   cudaStream_t s) {
   using C = KvPrefillCfg<FMT, D>;
   constexpr auto kernel = kv_prefill_kernel<C>;
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) return TORQ_ERR_LAUNCH;
+  if (!opt_in<kernel>(C::SMEM)) return TORQ_ERR_LAUNCH;
   launch_tc(kernel, 1, dim3((unsigned)sms), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads,
             static_cast<__nv_bfloat16*>(out), lse);
   return launch_status();
@@ -208,7 +221,7 @@ static torq_status weights_impl(const torq_kv_cache* cache, const torq_kv_scorin
   with_dim(v.dim, [&](auto D) {
     using C = KvWeightsCfg<FMT, decltype(D)::value>;
     constexpr auto kernel = kv_weights_kernel<C>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess) {
+    if (!opt_in<kernel>(C::SMEM)) {
       rc = TORQ_ERR_LAUNCH;
       return;
     }

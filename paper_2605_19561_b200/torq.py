@@ -172,6 +172,9 @@ _OPERATORS = (*(f"torq_{fmt}_{op}" for op in ("matvec", "gated_matvec", "gated_g
               "torq_add_rmsnorm", "torq_add_rmsnorm_mxfp8", "torq_matvec_workspace_bytes")
 
 
+_KV_FORMATS = ("mxfp4", "nvfp4", "mxint4")
+
+
 def _layer(*args):                               # until the first call has put the native function here
     global _layer
     _layer = _layer_native() or _layer_ctypes
@@ -202,6 +205,10 @@ def _native_binding():
     for set_address, names in ((binding.set_entry, _LAYER_ENTRIES), (binding.set_operator, _OPERATORS)):
         for kind, name in enumerate(names):
             set_address(kind, ctypes.cast(getattr(L, name), ctypes.c_void_p).value)
+    for op, name in enumerate(("append", "read", "attention", "weights", "evict")):
+        for fmt, entry in enumerate(_KV_FORMATS):
+            binding.set_kv(op, fmt, ctypes.cast(getattr(L, f"torq_{entry}_kv_{name}"), ctypes.c_void_p).value)
+    binding.set_kv(5, 0, ctypes.cast(L.torq_kv_attention_workspace_bytes, ctypes.c_void_p).value)
     _binding_module = binding
     return binding
 
@@ -973,7 +980,23 @@ def _kv_scoring(scale, softcap, slopes, window, prefix, first, dim, heads, batch
     return _KvScoring(dim ** -0.5 if scale is None else scale, softcap, _ptr(slopes), window, _ptr(prefix), _ptr(first))
 
 
+class _KvNative:
+    """The native functions of the cache's calls, looked up at the first one; -1 where they cannot be had."""
+
+    def __getattr__(self, name):
+        binding = _native_binding()
+        f = getattr(binding, name) if binding else lambda *args: -1
+        setattr(self, name, f)
+        return f
+
+
+_kv_native = _KvNative()
+
+
 def _kv_append(fmt, pages, table, lengths, K, V, scales, starts, stream):
+    r = _kv_native.kv_append(_KV_FORMATS.index(fmt), pages, table, lengths, K, V, starts, *(scales or (1.0, 1.0)), _handle(stream))
+    if r >= 0:
+        return _raise(r, f"torq_{fmt}_kv_append")
     strides = _kv_rows(K, _FLOATS, "K"), _kv_rows(V, (getattr(K, "dtype", None),), "V")
     cache = _kv_cache(fmt, pages, table, lengths, K.shape[2], scales, starts, K.shape[0])
     if K.shape != V.shape or K.shape[1] != pages.shape[1]:
@@ -983,6 +1006,13 @@ def _kv_append(fmt, pages, table, lengths, K, V, scales, starts, stream):
 
 
 def _kv_read(fmt, pages, table, lengths, head_dim, tokens, scales, starts, out_dtype, stream):
+    if out_dtype in _FLOATS:
+        r = _kv_native.kv_read(_KV_FORMATS.index(fmt), pages, table, lengths, head_dim, tokens, starts, *(scales or (1.0, 1.0)),
+                               out_dtype is torch.float32, _handle(stream))
+        if r.__class__ is not int:
+            return r
+        if r > 0:
+            raise TorqError(r, f"torq_{fmt}_kv_read")
     cache = _kv_cache(fmt, pages, table, lengths, head_dim, scales, starts, tokens)
     name = f"torq_{fmt}_kv_read"
     if out_dtype not in _FLOATS:
@@ -1004,6 +1034,13 @@ def _kv_queries(fmt, pages, table, lengths, Q, scales, starts):
 
 def _kv_attention(fmt, pages, table, lengths, Q, scales, starts, scale, softcap, slopes, window, prefix, first, out, return_lse, workspace,
                   stream):
+    r = _kv_native.kv_attention(_KV_FORMATS.index(fmt), pages, table, lengths, Q, starts, *(scales or (1.0, 1.0)), scale, softcap, slopes, window,
+                                prefix, first, out, return_lse, workspace, _handle(stream))
+    if r.__class__ is not int:
+        return r
+    if r > 0:
+        raise TorqError(r, f"torq_{fmt}_kv_attention")
+    # through ctypes, with reasons for what it refuses
     cache, stride, tokens, heads, dim = _kv_queries(fmt, pages, table, lengths, Q, scales, starts)
     scoring = _kv_scoring(scale, softcap, slopes, window, prefix, first, dim, heads, cache.batch, tokens)
     if out is None:
@@ -1025,6 +1062,11 @@ def _kv_attention(fmt, pages, table, lengths, Q, scales, starts, scale, softcap,
 
 
 def _kv_weights(fmt, pages, table, lengths, Q, lse, weights, scales, starts, scale, softcap, slopes, window, prefix, first, weights_out, stream):
+    r = _kv_native.kv_weights(_KV_FORMATS.index(fmt), pages, table, lengths, Q, lse, weights, starts, scales[0] if scales else 1.0, scale, softcap, slopes,
+                              window, prefix, first, weights_out, _handle(stream))
+    if r >= 0:
+        _raise(r, f"torq_{fmt}_kv_weights")
+        return weights if weights_out is None else weights_out
     cache, stride, tokens, heads, dim = _kv_queries(fmt, pages, table, lengths, Q, scales, starts)
     scoring = _kv_scoring(scale, softcap, slopes, window, prefix, first, dim, heads, cache.batch, tokens)
     _operand(lse, (torch.float32,), "lse", (tokens, heads))
@@ -1040,6 +1082,11 @@ def _kv_weights(fmt, pages, table, lengths, Q, lse, weights, scales, starts, sca
 
 
 def _kv_evict(fmt, pages, table, lengths, head_dim, weights, new_table, keep, recent, stream):
+    r = _kv_native.kv_evict(_KV_FORMATS.index(fmt), pages, table, lengths, head_dim, weights, new_table, keep, recent, _handle(stream))
+    if r.__class__ is not int:
+        return r
+    if r > 0:
+        raise TorqError(r, f"torq_{fmt}_kv_evict")
     cache = _kv_cache(fmt, pages, table, lengths, head_dim, (1.0, 1.0), None, table.shape[0] if isinstance(table, torch.Tensor) else 0)
     _operand(weights, (torch.float32,), "weights", (cache.num_pages, cache.kv_heads, cache.page_tokens))
     _operand(new_table, _INTS, "new_table")
