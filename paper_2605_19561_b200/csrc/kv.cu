@@ -93,6 +93,13 @@ static void with_dim(int dim, F f) {
   else f(std::integral_constant<int, 256>{});
 }
 
+// Tokens of a CTA at a time: one while there are few, so that they spread over the SMs, else four.
+template <typename F>
+static void with_tokens(int tokens, int sms, F f) {
+  if (tokens <= 8 * sms) f(std::integral_constant<int, 1>{}, (unsigned)tokens);
+  else f(std::integral_constant<int, 4>{}, grid_of(tokens, 4, (int64_t)sms * 64));
+}
+
 template <int FMT>
 static torq_status append_impl(const torq_kv_cache* cache, const void* K, const void* V, torq_dtype dtype, int64_t k_stride, int64_t v_stride,
                                const int32_t* starts, int64_t tokens, void* stream) {
@@ -107,13 +114,16 @@ static torq_status append_impl(const torq_kv_cache* cache, const void* K, const 
   if (!aligned16(K) || !aligned16(V) || k_stride % per16 != 0 || v_stride % per16 != 0) return TORQ_ERR_ALIGN;
   int sms;
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
-  const dim3 grid(grid_of(threads, 256, (int64_t)sms * 32));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == TORQ_F32)
-    launch_tc(kv_append_kernel<FMT, float>, 1, grid, dim3(256), 0, s, v, static_cast<const float*>(K), static_cast<const float*>(V), k_stride, v_stride);
-  else
-    launch_tc(kv_append_kernel<FMT, __nv_bfloat16>, 1, grid, dim3(256), 0, s, v, static_cast<const __nv_bfloat16*>(K), static_cast<const __nv_bfloat16*>(V),
-              k_stride, v_stride);
+  with_tokens(v.tokens, sms, [&](auto N, unsigned grid) {
+    constexpr int TOKENS = decltype(N)::value;
+    if (dtype == TORQ_F32)
+      launch_tc(kv_append_kernel<FMT, float, TOKENS>, 1, dim3(grid), dim3(256), 0, s, v, static_cast<const float*>(K), static_cast<const float*>(V), k_stride,
+                v_stride);
+    else
+      launch_tc(kv_append_kernel<FMT, __nv_bfloat16, TOKENS>, 1, dim3(grid), dim3(256), 0, s, v, static_cast<const __nv_bfloat16*>(K),
+                static_cast<const __nv_bfloat16*>(V), k_stride, v_stride);
+  });
   return launch_status();
 }
 
@@ -128,10 +138,12 @@ static torq_status read_impl(const torq_kv_cache* cache, const int32_t* starts, 
   if (!aligned16(K) || !aligned16(V)) return TORQ_ERR_ALIGN;
   int sms;
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
-  const dim3 grid(grid_of(threads, 256, (int64_t)sms * 32));
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (dtype == TORQ_F32) launch_tc(kv_read_kernel<FMT, float>, 1, grid, dim3(256), 0, s, v, static_cast<float*>(K), static_cast<float*>(V));
-  else launch_tc(kv_read_kernel<FMT, __nv_bfloat16>, 1, grid, dim3(256), 0, s, v, static_cast<__nv_bfloat16*>(K), static_cast<__nv_bfloat16*>(V));
+  with_tokens(v.tokens, sms, [&](auto N, unsigned grid) {
+    constexpr int TOKENS = decltype(N)::value;
+    if (dtype == TORQ_F32) launch_tc(kv_read_kernel<FMT, float, TOKENS>, 1, dim3(grid), dim3(256), 0, s, v, static_cast<float*>(K), static_cast<float*>(V));
+    else launch_tc(kv_read_kernel<FMT, __nv_bfloat16, TOKENS>, 1, dim3(grid), dim3(256), 0, s, v, static_cast<__nv_bfloat16*>(K), static_cast<__nv_bfloat16*>(V));
+  });
   return launch_status();
 }
 
@@ -248,10 +260,15 @@ static torq_status evict_impl(const torq_kv_cache* cache, float* weights, const 
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const unsigned items = (unsigned)(v.batch * v.heads);
-  launch_tc(kv_select_kernel, 1, dim3(items), dim3(KvSelectCfg::THREADS), 0, s, v, static_cast<const float*>(weights), (int)keep, (int)recent, new_lengths, kept);
+  // CTAs per sequence and head: as many as the SMs have room for, each with 2048 tokens at least
+  int cluster = 1;
+  while (cluster < 8 && (int64_t)items * cluster * 2 <= sms && room / (cluster * 2) >= 2048) cluster *= 2;
+  if (!opt_in<kv_select_kernel>(KvSelectCfg::SMEM)) return TORQ_ERR_LAUNCH;
+  launch_tc(kv_select_kernel, cluster, dim3(items * cluster), dim3(KvSelectCfg::THREADS), KvSelectCfg::SMEM, s, v, static_cast<const float*>(weights), (int)keep,
+            (int)recent, cluster, new_lengths, kept);
   if ((rc = launch_status()) != TORQ_OK) return rc;
   const int64_t moved = keep < room ? keep : room;
-  launch_tc(kv_move_kernel<FMT>, 1, dim3(grid_of(moved * (v.dim / 16), 256, 4096), items), dim3(256), 0, s, v, weights, new_table, (int)new_width, (int)keep,
+  launch_tc(kv_move_kernel<FMT>, 1, dim3(grid_of(moved * (v.dim / 16), 1024, 4096), items), dim3(256), 0, s, v, weights, new_table, (int)new_width, (int)keep,
             static_cast<const int32_t*>(kept));
   return launch_status();
 }

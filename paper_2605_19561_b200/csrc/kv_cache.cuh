@@ -134,34 +134,70 @@ __device__ __forceinline__ void kv_load8(const __nv_bfloat16* p, float (&v)[8]) 
   }
 }
 
-// A thread takes eight elements of a row (a new token's key or value of one head).  Tokens before the start of their sequence (more new ones
-// than its length) have no slot.
-template <int FMT, typename T>
+// Where the slots of TOKENS rows of the batch are, from row `first` on: the first thread of the CTA for each finds its page (its head 0), the others wait
+// for it.  -1: no place.
+struct KvSlot {
+  int64_t page;                          // bytes from the beginning of the pages
+  int slot;
+};
+template <int TOKENS>
+__device__ __forceinline__ void kv_find_slots(const KvView& c, int first, KvSlot* slots) {
+  if (threadIdx.x < TOKENS) {
+    const int i = first + (int)threadIdx.x, b = i < c.tokens ? kv_sequence_of(c, i) : -1;
+    KvSlot s = {-1, 0};
+    if (b >= 0) {
+      int row, count;
+      kv_new_tokens(c, b, row, count);
+      const int j = kv_length(c, b) - count + (i - row);
+      if (j >= 0) {                      // a token before the start of its sequence (more new ones than its length) has no slot
+        const int page = kv_page(c, c.table, c.width, b, j);
+        if (page >= 0) s.page = page * c.page_bytes;
+        s.slot = j & ((1 << c.page_shift) - 1);
+      }
+    }
+    slots[threadIdx.x] = s;
+  }
+  __syncthreads();
+}
+
+// A CTA takes TOKENS new tokens at a time, all heads, keys and values; a thread eight elements of a row of each.  (A thread to eight elements anywhere, each
+// finding its slot: 13040 tokens of 8 x 128 NVFP4 47 us.)
+template <int FMT, typename T, int TOKENS>
 __global__ void __launch_bounds__(256) kv_append_kernel(const KvView c, const T* K, const T* V, int64_t k_stride, int64_t v_stride) {
   griddep_wait_and_launch();
-  const uint32_t per_row = (uint32_t)c.dim / 8, total = (uint32_t)c.tokens * 2u * (uint32_t)c.heads * per_row;
-  for (uint32_t at = blockIdx.x * 256u + threadIdx.x; at - (threadIdx.x & 31u) < total; at += gridDim.x * 256u) {
-    const bool there = at < total;
-    const uint32_t e = at % per_row, row = at / per_row, head2 = row % (2u * c.heads), token = row / (2u * c.heads);
-    const bool value = head2 >= (uint32_t)c.heads;
-    const uint32_t head = value ? head2 - c.heads : head2;
-    float v[8] = {};
-    if (there) kv_load8((value ? V + token * v_stride : K + token * k_stride) + head * c.dim + e * 8, v);
-    uint32_t sbyte;
-    const uint32_t codes = kv_quantize8<FMT>(v, value ? c.v_ts : c.k_ts, sbyte);
-    const int b = there ? kv_sequence_of(c, (int)token) : -1;
-    if (b < 0) continue;                                 // whole rows; the shuffles are behind
-    int first, count;
-    kv_new_tokens(c, b, first, count);
-    const int j = kv_length(c, b) - count + ((int)token - first);
-    if (j < 0) continue;
-    const int page = kv_page(c, c.table, c.width, b, j);
-    if (page < 0) continue;
-    uint8_t* p = kv_head_page(c, page, (int)head);
-    const int slot = j & ((1 << c.page_shift) - 1), blocks = c.dim / kv_block(FMT);
-    *reinterpret_cast<uint32_t*>(p + (value ? c.v_codes : 0) + slot * (c.dim / 2) + e * 4) = codes;
-    constexpr uint32_t lanes = kv_block(FMT) / 8;
-    if (e % lanes == 0) p[(value ? c.v_scales : c.k_scales) + slot * blocks + e / lanes] = (uint8_t)sbyte;
+  __shared__ KvSlot slots[2][TOKENS];
+  const int shift = 31 - __clz(c.dim / 8), work = 2 * c.heads << shift, lane = threadIdx.x & 31;
+  int buffer = 0;
+  for (int first = blockIdx.x * TOKENS; first < c.tokens; first += gridDim.x * TOKENS, buffer ^= 1) {
+    bool found = false;
+    for (int at = threadIdx.x; at - lane < work; at += 256) {
+      const int e = at & ((1 << shift) - 1), head2 = at >> shift;
+      const bool value = head2 >= c.heads;
+      const int head = value ? head2 - c.heads : head2;
+      const T* from = (value ? V : K) + head * c.dim + e * 8;
+      const int64_t stride = value ? v_stride : k_stride;
+      float v[TOKENS][8];
+#pragma unroll
+      for (int u = 0; u < TOKENS; ++u) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[u][i] = 0.f;
+        if (at < work && first + u < c.tokens) kv_load8(from + (first + u) * stride, v[u]);
+      }
+      if (!found) kv_find_slots<TOKENS>(c, first, slots[buffer]);          // by all threads: the loops of all warps have a first turn
+      found = true;
+#pragma unroll
+      for (int u = 0; u < TOKENS; ++u) {
+        uint32_t sbyte;
+        const uint32_t codes = kv_quantize8<FMT>(v[u], value ? c.v_ts : c.k_ts, sbyte);
+        const KvSlot s = slots[buffer][u];
+        if (s.page < 0 || at >= work) continue;          // the shuffles are behind
+        uint8_t* p = c.pages + s.page + (int64_t)head * c.head_bytes;
+        *reinterpret_cast<uint32_t*>(p + (value ? c.v_codes : 0) + s.slot * (c.dim / 2) + e * 4) = codes;
+        constexpr int lanes = kv_block(FMT) / 8;
+        if (e % lanes == 0) p[(value ? c.v_scales : c.k_scales) + s.slot * (c.dim / kv_block(FMT)) + e / lanes] = (uint8_t)sbyte;
+      }
+    }
+    if (!found) kv_find_slots<TOKENS>(c, first, slots[buffer]);            // warps without work
   }
 }
 
@@ -177,33 +213,41 @@ __device__ __forceinline__ void kv_store8(__nv_bfloat16* p, const float (&v)[8])
 }
 
 // The same slots read: rows [tokens][heads][dim] of both, zeros for a token without a slot.
-template <int FMT, typename T>
+template <int FMT, typename T, int TOKENS>
 __global__ void __launch_bounds__(256) kv_read_kernel(const KvView c, T* K, T* V) {
   griddep_wait_and_launch();
-  const uint32_t per_row = (uint32_t)c.dim / 8, total = (uint32_t)c.tokens * 2u * (uint32_t)c.heads * per_row;
-  for (uint32_t at = blockIdx.x * 256u + threadIdx.x; at < total; at += gridDim.x * 256u) {
-    const uint32_t e = at % per_row, row = at / per_row, head2 = row % (2u * c.heads), token = row / (2u * c.heads);
-    const bool value = head2 >= (uint32_t)c.heads;
-    const uint32_t head = value ? head2 - c.heads : head2;
-    float v[8] = {};
-    const int b = kv_sequence_of(c, (int)token);
-    int first = 0, count = 0, page = -1, j = -1;
-    if (b >= 0) {
-      kv_new_tokens(c, b, first, count);
-      j = kv_length(c, b) - count + ((int)token - first);
-      if (j >= 0) page = kv_page(c, c.table, c.width, b, j);
-    }
-    if (page >= 0) {
-      const uint8_t* p = kv_head_page(c, page, (int)head);
-      const int slot = j & ((1 << c.page_shift) - 1), blocks = c.dim / kv_block(FMT);
-      const uint32_t codes = *reinterpret_cast<const uint32_t*>(p + (value ? c.v_codes : 0) + slot * (c.dim / 2) + e * 4);
-      const uint32_t sbyte = p[(value ? c.v_scales : c.k_scales) + slot * blocks + e * 8 / kv_block(FMT)];
-      const float s = kv_scale<FMT>(sbyte, 1.f), ts = value ? c.v_ts : c.k_ts;
-      kv_codes8<FMT>(codes, v);
+  __shared__ KvSlot slots[2][TOKENS];
+  const int shift = 31 - __clz(c.dim / 8), work = 2 * c.heads << shift;
+  int buffer = 0;
+  for (int first = blockIdx.x * TOKENS; first < c.tokens; first += gridDim.x * TOKENS, buffer ^= 1) {
+    kv_find_slots<TOKENS>(c, first, slots[buffer]);
+    for (int at = threadIdx.x; at < work; at += 256) {
+      const int e = at & ((1 << shift) - 1), head2 = at >> shift;
+      const bool value = head2 >= c.heads;
+      const int head = value ? head2 - c.heads : head2;
+      uint32_t codes[TOKENS], sbyte[TOKENS];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = v[i] * s * ts;  // code and scale byte multiply exactly
+      for (int u = 0; u < TOKENS; ++u) {
+        const KvSlot s = slots[buffer][u];
+        codes[u] = sbyte[u] = 0;
+        if (s.page < 0) continue;
+        const uint8_t* p = c.pages + s.page + (int64_t)head * c.head_bytes;
+        codes[u] = *reinterpret_cast<const uint32_t*>(p + (value ? c.v_codes : 0) + s.slot * (c.dim / 2) + e * 4);
+        sbyte[u] = p[(value ? c.v_scales : c.k_scales) + s.slot * (c.dim / kv_block(FMT)) + e * 8 / kv_block(FMT)];
+      }
+      const float ts = value ? c.v_ts : c.k_ts;
+      T* to = (value ? V : K) + ((int64_t)first * c.heads + head) * c.dim + e * 8;
+#pragma unroll
+      for (int u = 0; u < TOKENS; ++u) {
+        if (first + u >= c.tokens) break;
+        float v[8];
+        kv_codes8<FMT>(codes[u], v);
+        const float scale = kv_scale<FMT>(sbyte[u], 1.f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = v[i] * scale * ts;              // code and scale byte multiply exactly
+        kv_store8(to + (int64_t)u * c.heads * c.dim, v);
+      }
     }
-    kv_store8((value ? V : K) + ((int64_t)token * c.heads + head) * c.dim + e * 8, v);
   }
 }
 

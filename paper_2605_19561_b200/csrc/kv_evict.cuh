@@ -11,70 +11,122 @@ __device__ __forceinline__ uint32_t ordered_key(float v) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// One CTA per sequence and head writes the places of what stays, in their order, and -1 behind them.  The smallest weight that stays is found
-// eight bits of its key at a time (a count of every value of these bits among the keys that share the bits above).
-struct KvSelectCfg { static constexpr int THREADS = 1024, EACH = 4; };
-static __global__ void __launch_bounds__(KvSelectCfg::THREADS) kv_select_kernel(const KvView c, const float* weights, int keep, int recent,
+// A cluster of 1 to 8 CTAs per sequence and head (more where there are few of these) writes the places of what stays, in their order, and -1 behind them.
+// The smallest weight that stays is found 11 bits of its key at a time, 10 the last: every CTA counts the values of these bits among its keys that share
+// the bits above, all add up the counts of all through distributed shared memory, and the value is where the sum from above reaches the room.
+// A CTA reads its weights once, into shared memory, up to KEYS of them; longer parts are read again every time.
+// (One CTA with digits of eight bits, weights read five times: 65000 tokens, 8 heads 128 us, 64 times 4500 tokens 17 us.)
+struct KvSelectCfg {
+  static constexpr int THREADS = 1024, EACH = 4, KEYS = 24576, BINS = 2048, SMEM = KEYS * 4;
+};
+static __global__ void __launch_bounds__(KvSelectCfg::THREADS) kv_select_kernel(const KvView c, const float* weights, int keep, int recent, int cluster,
                                                                                 int32_t* new_lengths, int32_t* kept) {
   griddep_wait_and_launch();
-  __shared__ uint32_t count[256], chosen[2], sums[2][33];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, head = blockIdx.x % c.heads, b = blockIdx.x / c.heads;
+  using C = KvSelectCfg;
+  extern __shared__ uint32_t keys[];
+  __shared__ uint32_t count[2][C::BINS], chosen[2], sums[2][33], mine[2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x % cluster, item = blockIdx.x / cluster, head = item % c.heads,
+            b = item / c.heads;
   const int length = kv_length(c, b), stay = length < keep ? length : keep, newest = recent < stay ? recent : stay;
-  int32_t* to = kept + (int64_t)blockIdx.x * keep;
-  if (head == 0 && tid == 0) new_lengths[b] = stay;
+  int32_t* to = kept + (int64_t)item * keep;
+  if (head == 0 && rank == 0 && tid == 0) new_lengths[b] = stay;
   const int others = length - newest, room = stay - newest;     // `room` of `others` stay
-  auto key_of = [&](int j) {
-    const int page = kv_page(c, c.table, c.width, b, j);
+  const int part = ((others + cluster - 1) / cluster + 31) & ~31, first = min(rank * part, others), n = min(part, others - first);
+  const bool held = part <= C::KEYS;
+  auto read = [&](int i) {
+    const int j = first + i, page = kv_page(c, c.table, c.width, b, j);
     return page < 0 ? 0u : ordered_key(weights[(((int64_t)page * c.heads + head) << c.page_shift) + (j & ((1 << c.page_shift) - 1))]);
   };
   uint32_t edge = 0, left = (uint32_t)room;                      // of the keys that equal `edge`, `left` stay
-  if (room < others && room > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) count[tid] = 0;
+  const bool all = room == others, select = !all && room > 0;
+  if (select) {
+    if (held) {
+#pragma unroll 4
+      for (int i = tid; i < n; i += C::THREADS) keys[i] = read(i);
+    }
+    int above = 32;                                              // bits above which `edge` is known
+    for (int pass = 0; pass < 3; ++pass) {
+      const int bits = pass < 2 ? 11 : 10, shift = above - bits;
+      uint32_t* own = count[pass & 1];
+      own[tid] = own[tid + C::THREADS] = 0;
       __syncthreads();
-      for (int j = tid; j < others; j += KvSelectCfg::THREADS) {
-        const uint32_t key = key_of(j);
-        if (shift == 24 || (key >> (shift + 8)) == (edge >> (shift + 8))) atomicAdd(&count[key >> shift & 255u], 1u);
+      for (int i = tid; i < n; i += C::THREADS) {
+        const uint32_t key = held ? keys[i] : read(i);
+        if (pass == 0 || key >> above == edge >> above) atomicAdd(&own[key >> shift & ((1u << bits) - 1)], 1u);
       }
+      if (cluster > 1) cluster_sync_all();
+      else __syncthreads();
+      // two bins to a thread, the largest values first
+      uint32_t bin[2] = {0, 0};
+      for (int r = 0; r < cluster; ++r)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int value = C::BINS - 1 - (2 * tid + i);
+          bin[i] += cluster > 1 ? load_cluster_u32(map_to_cta(smem_u32(own + value), (uint32_t)r)) : own[value];
+        }
+      uint32_t s = bin[0] + bin[1];
+      const uint32_t both = s;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, s, o);
+        if (lane >= o) s += t;
+      }
+      if (lane == 31) sums[0][warp] = s;
       __syncthreads();
-      if (warp == 0) {                                           // the value at which the count from above reaches `left`
-        uint32_t own[8], sum = 0;
+      uint32_t over = s - both;
+      for (int w = 0; w < warp; ++w) over += sums[0][w];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += own[i] = count[255 - (lane * 8 + i)];
-        uint32_t above = sum;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, above, o);
-          if (lane >= o) above += t;
+      for (int i = 0; i < 2; ++i) {
+        if (over < left && left <= over + bin[i]) {
+          chosen[0] = (uint32_t)(C::BINS - 1 - (2 * tid + i));
+          chosen[1] = left - over;
         }
-        above -= sum;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          if (above < left && left <= above + own[i]) {
-            chosen[0] = 255u - (lane * 8 + i);
-            chosen[1] = left - above;
-          }
-          above += own[i];
-        }
+        over += bin[i];
       }
       __syncthreads();
       edge |= chosen[0] << shift;
       left = chosen[1];
+      above = shift;
+      __syncthreads();                                           // `sums` and `chosen` are written again
+    }
+  }
+  auto key_of = [&](int i) { return held ? keys[i] : read(i); };
+  // how many of the parts in front stay, and equal the edge
+  uint32_t equal_before = 0, kept_before = 0;
+  if (room > 0 && cluster > 1) {
+    if (tid < 2) mine[tid] = 0;
+    __syncthreads();
+    uint32_t more = 0, same = 0;
+    for (int i = tid; i < n; i += C::THREADS) {
+      const uint32_t key = all ? 1u : key_of(i);
+      more += key > edge;
+      same += key == edge;
+    }
+    more = __reduce_add_sync(0xFFFFFFFFu, more);
+    same = __reduce_add_sync(0xFFFFFFFFu, same);
+    if (lane == 0) {
+      atomicAdd(&mine[0], more);
+      atomicAdd(&mine[1], same);
+    }
+    cluster_sync_all();
+    for (int r = 0; r < rank; ++r) {
+      const uint32_t m = load_cluster_u32(map_to_cta(smem_u32(&mine[0]), (uint32_t)r)), e = load_cluster_u32(map_to_cta(smem_u32(&mine[1]), (uint32_t)r));
+      kept_before += m + (equal_before >= left ? 0u : min(e, left - equal_before));
+      equal_before += e;
     }
   }
   // places in their order: a thread takes EACH consecutive ones
-  uint32_t equal_before = 0, kept_before = 0;
-  for (int base = 0; base < others && room > 0; base += KvSelectCfg::THREADS * KvSelectCfg::EACH) {
-    uint32_t above[KvSelectCfg::EACH], equal[KvSelectCfg::EACH], equals = 0;
+  for (int base = 0; base < n && room > 0; base += C::THREADS * C::EACH) {
+    uint32_t above[C::EACH], equal[C::EACH], equals = 0;
 #pragma unroll
-    for (int i = 0; i < KvSelectCfg::EACH; ++i) {
-      const int j = base + tid * KvSelectCfg::EACH + i;
-      const uint32_t key = j < others ? (room == others ? 1u : key_of(j)) : 0u;
-      above[i] = j < others && key > edge;
-      equals += equal[i] = j < others && key == edge;
+    for (int i = 0; i < C::EACH; ++i) {
+      const int j = base + tid * C::EACH + i;
+      const uint32_t key = j < n ? (all ? 1u : key_of(j)) : 0u;
+      above[i] = j < n && key > edge;
+      equals += equal[i] = j < n && key == edge;
     }
-    auto before = [&](uint32_t mine, int which, uint32_t& total) {       // of the threads in front; the same for all in `total`
-      uint32_t s = mine;
+    auto before = [&](uint32_t own, int which, uint32_t& total) {        // of the threads in front; the same for all in `total`
+      uint32_t s = own;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, s, o);
@@ -82,62 +134,85 @@ static __global__ void __launch_bounds__(KvSelectCfg::THREADS) kv_select_kernel(
       }
       if (lane == 31) sums[which][warp] = s;
       __syncthreads();
-      if (warp == 0) {
-        uint32_t w = sums[which][lane], v = w;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const uint32_t t = __shfl_up_sync(0xFFFFFFFFu, v, o);
-          if (lane >= o) v += t;
-        }
-        sums[which][lane] = v - w;
-        if (lane == 31) sums[which][32] = v;
-      }
-      __syncthreads();
-      total = sums[which][32];
-      return s - mine + sums[which][warp];
+      uint32_t front = 0;
+      total = 0;
+      const uint32_t w = sums[which][lane];
+      total = __reduce_add_sync(0xFFFFFFFFu, w);
+      front = __reduce_add_sync(0xFFFFFFFFu, lane < warp ? w : 0u);
+      return s - own + front;
     };
-    uint32_t total, rank = equal_before + before(equals, 0, total), stays = 0, flag[KvSelectCfg::EACH];
+    uint32_t total, order = equal_before + before(equals, 0, total), stays = 0, flag[C::EACH];
     equal_before += total;
 #pragma unroll
-    for (int i = 0; i < KvSelectCfg::EACH; ++i) {
-      flag[i] = above[i] | (equal[i] & (uint32_t)(rank < left));
-      rank += equal[i];
+    for (int i = 0; i < C::EACH; ++i) {
+      flag[i] = above[i] | (equal[i] & (uint32_t)(order < left));
+      order += equal[i];
       stays += flag[i];
     }
     uint32_t at = kept_before + before(stays, 1, total);
     kept_before += total;
 #pragma unroll
-    for (int i = 0; i < KvSelectCfg::EACH; ++i)
-      if (flag[i]) to[at++] = base + tid * KvSelectCfg::EACH + i;
+    for (int i = 0; i < C::EACH; ++i)
+      if (flag[i]) to[at++] = first + base + tid * C::EACH + i;
     __syncthreads();                                             // `sums` is written again
   }
-  for (int r = room + tid; r < keep; r += KvSelectCfg::THREADS) to[r] = r < stay ? others + (r - room) : -1;
+  for (int r = room + rank * C::THREADS + tid; r < keep; r += cluster * C::THREADS) to[r] = r < stay ? others + (r - room) : -1;
+  if (cluster > 1) cluster_sync_all();                           // others may still read this CTA's shared memory
 }
 
-// D / 16 threads per token that stays, 32 codes and their scales each.
+// D / 16 threads per token that stays, 32 codes and their scales each, EACH tokens at a time: a copy hangs on three loads one behind the other.
 template <int FMT>
 __global__ void __launch_bounds__(256) kv_move_kernel(const KvView c, float* weights, const int32_t* new_table, int new_width, int keep,
                                                       const int32_t* kept) {
   griddep_wait_and_launch();
-  const int per_token = c.dim / 16, head = blockIdx.y % c.heads, b = blockIdx.y / c.heads;
-  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < (int64_t)keep * per_token; at += (int64_t)gridDim.x * 256) {
-    const int r = (int)(at / per_token), e = (int)(at % per_token);
-    const int j = kept[(int64_t)blockIdx.y * keep + r];
-    if (j < 0) break;                                            // nothing behind it either
-    const int from = kv_page(c, c.table, c.width, b, j), to = (r >> c.page_shift) < new_width ? kv_page(c, new_table, new_width, b, r) : -1;
-    if (from < 0 || to < 0) continue;
-    const int mask = (1 << c.page_shift) - 1, blocks = c.dim / kv_block(FMT), half = per_token / 2, chunk = e < half ? e : e - half;
-    const uint8_t* s = kv_head_page(c, from, head);
-    uint8_t* d = kv_head_page(c, to, head);
-    const int codes = (e < half ? 0 : c.v_codes) + chunk * 16, scales = (e < half ? c.k_scales : c.v_scales) + chunk * (32 / kv_block(FMT));
-    *reinterpret_cast<uint4*>(d + codes + (r & mask) * (c.dim / 2)) = *reinterpret_cast<const uint4*>(s + codes + (j & mask) * (c.dim / 2));
-    if constexpr (FMT == FMT_NVFP4)
-      *reinterpret_cast<uint16_t*>(d + scales + (r & mask) * blocks) = *reinterpret_cast<const uint16_t*>(s + scales + (j & mask) * blocks);
-    else
-      d[scales + (r & mask) * blocks] = s[scales + (j & mask) * blocks];
-    if (e == 0)
-      weights[(((int64_t)to * c.heads + head) << c.page_shift) + (r & mask)] =
-          weights[(((int64_t)from * c.heads + head) << c.page_shift) + (j & mask)];
+  constexpr int EACH = 4;
+  const int shift = 31 - __clz(c.dim / 16), head = blockIdx.y % c.heads, b = blockIdx.y / c.heads, mask = (1 << c.page_shift) - 1;
+  const int e = threadIdx.x & ((1 << shift) - 1), half = 1 << shift >> 1, chunk = e & (half - 1), blocks = c.dim / kv_block(FMT);
+  const int codes_at = (e < half ? 0 : c.v_codes) + chunk * 16, scales_at = (e < half ? c.k_scales : c.v_scales) + chunk * (32 / kv_block(FMT));
+  const int per_cta = 256 >> shift;
+  for (int64_t r0 = (int64_t)blockIdx.x * per_cta * EACH + (threadIdx.x >> shift); r0 < keep; r0 += (int64_t)gridDim.x * per_cta * EACH) {
+    int j[EACH];
+    const uint8_t* from[EACH];
+    uint8_t* to[EACH];
+    int64_t w_from[EACH], w_to[EACH];
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      const int64_t r = r0 + u * per_cta;
+      j[u] = r < keep ? kept[(int64_t)blockIdx.y * keep + r] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      const int r = (int)(r0 + u * per_cta);
+      to[u] = nullptr;
+      if (j[u] < 0) continue;
+      const int page = kv_page(c, c.table, c.width, b, j[u]), there = (r >> c.page_shift) < new_width ? kv_page(c, new_table, new_width, b, r) : -1;
+      if (page < 0 || there < 0) continue;
+      from[u] = kv_head_page(c, page, head);
+      to[u] = kv_head_page(c, there, head);
+      w_from[u] = (((int64_t)page * c.heads + head) << c.page_shift) + (j[u] & mask);
+      w_to[u] = (((int64_t)there * c.heads + head) << c.page_shift) + (r & mask);
+    }
+    uint4 codes[EACH];
+    uint32_t scales[EACH];
+    float weight[EACH];
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      if (!to[u]) continue;
+      codes[u] = *reinterpret_cast<const uint4*>(from[u] + codes_at + (j[u] & mask) * (c.dim / 2));
+      const uint8_t* s = from[u] + scales_at + (j[u] & mask) * blocks;
+      scales[u] = FMT == FMT_NVFP4 ? *reinterpret_cast<const uint16_t*>(s) : *s;
+      if (e == 0) weight[u] = weights[w_from[u]];
+    }
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      if (!to[u]) continue;
+      const int slot = (int)(r0 + u * per_cta) & mask;
+      *reinterpret_cast<uint4*>(to[u] + codes_at + slot * (c.dim / 2)) = codes[u];
+      uint8_t* s = to[u] + scales_at + slot * blocks;
+      if constexpr (FMT == FMT_NVFP4) *reinterpret_cast<uint16_t*>(s) = (uint16_t)scales[u];
+      else *s = (uint8_t)scales[u];
+      if (e == 0) weights[w_to[u]] = weight[u];
+    }
   }
 }
 
