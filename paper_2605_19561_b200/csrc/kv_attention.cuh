@@ -189,17 +189,20 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
     int64_t page[2];                                                       // where the pages of the next step's two groups of 16 tokens begin
     bool there[2];
     auto look_up = [&](int k) {
+      int p[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int j = first + k * C::STEP + 16 * i;
         there[i] = k < steps && j < it.hi && j + 16 > it.lo;
-        page[i] = 0;
-        if (there[i]) {
-          const int p = table[j >> c.page_shift];
-          there[i] = (unsigned)p < (unsigned)c.num_pages;
-          if (there[i]) page[i] = p * c.page_bytes;
-          else kv_bad_page(c);
+        p[i] = there[i] ? table[j >> c.page_shift] : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (there[i] && (unsigned)p[i] >= (unsigned)c.num_pages) {
+          kv_bad_page(c);
+          there[i] = false;
         }
+        page[i] = there[i] ? p[i] * c.page_bytes : 0;
       }
     };
     uint32_t dst = ring;                                                   // the stage that is filled next
@@ -671,17 +674,20 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
     int64_t page[2];
     bool there[2];
     auto look_up = [&](int k) {
+      int p[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int j = first + 32 * k + 16 * i;
         there[i] = k < steps && j < it.length && j + 16 > it.lo;
-        page[i] = 0;
-        if (there[i]) {
-          const int p = table[j >> c.page_shift];
-          there[i] = (unsigned)p < (unsigned)c.num_pages;
-          if (there[i]) page[i] = p * c.page_bytes;
-          else kv_bad_page(c);
+        p[i] = there[i] ? table[j >> c.page_shift] : 0;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (there[i] && (unsigned)p[i] >= (unsigned)c.num_pages) {
+          kv_bad_page(c);
+          there[i] = false;
         }
+        page[i] = there[i] ? p[i] * c.page_bytes : 0;
       }
     };
     uint32_t dst = ring;

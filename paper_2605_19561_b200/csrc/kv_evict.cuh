@@ -41,8 +41,32 @@ static __global__ void __launch_bounds__(KvSelectCfg::THREADS) kv_select_kernel(
   const bool all = room == others, select = !all && room > 0;
   if (select) {
     if (held) {
-#pragma unroll 4
-      for (int i = tid; i < n; i += C::THREADS) keys[i] = read(i);
+      // eight at a time, all loads of one kind before the first is looked at
+      constexpr int EACH = 8;
+      for (int i0 = tid; i0 < n; i0 += EACH * C::THREADS) {
+        int page[EACH];
+        float w[EACH];
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+          const int i = i0 + u * C::THREADS;
+          page[u] = i < n ? c.table[(int64_t)b * c.width + ((first + i) >> c.page_shift)] : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+          const int i = i0 + u * C::THREADS, j = first + i;
+          w[u] = 0.f;
+          if (i < n && (unsigned)page[u] < (unsigned)c.num_pages)
+            w[u] = weights[(((int64_t)page[u] * c.heads + head) << c.page_shift) + (j & ((1 << c.page_shift) - 1))];
+        }
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+          const int i = i0 + u * C::THREADS;
+          if (i >= n) break;
+          const bool good = (unsigned)page[u] < (unsigned)c.num_pages;
+          if (!good) kv_bad_page(c);
+          keys[i] = good ? ordered_key(w[u]) : 0u;
+        }
+      }
     }
     int above = 32;                                              // bits above which `edge` is known
     for (int pass = 0; pass < 3; ++pass) {
@@ -57,13 +81,17 @@ static __global__ void __launch_bounds__(KvSelectCfg::THREADS) kv_select_kernel(
       if (cluster > 1) cluster_sync_all();
       else __syncthreads();
       // two bins to a thread, the largest values first
-      uint32_t bin[2] = {0, 0};
-      for (int r = 0; r < cluster; ++r)
+      uint32_t bin[2], of[8][2];                                 // all loads on their way before the first is used
+#pragma unroll
+      for (int r = 0; r < 8; ++r)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int value = C::BINS - 1 - (2 * tid + i);
-          bin[i] += cluster > 1 ? load_cluster_u32(map_to_cta(smem_u32(own + value), (uint32_t)r)) : own[value];
+          of[r][i] = 0;
+          if (r < cluster) of[r][i] = cluster > 1 ? load_cluster_u32(map_to_cta(smem_u32(own + value), (uint32_t)r)) : own[value];
         }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) bin[i] = ((of[0][i] + of[1][i]) + (of[2][i] + of[3][i])) + ((of[4][i] + of[5][i]) + (of[6][i] + of[7][i]));
       uint32_t s = bin[0] + bin[1];
       const uint32_t both = s;
 #pragma unroll
@@ -73,8 +101,7 @@ static __global__ void __launch_bounds__(KvSelectCfg::THREADS) kv_select_kernel(
       }
       if (lane == 31) sums[0][warp] = s;
       __syncthreads();
-      uint32_t over = s - both;
-      for (int w = 0; w < warp; ++w) over += sums[0][w];
+      uint32_t over = s - both + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sums[0][lane] : 0u);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         if (over < left && left <= over + bin[i]) {
@@ -180,13 +207,24 @@ __global__ void __launch_bounds__(256) kv_move_kernel(const KvView c, float* wei
       const int64_t r = r0 + u * per_cta;
       j[u] = r < keep ? kept[(int64_t)blockIdx.y * keep + r] : -1;
     }
+    int page_of[EACH], there_of[EACH];                           // all loads before the first is looked at
 #pragma unroll
     for (int u = 0; u < EACH; ++u) {
       const int r = (int)(r0 + u * per_cta);
+      page_of[u] = there_of[u] = 0;
+      if (j[u] < 0) continue;
+      page_of[u] = c.table[(int64_t)b * c.width + (j[u] >> c.page_shift)];
+      there_of[u] = (r >> c.page_shift) < new_width ? new_table[(int64_t)b * new_width + (r >> c.page_shift)] : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      const int r = (int)(r0 + u * per_cta), page = page_of[u], there = there_of[u];
       to[u] = nullptr;
       if (j[u] < 0) continue;
-      const int page = kv_page(c, c.table, c.width, b, j[u]), there = (r >> c.page_shift) < new_width ? kv_page(c, new_table, new_width, b, r) : -1;
-      if (page < 0 || there < 0) continue;
+      if ((unsigned)page >= (unsigned)c.num_pages || (unsigned)there >= (unsigned)c.num_pages) {
+        kv_bad_page(c);
+        continue;
+      }
       from[u] = kv_head_page(c, page, head);
       to[u] = kv_head_page(c, there, head);
       w_from[u] = (((int64_t)page * c.heads + head) << c.page_shift) + (j[u] & mask);

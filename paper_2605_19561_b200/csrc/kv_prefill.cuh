@@ -372,19 +372,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
       const int groups = (it.tiles + 1) / 2;
       int page[N];                                                         // of the next group's chunks; -1: nothing there
-      auto look_up = [&](int g) {
+      auto look_up = [&](int g) {                                          // all loads before the first is looked at
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const int j = it.base + g * 128 + row0 + i * (128 / CH);
-          page[i] = -1;
-          if (g < groups && j < it.hi) {
-            page[i] = table[j >> c.page_shift];
-            if ((unsigned)page[i] >= (unsigned)c.num_pages) {
-              kv_bad_page(c);
-              page[i] = -1;
-            }
-          }
+          page[i] = g < groups && j < it.hi ? table[j >> c.page_shift] : -1;
         }
+      };
+      auto check = [&](int g) {
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          bad |= g < groups && it.base + g * 128 + row0 + i * (128 / CH) < it.hi && (unsigned)page[i] >= (unsigned)c.num_pages;
+          if ((unsigned)page[i] >= (unsigned)c.num_pages) page[i] = -1;
+        }
+        if (bad) kv_bad_page(c);
       };
       uint4 codes[2][N];
       uint32_t scale[2][N], next_scale[N];                                 // zero where there is nothing; the values' of the next group
@@ -417,6 +419,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         load_codes(g, 1);
       };
       look_up(0);
+      check(0);
       load_keys(0);
       load_values(0);
       look_up(1);
@@ -476,8 +479,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
               ++fill;
             }
           }
-          if (half == 0) load_keys(g + 1);
-          else load_values(g + 1);
+          if (half == 0) {
+            check(g + 1);
+            load_keys(g + 1);
+          } else {
+            load_values(g + 1);
+          }
         }
         look_up(g + 2);
       }
