@@ -25,8 +25,10 @@ template <int FMT_, int D_>
 struct KvPrefillCfg {
   static constexpr int FMT = FMT_, D = D_, TILES = D == 256 ? 1 : 2, ROWS = 128 * TILES, TOK = 64;
   static constexpr int CH = D / 32, SB = D / kv_block(FMT), THREADS = 512;
-  static constexpr int Q_BYTES = 128 * D * 2, KV_BYTES = TOK * D * 2, STAGES = D == 256 ? 5 : 8;
-  static constexpr int INFO_AT = TILES * Q_BYTES + STAGES * KV_BYTES, SMEM = INFO_AT + 256 + 1024;
+  static constexpr int Q_BYTES = 128 * D * 2, KV_BYTES = TOK * D * 2;
+  // A fill of the ring: the keys, or the values, of FT tiles (every barrier costs its waiters 100 to 300 cycles, so they are few).
+  static constexpr int FT = D == 256 ? 1 : 2, STAGES = D == 256 ? 5 : 4, FILL_BYTES = FT * KV_BYTES;
+  static constexpr int INFO_AT = TILES * Q_BYTES + STAGES * FILL_BYTES, SMEM = INFO_AT + 256 + 1024;
   static constexpr int O_COL = 256;
   static_assert(SMEM <= 232448, "shared memory");
 };
@@ -155,10 +157,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
     const bool special = a.softcap > 0.f || a.slopes;
     uint32_t phases[2] = {0, 0}, group_no = 0;                             // of s_full; of 128 tokens, over all items
     bool ok = true;
-    for (long long index = blockIdx.x; ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
+    // Two tiles of rows weigh in turn: side by side they wait for the exponentials of one another and then leave that unit idle together (2048 tokens behind
+    // 6144: 317 us, in turn 304).  The barriers for that are executed for every tile of tokens, also after a wait has given up, so that no warp is left in
+    // one.
+    for (long long index = blockIdx.x; kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
       const uint32_t first_group = group_no;
       group_no += (it.tiles + 1) / 2;
       if (128 * t >= it.rows) continue;
+      const bool in_turn = it.rows > 128;
       // S of tile k, or what comes after the last ones, is number k of its item on s_full: at k it is there, and P V of tile k - 2 is done
       auto wait_s = [&](int k) {
         ok = ok && mbar_wait_warp(s_full(t, k & 1), (phases[k & 1] + (k >> 1)) & 1, cta_abort, c.err_word, SITE_EPI_ACC_FULL);
@@ -195,7 +201,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           uint4 y;
 #pragma unroll
           for (int i = 0; i < 4; ++i) (&y.x)[i] = pack_f16(v[kv_query_order<FMT>(i, 0)], v[kv_query_order<FMT>(i, 1)]);
-          *reinterpret_cast<uint4*>(dst + (e >> 3) * (128 * 128) + (((e & 7) ^ (row & 7)) << 4)) = y;
+          if (ok) *reinterpret_cast<uint4*>(dst + (e >> 3) * (128 * 128) + (((e & 7) ^ (row & 7)) << 4)) = y;
         }
         factor = __uint_as_float((254u - field) << 23) * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e);
         if (there) {
@@ -204,12 +210,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         }
       }
       fence_proxy_async_smem();
-      mbar_arrive(q_full(t));
+      if (ok) mbar_arrive(q_full(t));
+      const int clear_lo = (int)__reduce_max_sync(0xFFFFFFFFu, there ? (uint32_t)max(lo, 0) : 0u);          // tiles within [clear_lo, clear_hi) need no mask
+      const int clear_hi = (int)__reduce_min_sync(0xFFFFFFFFu, there ? (uint32_t)max(hi, 0) : 0x7FFFFFFFu);
 
       float m = -1e30f, l = 0.f;
       int e_max = 27;
+      if (in_turn && t == 1) named_barrier_arrive(2, 256);                 // the first tile's turn
       for (int k = 0; k < it.tiles; ++k) {
-        if (!wait_s(k)) break;
+        if (!wait_s(k)) {
+          if (in_turn) {
+            named_barrier_sync(2 + t, 256);
+            named_barrier_arrive(3 - t, 256);
+          }
+          continue;
+        }
         tc_fence_after_sync();
         const int j0 = it.base + k * TOK;
         const uint32_t s_at = tmem + lanes + (2 * t + (k & 1)) * TOK;
@@ -226,11 +241,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           if (special) x = kv_score(x * kLn2, a.softcap, slope, abs(place - j));
           return j >= lo && j < hi ? x : -INFINITY;
         };
-        const bool slow = special || __any_sync(0xFFFFFFFFu, there && (j0 < lo || j0 + TOK > hi));
+        const bool slow = special || j0 < clear_lo || j0 + TOK > clear_hi;
         const int e_old = e_max;
         e_max = max(e_max, e_tile);
         const int down = e_max - e_tile;                                   // this tile's values are smaller: so are its weights
         const bool faint = down > 40;                                      // too small to matter, but they count in the sum
+        bool wrong = e_max != e_old;                                       // whether some row's O has to be corrected
         float fix = e_max - e_old > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (e_max - e_old)) << 23);      // of O
         const float off0 = kShift - (faint ? 0.f : (float)down);
         auto raised = [&](float top) {                                     // m is no longer near enough to the largest score
@@ -268,14 +284,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           sum = halves(sums).x + halves(sums).y;
           top = fmaxf(tops[0], tops[1]) * f;
         };
+        if (in_turn) named_barrier_sync(2 + t, 256);
         if (!slow) {
           weigh();
+          if (in_turn) named_barrier_arrive(3 - t, 256);
           if (__any_sync(0xFFFFFFFFu, top > m + kSlack)) {
+            wrong = true;
             raised(top);
             __syncwarp();
             weigh();
           }
         } else {
+          if (in_turn) named_barrier_arrive(3 - t, 256);
 #pragma unroll 1
           for (int x = 0; x < TOK; x += 32) {
             uint32_t v[32];
@@ -285,11 +305,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
             for (int i = 0; i < 32; ++i) top = fmaxf(top, score(__uint_as_float(v[i]), x + i));
             __syncwarp();
           }
+          wrong |= __any_sync(0xFFFFFFFFu, top > m + kSlack);
           raised(top);
           __syncwarp();
         }
-        if (k > 0 && __any_sync(0xFFFFFFFFu, fix != 1.f)) {
-          if (!wait_s(k + 1)) break;                                       // the products of the tile before are done
+        if (k > 0 && wrong) {
+          if (!wait_s(k + 1)) continue;                                    // the products of the tile before are done
           tc_fence_after_sync();
 #pragma unroll 1
           for (int x = 0; x < D; x += 16) {
@@ -330,9 +351,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         tc_fence_before_sync();
         mbar_arrive(p_full(t, k & 1));
       }
-      if (!ok || !wait_s(it.tiles + 1)) break;
+      if (in_turn && t == 0) named_barrier_sync(2, 256);                   // the second tile's last turn is over
+      wait_s(it.tiles + 1);
       phases[0] += (it.tiles + 3) / 2;
       phases[1] += (it.tiles + 2) / 2;
+      if (!ok) continue;
       tc_fence_after_sync();
       const float inv = (l > 0.f ? 1.f / l : 0.f) * (FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(e_max - 12) << 23));
       const int64_t to = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
@@ -418,22 +441,29 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         for (int i = 0; i < N; ++i) scale[1][i] = next_scale[i];
         load_codes(g, 1);
       };
+      // this warp's largest scale bytes of a group, keys' and values'
+      auto tell_top = [&](uint32_t no) {
+        if constexpr (FMT != FMT_NVFP4) {
+          uint32_t top[2] = {27, 27};
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            top[0] = max(top[0], scale[0][i]);
+            top[1] = max(top[1], next_scale[i]);
+          }
+          top[0] = __reduce_max_sync(0xFFFFFFFFu, top[0]);
+          top[1] = __reduce_max_sync(0xFFFFFFFFu, top[1]);
+          if (lane < 2) warp_top[(no & 1) * 8 + dw * 2 + lane] = (int)(lane ? top[1] : top[0]);
+        }
+      };
       look_up(0);
       check(0);
       load_keys(0);
+      tell_top(group_no);
       load_values(0);
       look_up(1);
       for (int g = 0; g < groups; ++g, ++group_no) {
         int down[2] = {0, 0};                                              // 27 - E
         if constexpr (FMT != FMT_NVFP4) {
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t top = 27;
-#pragma unroll
-            for (int i = 0; i < N; ++i) top = max(top, scale[half][i]);
-            top = __reduce_max_sync(0xFFFFFFFFu, top);
-            if (lane == 0) warp_top[(group_no & 1) * 8 + dw * 2 + half] = (int)top;
-          }
           named_barrier_sync(1, 128);
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
@@ -449,9 +479,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
 #pragma unroll
           for (int tile = 0; tile < 2; ++tile) {
             if (tile < tiles) {
-              if (ok) ok = mbar_wait_warp(kv_empty(fill), ((fill / C::STAGES) & 1) ^ 1, cta_abort, c.err_word, SITE_PRODUCER_EMPTY);
+              if (tile % C::FT == 0 && ok)
+                ok = mbar_wait_warp(kv_empty(fill), ((fill / C::STAGES) & 1) ^ 1, cta_abort, c.err_word, SITE_PRODUCER_EMPTY);
               if (ok) {
-                uint8_t* dst = smem_p + C::TILES * C::Q_BYTES + (fill % C::STAGES) * C::KV_BYTES + (ch >> 1) * (TOK * 128);
+                uint8_t* dst = smem_p + C::TILES * C::Q_BYTES + (fill % C::STAGES) * C::FILL_BYTES + tile % C::FT * C::KV_BYTES + (ch >> 1) * (TOK * 128);
 #pragma unroll
                 for (int i = tile * (N / 2); i < (tile + 1) * (N / 2); ++i) {
                   const int r = (row0 + i * (128 / CH)) & (TOK - 1);
@@ -473,11 +504,16 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
                     *reinterpret_cast<uint4*>(dst + r * 128 + ((((ch & 1) * 4 + x) ^ (r & 7)) << 4)) = y;
                   }
                 }
-                fence_proxy_async_smem();
-                mbar_arrive(kv_full(fill));
               }
-              ++fill;
+              if (tile % C::FT == C::FT - 1 || tile == tiles - 1) {
+                if (ok) {
+                  fence_proxy_async_smem();
+                  mbar_arrive(kv_full(fill));
+                }
+                ++fill;
+              }
             }
+            if (half == 1 && tile == 0) tell_top(group_no + 1);            // of the next group, whose scale bytes have come meanwhile
           }
           if (half == 0) {
             check(g + 1);
@@ -506,34 +542,44 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       // number i: P V of tile i - 2, then S of tile i into the place of that P
       for (int i = 0; i < tiles + 2 && ok; ++i) {
         const int k = i - 2;
-        const uint32_t kf = fill + 4 * (i >> 1) + (i & 1), vf = fill + 4 * (k >> 1) + min(2, tiles - (k & ~1)) + (k & 1);
-        if (k >= 0) ok = mbar_wait_warp(kv_full(vf), (vf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
-        if (ok && i < tiles) ok = mbar_wait_warp(kv_full(kf), (kf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
+        // the fills of tile i's keys and of tile k's values, and whether a tile is the first or last of its fill
+        uint32_t kf, vf;
+        if constexpr (C::FT == 2) {
+          kf = fill + 2 * (i >> 1);
+          vf = fill + 2 * (k >> 1) + 1;
+        } else {
+          kf = fill + 4 * (i >> 1) + (i & 1);
+          vf = fill + 4 * (k >> 1) + min(2, tiles - (k & ~1)) + (k & 1);
+        }
+        const bool k_first = i % C::FT == 0, k_last = i % C::FT == C::FT - 1 || i == tiles - 1, v_first = k % C::FT == 0,
+                   v_last = k % C::FT == C::FT - 1 || k == tiles - 1;
+        if (k >= 0 && v_first) ok = mbar_wait_warp(kv_full(vf), (vf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
+        if (ok && i < tiles && k_first) ok = mbar_wait_warp(kv_full(kf), (kf / C::STAGES) & 1, cta_abort, c.err_word, SITE_MMA_FULL);
         if (ok && active && k >= 0) ok = mbar_wait_warp(p_full(t, i & 1), p_count[i & 1]++ & 1, cta_abort, c.err_word, SITE_MMA_ACC_EMPTY);
         if (!ok) break;
         tc_fence_after_sync();
         const uint32_t s_at = tm + (2 * t + (i & 1)) * TOK;
         if (elect_one()) {
           if (active && k >= 0) {
-            const uint64_t v = make_desc(sm + C::TILES * C::Q_BYTES + (vf % C::STAGES) * C::KV_BYTES, TOK * 128, 1024, kSwizzle128);
+            const uint64_t v = make_desc(sm + C::TILES * C::Q_BYTES + (vf % C::STAGES) * C::FILL_BYTES + k % C::FT * C::KV_BYTES, TOK * 128, 1024, kSwizzle128);
 #pragma unroll
             for (int x = 0; x < TOK / 16; ++x)             // 16 tokens: 8 columns of P, 16 rows of V (2 KiB)
               mma_bf16_tmem_a(o_at, s_at + 8 * x, v + 128 * x, idesc_o, k > 0 || x > 0);
           }
           if (active && i < tiles) {
             const uint64_t q = make_desc(sm + t * C::Q_BYTES, 16, 1024, kSwizzle128);
-            const uint64_t y = make_desc(sm + C::TILES * C::Q_BYTES + (kf % C::STAGES) * C::KV_BYTES, 16, 1024, kSwizzle128);
+            const uint64_t y = make_desc(sm + C::TILES * C::Q_BYTES + (kf % C::STAGES) * C::FILL_BYTES + i % C::FT * C::KV_BYTES, 16, 1024, kSwizzle128);
 #pragma unroll
             for (int x = 0; x < D / 16; ++x)               // 16 elements: 32 bytes of a row of 128
               mma_bf16(s_at, q + (x >> 2) * (128 * 128 / 16) + 2 * (x & 3), y + (x >> 2) * (TOK * 128 / 16) + 2 * (x & 3), idesc_s, x > 0);
           }
           if (active) tc_commit(s_full(t, i & 1));
-          if (k >= 0) tc_commit(kv_empty(vf));             // a tile of rows that is not there gives the tokens back as they come
-          if (i < tiles) tc_commit(kv_empty(kf));
+          if (k >= 0 && v_last) tc_commit(kv_empty(vf));             // a tile of rows that is not there gives the tokens back as they come
+          if (i < tiles && k_last) tc_commit(kv_empty(kf));
         }
         __syncwarp();
       }
-      fill += 2 * tiles;
+      fill += C::FT == 2 ? 2 * ((tiles + 1) / 2) : 2 * tiles;
     }
   }
 
