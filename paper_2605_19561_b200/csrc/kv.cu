@@ -148,11 +148,13 @@ static torq_status read_impl(const torq_kv_cache* cache, const int32_t* starts, 
 }
 
 // ---- few queries per sequence
-constexpr int kMaxRanges = 2560;         // warps of the streaming kernel: the workspace does not depend on the device
-static int decode_groups(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads) {
-  return (tokens + batch - 1) / batch * (heads / kv_heads) <= 8 ? 1 : 2;
+// Warps of the streaming kernel at most: the workspace does not depend on the device.
+constexpr int max_ranges(int groups) { return groups == 1 ? 2560 : 1280; }
+// Rows of a sequence that are worked on at once, in eights.  Heads of 256: always eight rows, since the registers do not hold more.
+static int decode_groups(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t dim) {
+  return dim >= 256 || (tokens + batch - 1) / batch * (heads / kv_heads) <= 8 ? 1 : 2;
 }
-static size_t decode_workspace(int groups, int64_t dim) { return (size_t)kMaxRanges * 2 * 8 * groups * (size_t)(dim + 2) * sizeof(float); }
+static size_t decode_workspace(int groups, int64_t dim) { return (size_t)max_ranges(groups) * 2 * 8 * groups * (size_t)(dim + 2) * sizeof(float); }
 
 template <int FMT, int D, int NT>
 static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, const void* Q, int64_t q_stride, int heads, void* out, float* lse,
@@ -160,7 +162,7 @@ static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, c
   using C = KvDecodeCfg<FMT, D, NT>;
   constexpr auto kernel = kv_decode_kernel<C>;
   if (!opt_in<kernel>(C::SMEM)) return TORQ_ERR_LAUNCH;
-  const int most = sms * C::CTAS, ctas = most < kMaxRanges / C::WARPS ? most : kMaxRanges / C::WARPS, group = heads / v.heads;
+  const int most = sms * C::CTAS, ctas = most < max_ranges(NT) / C::WARPS ? most : max_ranges(NT) / C::WARPS, group = heads / v.heads;
   float* partials = static_cast<float*>(workspace);
   __nv_bfloat16* y = static_cast<__nv_bfloat16*>(out);
   launch_tc(kernel, 1, dim3((unsigned)ctas), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads, y, lse, partials);
@@ -187,8 +189,16 @@ static torq_status prefill_launch(const KvView& v, const KvScoring& a, int sms, 
             static_cast<__nv_bfloat16*>(out), lse);
   return launch_status();
 }
-static bool many_rows(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads) {
-  return tokens / batch * (heads / kv_heads) >= 64;
+// Which of the two.  The kernel for many queries gives a CTA up to 256 rows of a head (128 of 256 dimensions) and all their cached tokens: as long as
+// there is one CTA for each, it takes as long for one row as for all of them.  The streaming kernel divides whatever there is evenly.  A CTA of the first
+// takes as long for its tokens as the second does for 64 rows on one SM.  Measured, streaming against the other, us:
+//   16 sequences of up to 5000 tokens, 8 heads of 128:  64 rows at most 71, 92;  128: 137, 94;  512: 426, 168
+//   one sequence of 32768 tokens, 8 heads of 128:  64 rows 61, 527;  512: 369, 595;  1024: 722, 612
+//   64 sequences of up to 3000 tokens, 4 heads of 128:  64 rows 91, 115;  96: 133, 116
+//   8 sequences of up to 5000 tokens, 8 heads of 256:  128 rows 129, 217;  256: 300, 213
+static bool many_rows(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t dim, int sms) {
+  const int64_t rows = tokens / batch * (heads / kv_heads), items = batch * kv_heads, tile = dim == 256 ? 128 : 256;
+  return rows * items >= 64 * sms * ((items * ((rows + tile - 1) / tile) + sms - 1) / sms);
 }
 
 template <int FMT>
@@ -208,11 +218,13 @@ static torq_status attention_impl(const torq_kv_cache* cache, const torq_kv_scor
   int sms;
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
   cudaStream_t stm = static_cast<cudaStream_t>(stream);
-  const bool one = decode_groups(tokens, cache->batch, heads, v.heads) == 1, many = many_rows(tokens, cache->batch, heads, v.heads);
-  with_dim(v.dim, [&](auto D) {
-    rc = many ? prefill_launch<FMT, decltype(D)::value>(v, a, sms, Q, q_stride, (int)heads, out, lse, stm)
-         : one ? decode_launch<FMT, decltype(D)::value, 1>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm)
-             : decode_launch<FMT, decltype(D)::value, 2>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
+  const int groups = decode_groups(tokens, cache->batch, heads, v.heads, v.dim);
+  const bool many = many_rows(tokens, cache->batch, heads, v.heads, v.dim, sms);
+  with_dim(v.dim, [&](auto DIM) {
+    constexpr int D = decltype(DIM)::value;
+    if (many) rc = prefill_launch<FMT, D>(v, a, sms, Q, q_stride, (int)heads, out, lse, stm);
+    else if (groups == 1) rc = decode_launch<FMT, D, 1>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
+    else if constexpr (D < 256) rc = decode_launch<FMT, D, 2>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
   });
   return rc;
 }
@@ -286,7 +298,7 @@ size_t torq_kv_page_bytes(int64_t scale_block, int64_t page_tokens, int64_t head
 
 size_t torq_kv_attention_workspace_bytes(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t head_dim) {
   if (tokens < 1 || batch < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || head_dim < 1) return 0;
-  return decode_workspace(decode_groups(tokens, batch, heads, kv_heads), head_dim);
+  return decode_workspace(decode_groups(tokens, batch, heads, kv_heads, head_dim), head_dim);
 }
 
 #define TORQ_KV_ENTRIES(name, FMT)                                                                                                                   \

@@ -80,12 +80,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   return r;
 }
 
-// Registers per thread of a warpgroup, all its warps; N a multiple of 8.  The sum over the CTA may not exceed what it was launched with.
-template <int N>
-__device__ __forceinline__ void setmaxnreg_inc() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
-template <int N>
-__device__ __forceinline__ void setmaxnreg_dec() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-
 // ---- mbarrier --------------------------------------------------------------------------------
 __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
   asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
@@ -163,13 +157,6 @@ __device__ __forceinline__ void tc_fence_after_sync() {
 }
 __device__ __forceinline__ void named_barrier_sync(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");
-}
-// The same; true for all where `v` is true for any of the threads.
-__device__ __forceinline__ bool named_barrier_or(uint32_t id, uint32_t nthreads, bool v) {
-  uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %3, 0;\n\tbarrier.cta.red.or.pred q, %1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"(id), "r"(nthreads), "r"((uint32_t)v) : "memory");
-  return r != 0;
 }
 // Counts this warp's threads on the barrier without waiting: what they wrote before is visible to the threads that sync on it.
 __device__ __forceinline__ void named_barrier_arrive(uint32_t id, uint32_t nthreads) {

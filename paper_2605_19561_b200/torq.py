@@ -1027,7 +1027,7 @@ def _kv_queries(fmt, pages, table, lengths, Q, scales, starts):
     stride = _kv_rows(Q, (torch.bfloat16,), "Q")
     tokens, heads, dim = Q.shape
     cache = _kv_cache(fmt, pages, table, lengths, dim, scales, starts, tokens)
-    if heads % pages.shape[1]:
+    if not heads or not pages.shape[1] or heads % pages.shape[1]:
         raise ValueError(f"Q: {heads} heads do not share {pages.shape[1]} key/value heads evenly")
     return cache, stride, tokens, heads, dim
 
