@@ -742,9 +742,9 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
           if (y != -INFINITY) {
             off[e] = -y * kLog2e;
             kv_range(a, it.b, i, place[e], it.length, lo[e], hi[e]);
-            all_lo = max(all_lo, lo[e]);
-            all_hi = min(all_hi, hi[e]);
           }
+          all_lo = max(all_lo, lo[e]);
+          all_hi = min(all_hi, hi[e]);                                     // 0 where a row saw nothing: its scores may be no numbers
           if (a.slopes) slope[e] = a.slopes[h];
         }
       }
@@ -851,6 +851,257 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
       const float w = __shfl_sync(0xFFFFFFFFu, own, (lane & 7) * 4 + (lane >> 3));
       if (slot >= 0) weights_out[slot] = old + w;
       stage = stage == ring + (C::STAGES - 1) * C::STAGE ? ring : stage + C::STAGE;
+    }
+    cp_async_wait<0>();
+    __syncwarp();
+  }
+}
+
+// The same for many rows of a sequence.  What a group of eight rows costs is its queries: read from L2, scaled, its ranges and sums looked up, one behind
+// the other.  So the four warps of a CTA, each with 32 tokens as operands (D = 256: 16), take the same groups: each makes one of four ready in shared
+// memory, the loads for the next four in flight, and all go through the four.  Blocks of tokens that no row of a group sees are passed over.  48 rows of 4
+// heads over 3 sequences of up to 3000 tokens, 8 key/value heads: 22.6 us, of which the longest chain of a CTA is most; 70.5 by single warps.
+template <int FMT_, int D_>
+struct KvRowWeightsCfg {
+  static constexpr int FMT = FMT_, D = D_, WARPS = 4, THREADS = 128, CH = D / 32, SB = D / kv_block(FMT), CTAS = D == 256 ? 2 : 3;
+  static constexpr int TILES = D == 256 ? 1 : 2, OWN = 16 * TILES, TOK = WARPS * OWN;      // tokens of a warp, of a CTA
+  static constexpr int K_BYTES = OWN * D / 2, S_BYTES = 32 * SB, STAGE = K_BYTES + S_BYTES, ROOM = KvScaleRoom<FMT, D>::KEYS;
+  static constexpr int QUERIES = CH * 512, GROUP = QUERIES + 8 * 24 + 64;                  // a group: operand; per row factor, offset, slope, place, range; limits
+  static constexpr int GROUPS_AT = WARPS * (2 * STAGE + ROOM), SMEM = GROUPS_AT + 2 * WARPS * GROUP;
+};
+
+template <class C>
+__global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(const KvView c, const KvScoring a, const __nv_bfloat16* Q, int64_t q_stride,
+                                                                             int heads, const float* lse, const float* weights, float* weights_out) {
+  constexpr int FMT = C::FMT, D = C::D, CH = C::CH, SB = C::SB, TILES = C::TILES, OWN = C::OWN;
+  extern __shared__ __align__(128) uint8_t smem[];
+  griddep_wait_and_launch();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3, group = heads / c.heads;
+  KvItem it;
+  int groups, cost, per;                                                   // groups of rows; what a block of TOK tokens counts; blocks of a head
+  auto units_of = [&](int b) -> long long {
+    if (b >= c.batch) return 0;
+    it.b = b;
+    kv_new_tokens(c, b, it.first_token, it.count);
+    it.length = kv_length(c, b);
+    groups = (it.count * group + 7) / 8;
+    cost = 1 + (groups + 3) / 4;
+    per = (it.length + C::TOK - 1) / C::TOK;
+    const int p0 = it.length - it.count;
+    it.lo = a.window > 0 && p0 - a.window + 1 > 0 ? p0 - a.window + 1 : 0;
+    return (long long)cost * c.heads * per;
+  };
+  const long long mine = units_of(lane);
+  long long units = mine;
+#pragma unroll 4
+  for (int b0 = 32; b0 < c.batch; b0 += 32) units += units_of(b0 + lane);
+#pragma unroll
+  for (int o = 16; o; o >>= 1) units += __shfl_xor_sync(0xFFFFFFFFu, units, o);
+  const long long begin = kv_range_begin(units, blockIdx.x, gridDim.x), end = kv_range_begin(units, blockIdx.x + 1, gridDim.x);
+  if (begin >= end) return;                                                // the same for all warps, as is what follows from it
+  int b = 0;
+  long long sequence_begin = 0;
+  for (int b0 = 0;; b0 += 32) {                                            // ends, since begin < units
+    const long long v = b0 ? units_of(b0 + lane) : mine, sum = warp_scan(v, lane);
+    const uint32_t here = __ballot_sync(0xFFFFFFFFu, begin < sequence_begin + sum);
+    if (here) {
+      const int first = __ffs(here) - 1;
+      b = b0 + first;
+      sequence_begin += __shfl_sync(0xFFFFFFFFu, sum - v, first);
+      break;
+    }
+    sequence_begin += __shfl_sync(0xFFFFFFFFu, sum, 31);
+  }
+  long long sequence_units = units_of(b);
+  long long at = (begin - sequence_begin + cost - 1) / cost * cost + sequence_begin;       // the first block that begins in the range
+
+  uint8_t *ring_p = smem + warp * 2 * C::STAGE, *room = smem + C::WARPS * 2 * C::STAGE + warp * C::ROOM, *shared_groups = smem + C::GROUPS_AT;
+  const uint32_t ring = smem_u32(ring_p);
+  const int row_of = lane & 15, chunk_of = lane >> 4, mask = (1 << c.page_shift) - 1;
+  constexpr int PER_GROUP = CH / 2, PIECES = SB;                           // copies of a lane for the codes of 16 tokens; 16-byte pieces of their scale bytes
+  uint32_t to_chunk[CH == 8 ? 2 : 1];
+#pragma unroll
+  for (int i = 0; i < (CH == 8 ? 2 : 1); ++i) to_chunk[i] = 16 * kv_swizzled<D>((32 * i + lane) / CH, lane % CH) - 512 * i;
+  const bool special = a.softcap > 0.f || a.slopes;
+
+  while (at < end) {
+    while (at >= sequence_begin + sequence_units) {
+      sequence_begin += sequence_units;
+      sequence_units = units_of(++b);
+    }
+    const int block_of = (int)((at - sequence_begin) / cost);
+    it.head = block_of / per;
+    const int block0 = block_of - it.head * per;
+    const long long left = (end - at + cost - 1) / cost;                   // blocks that begin in the range
+    const int blocks = (int)(left < per - block0 ? left : per - block0);
+    at += (long long)blocks * cost;
+
+    const int32_t* table = c.table + (int64_t)b * c.width;
+    const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
+    auto fetch = [&](int k) {                                              // this warp's tokens of block k
+      const int j0 = (block0 + k) * C::TOK + warp * OWN;
+      const uint32_t dst = ring + (k & 1) * C::STAGE;
+#pragma unroll
+      for (int i = 0; i < TILES; ++i) {
+        const int j = j0 + 16 * i;
+        bool there = k < blocks && groups > 0 && j < it.length && j + 16 > it.lo;
+        const int p = there ? table[j >> c.page_shift] : 0;
+        if (there && (unsigned)p >= (unsigned)c.num_pages) {
+          kv_bad_page(c);
+          there = false;
+        }
+        const uint8_t* page = head_pages + (there ? p * c.page_bytes : 0);
+        const int slot = j & mask;
+#pragma unroll
+        for (int x = 0; x < PER_GROUP; ++x) {
+          const int y = i * PER_GROUP + x;
+          cp_async_16(dst + to_chunk[CH == 8 ? y & 1 : 0] + 512 * y, page + slot * (D / 2) + lane * 16 + 512 * x, there ? 16 : 0);
+        }
+        if (lane < PIECES) cp_async_16(dst + C::K_BYTES + (i * PIECES + lane) * 16, page + c.k_scales + slot * SB + lane * 16, there ? 16 : 0);
+      }
+      cp_async_commit();
+    };
+    // group n of eight rows: lane (g, t) has row g
+    uint4 raw[CH];
+    float row_lse = -INFINITY, row_slope = 0.f;
+    int row_place = 0, row_lo = 0, row_hi = 0;
+    auto load_group = [&](int n) {
+      const int r = 8 * n + g;
+      const bool have = r < it.count * group;
+      const int i = it.first_token + r / group, h = it.head * group + r % group;
+      row_lse = have ? lse[(int64_t)i * heads + h] : -INFINITY;
+      const __nv_bfloat16* q = Q + i * q_stride + h * D + 8 * t;
+#pragma unroll
+      for (int x = 0; x < CH; ++x) raw[x] = have ? *reinterpret_cast<const uint4*>(q + 32 * x) : make_uint4(0, 0, 0, 0);
+      row_slope = have && a.slopes ? a.slopes[h] : 0.f;
+      row_place = it.length - it.count + r / group;
+      row_lo = row_hi = 0;
+      if (have) kv_range(a, it.b, i, row_place, it.length, row_lo, row_hi);
+    };
+    auto store_group = [&](int n) {
+      if (8 * n >= it.count * group) return;                               // the same for the whole warp
+      uint8_t* to = shared_groups + (n / 4 & 1) * (4 * C::GROUP) + (n & 3) * C::GROUP;
+      if (row_lse == -INFINITY) {                                          // saw nothing: its queries may be no numbers
+        row_lo = row_hi = 0;
+#pragma unroll
+        for (int x = 0; x < CH; ++x) raw[x] = make_uint4(0, 0, 0, 0);
+      }
+      KvQuery<D> q;
+      const float back = kv_scale_query<FMT, D>(raw, q);
+#pragma unroll
+      for (int x = 0; x < CH; ++x) reinterpret_cast<uint4*>(to)[32 * x + lane] = make_uint4(q.q[x][0], q.q[x][1], q.q[x][2], q.q[x][3]);
+      const int in_all_lo = __reduce_max_sync(0xFFFFFFFFu, row_lo), in_all_hi = __reduce_min_sync(0xFFFFFFFFu, row_hi);
+      const int in_any_lo = __reduce_min_sync(0xFFFFFFFFu, row_hi > 0 ? row_lo : INT32_MAX), in_any_hi = __reduce_max_sync(0xFFFFFFFFu, row_hi);
+      if (t == 0) {
+        reinterpret_cast<float4*>(to + C::QUERIES)[g] = make_float4(back * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e), -row_lse * kLog2e, row_slope,
+                                                                    __int_as_float(row_place));
+        reinterpret_cast<int2*>(to + C::QUERIES + 128)[g] = make_int2(row_lo, row_hi);
+      }
+      if (lane == 0) *reinterpret_cast<int4*>(to + C::QUERIES + 192) = make_int4(in_all_lo, in_all_hi, in_any_lo, in_any_hi);
+    };
+
+    fetch(0);
+    for (int k = 0; k < blocks; ++k) {
+      if (groups > 0) load_group(warp);
+      fetch(k + 1);                                                        // into the stage that the last block has left
+      const int j0 = (block0 + k) * C::TOK + warp * OWN, mine_j = j0 + lane;
+      int64_t slot = -1;                                                   // of this lane's token in the account
+      float old = 0.f;
+      if (lane < OWN && mine_j < it.length) {
+        const int p = table[mine_j >> c.page_shift];
+        if ((unsigned)p < (unsigned)c.num_pages) {
+          slot = (((int64_t)p * c.heads + it.head) << c.page_shift) + (mine_j & mask);
+          if (mine_j < it.length - it.count) old = weights[slot];
+        }
+      }
+      if (groups > 0) store_group(warp);
+      cp_async_wait<1>();
+      __syncwarp();
+      const uint32_t stage = ring + (k & 1) * C::STAGE;
+      kv_ready_key_scales<FMT, D>(ring_p + (k & 1) * C::STAGE + C::K_BYTES, lane, room);
+      __syncwarp();
+      uint32_t keys[TILES][CH][2][4], scale[TILES][2][CH];
+      float part[TILES][2] = {};
+#pragma unroll
+      for (int u = 0; u < TILES; ++u) {
+        kv_key_scales<FMT, D>(room, 16 * u + g, t, scale[u][0]);
+        kv_key_scales<FMT, D>(room, 16 * u + g + 8, t, scale[u][1]);
+#pragma unroll
+        for (int c2 = 0; c2 < CH; c2 += 2) {
+          uint32_t codes[4];
+          ldmatrix_x4(stage + 16 * kv_swizzled<D>(16 * u + row_of, c2 + chunk_of), codes);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            kv_key_pairs<FMT>(codes[x], keys[u][c2 + x / 2][x & 1]);
+            if constexpr (FMT == FMT_NVFP4) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) keys[u][c2 + x / 2][x & 1][i] = mul_f16x2(keys[u][c2 + x / 2][x & 1][i], scale[u][x & 1][c2 + x / 2]);
+            }
+          }
+        }
+      }
+      __syncthreads();
+#pragma unroll 1
+      for (int n0 = 0; n0 < groups; n0 += 4) {
+        const bool more = n0 + 4 < groups;
+        if (more) load_group(n0 + 4 + warp);
+        const uint8_t* from = shared_groups + (n0 / 4 & 1) * (4 * C::GROUP);
+#pragma unroll 1
+        for (int n = n0; n < n0 + 4 && n < groups; ++n, from += C::GROUP) {
+          const int4 limits = *reinterpret_cast<const int4*>(from + C::QUERIES + 192);
+          if (j0 >= limits.w || j0 + OWN <= limits.z) continue;            // no row of the group sees any of these tokens
+          const bool border = j0 < limits.x || j0 + OWN > limits.y;
+          const float4 f[2] = {reinterpret_cast<const float4*>(from + C::QUERIES)[2 * t], reinterpret_cast<const float4*>(from + C::QUERIES)[2 * t + 1]};
+          float s[TILES][4] = {};
+#pragma unroll
+          for (int ch = 0; ch < CH; ++ch) {
+            const uint4 q = reinterpret_cast<const uint4*>(from)[32 * ch + lane];
+#pragma unroll
+            for (int u = 0; u < TILES; ++u) {
+              const uint32_t(&x)[2][4] = keys[u][ch];
+              if constexpr (FMT == FMT_NVFP4) {
+                mma_f16(s[u], x[0][0], x[1][0], x[0][1], x[1][1], q.x, q.y, s[u]);
+                mma_f16(s[u], x[0][2], x[1][2], x[0][3], x[1][3], q.z, q.w, s[u]);
+              } else {
+                const float zero[4] = {};
+                float y[4];
+                mma_f16(y, x[0][0], x[1][0], x[0][1], x[1][1], q.x, q.y, zero);
+                mma_f16(y, x[0][2], x[1][2], x[0][3], x[1][3], q.z, q.w, y);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[u][i] = fmaf(y[i], __uint_as_float(scale[u][i >> 1][ch]), s[u][i]);
+              }
+            }
+          }
+          if (special || border) {
+            const int4 range = *reinterpret_cast<const int4*>(from + C::QUERIES + 128 + 16 * t);
+            const int lo[2] = {range.x, range.z}, hi[2] = {range.y, range.w};
+#pragma unroll
+            for (int u = 0; u < TILES; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const int e = i & 1, j = j0 + 16 * u + g + 8 * (i >> 1);
+                float x = s[u][i] * f[e].x;
+                if (special) x = kv_score(x * kLn2, a.softcap, f[e].z, abs(__float_as_int(f[e].w) - j));
+                part[u][i >> 1] += j >= lo[e] && j < hi[e] ? ex2(x + f[e].y) : 0.f;
+              }
+          } else {
+#pragma unroll
+            for (int u = 0; u < TILES; ++u)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) part[u][i >> 1] += ex2(fmaf(s[u][i], f[i & 1].x, f[i & 1].y));
+          }
+        }
+        if (more) store_group(n0 + 4 + warp);
+        __syncthreads();                                                   // all have left this buffer, the next one is written
+      }
+#pragma unroll
+      for (int o = 1; o < 4; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < 2 * TILES; ++i) part[i >> 1][i & 1] += __shfl_xor_sync(0xFFFFFFFFu, part[i >> 1][i & 1], o);
+      const float low = t & 1 ? part[0][1] : part[0][0], high = t & 1 ? part[TILES - 1][1] : part[TILES - 1][0];
+      const float own = TILES == 2 && (t & 2) ? high : low;                // token g + 8 t
+      const float w = __shfl_sync(0xFFFFFFFFu, own, (lane & 7) * 4 + (lane >> 3));
+      if (slot >= 0) weights_out[slot] = old + w;
     }
     cp_async_wait<0>();
     __syncwarp();

@@ -191,21 +191,18 @@ template <int D>
 struct KvQuery {
   uint32_t q[D / 32][4];
 };
-// Row `p` (null: zeros) into float16, times a power of two that brings its largest magnitude to [2^14, 2^15): float16 then keeps all bits of a
+// A row into float16, times a power of two that brings its largest magnitude to [2^14, 2^15): float16 then keeps all bits of a
 // bfloat16 down to 2^-21 of the largest, and nothing is off by more than 2^-40 of it.  Returns the factor to be multiplied back, of row g.
 template <int FMT, int D>
-__device__ __forceinline__ float kv_load_query(const __nv_bfloat16* p, int t, KvQuery<D>& out) {
-  uint4 raw[D / 32];
+__device__ __forceinline__ float kv_scale_query(const uint4 (&raw)[D / 32], KvQuery<D>& out) {
   uint32_t top = 0;
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c) {
-    raw[c] = p ? load_once(p + 32 * c + 8 * t) : make_uint4(0, 0, 0, 0);
+  for (int c = 0; c < D / 32; ++c)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const uint32_t w = (&raw[c].x)[i] & 0x7FFF7FFFu;
       top = max(top, max(w >> 16, w & 0xFFFFu));
     }
-  }
   top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
   top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
   const uint32_t ef = top >> 7, field = ef > 15 ? 268u - ef : 253u;
@@ -222,6 +219,14 @@ __device__ __forceinline__ float kv_load_query(const __nv_bfloat16* p, int t, Kv
     for (int i = 0; i < 4; ++i) out.q[c][i] = pack_f16(v[kv_query_order<FMT>(i, 0)], v[kv_query_order<FMT>(i, 1)]);
   }
   return __uint_as_float((254u - field) << 23);
+}
+// Row `p`, null: zeros.
+template <int FMT, int D>
+__device__ __forceinline__ float kv_load_query(const __nv_bfloat16* p, int t, KvQuery<D>& out) {
+  uint4 raw[D / 32];
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) raw[c] = p ? load_once(p + 32 * c + 8 * t) : make_uint4(0, 0, 0, 0);
+  return kv_scale_query<FMT, D>(raw, out);
 }
 
 // Scores of 16 cached tokens (rows first_row ... of the tile at `keys`, their scales made ready in `room`) with NT groups of eight queries:
