@@ -476,7 +476,8 @@ int64_t torq_launch_count(void);
  * results are zeros (lse: minus infinity).  table, lengths, starts are int32 and 4-byte aligned, and are read on the device: one captured call
  * serves every step.  A page number that a call needs and that lies outside [0, num_pages), or a length that the table has no room for, latches
  * TORQ_ERR_PAGE in the device error word; nothing is read or written there, and the results of that sequence are unspecified.
- * Entries of table behind a sequence's length and what pages hold there are never looked at, so they may hold anything.
+ * Entries of table behind a sequence's length and what pages hold there are never looked at, so they may hold anything.  Sequences may have pages in
+ * common (a prompt that they share), but for slots that append or weights write.
  * Sizes: batch <= 65536, kv_heads <= 1024, table_width page_tokens <= 2^30, tokens <= 2^24. */
 typedef struct {
   void* pages;               /* [num_pages][kv_heads][torq_kv_page_bytes()], 16-byte aligned */
@@ -521,7 +522,10 @@ typedef struct {
  *   Q [tokens][heads][D] bf16, rows q_stride elements apart; heads % kv_heads == 0, query heads h G ... h G + G - 1 share key/value head h
  *   out [tokens][heads][D] bf16;  lse [tokens][heads] float32, natural logarithm, or NULL
  *   workspace: torq_kv_attention_workspace_bytes() bytes, 256-byte aligned; two calls that may overlap need one each
- * Scores, sums and the running maximum are float32.  Outputs overlap no operand. */
+ * Scores, sums and the running maximum are float32; Q is read to 2^-21 of a row's largest element at least, weights are float16 before they meet the values,
+ * 11 bits down to 2^-24 of the largest so far and never off by more than 2^-35 of it.  MXFP4, MXINT4: scales below 2^-26 (many rows: 2^-35) of the largest
+ * that the same features (many rows: 128 tokens) have among what the rows of a call see count as zero, of keys (many rows alone) and of values; so does scale
+ * byte 0.  Tokens that no row of a sequence sees may hold anything.  One or two launches.  Outputs overlap no operand. */
 size_t torq_kv_attention_workspace_bytes(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t head_dim);
 torq_status torq_mxfp4_kv_attention(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
                                     const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
@@ -533,7 +537,8 @@ torq_status torq_mxint4_kv_attention(const torq_kv_cache* cache, const torq_kv_s
 /* The account of the cache: what attention gave to each cached token, summed over the new rows and the query heads that share its head.
  *   weights_out[page][h][slot] = (weights[page][h][slot] of a token that is not new, else 0) + sum over rows and heads of exp(x_j - lse)
  * weights, weights_out [num_pages][kv_heads][page_tokens] float32 (16-byte aligned; they may be the same); only slots of the sequences' tokens are
- * written.  Q, scoring and starts as the attention call had them, lse [tokens][heads] what it gave.  The order of the sums is fixed.  One launch. */
+ * written, and a slot that two sequences have in common gets only one's.  Q, scoring and starts as the attention call had them, lse [tokens][heads] what
+ * it gave.  The order of the sums is fixed.  One launch. */
 torq_status torq_mxfp4_kv_weights(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
                                   const int32_t* starts, int64_t tokens, const float* lse, const float* weights, float* weights_out, void* stream);
 torq_status torq_nvfp4_kv_weights(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
@@ -543,7 +548,7 @@ torq_status torq_mxint4_kv_weights(const torq_kv_cache* cache, const torq_kv_sco
 
 /* Eviction by account: of each sequence and key/value head the `recent` newest tokens and, of the others, those with the largest weights stay, `keep`
  * in all (equal weights: the lower place stays; a sequence of at most `keep` tokens stays whole).  Codes, scale bytes and weights of what stays
- * are copied, in their order, to the pages of new_table [batch][new_width], which are no pages of the sequences.  Places count anew there: a
+ * are copied, in their order, to the pages of new_table [batch][new_width], which are no pages of the sequences and no page twice.  Places count anew there: a
  * bias by distance or a window then counts what is left.
  *   new_lengths [batch] int32 = min(length, keep);  kept [batch][kv_heads][keep] int32: the places of what stayed, -1 behind them
  * new_width page_tokens >= min(keep, table_width page_tokens); batch kv_heads <= 65535.  Weights that are no numbers are outside the contract.

@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
     // the queries, and what each row sees
     KvQuery<D> q[NT];
     float factor[NT][2], slope[NT][2], m[NT][2], l[NT][2];
-    int place[NT][2], lo[NT][2], hi[NT][2], all_lo = 0, all_hi = INT32_MAX;
+    int place[NT][2], lo[NT][2], hi[NT][2], all_lo = 0, all_hi = INT32_MAX, any_lo = INT32_MAX, any_hi = 0;   // what all rows see, what any does
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       const int r = it.first_row + 8 * n + g;
@@ -263,6 +263,8 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
           if (a.slopes) slope[n][e] = a.slopes[it.head * group + rr % group];
           all_lo = max(all_lo, lo[n][e]);
           all_hi = min(all_hi, hi[n][e]);
+          if (lo[n][e] < hi[n][e]) any_lo = min(any_lo, lo[n][e]);
+          any_hi = max(any_hi, hi[n][e]);
         }
         m[n][e] = -1e30f;
         l[n][e] = 0.f;
@@ -273,6 +275,8 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
       all_lo = max(all_lo, __shfl_xor_sync(0xFFFFFFFFu, all_lo, o));
       all_hi = min(all_hi, __shfl_xor_sync(0xFFFFFFFFu, all_hi, o));
     }
+    any_lo = __reduce_min_sync(0xFFFFFFFFu, any_lo);
+    any_hi = __reduce_max_sync(0xFFFFFFFFu, any_hi);
     const bool special = a.softcap > 0.f || a.slopes;
     float o[NT][CH][2][4];
 #pragma unroll
@@ -297,12 +301,12 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
       const uint8_t* scales = ring_p + (stage - ring) + 2 * C::K_BYTES;
       const bool border = j0 < all_lo || j0 + C::STEP > all_hi;
 
-      // scales of the 32 tokens; behind the last token may lie what is no number
+      // scales of the 32 tokens; those that no row sees may be no numbers, or larger than all others
       kv_ready_key_scales<FMT, D>(scales, lane, room);
       {
         uint32_t w[(SB + 3) / 4];
         kv_scale_words<SB>(scales + C::S_BYTES + lane * SB, w);
-        if (border && j0 + lane >= it.hi) {
+        if (border && (j0 + lane < any_lo || j0 + lane >= any_hi)) {
 #pragma unroll
           for (int i = 0; i < (SB + 3) / 4; ++i) w[i] = 0;
         }
@@ -661,9 +665,9 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
       sequence_begin += sequence_units;
       sequence_units = units_of(++b);
     }
-    const int step_of = (int)((at - sequence_begin) / cost);
-    it.head = step_of / per;
-    const int step0 = step_of - it.head * per;
+    const long long step_of = (at - sequence_begin) / cost;
+    it.head = (int)(step_of / per);
+    const int step0 = (int)(step_of - (long long)it.head * per);
     const long long left = (end - at + cost - 1) / cost;                   // steps that begin in the range
     const int steps = (int)(left < per - step0 ? left : per - step0);
     at += (long long)steps * cost;
@@ -929,9 +933,9 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
       sequence_begin += sequence_units;
       sequence_units = units_of(++b);
     }
-    const int block_of = (int)((at - sequence_begin) / cost);
-    it.head = block_of / per;
-    const int block0 = block_of - it.head * per;
+    const long long block_of = (at - sequence_begin) / cost;
+    it.head = (int)(block_of / per);
+    const int block0 = (int)(block_of - (long long)it.head * per);
     const long long left = (end - at + cost - 1) / cost;                   // blocks that begin in the range
     const int blocks = (int)(left < per - block0 ? left : per - block0);
     at += (long long)blocks * cost;

@@ -75,6 +75,12 @@ __device__ __forceinline__ bool kv_prefill_item(const KvView& c, const KvScoring
       if (a.prefix && a.prefix[it.b] > it.hi) it.hi = a.prefix[it.b];
       it.hi = min(it.hi, it.length);
       it.lo = a.window > 0 && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
+      if (a.first) {
+        const int t0 = it.first_token + it.first_row / group, t1 = it.first_token + (it.first_row + it.rows - 1) / group;
+        int least = INT32_MAX;
+        for (int i = t0 + lane; i <= t1; i += 32) least = min(least, a.first[i]);
+        it.lo = min(max(it.lo, __reduce_min_sync(0xFFFFFFFFu, least)), it.hi);
+      }
       it.base = it.lo & ~15;
       it.tiles = it.hi > it.base ? (it.hi - it.base + TOK - 1) / TOK : 1;  // rows that see nothing are an item all the same
       return true;
@@ -394,19 +400,20 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       const int32_t* table = c.table + (int64_t)it.b * c.width;
       const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
       const int groups = (it.tiles + 1) / 2;
-      int page[N];                                                         // of the next group's chunks; -1: nothing there
+      int page[N];                                                         // of the next group's chunks; -1: nothing there that any row sees
       auto look_up = [&](int g) {                                          // all loads before the first is looked at
 #pragma unroll
         for (int i = 0; i < N; ++i) {
           const int j = it.base + g * 128 + row0 + i * (128 / CH);
-          page[i] = g < groups && j < it.hi ? table[j >> c.page_shift] : -1;
+          page[i] = g < groups && j >= it.lo && j < it.hi ? table[j >> c.page_shift] : -1;
         }
       };
       auto check = [&](int g) {
         bool bad = false;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          bad |= g < groups && it.base + g * 128 + row0 + i * (128 / CH) < it.hi && (unsigned)page[i] >= (unsigned)c.num_pages;
+          const int j = it.base + g * 128 + row0 + i * (128 / CH);
+          bad |= g < groups && j >= it.lo && j < it.hi && (unsigned)page[i] >= (unsigned)c.num_pages;
           if ((unsigned)page[i] >= (unsigned)c.num_pages) page[i] = -1;
         }
         if (bad) kv_bad_page(c);

@@ -129,3 +129,26 @@ def test_what_lies_behind_a_sequence_is_not_read_into_it(fmt, new):
                 part[page, :, slot] = byte
         y, z = c.call("attention", Q, *c.scales, return_lse=True)
         assert torch.equal(y, out) and torch.equal(z, lse)
+
+
+@pytest.mark.parametrize("new", [[1, 1], [3, 2], [250, 200]], ids=["one", "few", "many"])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_what_no_row_sees_may_hold_anything(fmt, dim, new):
+    """Tokens in front of every row's document, of all scales up to no number: the same bits as with ordinary ones."""
+    c = Cache(fmt, [777, 540], 32, 2, dim, 32, new=new)
+    begins = [77, 301]
+    first = torch.cat([torch.full((n,), begins[b], dtype=torch.int32, device=DEV) for b, n in enumerate(new)])
+    Q = queries(c)
+    options = dict(first=first)
+    out, lse = run(c, Q, **options)
+    w = torch.rand(c.pages.shape[0], c.H, c.P, generator=gen(4), device=DEV)
+    account = c.call("weights", Q, lse, w.clone(), *c.scales[:1], **options)
+    for byte in (0x7E, 0x7F, 0xFD, 0xFE, 0xFF):
+        for b in range(2):
+            page, slot = c.at(b, torch.arange(begins[b], device=DEV))
+            for part in parts(c.pages, fmt, c.D):
+                part[page, :, slot] = byte
+        y, z = c.call("attention", Q, *c.scales, return_lse=True, **options)
+        assert torch.equal(y, out) and torch.equal(z, lse)
+        assert torch.equal(c.call("weights", Q, lse, w.clone(), *c.scales[:1], **options), account)
