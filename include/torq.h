@@ -525,7 +525,7 @@ typedef struct {
  * Scores, sums and the running maximum are float32; Q is read to 2^-21 of a row's largest element at least, weights are float16 before they meet the values,
  * 11 bits down to 2^-24 of the largest so far and never off by more than 2^-35 of it.  MXFP4, MXINT4: scales below 2^-26 (many rows: 2^-35) of the largest
  * that the same features (many rows: 128 tokens) have among what the rows of a call see count as zero, of keys (many rows alone) and of values; so does scale
- * byte 0.  Tokens that no row of a sequence sees may hold anything.  One or two launches.  Outputs overlap no operand. */
+ * byte 0.  Tokens that no row of a sequence sees may hold anything.  Two launches.  Outputs overlap no operand. */
 size_t torq_kv_attention_workspace_bytes(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t head_dim);
 torq_status torq_mxfp4_kv_attention(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
                                     const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);

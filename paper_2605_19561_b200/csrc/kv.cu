@@ -185,26 +185,30 @@ static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, c
 }
 
 // ---- many queries per sequence
+constexpr int kMaxPrefill = 160;         // CTAs; as max_ranges
+static size_t prefill_workspace(int64_t dim) { return (size_t)kMaxPrefill * 2 * (dim == 256 ? 128 : 256) * (size_t)(dim + 2) * sizeof(float); }
 template <int FMT, int D>
 static torq_status prefill_launch(const KvView& v, const KvScoring& a, int sms, const void* Q, int64_t q_stride, int heads, void* out, float* lse,
-                                  cudaStream_t s) {
+                                  void* workspace, cudaStream_t s) {
   using C = KvPrefillCfg<FMT, D>;
   constexpr auto kernel = kv_prefill_kernel<C>;
   if (!opt_in<kernel>(C::SMEM)) return TORQ_ERR_LAUNCH;
-  launch_tc(kernel, 1, dim3((unsigned)sms), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads,
-            static_cast<__nv_bfloat16*>(out), lse);
+  const int ctas = sms < kMaxPrefill ? sms : kMaxPrefill;
+  float* partials = static_cast<float*>(workspace);
+  __nv_bfloat16* y = static_cast<__nv_bfloat16*>(out);
+  launch_tc(kernel, 1, dim3((unsigned)ctas), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads, y, lse, partials);
+  const torq_status rc = launch_status();
+  if (rc != TORQ_OK || ctas == 1) return rc;
+  launch_tc(kv_prefill_join_kernel<C>, 1, dim3((unsigned)ctas - 1, C::ROWS / 32), dim3(256), 0, s, v, a, ctas, heads, static_cast<const float*>(partials), y, lse);
   return launch_status();
 }
-// Which of the two.  The kernel for many queries gives a CTA up to 256 rows of a head (128 of 256 dimensions) and all their cached tokens: as long as
-// there is one CTA for each, it takes as long for one row as for all of them.  The streaming kernel divides whatever there is evenly.  A CTA of the first
-// takes as long for its tokens as the second does for 64 rows on one SM.  Measured, streaming against the other, us:
-//   16 sequences of up to 5000 tokens, 8 heads of 128:  64 rows at most 71, 92;  128: 137, 94;  512: 426, 168
-//   one sequence of 32768 tokens, 8 heads of 128:  64 rows 61, 527;  512: 369, 595;  1024: 722, 612
-//   64 sequences of up to 3000 tokens, 4 heads of 128:  64 rows 91, 115;  96: 133, 116
-//   8 sequences of up to 5000 tokens, 8 heads of 256:  128 rows 129, 217;  256: 300, 213
-static bool many_rows(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t dim, int sms) {
-  const int64_t rows = tokens / batch * (heads / kv_heads), items = batch * kv_heads, tile = dim == 256 ? 128 : 256;
-  return rows * items >= 64 * sms * ((items * ((rows + tile - 1) / tile) + sms - 1) / sms);
+// Which of the two: the streaming kernel widens the cache anew for every 16 rows of a head (8 of 256 dimensions), the other once for 256 (128), but takes as long for
+// one row as for all.  Measured, streaming against the other, us, by rows on average:
+//   one sequence of 32768 tokens, 8 heads of 128: 64 rows 60, 65;  96: 83, 67;  512: 362, 122;  of 256: 64 rows 118, 120;  128: 216, 137
+//   16 sequences of up to 5000 tokens, 8 heads of 128: about 45 rows 71, 95;  65: 91, 94;  90: 138, 102
+//   64 sequences of up to 3000 tokens, 4 heads of 128: about 45 rows 90, 115;  65: 133, 116
+static bool many_rows(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads) {
+  return tokens / batch * (heads / kv_heads) >= 64;
 }
 
 template <int FMT>
@@ -225,10 +229,10 @@ static torq_status attention_impl(const torq_kv_cache* cache, const torq_kv_scor
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
   cudaStream_t stm = static_cast<cudaStream_t>(stream);
   const int groups = decode_groups(tokens, cache->batch, heads, v.heads, v.dim);
-  const bool many = many_rows(tokens, cache->batch, heads, v.heads, v.dim, sms);
+  const bool many = many_rows(tokens, cache->batch, heads, v.heads);
   with_dim(v.dim, [&](auto DIM) {
     constexpr int D = decltype(DIM)::value;
-    if (many) rc = prefill_launch<FMT, D>(v, a, sms, Q, q_stride, (int)heads, out, lse, stm);
+    if (many) rc = prefill_launch<FMT, D>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
     else if (groups == 1) rc = decode_launch<FMT, D, 1>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
     else if constexpr (D < 256) rc = decode_launch<FMT, D, 2>(v, a, sms, Q, q_stride, (int)heads, out, lse, workspace, stm);
   });
@@ -313,7 +317,8 @@ size_t torq_kv_page_bytes(int64_t scale_block, int64_t page_tokens, int64_t head
 
 size_t torq_kv_attention_workspace_bytes(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t head_dim) {
   if (tokens < 1 || batch < 1 || heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || head_dim < 1) return 0;
-  return decode_workspace(decode_groups(tokens, batch, heads, kv_heads, head_dim), head_dim);
+  return many_rows(tokens, batch, heads, kv_heads) ? prefill_workspace(head_dim)
+                                                   : decode_workspace(decode_groups(tokens, batch, heads, kv_heads, head_dim), head_dim);
 }
 
 #define TORQ_KV_ENTRIES(name, FMT)                                                                                                                   \

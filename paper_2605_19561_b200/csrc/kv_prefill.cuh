@@ -8,6 +8,9 @@
 // scales down to 2^-35 of that; 2^E of the keys goes into the scores' factor, that of the values into the weights: P = exp2(x - m + 10 + E - E_max), E_max the
 // largest E so far, so a tile with smaller values has smaller weights.  What is summed for the softmax does not have it.
 //
+// Bound by the softmax warps: about 2250 cycles per 64 tokens and 256 rows, of which the exponentials' rate is 1024; the tensor pipe is busy for 40 %.  2048 tokens
+// behind 6144, 8 heads of 128 with 4 queries: 302 us, 145 as products alone.
+//
 // Warp-specialised, one CTA per SM, persistent over the items (sequence, head, tiles of rows):
 //   warps 0 - 3, 4 - 7   softmax of the first and second tile, a row to each thread: loads its query, keeps maximum and sum, corrects O when the maximum has
 //                        grown by more than 2^5 (seldom), writes the result
@@ -30,6 +33,7 @@ struct KvPrefillCfg {
   static constexpr int FT = D == 256 ? 1 : 2, STAGES = D == 256 ? 5 : 4, FILL_BYTES = FT * KV_BYTES;
   static constexpr int INFO_AT = TILES * Q_BYTES + STAGES * FILL_BYTES, SMEM = INFO_AT + 256 + 1024;
   static constexpr int O_COL = 256;
+  static constexpr int PARTIAL = ROWS * (D + 2);                           // floats: results, maxima, sums
   static_assert(SMEM <= 232448, "shared memory");
 };
 // kind::f16 with float16 operands, as idesc_bf16.
@@ -46,53 +50,141 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
 
 struct KvPrefillItem {
   int b, head, first_token, count, length, first_row, rows, base, lo, hi, tiles;       // rows of the item; cached tokens [lo, hi), base <= lo; tiles of tokens
+  int part;                              // -1: all tokens that its rows see; 1, 0: some of them, the first ones among them or not
+};
+// CTAs take whole items in turn, those with the most tokens of a sequence first; or, where that would take longer, equal ranges of the list of all items
+// (sequence after sequence, tile after tile, heads inside).  There every item of a sequence counts as many units as its longest has groups of 128 tokens, so that
+// a place in the list is found by divisions (counted exactly, tile by tile, it took every warp 5 us); of an item with fewer groups a part has its
+// share.  An item that a border cuts leaves partial results, as in the streaming kernel.
+struct KvPrefillWalk {
+  long long at, end, units;              // items, or units (and how many there are)
+  int ranges;                            // 0: whole items
 };
 
-// Item `index` of the list (sequence after sequence, the tiles with the most tokens first, heads inside); false behind the last.  Whole warps.
+// Of sequence b: its new rows, and how many tiles of rows they make for a head.
+template <int ROWS>
+__device__ __forceinline__ int kv_prefill_sequence(const KvView& c, int group, int b, KvPrefillItem& it) {
+  it.b = b;
+  kv_new_tokens(c, b, it.first_token, it.count);
+  it.length = kv_length(c, b);
+  return it.length > 0 ? (it.count * group + ROWS - 1) / ROWS : 0;
+}
+// Tile `tile` of its rows and the tokens that they see.  Returns the groups of 128 tokens, one at least: rows that see nothing are an item all the same.
 template <int ROWS, int TOK>
-__device__ __forceinline__ bool kv_prefill_item(const KvView& c, const KvScoring& a, int group, long long index, int lane, KvPrefillItem& it) {
+__device__ __forceinline__ int kv_prefill_tile(const KvScoring& a, int group, int tile, KvPrefillItem& it) {
+  it.first_row = tile * ROWS;
+  it.rows = min(ROWS, it.count * group - it.first_row);
+  const int p0 = it.length - it.count, p_first = p0 + it.first_row / group, p_last = p0 + (it.first_row + it.rows - 1) / group;
+  it.hi = p_last + 1;
+  if (a.prefix && a.prefix[it.b] > it.hi) it.hi = a.prefix[it.b];
+  it.hi = min(it.hi, it.length);
+  it.lo = a.window > 0 && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
+  it.base = it.lo & ~15;
+  it.tiles = it.hi > it.base ? (it.hi - it.base + TOK - 1) / TOK : 1;
+  return (it.tiles + 1) / 2;
+}
+// Items of sequence b, and the units of each.
+template <int ROWS, int TOK>
+__device__ __forceinline__ long long kv_prefill_items(const KvView& c, const KvScoring& a, int group, int b, int& each) {
+  each = 0;
+  if (b >= c.batch) return 0;
+  KvPrefillItem it;
+  const int tiles = kv_prefill_sequence<ROWS>(c, group, b, it);
+  if (tiles == 0) return 0;
+  each = max(kv_prefill_tile<ROWS, TOK>(a, group, tiles - 1, it), kv_prefill_tile<ROWS, TOK>(a, group, max(tiles - 2, 0), it));
+  return (long long)tiles * c.heads;
+}
+// Whole items where a range, with what cutting costs (more starts, partial results and their join, in all as much as EXTRA groups), would not take less
+// time; ranges have LEAST units at least.  Measured, whole items against ranges, us: one sequence of 32768 tokens, 8 heads of 128: 256 rows of a head 608, 92;
+// 1024: 600, 182; of 256 dimensions, 1024 rows: 1313, 617.  2048 tokens behind 6144, 8 heads of 128 with 4 queries: 303, 329; 16 sequences of up to 5000,
+// 1024 rows: 260, 342.
+template <int ROWS, int TOK>
+__device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const KvScoring& a, int group, int lane, int which, int ctas) {
+  constexpr int EXTRA = ROWS == 128 ? 12 : 24, LEAST = 4;
+  long long units = 0, items = 0;
+  int longest = 0;
+  for (int b = lane; b < c.batch; b += 32) {
+    int each;
+    const long long n = kv_prefill_items<ROWS, TOK>(c, a, group, b, each);
+    items += n;
+    units += n * each;
+    longest = max(longest, each);
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) {
+    units += __shfl_xor_sync(0xFFFFFFFFu, units, o);
+    items += __shfl_xor_sync(0xFFFFFFFFu, items, o);
+  }
+  longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+  KvPrefillWalk w;
+  w.units = units;
+  if ((items + ctas - 1) / ctas * longest <= units / ctas + EXTRA) {
+    w.ranges = 0;
+    w.at = which;
+    w.end = items;
+  } else {
+    w.ranges = (int)min((long long)ctas, max(units / LEAST, 1ll));
+    w.at = which < w.ranges ? kv_range_begin(units, which, w.ranges) : 0;
+    w.end = which < w.ranges ? kv_range_begin(units, which + 1, w.ranges) : 0;
+  }
+  return w;
+}
+// Where number `at` of the list lies: the item (its tokens all of them), its groups, and which of its units; false behind the last.  Whole warps.
+template <int ROWS, int TOK>
+__device__ __forceinline__ bool kv_prefill_find(const KvView& c, const KvScoring& a, int group, long long at, bool items, int lane, KvPrefillItem& it, int& unit,
+                                                int& each, int& groups) {
   long long before = 0;
   for (int b0 = 0; b0 < c.batch; b0 += 32) {
-    int first = 0, count = 0, tiles = 0;
-    if (b0 + lane < c.batch) {
-      kv_new_tokens(c, b0 + lane, first, count);
-      tiles = kv_length(c, b0 + lane) > 0 ? (count * group + ROWS - 1) / ROWS : 0;
-    }
-    const long long items = (long long)tiles * c.heads, sum = warp_scan(items, lane);
-    const uint32_t here = __ballot_sync(0xFFFFFFFFu, index < before + sum);
+    const long long n = kv_prefill_items<ROWS, TOK>(c, a, group, b0 + lane, each) * (items ? 1 : max(each, 0)), sum = warp_scan(n, lane);
+    const uint32_t here = __ballot_sync(0xFFFFFFFFu, at < before + sum);
     if (here) {
       const int l = __ffs(here) - 1;
-      const int local = (int)(index - before - __shfl_sync(0xFFFFFFFFu, sum - items, l));
-      tiles = __shfl_sync(0xFFFFFFFFu, tiles, l);
-      it.b = b0 + l;
-      kv_new_tokens(c, it.b, it.first_token, it.count);
-      it.length = kv_length(c, it.b);
-      it.head = local % c.heads;
-      it.first_row = (tiles - 1 - local / c.heads) * ROWS;
-      it.rows = min(ROWS, it.count * group - it.first_row);
-      const int p0 = it.length - it.count, p_first = p0 + it.first_row / group, p_last = p0 + (it.first_row + it.rows - 1) / group;
-      it.hi = p_last + 1;
-      if (a.prefix && a.prefix[it.b] > it.hi) it.hi = a.prefix[it.b];
-      it.hi = min(it.hi, it.length);
-      it.lo = a.window > 0 && p_first - a.window + 1 > 0 ? p_first - a.window + 1 : 0;
-      if (a.first) {
-        const int t0 = it.first_token + it.first_row / group, t1 = it.first_token + (it.first_row + it.rows - 1) / group;
-        int least = INT32_MAX;
-        for (int i = t0 + lane; i <= t1; i += 32) least = min(least, a.first[i]);
-        it.lo = min(max(it.lo, __reduce_min_sync(0xFFFFFFFFu, least)), it.hi);
-      }
-      it.base = it.lo & ~15;
-      it.tiles = it.hi > it.base ? (it.hi - it.base + TOK - 1) / TOK : 1;  // rows that see nothing are an item all the same
+      const long long rest = at - before - __shfl_sync(0xFFFFFFFFu, sum - n, l);
+      each = __shfl_sync(0xFFFFFFFFu, each, l);
+      const int tiles = kv_prefill_sequence<ROWS>(c, group, b0 + l, it);
+      const int item = (int)(items ? rest : rest / each);
+      unit = items ? 0 : (int)(rest - (long long)item * each);
+      it.head = item % c.heads;
+      groups = kv_prefill_tile<ROWS, TOK>(a, group, items ? tiles - 1 - item / c.heads : item / c.heads, it);
       return true;
     }
     before += __shfl_sync(0xFFFFFFFFu, sum, 31);
   }
   return false;
 }
+// The next item of a CTA, or the part of it that lies in its range.
+template <int ROWS, int TOK>
+__device__ __forceinline__ bool kv_prefill_item(const KvView& c, const KvScoring& a, int group, KvPrefillWalk& w, int lane, KvPrefillItem& it) {
+  int unit, each, groups;
+  if (w.at >= w.end || !kv_prefill_find<ROWS, TOK>(c, a, group, w.at, w.ranges == 0, lane, it, unit, each, groups)) return false;
+  it.part = -1;
+  if (w.ranges == 0) {
+    w.at += gridDim.x;
+  } else {
+    const int n = (int)min(w.end - w.at, (long long)(each - unit));
+    w.at += n;
+    if (n < each) {
+      it.part = unit == 0 ? 1 : 0;
+      const int from = (int)((long long)unit * groups / each), to = (int)((long long)(unit + n) * groups / each);
+      it.lo = max(it.lo, it.base + 128 * from);
+      it.hi = min(it.hi, it.base + 128 * to);
+    }
+  }
+  if (a.first) {
+    const int t0 = it.first_token + it.first_row / group, t1 = it.first_token + (it.first_row + it.rows - 1) / group;
+    int least = INT32_MAX;
+    for (int i = t0 + lane; i <= t1; i += 32) least = min(least, a.first[i]);
+    it.lo = max(it.lo, __reduce_min_sync(0xFFFFFFFFu, least));
+  }
+  it.lo = min(it.lo, max(it.hi, 0));
+  it.base = it.lo & ~15;
+  it.tiles = it.hi > it.base ? (it.hi - it.base + TOK - 1) / TOK : 1;
+  return true;
+}
 
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView c, const KvScoring a, const __nv_bfloat16* Q, int64_t q_stride, int heads,
-                                                                   __nv_bfloat16* out, float* lse) {
+                                                                   __nv_bfloat16* out, float* lse, float* partials) {
   constexpr int FMT = C::FMT, D = C::D, CH = C::CH, SB = C::SB, TOK = C::TOK;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t bars[2 * C::STAGES + 10];
@@ -136,6 +228,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
   const uint32_t tmem = tmem_slot;
   griddep_wait_and_launch();
   KvPrefillItem it;
+  KvPrefillWalk walk = kv_prefill_walk<C::ROWS, TOK>(c, a, group, lane, blockIdx.x, gridDim.x);
 
   if (warp < 8) {
     // ------------------------------------------------------------------ softmax
@@ -166,7 +259,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
     // Two tiles of rows weigh in turn: side by side they wait for the exponentials of one another and then leave that unit idle together (2048 tokens behind
     // 6144: 317 us, in turn 304).  The barriers for that are executed for every tile of tokens, also after a wait has given up, so that no warp is left in
     // one.
-    for (long long index = blockIdx.x; kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
+    while (kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it)) {
       const uint32_t first_group = group_no;
       group_no += (it.tiles + 1) / 2;
       if (128 * t >= it.rows) continue;
@@ -212,6 +305,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         factor = __uint_as_float((254u - field) << 23) * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e);
         if (there) {
           kv_range(a, it.b, token, place, it.length, lo, hi);
+          lo = max(lo, it.lo);
+          hi = min(hi, it.hi);
           if (a.slopes) slope = a.slopes[h];
         }
       }
@@ -363,27 +458,38 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       phases[1] += (it.tiles + 2) / 2;
       if (!ok) continue;
       tc_fence_after_sync();
-      const float inv = (l > 0.f ? 1.f / l : 0.f) * (FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(e_max - 12) << 23));
+      const float inv = (it.part >= 0 ? 1.f : l > 0.f ? 1.f / l : 0.f) * (FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(e_max - 12) << 23));
       const int64_t to = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
+      float* part = partials + (int64_t)(2 * blockIdx.x + it.part) * C::PARTIAL;
 #pragma unroll 1
       for (int x = 0; x < D; x += 16) {
         uint32_t v[16];
         tmem_ld_32x32_x16(o_at + x, v);
         tmem_ld_wait();
+        constexpr auto column = [](int el) { return FMT == FMT_MXINT4 ? (el < 4 ? 2 * el : 2 * (el - 4) + 1) : el; };   // the elements lie in the order of kv_query_order
 #pragma unroll
         for (int e = 0; e < 16; e += 8) {
-          uint4 y;
+          float z[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                                    // MXINT4: the elements lie in the order of kv_query_order
-            constexpr auto column = [](int el) { return FMT == FMT_MXINT4 ? (el < 4 ? 2 * el : 2 * (el - 4) + 1) : el; };
-            asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"((&y.x)[i]) : "f"(__uint_as_float(v[e + column(2 * i + 1)]) * inv),
-                "f"(__uint_as_float(v[e + column(2 * i)]) * inv));
+          for (int i = 0; i < 8; ++i) z[i] = __uint_as_float(v[e + column(i)]) * inv;
+          if (!there) continue;
+          if (it.part >= 0) {
+            float4* y = reinterpret_cast<float4*>(part + (128 * t + row) * D + x + e);
+            y[0] = make_float4(z[0], z[1], z[2], z[3]);
+            y[1] = make_float4(z[4], z[5], z[6], z[7]);
+          } else {
+            uint4 y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"((&y.x)[i]) : "f"(z[2 * i + 1]), "f"(z[2 * i]));
+            *reinterpret_cast<uint4*>(out + to * D + x + e) = y;
           }
-          if (there) *reinterpret_cast<uint4*>(out + to * D + x + e) = y;
         }
         __syncwarp();
       }
-      if (there && lse) lse[to] = l > 0.f ? (m - kShift + log2f(l)) * kLn2 : -INFINITY;
+      if (there && it.part >= 0) {
+        part[C::ROWS * D + 128 * t + row] = m;
+        part[C::ROWS * D + C::ROWS + 128 * t + row] = l;
+      } else if (there && lse) lse[to] = l > 0.f ? (m - kShift + log2f(l)) * kLn2 : -INFINITY;
       tc_fence_before_sync();
     }
   } else if (warp < 12) {
@@ -396,7 +502,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
     const int ch = dt % CH, row0 = dt / CH;                                // of chunk i: row row0 + i 128 / CH of the group
     uint32_t fill = 0, group_no = 0;
     bool ok = true;
-    for (long long index = blockIdx.x; kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
+    while (kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it)) {
       const int32_t* table = c.table + (int64_t)it.b * c.width;
       const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
       const int groups = (it.tiles + 1) / 2;
@@ -541,7 +647,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
     // result of a reduction does.
     const int t = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)warp) - 12;                  // the tile of rows
     const uint32_t tm = __reduce_max_sync(0xFFFFFFFFu, tmem), sm = __reduce_max_sync(0xFFFFFFFFu, smem);
-    for (long long index = blockIdx.x; t < C::TILES && ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, index, lane, it); index += gridDim.x) {
+    while (t < C::TILES && ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it)) {
       const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)it.tiles);
       const bool active = 128 * t < (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)it.rows);
       const uint32_t o_at = tm + C::O_COL + t * D;
@@ -598,6 +704,65 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
   if (warp == 12) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
+  }
+}
+
+// Joins the parts of an item that borders have cut.  CTA (k, y): the item that goes over from range k to k + 1, where k has its beginning; 32 of its rows, a
+// row to a warp at a time.
+template <class C>
+__global__ void __launch_bounds__(256) kv_prefill_join_kernel(const KvView c, const KvScoring a, int ctas, int heads, const float* partials, __nv_bfloat16* out,
+                                                              float* lse) {
+  constexpr int D = C::D, EACH = D / 32, BATCH = 8;
+  griddep_launch_dependents();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = heads / c.heads;
+  const KvPrefillWalk w = kv_prefill_walk<C::ROWS, C::TOK>(c, a, group, lane, blockIdx.x + 1, ctas);
+  KvPrefillItem it;
+  int unit = 0, each = 1, groups = 0, from = 0, to = -1;
+  auto range_of = [&](long long unit) { return (int)(((unit + 1) * w.ranges + w.units - 1) / w.units) - 1; };
+  if (w.ranges && w.at < w.end && kv_prefill_find<C::ROWS, C::TOK>(c, a, group, w.at, false, lane, it, unit, each, groups) && unit > 0) {
+    from = range_of(w.at - unit);
+    to = range_of(w.at - unit + each - 1);
+  }
+  griddep_wait();                                                          // every CTA waits: what stands behind this kernel relies on that
+  if (from != (int)blockIdx.x) return;
+  for (int i = 0; i < 4; ++i) {
+    const int r = 32 * blockIdx.y + 8 * i + warp;
+    if (r >= it.rows || to < from) return;
+    float m = -INFINITY, l = 0.f, o[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) o[e] = 0.f;
+    for (int k0 = from; k0 <= to; k0 += BATCH) {
+      float pm[BATCH], pl[BATCH], v[BATCH][EACH], top = m;
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x) {
+        const bool have = k0 + x <= to;
+        const float* p = partials + (int64_t)(2 * (k0 + x) + (k0 + x == from ? 1 : 0)) * C::PARTIAL;
+        pm[x] = have ? p[C::ROWS * D + r] : -INFINITY;
+        pl[x] = have ? p[C::ROWS * D + C::ROWS + r] : 0.f;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) v[x][e] = have ? p[r * D + e * 32 + lane] : 0.f;
+      }
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x) top = fmaxf(top, pm[x]);
+      const float old = ex2(m - top);
+      l *= old;
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) o[e] *= old;
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x) {
+        const float f = ex2(pm[x] - top);
+        l += pl[x] * f;
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) o[e] += v[x][e] * f;
+      }
+      m = top;
+    }
+    const int rr = it.first_row + r;
+    const int64_t row = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
+    if (lse && lane == 0) lse[row] = l > 0.f ? (m - kShift + log2f(l)) * kLn2 : -INFINITY;
   }
 }
 

@@ -49,10 +49,10 @@ def test_uneven_batch(fmt):
 @pytest.mark.parametrize("new", [7, 8, 9, 16, 17, 37, 38, 39, 40, 75, 148])
 @pytest.mark.parametrize("dim", [64, 256])
 def test_either_side_of_the_borders(dim, new):
-    """64 heads: the other kernel is taken from 148 rows of a head on."""
+    """The other kernel is taken from 64 rows of a head on."""
     c = Cache("mxfp4", [333], 64, 4, dim, 16, new=[new])
     Q = queries(c)
-    assert ("prefill" in kernel(c, Q)) == (new * 4 >= 148)
+    assert ("prefill" in kernel(c, Q)) == (new * 4 >= 64)
     run(c, Q)
 
 
@@ -152,3 +152,12 @@ def test_what_no_row_sees_may_hold_anything(fmt, dim, new):
         y, z = c.call("attention", Q, *c.scales, return_lse=True, **options)
         assert torch.equal(y, out) and torch.equal(z, lse)
         assert torch.equal(c.call("weights", Q, lse, w.clone(), *c.scales[:1], **options), account)
+
+
+@pytest.mark.parametrize("o", [dict(), dict(window=700), dict(first=True), dict(prefix=True, slopes=True)], ids=lambda o: "-".join(o) or "plain")
+@pytest.mark.parametrize("fmt,dim", [("mxfp4", 128), ("nvfp4", 64), ("mxint4", 256)])
+@pytest.mark.parametrize("lens,new,heads", [([20000], [300], 1), ([3000, 17, 9000], [300, 3, 150], 2), ([6000], [6000], 1), ([5000, 5001], [65, 700], 3)])
+def test_items_that_ranges_cut(lens, new, heads, fmt, dim, o):
+    """Few items with many tokens: CTAs share them, their parts are joined."""
+    c = Cache(fmt, lens, heads, 2, dim, 64, new=new)
+    run(c, queries(c), **options_of(c, o))
