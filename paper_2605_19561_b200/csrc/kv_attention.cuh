@@ -483,7 +483,6 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
                                                       float* lse) {
   constexpr int ROWS = 8 * NT, PARTIAL = ROWS * (D + 2), EACH = D / 32;
   __shared__ float parts[SPLIT == 1 ? 1 : 8][D + 2];
-  griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, which = warp % SPLIT, group = heads / c.heads;
   const int r = blockIdx.y * (8 / SPLIT) + warp / SPLIT;
   KvItem it;
@@ -520,7 +519,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
   // the range that has this step: the last that begins at or before it
   auto range_of = [&](long long unit) { return (int)(((unit + 1) * ranges + units - 1) / units) - 1; };
   const int from = range_of(begin), to = range_of(end - 1);
-  griddep_wait();
+  griddep_wait_and_launch();
   if (from == to) return;                                                  // finished
   float m = -1e30f, l = 0.f, o[EACH] = {};
   constexpr int BATCH = 4;

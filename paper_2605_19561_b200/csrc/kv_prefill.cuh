@@ -713,7 +713,6 @@ template <class C>
 __global__ void __launch_bounds__(256) kv_prefill_join_kernel(const KvView c, const KvScoring a, int ctas, int heads, const float* partials, __nv_bfloat16* out,
                                                               float* lse) {
   constexpr int D = C::D, EACH = D / 32, BATCH = 8;
-  griddep_launch_dependents();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, group = heads / c.heads;
   const KvPrefillWalk w = kv_prefill_walk<C::ROWS, C::TOK>(c, a, group, lane, blockIdx.x + 1, ctas);
   KvPrefillItem it;
@@ -723,7 +722,7 @@ __global__ void __launch_bounds__(256) kv_prefill_join_kernel(const KvView c, co
     from = range_of(w.at - unit);
     to = range_of(w.at - unit + each - 1);
   }
-  griddep_wait();                                                          // every CTA waits: what stands behind this kernel relies on that
+  griddep_wait_and_launch();                                               // every CTA waits: what stands behind this kernel relies on that
   if (from != (int)blockIdx.x) return;
   for (int i = 0; i < 4; ++i) {
     const int r = 32 * blockIdx.y + 8 * i + warp;
