@@ -94,10 +94,10 @@ __device__ __forceinline__ long long kv_prefill_items(const KvView& c, const KvS
   each = max(kv_prefill_tile<ROWS, TOK>(a, group, tiles - 1, it), kv_prefill_tile<ROWS, TOK>(a, group, max(tiles - 2, 0), it));
   return (long long)tiles * c.heads;
 }
-// Whole items where a range, with what cutting costs (more starts, partial results and their join, in all as much as EXTRA groups), would not take less
-// time; ranges have LEAST units at least.  Measured, whole items against ranges, us: one sequence of 32768 tokens, 8 heads of 128: 256 rows of a head 608, 92;
-// 1024: 600, 182; of 256 dimensions, 1024 rows: 1313, 617.  2048 tokens behind 6144, 8 heads of 128 with 4 queries: 303, 329; 16 sequences of up to 5000,
-// 1024 rows: 260, 342.
+// Whole items where ranges, with what cutting costs (partial results and their join: as much as EXTRA groups of each CTA; a start from the middle: 8 for an item),
+// would not take less time; ranges have LEAST units at least.  Measured, whole items against ranges, us: one sequence of 32768 tokens, 8 heads of 128: 256
+// rows of a head 608, 92;  1024: 600, 182;  of 256 dimensions, 1024 rows: 1313, 617.  8 sequences of up to 5000 tokens, 8 heads of 256, up to 1024 rows: 582,
+// 468.  2048 tokens behind 6144, 8 heads of 128 with 4 queries: 303, 329.  16 sequences of up to 5000 tokens, up to 1024 rows: 260, 342.
 template <int ROWS, int TOK>
 __device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const KvScoring& a, int group, int lane, int which, int ctas) {
   constexpr int EXTRA = ROWS == 128 ? 12 : 24, LEAST = 4;
@@ -118,7 +118,8 @@ __device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const 
   longest = __reduce_max_sync(0xFFFFFFFFu, longest);
   KvPrefillWalk w;
   w.units = units;
-  if ((items + ctas - 1) / ctas * longest <= units / ctas + EXTRA) {
+  const long long turns = (items + ctas - 1) / ctas;                       // of whole items; the longest is in one of them, the others are like the average
+  if (items == 0 || (turns - 1) * units / items + longest <= units / ctas + EXTRA + 8 * items / ctas) {
     w.ranges = 0;
     w.at = which;
     w.end = items;
