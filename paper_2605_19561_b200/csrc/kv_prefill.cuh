@@ -9,7 +9,7 @@
 // largest E so far, so a tile with smaller values has smaller weights.  What is summed for the softmax does not have it.
 //
 // Bound by the softmax warps: about 2250 cycles per 64 tokens and 256 rows, of which the exponentials' rate is 1024; the tensor pipe is busy for 40 %.  2048 tokens
-// behind 6144, 8 heads of 128 with 4 queries: 302 us, 145 as products alone.
+// behind 6144, 8 heads of 128 with 4 queries: 310 us, 145 as products alone.
 //
 // Warp-specialised, one CTA per SM, persistent over the items (sequence, head, tiles of rows):
 //   warps 0 - 3, 4 - 7   softmax of the first and second tile, a row to each thread: loads its query, keeps maximum and sum, corrects O when the maximum has
@@ -97,7 +97,7 @@ __device__ __forceinline__ long long kv_prefill_items(const KvView& c, const KvS
 // Whole items where ranges, with what cutting costs (partial results and their join: as much as EXTRA groups of each CTA; a start from the middle: 8 for an item),
 // would not take less time; ranges have LEAST units at least.  Measured, whole items against ranges, us: one sequence of 32768 tokens, 8 heads of 128: 256
 // rows of a head 608, 92;  1024: 600, 182;  of 256 dimensions, 1024 rows: 1313, 617.  8 sequences of up to 5000 tokens, 8 heads of 256, up to 1024 rows: 582,
-// 468.  2048 tokens behind 6144, 8 heads of 128 with 4 queries: 303, 329.  16 sequences of up to 5000 tokens, up to 1024 rows: 260, 342.
+// 468.  2048 tokens behind 6144, 8 heads of 128 with 4 queries: 303 to 310, 329.  16 sequences of up to 5000 tokens, up to 1024 rows: 260, 342.
 template <int ROWS, int TOK>
 __device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const KvScoring& a, int group, int lane, int which, int ctas) {
   constexpr int EXTRA = ROWS == 128 ? 12 : 24, LEAST = 4;
@@ -118,8 +118,9 @@ __device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const 
   longest = __reduce_max_sync(0xFFFFFFFFu, longest);
   KvPrefillWalk w;
   w.units = units;
-  const long long turns = (items + ctas - 1) / ctas;                       // of whole items; the longest is in one of them, the others are like the average
-  if (items == 0 || (turns - 1) * units / items + longest <= units / ctas + EXTRA + 8 * items / ctas) {
+  // turns of whole items: the longest is in one of them, the others are like the average
+  const float n = (float)items, u = (float)units, k = (float)ctas;
+  if (items == 0 || (ceilf(n / k) - 1.f) * (u / n) + (float)longest <= u / k + (float)EXTRA + 8.f * n / k) {
     w.ranges = 0;
     w.at = which;
     w.end = items;
