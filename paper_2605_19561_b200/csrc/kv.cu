@@ -1,6 +1,8 @@
 // C-ABI entry points of the 4-bit key/value cache (see include/torq.h): argument validation, kernel selection and launch.
 #include <cuda_runtime.h>
 #include <atomic>
+#include <cfloat>
+#include <cmath>
 #include <type_traits>
 
 #include "../../include/torq.h"
@@ -55,6 +57,7 @@ static torq_status kv_scoring(const torq_kv_scoring* s, KvScoring* a) {
   if (!aligned4(s->slopes) || !aligned4(s->prefix) || !aligned4(s->first)) return TORQ_ERR_ALIGN;
   a->scale = s->scale;
   a->softcap = s->softcap;
+  a->per_cap = s->softcap > 0.f ? fminf(1.f / s->softcap, FLT_MAX) : 0.f;   // zero times infinity would be no number
   a->slopes = s->slopes;
   a->prefix = s->prefix;
   a->first = s->first;
