@@ -56,8 +56,8 @@ static torq_status kv_scoring(const torq_kv_scoring* s, KvScoring* a) {
   if (!(s->scale > 0.f && s->scale <= 1e30f) || !(s->softcap >= 0.f && s->softcap <= 1e30f) || s->window < 0) return TORQ_ERR_SHAPE;
   if (!aligned4(s->slopes) || !aligned4(s->prefix) || !aligned4(s->first)) return TORQ_ERR_ALIGN;
   a->scale = s->scale;
-  a->softcap = s->softcap;
-  a->per_cap = s->softcap > 0.f ? fminf(1.f / s->softcap, FLT_MAX) : 0.f;   // zero times infinity would be no number
+  a->softcap = s->softcap * kLog2e;
+  a->per_cap = s->softcap > 0.f ? fminf(1.f / a->softcap, FLT_MAX) : 0.f;   // zero times infinity would be no number
   a->slopes = s->slopes;
   a->prefix = s->prefix;
   a->first = s->first;

@@ -9,7 +9,7 @@
 namespace torq {
 
 struct KvScoring {
-  float scale, softcap, per_cap;         // softcap 0: none; per_cap = 1 / softcap
+  float scale, softcap, per_cap;         // softcap, times log2 e as scores are: 0: none; per_cap = 1 / softcap
   const float* slopes;                   // [query heads], or null
   const int32_t* prefix;                 // [batch], or null
   const int32_t* first;                  // [tokens], or null
@@ -41,10 +41,10 @@ __device__ __forceinline__ float kv_cap(float x, float softcap, float per_cap) {
   const float e = exp2f(u * (-2.f * kLog2e));
   return copysignf(softcap * __fdividef(1.f - e, 1.f + e), x);
 }
-// A scaled score with what comes behind, in powers of two.
+// What comes behind a scaled score; all of it, the slope too, times log2 e.
 __device__ __forceinline__ float kv_score(float x, const KvScoring& a, float slope, int distance) {
   if (a.softcap > 0.f) x = kv_cap(x, a.softcap, a.per_cap);
-  return (x - slope * (float)distance) * kLog2e;
+  return x - slope * (float)distance;
 }
 
 
@@ -268,7 +268,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
           const int token = rr / group;
           place[n][e] = it.length - it.count + token;
           kv_range(a, it.b, it.first_token + token, place[n][e], it.length, lo[n][e], hi[n][e]);
-          if (a.slopes) slope[n][e] = a.slopes[it.head * group + rr % group];
+          if (a.slopes) slope[n][e] = a.slopes[it.head * group + rr % group] * kLog2e;
           all_lo = max(all_lo, lo[n][e]);
           all_hi = min(all_hi, hi[n][e]);
           if (lo[n][e] < hi[n][e]) any_lo = min(any_lo, lo[n][e]);
@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
             for (int i = 0; i < 4; ++i) {
               const int e = i & 1, j = j0 + 16 * u + g + 8 * (i >> 1);
               float x = s[u][n][i] * factor[n][e];
-              if (special) x = kv_score(x * kLn2, a, slope[n][e], abs(place[n][e] - j));
+              if (special) x = kv_score(x, a, slope[n][e], abs(place[n][e] - j));
               s[u][n][i] = j >= lo[n][e] && j < hi[n][e] ? x : -INFINITY;
             }
           f[0] = f[1] = 1.f;
@@ -756,7 +756,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
           }
           all_lo = max(all_lo, lo[e]);
           all_hi = min(all_hi, hi[e]);                                     // 0 where a row saw nothing: its scores may be no numbers
-          if (a.slopes) slope[e] = a.slopes[h];
+          if (a.slopes) slope[e] = a.slopes[h] * kLog2e;
         }
       }
 #pragma unroll
@@ -838,7 +838,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
                 for (int i = 0; i < 4; ++i) {
                   const int e = i & 1, j = j0 + 16 * (u0 + u) + g + 8 * (i >> 1);
                   float x = s[i] * factor[e];
-                  if (special) x = kv_score(x * kLn2, a, slope[e], abs(place[e] - j));
+                  if (special) x = kv_score(x, a, slope[e], abs(place[e] - j));
                   part[u][i >> 1] += j >= lo[e] && j < hi[e] ? ex2(x + off[e]) : 0.f;
                 }
               } else {
@@ -984,7 +984,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
       const __nv_bfloat16* q = Q + i * q_stride + h * D + 8 * t;
 #pragma unroll
       for (int x = 0; x < CH; ++x) raw[x] = have ? *reinterpret_cast<const uint4*>(q + 32 * x) : make_uint4(0, 0, 0, 0);
-      row_slope = have && a.slopes ? a.slopes[h] : 0.f;
+      row_slope = have && a.slopes ? a.slopes[h] * kLog2e : 0.f;
       row_place = it.length - it.count + r / group;
       row_lo = row_hi = 0;
       if (have) kv_range(a, it.b, i, row_place, it.length, row_lo, row_hi);
@@ -1092,7 +1092,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
               for (int i = 0; i < 4; ++i) {
                 const int e = i & 1, j = j0 + 16 * u + g + 8 * (i >> 1);
                 float x = s[u][i] * f[e].x;
-                if (special) x = kv_score(x * kLn2, a, f[e].z, abs(__float_as_int(f[e].w) - j));
+                if (special) x = kv_score(x, a, f[e].z, abs(__float_as_int(f[e].w) - j));
                 part[u][i >> 1] += j >= lo[e] && j < hi[e] ? ex2(x + f[e].y) : 0.f;
               }
           } else {

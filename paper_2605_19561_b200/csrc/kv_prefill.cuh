@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           kv_range(a, it.b, token, place, it.length, lo, hi);
           lo = max(lo, it.lo);
           hi = min(hi, it.hi);
-          if (a.slopes) slope = a.slopes[h];
+          if (a.slopes) slope = a.slopes[h] * kLog2e;
         }
       }
       fence_proxy_async_smem();
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         auto score = [&](float s, int col) {                               // where there is more to a score than its factor
           const int j = j0 + col;
           float x = s * f;
-          if (special) x = kv_score(x * kLn2, a, slope, abs(place - j));
+          if (special) x = kv_score(x, a, slope, abs(place - j));
           return j >= lo && j < hi ? x : -INFINITY;
         };
         const bool slow = special || j0 < clear_lo || j0 + TOK > clear_hi;
