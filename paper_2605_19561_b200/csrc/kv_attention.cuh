@@ -458,12 +458,12 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
         for (int x = 4; x < 32; x <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], x);
         const int r = 8 * n + 2 * t + e;
         if (r >= it.rows) continue;
-        const float inv = whole ? (l[n][e] > 0.f ? 1.f / l[n][e] : 0.f) : 1.f;
+        const float inv = l[n][e] > 0.f ? 1.f / l[n][e] : 0.f;            // of a part too: its result is as large as its values, its sum stands beside it
         const int64_t row = kv_out_row(it, r, heads, group);
 #pragma unroll
         for (int ch = 0; ch < CH; ++ch) {
-          const float fs = FMT == FMT_NVFP4 ? inv * c.v_ts : inv * __uint_as_float((uint32_t)(top_scale[ch] - 12) << 23);
-          const float4 v = make_float4(o[n][ch][0][e] * fs, o[n][ch][0][e + 2] * fs, o[n][ch][1][e] * fs, o[n][ch][1][e + 2] * fs);
+          const float fs = FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(top_scale[ch] - 12) << 23);      // inv times it may be too small a number
+          const float4 v = make_float4(o[n][ch][0][e] * inv * fs, o[n][ch][0][e + 2] * inv * fs, o[n][ch][1][e] * inv * fs, o[n][ch][1][e + 2] * inv * fs);
           if (whole) {
             uint2 y;
             asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(y.x) : "f"(v.y), "f"(v.x));
@@ -482,6 +482,25 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
         }
       }
   }
+}
+
+// N parts with maxima pm, sums pl and results v, into m, l and o; `top`: the largest of all maxima.  Results are averages, of the parts and of what is joined so
+// far: the factors add up to one, so nothing is larger than the values are.
+template <int N, int EACH>
+__device__ __forceinline__ void kv_join(const float (&pm)[N], const float (&pl)[N], const float (&v)[N][EACH], float top, float& m, float& l, float (&o)[EACH]) {
+  const float before = l * ex2(m - top);
+  float w[N], sum = before;
+#pragma unroll
+  for (int x = 0; x < N; ++x) sum += w[x] = pl[x] * ex2(pm[x] - top);
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) o[e] *= before * inv;
+#pragma unroll
+  for (int x = 0; x < N; ++x)
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) o[e] += v[x][e] * (w[x] * inv);
+  l = sum;
+  m = top;
 }
 
 // Joins the results of an item that more than one warp has worked on.  CTA (i, j): item i of the list, its rows from j (8 / SPLIT) on; SPLIT warps to a
@@ -554,18 +573,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
     float top = m;
 #pragma unroll
     for (int x = 0; x < BATCH; ++x) top = fmaxf(top, pm[x]);
-    const float old = ex2(m - top);
-    l *= old;
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) o[e] *= old;
-#pragma unroll
-    for (int x = 0; x < BATCH; ++x) {
-      const float f = ex2(pm[x] - top);
-      l += pl[x] * f;
-#pragma unroll
-      for (int e = 0; e < EACH; ++e) o[e] += v[x][e] * f;
-    }
-    m = top;
+    kv_join<BATCH, EACH>(pm, pl, v, top, m, l, o);
   }
   if constexpr (SPLIT > 1) {
 #pragma unroll
@@ -576,26 +584,22 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
     }
     __syncthreads();
     if (which) return;
-    float top = m;
-#pragma unroll
-    for (int x = 1; x < SPLIT; ++x) top = fmaxf(top, parts[warp + x][D]);
-    l = 0.f;
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) o[e] = 0.f;
+    float top = m, pm[SPLIT], pl[SPLIT], v[SPLIT][EACH];
 #pragma unroll
     for (int x = 0; x < SPLIT; ++x) {
-      const float f = ex2(parts[warp + x][D] - top);
-      l += parts[warp + x][D + 1] * f;
+      pm[x] = parts[warp + x][D];
+      pl[x] = parts[warp + x][D + 1];
+      top = fmaxf(top, pm[x]);
 #pragma unroll
-      for (int e = 0; e < EACH; ++e) o[e] += parts[warp + x][e * 32 + lane] * f;
+      for (int e = 0; e < EACH; ++e) v[x][e] = parts[warp + x][e * 32 + lane];
     }
-    m = top;
+    l = 0.f;
+    kv_join<SPLIT, EACH>(pm, pl, v, top, m, l, o);
   }
   if (r >= it.rows) return;
   const int64_t row = kv_out_row(it, r, heads, group);
-  const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-  for (int e = 0; e < EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
+  for (int e = 0; e < EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e]);
   if (lse && lane == 0) lse[row] = l > 0.f ? (m - kShift + log2f(l)) * kLn2 : -INFINITY;
 }
 

@@ -460,7 +460,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       phases[1] += (it.tiles + 2) / 2;
       if (!ok) continue;
       tc_fence_after_sync();
-      const float inv = (it.part >= 0 ? 1.f : l > 0.f ? 1.f / l : 0.f) * (FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(e_max - 12) << 23));
+      // of a part too, as in the streaming kernel
+      const float inv = l > 0.f ? 1.f / l : 0.f, fs = FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(e_max - 12) << 23);
       const int64_t to = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
       float* part = partials + (int64_t)(2 * blockIdx.x + it.part) * C::PARTIAL;
 #pragma unroll 1
@@ -473,7 +474,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         for (int e = 0; e < 16; e += 8) {
           float z[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) z[i] = __uint_as_float(v[e + column(i)]) * inv;
+          for (int i = 0; i < 8; ++i) z[i] = __uint_as_float(v[e + column(i)]) * inv * fs;
           if (!there) continue;
           if (it.part >= 0) {
             float4* y = reinterpret_cast<float4*>(part + (128 * t + row) * D + x + e);
@@ -745,24 +746,12 @@ __global__ void __launch_bounds__(256) kv_prefill_join_kernel(const KvView c, co
       }
 #pragma unroll
       for (int x = 0; x < BATCH; ++x) top = fmaxf(top, pm[x]);
-      const float old = ex2(m - top);
-      l *= old;
-#pragma unroll
-      for (int e = 0; e < EACH; ++e) o[e] *= old;
-#pragma unroll
-      for (int x = 0; x < BATCH; ++x) {
-        const float f = ex2(pm[x] - top);
-        l += pl[x] * f;
-#pragma unroll
-        for (int e = 0; e < EACH; ++e) o[e] += v[x][e] * f;
-      }
-      m = top;
+      kv_join<BATCH, EACH>(pm, pl, v, top, m, l, o);
     }
     const int rr = it.first_row + r;
     const int64_t row = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e] * inv);
+    for (int e = 0; e < EACH; ++e) out[row * D + e * 32 + lane] = __float2bfloat16(o[e]);
     if (lse && lane == 0) lse[row] = l > 0.f ? (m - kShift + log2f(l)) * kLn2 : -INFINITY;
   }
 }
