@@ -251,7 +251,8 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
 
     // the queries, and what each row sees
     KvQuery<D> q[NT];
-    float factor[NT][2], slope[NT][2], m[NT][2], l[NT][2];
+    const float unit = a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e;
+    float factor[NT][2], slope[NT][2], m[NT][2], l[NT][2];                 // a score's factor: times `unit` and what keys are taken smaller by
     int place[NT][2], lo[NT][2], hi[NT][2], all_lo = 0, all_hi = INT32_MAX, any_lo = INT32_MAX, any_hi = 0;   // what all rows see, what any does
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int col = 8 * n + 2 * t + e, rr = it.first_row + col;
-        factor[n][e] = __shfl_sync(0xFFFFFFFFu, back, 8 * t + 4 * e) * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e);
+        factor[n][e] = __shfl_sync(0xFFFFFFFFu, back, 8 * t + 4 * e);
         lo[n][e] = hi[n][e] = place[n][e] = 0;
         slope[n][e] = 0.f;
         if (col < it.rows) {
@@ -310,11 +311,12 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
       const bool border = j0 < all_lo || j0 + C::STEP > all_hi;
 
       // scales of the 32 tokens; those that no row sees may be no numbers, or larger than all others
-      kv_ready_key_scales<FMT, D>(scales, lane, room);
+      const bool seen = j0 + lane >= any_lo && j0 + lane < any_hi;
+      const float now = unit * kv_ready_key_scales<FMT, D>(scales, lane, seen, room);
       {
         uint32_t w[(SB + 3) / 4];
         kv_scale_words<SB>(scales + C::S_BYTES + lane * SB, w);
-        if (border && (j0 + lane < any_lo || j0 + lane >= any_hi)) {
+        if (border && !seen) {
 #pragma unroll
           for (int i = 0; i < (SB + 3) / 4; ++i) w[i] = 0;
         }
@@ -367,14 +369,14 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
       for (int u = 0; u < 2; ++u) kv_tile_scores<FMT, D, NT>(stage, room, 16 * u, lane, q, s[u]);
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        float f[2] = {factor[n][0], factor[n][1]};
+        float f[2] = {factor[n][0] * now, factor[n][1] * now};
         if (special || border) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const int e = i & 1, j = j0 + 16 * u + g + 8 * (i >> 1);
-              float x = s[u][n][i] * factor[n][e];
+              float x = s[u][n][i] * f[e];
               if (special) x = kv_score(x, a, slope[n][e], abs(place[n][e] - j));
               s[u][n][i] = j >= lo[n][e] && j < hi[n][e] ? x : -INFINITY;
             }
@@ -734,7 +736,9 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
       look_up(k + 1);
     }
 
-    // eight rows: their operand, factors to powers of two, ranges.  A row that is not there, or that saw nothing, counts exp2(-inf).
+    const float unit = a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e;
+    // eight rows: their operand, factors to powers of two (times `unit` and what keys are taken smaller by: a product for each score, since one for each group
+    // would need two registers that there are not: 47 us instead of 42), ranges.  A row that is not there, or that saw nothing, counts exp2(-inf).
     KvQuery<D> q[1];
     float factor[2], off[2], slope[2];
     int place[2], lo[2], hi[2], all_lo, all_hi;
@@ -746,7 +750,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int rr = 8 * n + 2 * t + e;
-        factor[e] = __shfl_sync(0xFFFFFFFFu, back, 8 * t + 4 * e) * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e);
+        factor[e] = __shfl_sync(0xFFFFFFFFu, back, 8 * t + 4 * e);
         lo[e] = hi[e] = place[e] = 0;
         slope[e] = 0.f;
         off[e] = -INFINITY;
@@ -791,7 +795,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
       }
       float sum[2][2] = {};                                                // tokens g, g + 8, g + 16, g + 24, of this lane's columns
       if (groups > 0 && j0 + 32 > it.lo) {
-        kv_ready_key_scales<FMT, D>(ring_p + (stage - ring) + C::K_BYTES, lane, room);
+        const float now = unit * kv_ready_key_scales<FMT, D>(ring_p + (stage - ring) + C::K_BYTES, lane, mine_j >= it.lo && mine_j < it.length, room);
         __syncwarp();
 #pragma unroll 1
         for (int u0 = 0; u0 < 2; u0 += TILES) {
@@ -841,13 +845,13 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                   const int e = i & 1, j = j0 + 16 * (u0 + u) + g + 8 * (i >> 1);
-                  float x = s[i] * factor[e];
+                  float x = s[i] * factor[e] * now;
                   if (special) x = kv_score(x, a, slope[e], abs(place[e] - j));
                   part[u][i >> 1] += j >= lo[e] && j < hi[e] ? ex2(x + off[e]) : 0.f;
                 }
               } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) part[u][i >> 1] += ex2(fmaf(s[i], factor[i & 1], off[i & 1]));
+                for (int i = 0; i < 4; ++i) part[u][i >> 1] += ex2(fmaf(s[i] * factor[i & 1], now, off[i & 1]));
               }
             }
           }
@@ -1008,8 +1012,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
       const int in_all_lo = __reduce_max_sync(0xFFFFFFFFu, row_lo), in_all_hi = __reduce_min_sync(0xFFFFFFFFu, row_hi);
       const int in_any_lo = __reduce_min_sync(0xFFFFFFFFu, row_hi > 0 ? row_lo : INT32_MAX), in_any_hi = __reduce_max_sync(0xFFFFFFFFu, row_hi);
       if (t == 0) {
-        reinterpret_cast<float4*>(to + C::QUERIES)[g] = make_float4(back * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e), -row_lse * kLog2e, row_slope,
-                                                                    __int_as_float(row_place));
+        reinterpret_cast<float4*>(to + C::QUERIES)[g] = make_float4(back, -row_lse * kLog2e, row_slope, __int_as_float(row_place));
         reinterpret_cast<int2*>(to + C::QUERIES + 128)[g] = make_int2(row_lo, row_hi);
       }
       if (lane == 0) *reinterpret_cast<int4*>(to + C::QUERIES + 192) = make_int4(in_all_lo, in_all_hi, in_any_lo, in_any_hi);
@@ -1033,7 +1036,9 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
       cp_async_wait<1>();
       __syncwarp();
       const uint32_t stage = ring + (k & 1) * C::STAGE;
-      kv_ready_key_scales<FMT, D>(ring_p + (k & 1) * C::STAGE + C::K_BYTES, lane, room);
+      const int token = lane % OWN;                                        // D = 256: two lanes to a token
+      const float now = a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e *
+                        kv_ready_key_scales<FMT, D>(ring_p + (k & 1) * C::STAGE + C::K_BYTES, token, j0 + token >= it.lo && j0 + token < it.length, room);
       __syncwarp();
       uint32_t keys[TILES][CH][2][4], scale[TILES][2][CH];
       float part[TILES][2] = {};
@@ -1066,7 +1071,9 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
           const int4 limits = *reinterpret_cast<const int4*>(from + C::QUERIES + 192);
           if (j0 >= limits.w || j0 + OWN <= limits.z) continue;            // no row of the group sees any of these tokens
           const bool border = j0 < limits.x || j0 + OWN > limits.y;
-          const float4 f[2] = {reinterpret_cast<const float4*>(from + C::QUERIES)[2 * t], reinterpret_cast<const float4*>(from + C::QUERIES)[2 * t + 1]};
+          float4 f[2] = {reinterpret_cast<const float4*>(from + C::QUERIES)[2 * t], reinterpret_cast<const float4*>(from + C::QUERIES)[2 * t + 1]};
+          f[0].x *= now;
+          f[1].x *= now;
           float s[TILES][4] = {};
 #pragma unroll
           for (int ch = 0; ch < CH; ++ch) {

@@ -152,12 +152,34 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w) {
     w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
   }
 }
-// The scale bytes of key `token` of the 32 (E8M0 byte 0 counts as zero).
+// The scale bytes of key `token` of the 32 (E8M0 byte 0 counts as zero).  Queries are scaled up, so their products with a large key may pass float32 though
+// the score does not.  Where a byte is 192 or more (2^65), which is seldom, all 32 keys are taken 2^(E - 191) times smaller, E the largest byte of the tokens
+// that may be seen (`seen`: whether this one may; the others count as zero then), and the power of two to be multiplied back is returned, the same for all lanes.
+// So the sums stay below 2^64 times 2^26, that of 256 products of a code (8 at most) and an element of a query (2^15).
 template <int FMT, int D>
-__device__ __forceinline__ void kv_ready_key_scales(const uint8_t* scales, int token, uint8_t* room) {
+__device__ __forceinline__ float kv_ready_key_scales(const uint8_t* scales, int token, bool seen, uint8_t* room) {
   constexpr int CH = D / 32, SB = D / kv_block(FMT), V = CH < 4 ? CH : 4;
   uint32_t w[(SB + 3) / 4];
   kv_scale_words<SB>(scales + token * SB, w);
+  float back = 1.f;
+  if constexpr (FMT != FMT_NVFP4) {
+    uint32_t high = 0;
+#pragma unroll
+    for (int i = 0; i < (SB + 3) / 4; ++i) high |= w[i] & w[i] << 1;
+    if (__any_sync(0xFFFFFFFFu, (high & 0x80808080u) != 0)) {
+      uint32_t most = 0;
+#pragma unroll
+      for (int i = 0; i < (SB + 3) / 4; ++i) {
+        if (!seen) w[i] = 0;
+        most = __vmaxu4(most, w[i]);
+      }
+      most = max(max(most & 0xFFu, most >> 8 & 0xFFu), max(most >> 16 & 0xFFu, most >> 24));
+      const uint32_t top = __reduce_max_sync(0xFFFFFFFFu, most), down = top > 191u ? top - 191u : 0u;
+#pragma unroll
+      for (int i = 0; i < (SB + 3) / 4; ++i) w[i] = __vsubus4(w[i], down * 0x01010101u);
+      back = __uint_as_float((127u + down) << 23);
+    }
+  }
   uint32_t even[CH], odd[CH];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -175,6 +197,7 @@ __device__ __forceinline__ void kv_ready_key_scales(const uint8_t* scales, int t
     store_words<V>(room + (c / V * 32 + token) * (4 * V), even + c);
     if constexpr (FMT == FMT_NVFP4) store_words<V>(room + KvScaleRoom<FMT, D>::KEYS / 2 + (c / V * 32 + token) * (4 * V), odd + c);
   }
+  return back;
 }
 // ... as lane t needs them.
 template <int FMT, int D>

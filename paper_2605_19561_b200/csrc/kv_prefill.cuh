@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           for (int i = 0; i < 4; ++i) (&y.x)[i] = pack_f16(v[kv_query_order<FMT>(i, 0)], v[kv_query_order<FMT>(i, 1)]);
           if (ok) *reinterpret_cast<uint4*>(dst + (e >> 3) * (128 * 128) + (((e & 7) ^ (row & 7)) << 4)) = y;
         }
-        factor = __uint_as_float((254u - field) << 23) * (a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e);
+        factor = __uint_as_float((254u - field) << 23);
         if (there) {
           kv_range(a, it.b, token, place, it.length, lo, hi);
           lo = max(lo, it.lo);
@@ -331,13 +331,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         tc_fence_after_sync();
         const int j0 = it.base + k * TOK;
         const uint32_t s_at = tmem + lanes + (2 * t + (k & 1)) * TOK;
-        float f = factor;
+        float f = a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e;    // the keys' power of two before the query's: with that it may be too small a number
         int e_tile = 27;
         if constexpr (FMT != FMT_NVFP4) {
           const volatile int* tops = tile_top + 2 * ((first_group + (k >> 1)) & 7);
           f *= __uint_as_float((uint32_t)(tops[0] - 12) << 23);
           e_tile = tops[1];
         }
+        f *= factor;
         auto score = [&](float s, int col) {                               // where there is more to a score than its factor
           const int j = j0 + col;
           float x = s * f;
