@@ -609,7 +609,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
                     f[0] = __byte_perm(two, 0, 0x1010);
                     f[1] = __byte_perm(two, 0, 0x3232);
                   } else {
-                    f[0] = f[1] = (uint32_t)max((int)scale[half][i] + down[half], 0) * 0x04000400u;
+                    // 2^(e - E + 12): its exponent in float16, or, for e - E from -27 to -35, a number below the normal ones
+                    const int field = (int)scale[half][i] + down[half];
+                    const uint32_t small = scale[half][i] ? 0x200u >> min(max(-field, 0), 31) & 0x3FEu : 0u;
+                    f[0] = f[1] = (field > 0 ? (uint32_t)field << 10 : small) * 0x00010001u;
                   }
 #pragma unroll
                   for (int x = 0; x < 4; ++x) {
