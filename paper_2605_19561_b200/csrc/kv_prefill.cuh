@@ -4,9 +4,11 @@
 //   P = exp2(...)    from tensor memory and back into it as float16, in the place of S
 //   O += P V         P from tensor memory, V from shared memory
 // Keys and values are widened to float16 once per CTA and tile, whatever the number of rows: codes are exact there, with the scales as follows.
-// NVFP4: code times E4M3 scale, exact.  MXFP4, MXINT4: code times 2^(e - E + 12), E the largest exponent in the tile (keys and values apart), exact for
-// scales down to 2^-35 of that; 2^E of the keys goes into the scores' factor, that of the values into the weights: P = exp2(x - m + 10 + E - E_max), E_max the
-// largest E so far, so a tile with smaller values has smaller weights.  What is summed for the softmax does not have it.
+// NVFP4: code times E4M3 scale, exact.  MXFP4, MXINT4: code times 2^(e - E + 12), E the largest exponent in 128 tokens (keys and values apart), exact for
+// scales down to 2^-35 of that; 2^E of the keys goes into the scores' factor, that of the values into the weights: P = exp2(x - m + 10 + E - e), where m and e,
+// for each row, follow the largest score and the largest product of a weight and 2^E: that one's P lies in [2^10, 2^15].  So a weight counts by what its values
+// make of it, and tokens that a row does not see, or hardly, do not lower the precision of others.  What is summed for the softmax does not have 2^E.
+// (One e for all rows, the largest E so far: no faster, and values 2^30 smaller than some that a row gives no weight had 4 bits of their weights left.)
 //
 // Bound by the softmax warps: about 2250 cycles per 64 tokens and 256 rows, of which the exponentials' rate is 1024; the tensor pipe is busy for 40 %.  2048 tokens
 // behind 6144, 8 heads of 128 with 4 queries: 310 us, 145 as products alone.
@@ -202,7 +204,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
   auto p_full = [&](int t, int buffer) { return bar + 8 * (2 * C::STAGES + 4 + 2 * t + buffer); };
   auto q_full = [&](int t) { return bar + 8 * (2 * C::STAGES + 8 + t); };
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, group = heads / c.heads;
-  volatile int* tile_top = reinterpret_cast<volatile int*>(smem_p + C::INFO_AT);                   // [8][2]: E of the keys and of the values of 128 tokens
+  volatile int* tile_top = reinterpret_cast<volatile int*>(smem_p + C::INFO_AT);                   // [8][2]: E of the keys and (as a float) of the values of 128 tokens
   int* warp_top = reinterpret_cast<int*>(smem_p + C::INFO_AT + 64);                                // [2][4][2]
 
   if (tid == 0) {
@@ -318,7 +320,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       const int clear_hi = (int)__reduce_min_sync(0xFFFFFFFFu, there ? (uint32_t)max(hi, 0) : 0x7FFFFFFFu);
 
       float m = -1e30f, l = 0.f;
-      int e_max = 27;
+      float e_row = 27.f;                                                  // O is held times 2^(10 - m - e_row), e_row the E of the largest product so far or near it
       if (in_turn && t == 1) named_barrier_arrive(2, 256);                 // the first tile's turn
       for (int k = 0; k < it.tiles; ++k) {
         if (!wait_s(k)) {
@@ -332,11 +334,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         const int j0 = it.base + k * TOK;
         const uint32_t s_at = tmem + lanes + (2 * t + (k & 1)) * TOK;
         float f = a.scale * (FMT == FMT_NVFP4 ? c.k_ts : 1.f) * kLog2e;    // the keys' power of two before the query's: with that it may be too small a number
-        int e_tile = 27;
+        float e_tile = 27.f;
         if constexpr (FMT != FMT_NVFP4) {
           const volatile int* tops = tile_top + 2 * ((first_group + (k >> 1)) & 7);
           f *= __uint_as_float((uint32_t)(tops[0] - 12) << 23);
-          e_tile = tops[1];
+          e_tile = __int_as_float(tops[1]);
         }
         f *= factor;
         auto score = [&](float s, int col) {                               // where there is more to a score than its factor
@@ -346,19 +348,25 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           return j >= lo && j < hi ? x : -INFINITY;
         };
         const bool slow = special || j0 < clear_lo || j0 + TOK > clear_hi;
-        const int e_old = e_max;
-        e_max = max(e_max, e_tile);
-        const int down = e_max - e_tile;                                   // this tile's values are smaller: so are its weights
-        const bool faint = down > 40;                                      // too small to matter, but they count in the sum
-        bool wrong = e_max != e_old;                                       // whether some row's O has to be corrected
-        float fix = e_max - e_old > 126 ? 0.f : __uint_as_float((uint32_t)(127 - (e_max - e_old)) << 23);      // of O
-        const float off0 = kShift - (faint ? 0.f : (float)down);
-        auto raised = [&](float top) {                                     // m is no longer near enough to the largest score
-          if (top <= m + kSlack) return;
-          const float old = ex2(m - top);
-          m = top;
-          l *= old;
-          fix *= old;
+        // This tile's values are 2^down smaller than e_row says: so are its weights.  (Down to 2^-80, where they are nothing in float16; in the sum they count.)
+        float down = FMT == FMT_NVFP4 ? 0.f : fminf(e_row - e_tile, 80.f);
+        // Whether m and e_row do not do for a score.  Where the tile's values are larger than e_row says, its weights are too: products count, not weights.
+        auto beyond = [&](float top) { return top > m + (kSlack + fminf(down, 0.f)); };
+        bool wrong = false;                                                // whether some row's O has to be corrected
+        float fix = 1.f;                                                   // of O
+        auto raised = [&](float top) {
+          if (!beyond(top)) return;
+          const float now = top > m + kSlack ? top : m, less = m - now;
+          fix = ex2(less);
+          l *= fix;
+          m = now;
+          if constexpr (FMT != FMT_NVFP4) {
+            // whole numbers, so that weights and their sum differ by a power of two
+            const float e = fmaxf(floorf(fmaxf(less, -1024.f)) + e_row, floorf(top - now) + e_tile);
+            fix = ex2(less + (e_row - e));
+            e_row = e;
+            down = fminf(e_row - e_tile, 80.f);
+          }
         };
         // In one pass with the maximum so far; a second one where a score turns out to exceed it by too much (the first tiles).  P stays in
         // registers until it may take the place of S.  What is seldom needed has loops of its own: in one loop with the plain case it
@@ -366,7 +374,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         uint32_t w[2][16];
         float sum = 0.f, top = -INFINITY;
         auto weigh = [&]() {
-          const uint64_t f2 = pair_of(f), off2 = pair_of(off0 - m);
+          const uint64_t f2 = pair_of(f), off2 = pair_of(kShift - down - m);
           uint64_t sums = 0;
           float tops[2] = {-INFINITY, -INFINITY};
           uint32_t v[2][32];
@@ -392,7 +400,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         if (!slow) {
           weigh();
           if (in_turn) named_barrier_arrive(3 - t, 256);
-          if (__any_sync(0xFFFFFFFFu, top > m + kSlack)) {
+          if (__any_sync(0xFFFFFFFFu, beyond(top))) {
             wrong = true;
             raised(top);
             __syncwarp();
@@ -409,7 +417,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
             for (int i = 0; i < 32; ++i) top = fmaxf(top, score(__uint_as_float(v[i]), x + i));
             __syncwarp();
           }
-          wrong |= __any_sync(0xFFFFFFFFu, top > m + kSlack);
+          wrong = __any_sync(0xFFFFFFFFu, beyond(top));
           raised(top);
           __syncwarp();
         }
@@ -435,22 +443,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              const float p = ex2(score(__uint_as_float(v[i]), x + i) + (off0 - m)), p2 = ex2(score(__uint_as_float(v[i + 1]), x + i + 1) + (off0 - m));
+              const float p = ex2(score(__uint_as_float(v[i]), x + i) + (kShift - down - m)), p2 = ex2(score(__uint_as_float(v[i + 1]), x + i + 1) + (kShift - down - m));
               sum += p + p2;
-              y[i / 2] = faint ? 0u : pack_f16(p, p2);
+              y[i / 2] = pack_f16(p, p2);
             }
             __syncwarp();
             tmem_st_32x32_x16(s_at + x / 2, y);
           }
         } else {
-          if (faint) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) w[i / 16][i % 16] = 0;
-          }
           tmem_st_32x32_x16(s_at, w[0]);
           tmem_st_32x32_x16(s_at + 16, w[1]);
         }
-        l += sum * (faint ? 1.f : __uint_as_float((uint32_t)(127 + down) << 23));
+        l += FMT == FMT_NVFP4 ? sum : sum * ex2(down);
         tmem_st_wait();
         tc_fence_before_sync();
         mbar_arrive(p_full(t, k & 1));
@@ -462,7 +466,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       if (!ok) continue;
       tc_fence_after_sync();
       // of a part too, as in the streaming kernel
-      const float inv = l > 0.f ? 1.f / l : 0.f, fs = FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)(e_max - 12) << 23);
+      const float inv = l > 0.f ? 1.f / l : 0.f, fs = FMT == FMT_NVFP4 ? c.v_ts : __uint_as_float((uint32_t)((int)e_row - 12) << 23);
       const int64_t to = (int64_t)(it.first_token + rr / group) * heads + it.head * group + rr % group;
       float* part = partials + (int64_t)(2 * blockIdx.x + it.part) * C::PARTIAL;
 #pragma unroll 1
@@ -587,7 +591,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
             const int* w = warp_top + (group_no & 1) * 8 + half;
             const int most = max(max(w[0], w[2]), max(w[4], w[6]));
             down[half] = 27 - most;
-            if (dt == 0) tile_top[2 * (group_no & 7) + half] = most;
+            if (dt == 0) tile_top[2 * (group_no & 7) + half] = half ? __float_as_int((float)most) : most;
           }
         }
         const int tiles = min(2, it.tiles - 2 * g);
