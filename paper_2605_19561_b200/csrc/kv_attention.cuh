@@ -19,6 +19,8 @@ struct KvScoring {
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // Weights are exp2(x - m + kShift), m raised when a score exceeds it by kSlack: in float16 they are at most 2^15, and those of 2^-14 - kShift keep 11 bits.
 constexpr float kShift = 10.f, kSlack = 5.f;
+// Where a maximum starts: below every score that float32 has room for, and finite.
+constexpr float kLowest = -3.4e38f;
 
 // The range [lo, hi) of cached tokens that row `i`, place p of sequence b with `length` tokens, sees.
 __device__ __forceinline__ void kv_range(const KvScoring& a, int b, int i, int p, int length, int& lo, int& hi) {
@@ -275,7 +277,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
           if (lo[n][e] < hi[n][e]) any_lo = min(any_lo, lo[n][e]);
           any_hi = max(any_hi, hi[n][e]);
         }
-        m[n][e] = -1e30f;
+        m[n][e] = kLowest;
         l[n][e] = 0.f;
       }
     }
@@ -550,7 +552,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
   const int from = range_of(begin), to = range_of(end - 1);
   griddep_wait_and_launch();
   if (from == to) return;                                                  // finished
-  float m = -1e30f, l = 0.f, o[EACH] = {};
+  float m = kLowest, l = 0.f, o[EACH] = {};
   constexpr int BATCH = 4;
   const bool dense = units >= ranges;                                      // else a range has one step at most, and most have none
   const int parts_n = dense ? to - from + 1 : per;
@@ -559,7 +561,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
 #pragma unroll
     for (int x = 0; x < BATCH; ++x) {
       const int k = i + x * SPLIT;
-      pm[x] = -1e30f;
+      pm[x] = kLowest;
       pl[x] = 0.f;
 #pragma unroll
       for (int e = 0; e < EACH; ++e) v[x][e] = 0.f;

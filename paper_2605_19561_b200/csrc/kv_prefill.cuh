@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       const int clear_lo = (int)__reduce_max_sync(0xFFFFFFFFu, there ? (uint32_t)max(lo, 0) : 0u);          // tiles within [clear_lo, clear_hi) need no mask
       const int clear_hi = (int)__reduce_min_sync(0xFFFFFFFFu, there ? (uint32_t)max(hi, 0) : 0x7FFFFFFFu);
 
-      float m = -1e30f, l = 0.f;
+      float m = kLowest, l = 0.f;
       float e_row = 27.f;                                                  // O is held times 2^(10 - m - e_row), e_row the E of the largest product so far or near it
       if (in_turn && t == 1) named_barrier_arrive(2, 256);                 // the first tile's turn
       for (int k = 0; k < it.tiles; ++k) {
