@@ -21,6 +21,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kShift = 10.f, kSlack = 5.f;
 // Where a maximum starts: below every score that float32 has room for, and finite.
 constexpr float kLowest = -3.4e38f;
+// From here on a maximum is so far from zero that the rounding of the product that it comes from may count in an exponent: scores are rounded as it was before
+// it is taken off (fused, a score of 2^27 could be 8 more than itself, and a float16 weight infinite).
+constexpr float kFar = 1048576.f;
+__device__ __forceinline__ bool kv_far(float m) { return fabsf(m) > kFar && m > kLowest; }
 
 // The range [lo, hi) of cached tokens that row `i`, place p of sequence b with `length` tokens, sees.
 __device__ __forceinline__ void kv_range(const KvScoring& a, int b, int i, int p, int length, int& lo, int& hi) {
@@ -302,6 +306,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
       top_pair[i / 2] = 0x001B001Bu;
     }
 
+    bool far = false;                                                      // whether some row's maximum is
     uint32_t stage = ring;
     for (int k = 0; k < steps; ++k) {
       cp_async_wait<C::STAGES - 2>();
@@ -389,7 +394,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           most[e] = fmaxf(fmaxf(s[0][n][e], s[0][n][e + 2]), fmaxf(s[1][n][e], s[1][n][e + 2])) * f[e];
-          raise |= most[e] > m[n][e] + kSlack;
+          raise |= most[e] - m[n][e] > kSlack;
         }
         if (__any_sync(0xFFFFFFFFu, raise)) {
 #pragma unroll
@@ -406,8 +411,17 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
               o[n][i / 2][i % 2][e + 2] *= old;
             }
           }
+          far |= __any_sync(0xFFFFFFFFu, kv_far(m[n][0]) || kv_far(m[n][1]));
         }
-        const float off[2] = {kShift - m[n][0], kShift - m[n][1]};
+        float off[2] = {kShift - m[n][0], kShift - m[n][1]};
+        if (far) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[u][n][i] = __fsub_rn(__fmul_rn(s[u][n][i], f[i & 1]), m[n][i & 1]);
+          f[0] = f[1] = 1.f;
+          off[0] = off[1] = kShift;
+        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll

@@ -320,6 +320,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
       const int clear_hi = (int)__reduce_min_sync(0xFFFFFFFFu, there ? (uint32_t)max(hi, 0) : 0x7FFFFFFFu);
 
       float m = kLowest, l = 0.f;
+      bool far = false;                                                    // whether some row's m is
       float e_row = 27.f;                                                  // O is held times 2^(10 - m - e_row), e_row the E of the largest product so far or near it
       if (in_turn && t == 1) named_barrier_arrive(2, 256);                 // the first tile's turn
       for (int k = 0; k < it.tiles; ++k) {
@@ -343,20 +344,20 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
         f *= factor;
         auto score = [&](float s, int col) {                               // where there is more to a score than its factor
           const int j = j0 + col;
-          float x = s * f;
+          float x = __fmul_rn(s, f);                                       // not fused with what is taken off it
           if (special) x = kv_score(x, a, slope, abs(place - j));
           return j >= lo && j < hi ? x : -INFINITY;
         };
-        const bool slow = special || j0 < clear_lo || j0 + TOK > clear_hi;
+        bool slow = special || far || j0 < clear_lo || j0 + TOK > clear_hi;
         // This tile's values are 2^down smaller than e_row says: so are its weights.  (Down to 2^-80, where they are nothing in float16; in the sum they count.)
         float down = FMT == FMT_NVFP4 ? 0.f : fminf(e_row - e_tile, 80.f);
         // Whether m and e_row do not do for a score.  Where the tile's values are larger than e_row says, its weights are too: products count, not weights.
-        auto beyond = [&](float top) { return top > m + (kSlack + fminf(down, 0.f)); };
+        auto beyond = [&](float top) { return top - m > kSlack + fminf(down, 0.f); };
         bool wrong = false;                                                // whether some row's O has to be corrected
         float fix = 1.f;                                                   // of O
         auto raised = [&](float top) {
           if (!beyond(top)) return;
-          const float now = top > m + kSlack ? top : m, less = m - now;
+          const float now = top - m > kSlack ? top : m, less = m - now;
           fix = ex2(less);
           l *= fix;
           m = now;
@@ -403,8 +404,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           if (__any_sync(0xFFFFFFFFu, beyond(top))) {
             wrong = true;
             raised(top);
-            __syncwarp();
-            weigh();
+            slow = far = __any_sync(0xFFFFFFFFu, kv_far(m));
+            if (!far) weigh();
           }
         } else {
           if (in_turn) named_barrier_arrive(3 - t, 256);
@@ -419,7 +420,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           }
           wrong = __any_sync(0xFFFFFFFFu, beyond(top));
           raised(top);
-          __syncwarp();
+          far = __any_sync(0xFFFFFFFFu, kv_far(m));
         }
         if (k > 0 && wrong) {
           if (!wait_s(k + 1)) continue;                                    // the products of the tile before are done
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
             tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 32; i += 2) {
-              const float p = ex2(score(__uint_as_float(v[i]), x + i) + (kShift - down - m)), p2 = ex2(score(__uint_as_float(v[i + 1]), x + i + 1) + (kShift - down - m));
+              const float p = ex2(__fsub_rn(score(__uint_as_float(v[i]), x + i), m) + (kShift - down)), p2 = ex2(__fsub_rn(score(__uint_as_float(v[i + 1]), x + i + 1), m) + (kShift - down));
               sum += p + p2;
               y[i / 2] = pack_f16(p, p2);
             }
