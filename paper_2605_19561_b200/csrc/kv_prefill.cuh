@@ -120,9 +120,11 @@ __device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const 
   longest = __reduce_max_sync(0xFFFFFFFFu, longest);
   KvPrefillWalk w;
   w.units = units;
-  // turns of whole items: the longest is in one of them, the others are like the average
+  // Turns of whole items: the longest is in one of them, the others are like the average.  Two kernels decide this, each for itself, and have to agree: every
+  // operation is rounded by itself, so that no compilation fuses some of them.
   const float n = (float)items, u = (float)units, k = (float)ctas;
-  if (items == 0 || (ceilf(n / k) - 1.f) * (u / n) + (float)longest <= u / k + (float)EXTRA + 8.f * n / k) {
+  if (items == 0 || __fadd_rn(__fmul_rn(ceilf(__fdiv_rn(n, k)) - 1.f, __fdiv_rn(u, n)), (float)longest) <=
+                        __fadd_rn(__fadd_rn(__fdiv_rn(u, k), (float)EXTRA), __fdiv_rn(8.f * n, k))) {
     w.ranges = 0;
     w.at = which;
     w.end = items;
