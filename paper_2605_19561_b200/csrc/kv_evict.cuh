@@ -5,9 +5,9 @@
 
 namespace torq {
 
-// Larger numbers have larger keys.
+// Larger numbers have larger keys; zeros of either sign the same.
 __device__ __forceinline__ uint32_t ordered_key(float v) {
-  const uint32_t u = __float_as_uint(v);
+  const uint32_t u = v == 0.f ? 0u : __float_as_uint(v);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
