@@ -23,7 +23,7 @@ static torq_status kv_view(const torq_kv_cache* c, const int32_t* starts, int64_
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return TORQ_ERR_SHAPE;
   if (c->page_tokens < 16 || c->page_tokens > 1024 || (c->page_tokens & (c->page_tokens - 1))) return TORQ_ERR_SHAPE;
   if (c->kv_heads < 1 || c->kv_heads > 1024 || c->num_pages < 1 || c->num_pages > INT32_MAX || c->batch < 1 || c->batch > (1 << 16) ||
-      c->table_width < 1 || c->table_width * c->page_tokens > (1 << 30))
+      c->table_width < 1 || c->table_width > (1 << 30) / c->page_tokens)
     return TORQ_ERR_SHAPE;
   if (tokens < 1 || tokens > (1 << 24) || (!starts && tokens != c->batch)) return TORQ_ERR_SHAPE;
   const bool nv = FMT == FMT_NVFP4;
