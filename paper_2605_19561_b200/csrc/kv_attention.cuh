@@ -633,6 +633,14 @@ struct KvWeightsCfg {
   static constexpr int ROOM = KvScaleRoom<FMT, D>::KEYS, SMEM = WARPS * (STAGES * STAGE + ROOM), TILES = D == 256 ? 1 : 2;
 };
 
+// The first token that any new row of the item's sequence sees, by `first`: what lies in front is not looked at, since it may hold anything.
+__device__ __forceinline__ void kv_first_seen(const KvScoring& a, int lane, KvItem& it) {
+  if (!a.first) return;
+  int least = INT32_MAX;
+  for (int i = it.first_token + lane; i < it.first_token + it.count; i += 32) least = min(least, a.first[i]);
+  it.lo = max(it.lo, __reduce_min_sync(0xFFFFFFFFu, least));
+}
+
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const KvView c, const KvScoring a, const __nv_bfloat16* Q, int64_t q_stride, int heads,
                                                                          const float* lse, const float* weights, float* weights_out) {
@@ -697,6 +705,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
     const long long step_of = (at - sequence_begin) / cost;
     it.head = (int)(step_of / per);
     const int step0 = (int)(step_of - (long long)it.head * per);
+    kv_first_seen(a, lane, it);
     const long long left = (end - at + cost - 1) / cost;                   // steps that begin in the range
     const int steps = (int)(left < per - step0 ? left : per - step0);
     at += (long long)steps * cost;
@@ -967,6 +976,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
     const long long block_of = (at - sequence_begin) / cost;
     it.head = (int)(block_of / per);
     const int block0 = (int)(block_of - (long long)it.head * per);
+    kv_first_seen(a, lane, it);
     const long long left = (end - at + cost - 1) / cost;                   // blocks that begin in the range
     const int blocks = (int)(left < per - block0 ? left : per - block0);
     at += (long long)blocks * cost;
