@@ -476,9 +476,11 @@ int64_t torq_launch_count(void);
  * results are zeros (lse: minus infinity).  table, lengths, starts are int32 and 4-byte aligned, and are read on the device: one captured call
  * serves every step.  A page number that a call needs and that lies outside [0, num_pages), or a length that the table has no room for, latches
  * TORQ_ERR_PAGE in the device error word; nothing is read or written there, and the results of that sequence are unspecified.
- * Entries of table behind a sequence's length and what pages hold there are never looked at, so they may hold anything.  Sequences may have pages in
- * common (a prompt that they share), but for slots that append or weights write.
- * Sizes: batch <= 65536, kv_heads <= 1024, table_width page_tokens <= 2^30, tokens <= 2^24. */
+ * Entries of table behind a sequence's length and what pages hold there are never looked at, so they may hold anything.  A length below zero counts as none.
+ * Sequences may have pages in common (a prompt that they share), but no two of them slots that append writes, nor any page in a call of weights, which writes
+ * all of a sequence's.
+ * Sizes: batch <= 65536, kv_heads <= 1024, table_width page_tokens <= 2^30, tokens <= 2^24; append and read: tokens kv_heads head_dim / 4 < 2^31; attention and
+ * weights: heads <= 65536, tokens heads < 2^31.  Tensor scales above 0 and up to 3e38. */
 typedef struct {
   void* pages;               /* [num_pages][kv_heads][torq_kv_page_bytes()], 16-byte aligned */
   const int32_t* table;      /* [batch][table_width] */
@@ -508,7 +510,8 @@ torq_status torq_mxint4_kv_read(const torq_kv_cache* cache, const int32_t* start
 /* How a query at place p of its sequence (its last new row is at length - 1) scores and sees the token at place j:
  *   x_j = cap(scale q k_j) - slopes[head] |p - j|,   cap(x) = softcap tanh(x / softcap), or x where softcap is 0
  *   p - window < j (window > 0),   j <= max(p, prefix[b] - 1),   first[row] <= j < length
- * slopes [heads] float32, prefix [batch] and first [tokens] int32, each or all NULL: no bias by distance, causal, from the beginning. */
+ * slopes [heads] float32, prefix [batch] and first [tokens] int32, each or all NULL: no bias by distance, causal, from the beginning.
+ * 0 < scale <= 1e30, 0 <= softcap <= 1e30, window >= 0. */
 typedef struct {
   float scale, softcap;
   const float* slopes;
@@ -522,10 +525,15 @@ typedef struct {
  *   Q [tokens][heads][D] bf16, rows q_stride elements apart; heads % kv_heads == 0, query heads h G ... h G + G - 1 share key/value head h
  *   out [tokens][heads][D] bf16;  lse [tokens][heads] float32, natural logarithm, or NULL
  *   workspace: torq_kv_attention_workspace_bytes() bytes, 256-byte aligned; two calls that may overlap need one each
- * Scores, sums and the running maximum are float32; Q is read to 2^-21 of a row's largest element at least, weights are float16 before they meet the values,
- * 11 bits down to 2^-24 of the largest so far and never off by more than 2^-35 of it.  MXFP4, MXINT4: scales below 2^-26 (many rows: 2^-35) of the largest
- * that the same features (many rows: 128 tokens) have among what the rows of a call see count as zero, of keys (many rows alone) and of values; so does scale
- * byte 0.  Tokens that no row of a sequence sees may hold anything.  Two launches.  Outputs overlap no operand. */
+ * Scores, sums and the running maximum are float32: scores may be of any size there, with the relative error of float32, as long as scale times a row's largest
+ * element times the largest key that it meets is below 2^110.  Q is held as float16 relative to a row's largest element: all bits of what is down to 2^-21 of it,
+ * and nothing is off by more than 2^-39 (rows whose largest is below 2^-112: of 2^-112).  A weight is float16 when it meets the values: 11 bits, but off by 2^-35 of
+ * the row's largest so far where that is more.  MXFP4, MXINT4: scale byte 0 counts as zero, and further
+ *   few rows (tokens / batch, whole, times heads / kv_heads below 64): values' scales below 2^-26 of the largest so far that the same 32 features have among the
+ *   tokens that any of the 8 or 16 rows worked on together sees; keys' scales below 2^-190 of the largest of the same 32 tokens
+ *   many rows: scales below 2^-35 of the largest of the same 128 tokens, keys' and values' apart; a weight times the largest scale of its 128 tokens is off by
+ *   2^-35 of the row's largest such product so far, instead of the weights alone
+ * Tokens that no row of a sequence sees may hold anything.  Two launches.  Outputs overlap no operand. */
 size_t torq_kv_attention_workspace_bytes(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads, int64_t head_dim);
 torq_status torq_mxfp4_kv_attention(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
                                     const int32_t* starts, int64_t tokens, void* out, float* lse, void* workspace, size_t workspace_bytes, void* stream);
@@ -537,8 +545,10 @@ torq_status torq_mxint4_kv_attention(const torq_kv_cache* cache, const torq_kv_s
 /* The account of the cache: what attention gave to each cached token, summed over the new rows and the query heads that share its head.
  *   weights_out[page][h][slot] = (weights[page][h][slot] of a token that is not new, else 0) + sum over rows and heads of exp(x_j - lse)
  * weights, weights_out [num_pages][kv_heads][page_tokens] float32 (16-byte aligned; they may be the same); only slots of the sequences' tokens are
- * written, and a slot that two sequences have in common gets only one's.  Q, scoring and starts as the attention call had them, lse [tokens][heads] what
- * it gave.  The order of the sums is fixed.  One launch. */
+ * written.  Q, scoring and starts as the attention call had them, lse [tokens][heads] what it gave.  The order of the sums is fixed.  One launch.
+ * No two sequences of a call have a page in common: what its slots get would be one's sum or the other's or both.  For sequences that share pages make one call
+ * after the other, each with its rows, its row of table and its length, in place: every slot then has the sum over all of them.
+ * An exponent x_j - lse is off by what float32 keeps of a score and of lse, 2^-20 of the larger: where scores are beyond some thousands, so is the account. */
 torq_status torq_mxfp4_kv_weights(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
                                   const int32_t* starts, int64_t tokens, const float* lse, const float* weights, float* weights_out, void* stream);
 torq_status torq_nvfp4_kv_weights(const torq_kv_cache* cache, const torq_kv_scoring* scoring, const void* Q, int64_t q_stride, int64_t heads,
@@ -547,11 +557,11 @@ torq_status torq_mxint4_kv_weights(const torq_kv_cache* cache, const torq_kv_sco
                                    const int32_t* starts, int64_t tokens, const float* lse, const float* weights, float* weights_out, void* stream);
 
 /* Eviction by account: of each sequence and key/value head the `recent` newest tokens and, of the others, those with the largest weights stay, `keep`
- * in all (equal weights: the lower place stays; a sequence of at most `keep` tokens stays whole).  Codes, scale bytes and weights of what stays
+ * in all (equal weights, zeros of either sign among them: the lower place stays; a sequence of at most `keep` tokens stays whole).  Codes, scale bytes and weights of what stays
  * are copied, in their order, to the pages of new_table [batch][new_width], which are no pages of the sequences and no page twice.  Places count anew there: a
  * bias by distance or a window then counts what is left.
  *   new_lengths [batch] int32 = min(length, keep);  kept [batch][kv_heads][keep] int32: the places of what stayed, -1 behind them
- * new_width page_tokens >= min(keep, table_width page_tokens); batch kv_heads <= 65535.  Weights that are no numbers are outside the contract.
+ * 1 <= keep <= 2^30, 0 <= recent <= keep, new_width <= 2^26, new_width page_tokens >= min(keep, table_width page_tokens); batch kv_heads <= 65535.  Weights that are no numbers are outside the contract.
  * Two launches. */
 torq_status torq_mxfp4_kv_evict(const torq_kv_cache* cache, float* weights, const int32_t* new_table, int64_t new_width, int64_t keep, int64_t recent,
                                 int32_t* new_lengths, int32_t* kept, void* stream);

@@ -215,7 +215,7 @@ struct KvQuery {
   uint32_t q[D / 32][4];
 };
 // A row into float16, times a power of two that brings its largest magnitude to [2^14, 2^15): float16 then keeps all bits of a
-// bfloat16 down to 2^-21 of the largest, and nothing is off by more than 2^-40 of it.  Returns the factor to be multiplied back, of row g.
+// bfloat16 down to 2^-21 of the largest, and nothing is off by more than 2^-39 of it.  Returns the factor to be multiplied back, of row g.
 template <int FMT, int D>
 __device__ __forceinline__ float kv_scale_query(const uint4 (&raw)[D / 32], KvQuery<D>& out) {
   uint32_t top = 0;

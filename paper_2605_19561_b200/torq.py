@@ -1160,7 +1160,7 @@ def torq_mxint4_kv_attention(pages, table, lengths, Q, starts=None, scale=None, 
 def torq_mxfp4_kv_weights(pages, table, lengths, Q, lse, weights, starts=None, scale=None, softcap: float = 0.0, slopes=None,
                           window: int = 0, prefix=None, first=None, weights_out=None, stream=None):
     """What attention (same arguments, its lse) gave to each cached token, added to weights [num_pages, kv_heads, page_tokens] float32
-    (a new token's starts at zero): in place, or to weights_out."""
+    (a new token's starts at zero): in place, or to weights_out.  No two sequences of a call share a page: those that do get calls of their own."""
     return _kv_weights("mxfp4", pages, table, lengths, Q, lse, weights, None, starts, scale, softcap, slopes, window, prefix, first,
                        weights_out, stream)
 
