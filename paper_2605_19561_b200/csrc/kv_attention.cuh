@@ -47,6 +47,8 @@ __device__ __forceinline__ float kv_cap(float x, float softcap, float per_cap) {
   const float e = exp2f(u * (-2.f * kLog2e));
   return copysignf(softcap * __fdividef(1.f - e, 1.f + e), x);
 }
+// A slope times log2 e, finite: at distance zero it counts nothing, however steep.
+__device__ __forceinline__ float kv_slope(const KvScoring& a, int head) { return fminf(fmaxf(a.slopes[head] * kLog2e, kLowest), -kLowest); }
 // What comes behind a scaled score; all of it, the slope too, times log2 e.
 __device__ __forceinline__ float kv_score(float x, const KvScoring& a, float slope, int distance) {
   if (a.softcap > 0.f) x = kv_cap(x, a.softcap, a.per_cap);
@@ -275,7 +277,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_decode_kernel(const Kv
           const int token = rr / group;
           place[n][e] = it.length - it.count + token;
           kv_range(a, it.b, it.first_token + token, place[n][e], it.length, lo[n][e], hi[n][e]);
-          if (a.slopes) slope[n][e] = a.slopes[it.head * group + rr % group] * kLog2e;
+          if (a.slopes) slope[n][e] = kv_slope(a, it.head * group + rr % group);
           all_lo = max(all_lo, lo[n][e]);
           all_hi = min(all_hi, hi[n][e]);
           if (lo[n][e] < hi[n][e]) any_lo = min(any_lo, lo[n][e]);
@@ -789,7 +791,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
           }
           all_lo = max(all_lo, lo[e]);
           all_hi = min(all_hi, hi[e]);                                     // 0 where a row saw nothing: its scores may be no numbers
-          if (a.slopes) slope[e] = a.slopes[h] * kLog2e;
+          if (a.slopes) slope[e] = kv_slope(a, h);
         }
       }
 #pragma unroll
@@ -1018,7 +1020,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_row_weights_kernel(con
       const __nv_bfloat16* q = Q + i * q_stride + h * D + 8 * t;
 #pragma unroll
       for (int x = 0; x < CH; ++x) raw[x] = have ? *reinterpret_cast<const uint4*>(q + 32 * x) : make_uint4(0, 0, 0, 0);
-      row_slope = have && a.slopes ? a.slopes[h] * kLog2e : 0.f;
+      row_slope = have && a.slopes ? kv_slope(a, h) : 0.f;
       row_place = it.length - it.count + r / group;
       row_lo = row_hi = 0;
       if (have) kv_range(a, it.b, i, row_place, it.length, row_lo, row_hi);

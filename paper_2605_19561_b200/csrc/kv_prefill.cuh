@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
           kv_range(a, it.b, token, place, it.length, lo, hi);
           lo = max(lo, it.lo);
           hi = min(hi, it.hi);
-          if (a.slopes) slope = a.slopes[h] * kLog2e;
+          if (a.slopes) slope = kv_slope(a, h);
         }
       }
       fence_proxy_async_smem();
