@@ -207,9 +207,11 @@ static torq_status prefill_launch(const KvView& v, const KvScoring& a, int sms, 
 }
 // Which of the two: the streaming kernel widens the cache anew for every 16 rows of a head (8 of 256 dimensions), the other once for 256 (128), but takes as long for
 // one row as for all.  Measured, streaming against the other, us, by rows on average:
-//   one sequence of 32768 tokens, 8 heads of 128: 64 rows 60, 65;  96: 83, 67;  512: 362, 122;  of 256: 64 rows 118, 120;  128: 216, 137
-//   16 sequences of up to 5000 tokens, 8 heads of 128: about 45 rows 71, 95;  65: 91, 94;  90: 138, 102
-//   64 sequences of up to 3000 tokens, 4 heads of 128: about 45 rows 90, 115;  65: 133, 116
+//   one sequence of 32768 tokens, 8 heads of 128: 64 rows 62, 65;  96: 87, 69;  512: 380, 126;  of 256: 64 rows 124, 122;  128: 226, 140
+//   16 sequences of up to 5000 tokens, 8 heads of 128: about 45 rows 73, 102;  65: 94, 102;  90: 142, 103
+//   64 sequences of up to 3000 tokens, 4 heads of 128: about 45 rows 92, 127;  65: 136, 127
+// The rule knows the average alone, and these batches are of sequences alike.  Where many decode and one brings a prompt, all of them get one kernel, and the sequences
+// that it is not meant for take longer than they would by themselves.
 static bool many_rows(int64_t tokens, int64_t batch, int64_t heads, int64_t kv_heads) {
   return tokens / batch * (heads / kv_heads) >= 64;
 }
@@ -255,8 +257,8 @@ static torq_status weights_impl(const torq_kv_cache* cache, const torq_kv_scorin
   if (!aligned4(lse) || !aligned16(weights) || !aligned16(weights_out)) return TORQ_ERR_ALIGN;
   int sms;
   if ((rc = current_device(&sms, &v.err_word)) != TORQ_OK) return rc;
-  // By single warps up to one group of eight rows.  Measured, single warps against CTAs, us: 16 sequences of up to 5000 tokens, 8 heads of 128: 8 rows 18.8,
-  // 21.5; 12 rows 36.6, 23.5; 64: 89.7, 42.5.  One sequence of 32768 tokens, 8 heads of 256: 8 rows 19.8, 32.5; 12: 55.2, 39.2; 64: 185, 79
+  // By single warps up to one group of eight rows, on average.  Measured, single warps against CTAs, us: 16 sequences of up to 5000 tokens, 8 heads of 128: 8 rows
+  // 18.6, 21.6; 12 rows 37.4, 23.1; 64: 91.3, 42.6.  One sequence of 32768 tokens, 8 heads of 256: 8 rows 20.1, 32.1; 12: 55.0, 39.2; 64: 186, 80
   const bool one = (tokens + cache->batch - 1) / cache->batch * (heads / v.heads) <= 8;
   with_dim(v.dim, [&](auto DIM) {
     constexpr int D = decltype(DIM)::value;

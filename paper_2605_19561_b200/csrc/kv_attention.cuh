@@ -37,7 +37,8 @@ __device__ __forceinline__ void kv_range(const KvScoring& a, int b, int i, int p
   if (a.first && a.first[i] > lo) lo = a.first[i];
 }
 // softcap tanh(x / softcap), with u = |x| / softcap.  From u = 1/4 on by (1 - e) / (1 + e), e = exp(-2 u).  Below, 1 - e would cancel (at u = 2^-24 to nothing), so
-// there the series of tanh, x (1 - u^2/3 + 2 u^4/15 - 17 u^6/315 + 62 u^8/2835): what it leaves out is at most 0.0089 u^10 < 2^-26 of x.
+// there the series of tanh, x (1 - u^2/3 + 2 u^4/15 - 17 u^6/315 + 62 u^8/2835): what it leaves out is at most 0.0089 u^10 < 2^-26 of x.  (Both computed and one
+// taken: the account of 32 sequences 47 us instead of 42, for registers, though 48 sequences with a cap 71.4 instead of 72.9.)
 __device__ __forceinline__ float kv_cap(float x, float softcap, float per_cap) {
   const float u = fabsf(x) * per_cap;
   if (u < 0.25f) {
@@ -65,7 +66,9 @@ __device__ __forceinline__ float kv_score(float x, const KvScoring& a, float slo
 // 32 sequences of up to 8192 tokens 73.6 us, SMs idle for a quarter of it, since a CTA with more items in its range took longer.)
 //
 // A warp keeps a maximum m of its scores in powers of two that is raised only when a score exceeds it by 5, so weights are exp2(x - m + 10) <= 2^15 in
-// float16; they keep 11 bits down to 2^-24 of the largest.  The same goes for the values' scales (see kv_fragments.cuh).
+// float16; they keep 11 bits down to 2^-24 of the largest.  The same goes for the values' scales (see kv_fragments.cuh).  float16 because the values are exact in it and
+// both operands have one type; a weight is off by 2^-12 then, where the result is rounded by 2^-9: against 64 bits results are off by 0.0017 of their norm,
+// as they are with weights in float32.
 template <int FMT_, int D_, int NT_>
 struct KvDecodeCfg {
   static constexpr int FMT = FMT_, D = D_, NT = NT_;
@@ -627,7 +630,7 @@ __global__ void __launch_bounds__(256) kv_join_kernel(const KvView c, const KvSc
 // weights_out[token] = (old or, of a new token, 0) + sum over the rows of its sequence and the heads of its group of exp2(x log2 e - lse log2 e).
 // Only keys are read.  The list of steps of 32 cached tokens is cut into equal ranges for warps as above, a step counting as often as its sequence
 // has groups of eight rows; a step belongs to the range that it begins in, so every slot is written once and the order of its sum is fixed.  A warp holds
-// the keys of a step as operands (D = 256: of half a step) and goes through the groups.
+// the keys of a step as operands (D = 256: of half a step, with 112 bytes of registers spilled all the same) and goes through the groups.
 template <int FMT_, int D_>
 struct KvWeightsCfg {
   static constexpr int FMT = FMT_, D = D_, WARPS = 4, THREADS = 128, CH = D / 32, SB = D / kv_block(FMT), CTAS = D == 64 ? 4 : 3;
@@ -906,7 +909,7 @@ __global__ void __launch_bounds__(C::THREADS, C::CTAS) kv_weights_kernel(const K
 // The same for many rows of a sequence.  What a group of eight rows costs is its queries: read from L2, scaled, its ranges and sums looked up, one behind
 // the other.  So the four warps of a CTA, each with 32 tokens as operands (D = 256: 16), take the same groups: each makes one of four ready in shared
 // memory, the loads for the next four in flight, and all go through the four.  Blocks of tokens that no row of a group sees are passed over.  48 rows of 4
-// heads over 3 sequences of up to 3000 tokens, 8 key/value heads: 22.6 us, of which the longest chain of a CTA is most; 70.5 by single warps.
+// heads over 3 sequences of up to 3000 tokens, 8 key/value heads: 22.9 us, of which the longest chain of a CTA is most; 70.5 by single warps.
 template <int FMT_, int D_>
 struct KvRowWeightsCfg {
   static constexpr int FMT = FMT_, D = D_, WARPS = 4, THREADS = 128, CH = D / 32, SB = D / kv_block(FMT), CTAS = D == 256 ? 2 : 3;

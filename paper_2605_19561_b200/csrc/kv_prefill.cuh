@@ -8,10 +8,10 @@
 // scales down to 2^-35 of that; 2^E of the keys goes into the scores' factor, that of the values into the weights: P = exp2(x - m + 10 + E - e), where m and e,
 // for each row, follow the largest score and the largest product of a weight and 2^E: that one's P lies in [2^10, 2^15].  So a weight counts by what its values
 // make of it, and tokens that a row does not see, or hardly, do not lower the precision of others.  What is summed for the softmax does not have 2^E.
-// (One e for all rows, the largest E so far: no faster, and values 2^30 smaller than some that a row gives no weight had 4 bits of their weights left.)
+// (One e for all rows, the largest E so far: 313 us instead of 315, but values 2^30 smaller than some that a row gives no weight had 4 bits of their weights left.)
 //
-// Bound by the softmax warps: about 2250 cycles per 64 tokens and 256 rows, of which the exponentials' rate is 1024; the tensor pipe is busy for 40 %.  2048 tokens
-// behind 6144, 8 heads of 128 with 4 queries: 310 us, 145 as products alone.
+// Bound by the softmax warps: about 2300 cycles per 64 tokens and 256 rows, of which the exponentials' rate is 1024; the tensor pipe is busy for 43 %.  2048 tokens
+// behind 6144, 8 heads of 128 with 4 queries: 315 us, 145 as products alone.  Heads of 256 spill 44 to 76 bytes of registers.
 //
 // Warp-specialised, one CTA per SM, persistent over the items (sequence, head, tiles of rows):
 //   warps 0 - 3, 4 - 7   softmax of the first and second tile, a row to each thread: loads its query, keeps maximum and sum, corrects O when the maximum has
@@ -98,8 +98,8 @@ __device__ __forceinline__ long long kv_prefill_items(const KvView& c, const KvS
 }
 // Whole items where ranges, with what cutting costs (partial results and their join: as much as EXTRA groups of each CTA; a start from the middle: 8 for an item),
 // would not take less time; ranges have LEAST units at least.  Measured, whole items against ranges, us: one sequence of 32768 tokens, 8 heads of 128: 256
-// rows of a head 608, 92;  1024: 600, 182;  of 256 dimensions, 1024 rows: 1313, 617.  8 sequences of up to 5000 tokens, 8 heads of 256, up to 1024 rows: 582,
-// 468.  2048 tokens behind 6144, 8 heads of 128 with 4 queries: 303 to 310, 329.  16 sequences of up to 5000 tokens, up to 1024 rows: 260, 342.
+// rows of a head 618, 93;  1024: 621, 188;  of 256 dimensions, 1024 rows: 1344, 634.  8 sequences of up to 5000 tokens, 8 heads of 256, up to 1024 rows: 587,
+// 477.  2048 tokens behind 6144, 8 heads of 128 with 4 queries: 316, 341.  16 sequences of up to 5000 tokens, up to 1024 rows: 256, 351.
 template <int ROWS, int TOK>
 __device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const KvScoring& a, int group, int lane, int which, int ctas) {
   constexpr int EXTRA = ROWS == 128 ? 12 : 24, LEAST = 4;
