@@ -177,13 +177,15 @@ static torq_status decode_launch(const KvView& v, const KvScoring& a, int sms, c
   launch_tc(kernel, 1, dim3((unsigned)ctas), dim3(C::THREADS), C::SMEM, s, v, a, static_cast<const __nv_bfloat16*>(Q), q_stride, heads, y, lse, partials);
   const torq_status rc = launch_status();
   if (rc != TORQ_OK) return rc;
-  // items at most: every sequence may have a group that is not full.  Few items: a row to each CTA, with the ranges shared among its warps
+  // Items at most: every sequence may have a group that is not full.  No more than there are borders can be cut.  Few items: a row to each CTA, with the ranges
+  // shared among its warps.
   const int64_t items = ((int64_t)v.tokens * group / C::ROWS + (v.tokens < v.batch ? v.tokens : v.batch)) * v.heads;
-  if (items > INT32_MAX) return TORQ_ERR_SHAPE;
-  if (items <= 64)
-    launch_tc(kv_join_kernel<D, NT, 8>, 1, dim3((unsigned)items, C::ROWS), dim3(256), 0, s, v, a, ctas * C::WARPS, heads, static_cast<const float*>(partials), y, lse);
-  else
-    launch_tc(kv_join_kernel<D, NT, 1>, 1, dim3((unsigned)items, NT), dim3(256), 0, s, v, a, ctas * C::WARPS, heads, static_cast<const float*>(partials), y, lse);
+  const int ranges = ctas * C::WARPS;
+  const bool by_border = items > ranges - 1;
+  const unsigned grid = (unsigned)(by_border ? ranges - 1 : items);
+  const float* parts = partials;
+  if (items <= 64) launch_tc(kv_join_kernel<D, NT, 8>, 1, dim3(grid, C::ROWS), dim3(256), 0, s, v, a, ranges, by_border, heads, parts, y, lse);
+  else launch_tc(kv_join_kernel<D, NT, 1>, 1, dim3(grid, NT), dim3(256), 0, s, v, a, ranges, by_border, heads, parts, y, lse);
   return launch_status();
 }
 
