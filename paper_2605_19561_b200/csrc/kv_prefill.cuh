@@ -135,16 +135,27 @@ __device__ __forceinline__ KvPrefillWalk kv_prefill_walk(const KvView& c, const 
   }
   return w;
 }
-// Where number `at` of the list lies: the item (its tokens all of them), its groups, and which of its units; false behind the last.  Whole warps.
+// Where number `at` of the list lies: the item (its tokens all of them), its groups, and which of its units; false behind the last.  Whole warps.  `from`, if any,
+// in shared memory: of this warp's last search the 32 sequences that it ended at and what lies in front of them, where the next one begins, since a CTA's numbers
+// ascend.  (From the first sequence each time: 4096 sequences with 24 new tokens each 14 ms.)
+struct KvPrefillFrom {
+  long long before;
+  int b0;
+};
 template <int ROWS, int TOK>
 __device__ __forceinline__ bool kv_prefill_find(const KvView& c, const KvScoring& a, int group, long long at, bool items, int lane, KvPrefillItem& it, int& unit,
-                                                int& each, int& groups) {
-  long long before = 0;
-  for (int b0 = 0; b0 < c.batch; b0 += 32) {
+                                                int& each, int& groups, KvPrefillFrom* from) {
+  long long before = from ? from->before : 0;
+  for (int b0 = from ? from->b0 : 0; b0 < c.batch; b0 += 32) {
     const long long n = kv_prefill_items<ROWS, TOK>(c, a, group, b0 + lane, each) * (items ? 1 : max(each, 0)), sum = warp_scan(n, lane);
     const uint32_t here = __ballot_sync(0xFFFFFFFFu, at < before + sum);
     if (here) {
       const int l = __ffs(here) - 1;
+      if (from) {
+        __syncwarp();                                                      // all have read
+        if (lane == 0) *from = {before, b0};
+        __syncwarp();
+      }
       const long long rest = at - before - __shfl_sync(0xFFFFFFFFu, sum - n, l);
       each = __shfl_sync(0xFFFFFFFFu, each, l);
       const int tiles = kv_prefill_sequence<ROWS>(c, group, b0 + l, it);
@@ -160,9 +171,9 @@ __device__ __forceinline__ bool kv_prefill_find(const KvView& c, const KvScoring
 }
 // The next item of a CTA, or the part of it that lies in its range.
 template <int ROWS, int TOK>
-__device__ __forceinline__ bool kv_prefill_item(const KvView& c, const KvScoring& a, int group, KvPrefillWalk& w, int lane, KvPrefillItem& it) {
+__device__ __forceinline__ bool kv_prefill_item(const KvView& c, const KvScoring& a, int group, KvPrefillWalk& w, int lane, KvPrefillItem& it, KvPrefillFrom* from) {
   int unit, each, groups;
-  if (w.at >= w.end || !kv_prefill_find<ROWS, TOK>(c, a, group, w.at, w.ranges == 0, lane, it, unit, each, groups)) return false;
+  if (w.at >= w.end || !kv_prefill_find<ROWS, TOK>(c, a, group, w.at, w.ranges == 0, lane, it, unit, each, groups, from)) return false;
   it.part = -1;
   if (w.ranges == 0) {
     w.at += gridDim.x;
@@ -196,6 +207,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
   __shared__ __align__(8) uint64_t bars[2 * C::STAGES + 10];
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_flag;
+  __shared__ KvPrefillFrom froms[C::THREADS / 32];
   const uint32_t smem = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* smem_p = smem_raw + (smem - smem_u32(smem_raw));
   volatile int* cta_abort = &abort_flag;
@@ -233,6 +245,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
   tc_fence_after_sync();
   const uint32_t tmem = tmem_slot;
   griddep_wait_and_launch();
+  KvPrefillFrom* from = froms + warp;
+  if (lane == 0) *from = {0, 0};
+  __syncwarp();
   KvPrefillItem it;
   KvPrefillWalk walk = kv_prefill_walk<C::ROWS, TOK>(c, a, group, lane, blockIdx.x, gridDim.x);
 
@@ -265,7 +280,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
     // Two tiles of rows weigh in turn: side by side they wait for the exponentials of one another and then leave that unit idle together (2048 tokens behind
     // 6144: 317 us, in turn 304).  The barriers for that are executed for every tile of tokens, also after a wait has given up, so that no warp is left in
     // one.
-    while (kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it)) {
+    while (kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it, from)) {
       const uint32_t first_group = group_no;
       group_no += (it.tiles + 1) / 2;
       if (128 * t >= it.rows) continue;
@@ -513,7 +528,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
     const int ch = dt % CH, row0 = dt / CH;                                // of chunk i: row row0 + i 128 / CH of the group
     uint32_t fill = 0, group_no = 0;
     bool ok = true;
-    while (kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it)) {
+    while (kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it, from)) {
       const int32_t* table = c.table + (int64_t)it.b * c.width;
       const uint8_t* head_pages = c.pages + (int64_t)it.head * c.head_bytes;
       const int groups = (it.tiles + 1) / 2;
@@ -661,7 +676,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) kv_prefill_kernel(const KvView 
     // result of a reduction does.
     const int t = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)warp) - 12;                  // the tile of rows
     const uint32_t tm = __reduce_max_sync(0xFFFFFFFFu, tmem), sm = __reduce_max_sync(0xFFFFFFFFu, smem);
-    while (t < C::TILES && ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it)) {
+    while (t < C::TILES && ok && kv_prefill_item<C::ROWS, TOK>(c, a, group, walk, lane, it, from)) {
       const int tiles = (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)it.tiles);
       const bool active = 128 * t < (int)__reduce_max_sync(0xFFFFFFFFu, (uint32_t)it.rows);
       const uint32_t o_at = tm + C::O_COL + t * D;
@@ -732,7 +747,7 @@ __global__ void __launch_bounds__(256) kv_prefill_join_kernel(const KvView c, co
   KvPrefillItem it;
   int unit = 0, each = 1, groups = 0, from = 0, to = -1;
   auto range_of = [&](long long unit) { return (int)(((unit + 1) * w.ranges + w.units - 1) / w.units) - 1; };
-  if (w.ranges && w.at < w.end && kv_prefill_find<C::ROWS, C::TOK>(c, a, group, w.at, false, lane, it, unit, each, groups) && unit > 0) {
+  if (w.ranges && w.at < w.end && kv_prefill_find<C::ROWS, C::TOK>(c, a, group, w.at, false, lane, it, unit, each, groups, nullptr) && unit > 0) {
     from = range_of(w.at - unit);
     to = range_of(w.at - unit + each - 1);
   }
