@@ -38,7 +38,7 @@ __device__ __forceinline__ void kv_range(const KvScoring& a, int b, int i, int p
 }
 // softcap tanh(x / softcap), with u = |x| / softcap.  From u = 1/4 on by (1 - e) / (1 + e), e = exp(-2 u).  Below, 1 - e would cancel (at u = 2^-24 to nothing), so
 // there the series of tanh, x (1 - u^2/3 + 2 u^4/15 - 17 u^6/315 + 62 u^8/2835): what it leaves out is at most 0.0089 u^10 < 2^-26 of x.  (Both computed and one
-// taken: the account of 32 sequences 47 us instead of 42, for registers, though 48 sequences with a cap 71.4 instead of 72.9.)
+// taken: the account of 32 sequences 47 us instead of 42, for registers; attention takes as long.)
 __device__ __forceinline__ float kv_cap(float x, float softcap, float per_cap) {
   const float u = fabsf(x) * per_cap;
   if (u < 0.25f) {

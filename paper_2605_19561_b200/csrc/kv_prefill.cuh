@@ -11,7 +11,7 @@
 // (One e for all rows, the largest E so far: 313 us instead of 315, but values 2^30 smaller than some that a row gives no weight had 4 bits of their weights left.)
 //
 // Bound by the softmax warps: about 2300 cycles per 64 tokens and 256 rows, of which the exponentials' rate is 1024; the tensor pipe is busy for 43 %.  2048 tokens
-// behind 6144, 8 heads of 128 with 4 queries: 315 us, 145 as products alone.  Heads of 256 spill 44 to 76 bytes of registers.
+// behind 6144, 8 heads of 128 with 4 queries: 315 us, 145 as products alone.  Heads of 256 spill 48 to 72 bytes of registers.
 //
 // Warp-specialised, one CTA per SM, persistent over the items (sequence, head, tiles of rows):
 //   warps 0 - 3, 4 - 7   softmax of the first and second tile, a row to each thread: loads its query, keeps maximum and sum, corrects O when the maximum has
